@@ -326,6 +326,53 @@ int mqa_beam_reorder_kv(const void* K_src, const void* V_src, const int32_t* len
                         void* K_dst, void* V_dst, int32_t* lens_dst,
                         int n, int h_kv, int cap, int k, int v, mqa_dtype dt, void* stream);
 
+/*
+ * Paged caches.  K and V rows lie in pools of pages, K_pages [num_pages,h_kv,page_size,k] and V_pages [num_pages,h_kv,page_size,v] (h_kv = 1: multi-query;
+ * h_kv = h: multi-head; anything that divides h between them), of float32 or bfloat16.  table [b,max_pages] (int32) names the pages of a sequence in order:
+ * position p is row p % page_size of page table[i, p / page_size]; a sequence holds up to max_pages * page_size positions.  An entry outside [0,num_pages)
+ * names a page that holds nothing: rows for it are dropped, and its positions count for nothing in the attention and in an eviction.  Only the entries of
+ * positions below a sequence's length (behind an append: its new length) are looked at.  Sequences may share pages (a common prompt); a page that a call writes to
+ * must not be one that it reads or writes for another sequence.  Limits: k, v multiples of 8 up to 256; max_pages * page_size <= 2^24,
+ * b * h_kv * max(256, max_pages * page_size) <= 2^31, num_pages * h_kv * page_size < 2^31.
+ *
+ * mqa_paged_append_kv_rows: rows k_new [b,n,h_kv,k], v_new [b,n,h_kv,v] (float32) go behind the lens_in[i] rows that sequence i has, rounded as in
+ * mqa_append_kv; of a padded batch only the first counts[i] (clamped to [0,n]; NULL: all n); lens_out[i] = lens_in[i] + their number.  A sequence that cannot
+ * hold them keeps its rows and its length.  lens_in and lens_out must be different arrays (MQA_ERR_SHAPE if they are the same pointer).
+ */
+int mqa_paged_append_kv_rows(const float* k_new, const float* v_new, const int32_t* counts, void* K_pages, void* V_pages, const int32_t* table,
+                             const int32_t* lens_in, int32_t* lens_out, int b, int n, int h_kv, int num_pages, int page_size, int max_pages,
+                             int k, int v, mqa_dtype dt, void* stream);
+
+/*
+ * Attention of the newest n tokens of every sequence, n = 1 (a decoding step) or more (drafted tokens, the end of a prompt), after their rows have been
+ * appended: q [b,n,h,k] -> o [b,n,h,v].  Query j of sequence i sees the positions below lens[i] - (n - 1 - j); head e of q reads K/V head e / (h / h_kv).  A row that
+ * sees nothing is 0; what a row does not see may hold anything (infinities and NaN included).  n * h / h_kv <= 1024, b * n * h <= 2^22.
+ * Products and sums are float32's (a bfloat16 cache's values are multiplied by three bfloat16 terms of q and of the weights, which together are the float32).
+ *
+ * scores_out (or NULL), [b,h_kv,max_pages * page_size] float32: the attention weight that each position has received, summed over the n * h / h_kv rows of
+ * its head and over the steps: scores_in (NULL: zeros) plus this step's, the newest n positions from 0 on; scores_in and scores_out may be the same array.
+ * Positions at and behind the length are left as they were.
+ *
+ * The workspace: mqa_paged_decode_workspace_bytes(...) bytes (16-byte aligned; 0 = none, or unsupported sizes), written and read by this call's launches only.
+ */
+size_t mqa_paged_decode_workspace_bytes(int b, int n, int h, int h_kv, int page_size, int max_pages, int k, int v, mqa_dtype dt, int with_scores);
+int mqa_paged_decode_step(const float* q, const void* K_pages, const void* V_pages, const int32_t* table, const int32_t* lens, float* o,
+                          const float* scores_in, float* scores_out, int b, int n, int h, int h_kv, int num_pages, int page_size, int max_pages,
+                          int k, int v, mqa_dtype dt, float scale, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Eviction: of every sequence and K/V head at most `budget` positions are kept, the latest `recent` (<= budget) and of the older ones those with the largest
+ * scores_in [b,h_kv,max_pages_in * page_size] (the lower position among equals; NaN as -infinity), and copied in their order to positions 0, 1, ... of the pages
+ * that table_out [b,max_pages_out] names in the same pools; a sequence of no more than `budget` positions is copied whole.  lens_out[i]: how many;
+ * kept [b,h_kv,budget]: which (-1 behind them); scores_out [b,h_kv,max_pages_out * page_size]: their scores (left as they were behind them).  Attention does not
+ * depend on the order of positions, but causal rows and the next eviction's `recent` do: the order is kept.  The pages of table_out must be
+ * none of table_in's of any sequence; the source's rows stay as they are (other sequences may share them), its pages are the caller's again.
+ * budget <= max_pages_out * page_size; table_in and table_out, lens_in and lens_out, scores_in and scores_out must be different arrays.
+ */
+int mqa_paged_evict_kv(void* K_pages, void* V_pages, const int32_t* table_in, const int32_t* lens_in, const float* scores_in, const int32_t* table_out,
+                       int32_t* lens_out, float* scores_out, int32_t* kept, int b, int h_kv, int num_pages, int page_size, int max_pages_in,
+                       int max_pages_out, int k, int v, mqa_dtype dt, int budget, int recent, void* stream);
+
 /* Same as mqa_decode_step / mha_decode_step with explicit launch tuning (NULL = defaults). */
 int mqa_decode_step_ex(const float* q, const void* K, const void* V, const int32_t* lens, float* o,
                        int b, int h, int cap, int k, int v, mqa_dtype dt, float scale,
@@ -422,6 +469,22 @@ int mqa_stack_argmax(const float* x, int32_t* out, int rows, int n, void* stream
 int mqa_stack_feed_forward_plan(int rows, int d, int ff, size_t* workspace_bytes);
 int mqa_stack_feed_forward(const float* W1, const float* W2, float* x, int rows, int d, int ff, float eps, void* workspace,
                            size_t workspace_bytes, void* stream);
+
+/*
+ * Drafted tokens against the target's probabilities, and the token that follows them (speculative decoding).  logits [b,n+1,vocab]: the target's, row j those of the token at
+ * draft j's place, row n behind the last; drafts [b,n]; draft_logits [b,n,vocab]: what the drafts were drawn from (NULL: each was certain); counts [b]: how many drafts
+ * each sequence has (clamped to [0,n]; NULL: n each); u [b,n+1]: random numbers of [0,1).  With p_j, q_j = softmax(logits / temperature), draft j stands while
+ * those before it do and u[i,j] q_j(t) < p_j(t).  tokens [b,n+1]: the accepted[i] drafts that stand, then one token drawn by u[i,n] (from
+ * max(p - q, 0) / sum at the first refused draft, from p behind the last of counts[i]: the lowest index whose running sum exceeds u times the whole; the most probable token
+ * where there is nothing to draw from), then -1.  temperature 0: a draft stands where it is mqa_stack_argmax's token, which follows the last that stands (u and draft_logits are not
+ * looked at).  n = 0: one token is drawn from logits [b,1,vocab] (drafts may be NULL).  NaN counts as -infinity, +infinity as the largest number; a
+ * drafted token outside [0,vocab) is refused.  Probabilities are held in float64.
+ * The workspace: mqa_stack_verify_workspace_bytes(...) bytes (16-byte aligned; 0 = unsupported sizes).
+ */
+size_t mqa_stack_verify_workspace_bytes(int b, int n, int vocab);
+int mqa_stack_verify_drafts(const float* logits, const float* draft_logits, const int32_t* drafts, const int32_t* counts, const float* u,
+                            int32_t* tokens, int32_t* accepted, int b, int n, int vocab, float temperature, void* workspace, size_t workspace_bytes,
+                            void* stream);
 
 const char* mqa_status_string(int status);
 

@@ -26,6 +26,8 @@ EXPORTS = [
     "mqa_stream_read", "mqa_stream_copy", "mqa_status_string",
     "mqa_stack_layernorm", "mqa_stack_embed", "mqa_stack_add", "mqa_stack_relu", "mqa_stack_argmax",
     "mqa_stack_feed_forward_plan", "mqa_stack_feed_forward",
+    "mqa_paged_append_kv_rows", "mqa_paged_decode_workspace_bytes", "mqa_paged_decode_step", "mqa_paged_evict_kv",
+    "mqa_stack_verify_workspace_bytes", "mqa_stack_verify_drafts",
 ]
 
 
@@ -122,12 +124,20 @@ def load_library(path: str = LIB_PATH):
     lib.mqa_stack_argmax.argtypes = [vp, vp, ci, ci, vp]
     lib.mqa_stack_feed_forward_plan.argtypes = [ci, ci, ci, ctypes.POINTER(sz)]
     lib.mqa_stack_feed_forward.argtypes = [vp, vp, vp, ci, ci, ci, cf, vp, sz, vp]
+    lib.mqa_paged_append_kv_rows.argtypes = [vp] * 8 + [ci] * 9 + [vp]
+    lib.mqa_paged_decode_workspace_bytes.argtypes = [ci] * 10
+    lib.mqa_paged_decode_workspace_bytes.restype = sz
+    lib.mqa_paged_decode_step.argtypes = [vp] * 8 + [ci] * 10 + [cf, vp, sz, vp]
+    lib.mqa_paged_evict_kv.argtypes = [vp] * 9 + [ci] * 11 + [vp]
+    lib.mqa_stack_verify_workspace_bytes.argtypes = [ci] * 3
+    lib.mqa_stack_verify_workspace_bytes.restype = sz
+    lib.mqa_stack_verify_drafts.argtypes = [vp] * 7 + [ci] * 3 + [cf, vp, sz, vp]
     lib.mqa_status_string.argtypes = [ci]
     lib.mqa_status_string.restype = ctypes.c_char_p
     for name in EXPORTS:
         if name not in ("mqa_decode_workspace_bytes", "mha_decode_workspace_bytes", "mqa_status_string",
                         "mqa_decode_beams_workspace_bytes", "mqa_decode_workspace_bytes_default", "mqa_project_kv_workspace_bytes",
-                        "mqa_project_add_layernorm_workspace_bytes"):
+                        "mqa_project_add_layernorm_workspace_bytes", "mqa_paged_decode_workspace_bytes", "mqa_stack_verify_workspace_bytes"):
             getattr(lib, name).restype = ci
     _native = _load_native(lib)
     _lib = lib
@@ -742,6 +752,130 @@ def mqa_project_add_layernorm(mode, x, P, acc, out=None, eps=1e-6, workspace=Non
     return out
 
 
+def _one_device(*tensors):
+    """The device of a call's tensors (None among them is passed over): one of them all."""
+    device = None
+    for t in tensors:
+        if t is not None:
+            if device is None:
+                device = t.device
+            elif t.device != device:
+                raise ValueError(f"tensors of one call on {device} and {t.device}")
+    return device
+
+
+def _on(device, stream):
+    """With the call's stream and the tensors' device current: what is allocated now is the stream's."""
+    if stream is None:
+        return torch.cuda.device(device)
+    if not isinstance(stream, torch.cuda.Stream):      # (any object with a cuda_stream will do)
+        stream = torch.cuda.ExternalStream(stream.cuda_stream, device=device) if stream.cuda_stream else torch.cuda.default_stream(device)
+    return torch.cuda.stream(stream)
+
+
+def _pages(K_pages, V_pages, table, b):
+    """(h_kv, num_pages, page_size, max_pages, k, v) of a paged cache, or ValueError."""
+    _check(K_pages, "K_pages"), _check(V_pages, "V_pages", K_pages.dtype), _check(table, "table", torch.int32)
+    if K_pages.dim() not in (3, 4) or V_pages.shape[:-1] != K_pages.shape[:-1] or table.dim() != 2 or table.shape[0] != b:
+        raise ValueError(f"shape mismatch: K_pages {tuple(K_pages.shape)} V_pages {tuple(V_pages.shape)} table {tuple(table.shape)} for {b} sequences")
+    h_kv = K_pages.shape[1] if K_pages.dim() == 4 else 1
+    return h_kv, K_pages.shape[0], K_pages.shape[-2], table.shape[1], K_pages.shape[-1], V_pages.shape[-1]
+
+
+def mqa_paged_append_kv_rows(K_pages, V_pages, table, k_new, v_new, lens, lens_out, counts=None, stream=None):
+    """K_pages [num_pages,page_size,k] (multi-query) or [num_pages,h_kv,page_size,k], V_pages likewise (float32 or bfloat16), table
+    [b,max_pages] int32: rows k_new [b,n,k] or [b,n,h_kv,k] / v_new, of sequence i the first counts[i] (None: all), go behind the lens[i] rows it has.
+    lens_out [b] int32, another tensor than lens, receives the new lengths and is returned."""
+    lib = load_library()
+    _check(k_new, "k_new", torch.float32), _check(v_new, "v_new", torch.float32)
+    _check(lens, "lens", torch.int32), _check(lens_out, "lens_out", torch.int32)
+    if counts is not None:
+        _check(counts, "counts", torch.int32)
+    b, n = k_new.shape[:2]
+    h_kv, num_pages, page_size, max_pages, k, v = _pages(K_pages, V_pages, table, b)
+    row = (b, n) if K_pages.dim() == 3 else (b, n, h_kv)
+    if (k_new.shape != row + (k,) or v_new.shape != row + (v,) or lens.numel() != b or lens_out.numel() != b
+            or (counts is not None and counts.numel() != b)):
+        raise ValueError(f"shape mismatch in mqa_paged_append_kv_rows: k_new {tuple(k_new.shape)} v_new {tuple(v_new.shape)} K_pages {tuple(K_pages.shape)}")
+    dt = _cache_dtype(K_pages)
+    with _on(_one_device(K_pages, V_pages, table, k_new, v_new, lens, lens_out, counts), stream):
+        rc = lib.mqa_paged_append_kv_rows(_ptr(k_new), _ptr(v_new), _ptr(counts), _ptr(K_pages), _ptr(V_pages), _ptr(table), _ptr(lens), _ptr(lens_out),
+                                          b, n, h_kv, num_pages, page_size, max_pages, k, v, dt, _stream(stream))
+    if rc != 0:
+        raise MqaError("mqa_paged_append_kv_rows", rc)
+    return lens_out
+
+
+def mqa_paged_decode_workspace_bytes(b, n, h, h_kv, page_size, max_pages, k, v, dt, with_scores=False) -> int:
+    """Scratch bytes that mqa_paged_decode_step uses for these sizes (0: none)."""
+    return int(load_library().mqa_paged_decode_workspace_bytes(b, n, h, h_kv, page_size, max_pages, k, v, int(dt), int(with_scores)))
+
+
+def mqa_paged_decode_step(q, K_pages, V_pages, table, lens, o=None, scale=1.0, scores=None, scores_out=None, workspace=None, stream=None):
+    """q [b,h,k], or [b,n,h,k] for the newest n tokens of every sequence (causal among them), over pages as in mqa_paged_append_kv_rows, lens [b]
+    int32 (behind their append) -> o [b,h,v] or [b,n,h,v].  scores [b,positions] (multi-query) or [b,h_kv,positions], positions = max_pages * page_size: the
+    attention weight that each position has received; scores_out receives it with this step's added (None: scores itself; scores None: from 0).
+    Workspace: a block of the call's own unless given."""
+    lib = load_library()
+    _check(q, "q", torch.float32), _check(lens, "lens", torch.int32)
+    if q.dim() not in (3, 4):
+        raise ValueError(f"q must be [b,h,k] or [b,n,h,k], not {tuple(q.shape)}")
+    b, h, n = q.shape[0], q.shape[-2], q.shape[1] if q.dim() == 4 else 1
+    h_kv, num_pages, page_size, max_pages, k, v = _pages(K_pages, V_pages, table, b)
+    if q.shape[-1] != k or lens.numel() != b:
+        raise ValueError(f"shape mismatch in mqa_paged_decode_step: q {tuple(q.shape)} K_pages {tuple(K_pages.shape)} lens {tuple(lens.shape)}")
+    if scores_out is None:
+        scores_out = scores
+    per_position = (b, max_pages * page_size) if K_pages.dim() == 3 else (b, h_kv, max_pages * page_size)
+    for name, t in (("scores", scores), ("scores_out", scores_out)):
+        if t is not None:
+            _check(t, name, torch.float32)
+            if t.shape != per_position:
+                raise ValueError(f"{name} must be {per_position}, not {tuple(t.shape)}")
+    dt = _cache_dtype(K_pages)
+    device = _one_device(q, K_pages, V_pages, table, lens, o, scores, scores_out, workspace)
+    with _on(device, stream):
+        if o is None:
+            o = torch.empty((*q.shape[:-1], v), dtype=torch.float32, device=device)
+        _check(o, "o", torch.float32)
+        if o.shape != (*q.shape[:-1], v):
+            raise ValueError(f"o must be {(*q.shape[:-1], v)}, not {tuple(o.shape)}")
+        if workspace is None:
+            workspace, nbytes = _call_workspace(mqa_paged_decode_workspace_bytes(b, n, h, h_kv, page_size, max_pages, k, v, dt, scores_out is not None),
+                                                device, stream)
+        else:
+            nbytes = workspace.numel() * workspace.element_size()
+        rc = lib.mqa_paged_decode_step(_ptr(q), _ptr(K_pages), _ptr(V_pages), _ptr(table), _ptr(lens), _ptr(o), _ptr(scores), _ptr(scores_out),
+                                       b, n, h, h_kv, num_pages, page_size, max_pages, k, v, dt, float(scale), _ptr(workspace), nbytes, _stream(stream))
+    if rc != 0:
+        raise MqaError("mqa_paged_decode_step", rc)
+    return o
+
+
+def mqa_paged_evict_kv(K_pages, V_pages, table, lens, scores, table_out, lens_out, scores_out, kept, recent, stream=None):
+    """Of every sequence (and K/V head) the latest `recent` positions and those with the largest scores, budget = kept.shape[-1] in all, are copied in their order to
+    the pages of table_out [b,max_pages_out]; lens_out [b], scores_out (as scores, for table_out's positions) and kept [b,budget] or
+    [b,h_kv,budget] int32 receive their number, their scores and which they were (-1 behind them).  Returns kept."""
+    lib = load_library()
+    i32 = torch.int32
+    _check(lens, "lens", i32), _check(lens_out, "lens_out", i32), _check(table_out, "table_out", i32), _check(kept, "kept", i32)
+    _check(scores, "scores", torch.float32), _check(scores_out, "scores_out", torch.float32)
+    b = lens.numel()
+    h_kv, num_pages, page_size, max_pages, k, v = _pages(K_pages, V_pages, table, b)
+    _, _, _, max_pages_out, _, _ = _pages(K_pages, V_pages, table_out, b)
+    lead = (b,) if K_pages.dim() == 3 else (b, h_kv)
+    if (scores.shape != lead + (max_pages * page_size,) or scores_out.shape != lead + (max_pages_out * page_size,)
+            or kept.shape[:-1] != lead or lens_out.numel() != b):
+        raise ValueError(f"shape mismatch in mqa_paged_evict_kv: scores {tuple(scores.shape)} scores_out {tuple(scores_out.shape)} kept {tuple(kept.shape)}")
+    dt = _cache_dtype(K_pages)
+    with _on(_one_device(K_pages, V_pages, table, lens, scores, table_out, lens_out, scores_out, kept), stream):
+        rc = lib.mqa_paged_evict_kv(_ptr(K_pages), _ptr(V_pages), _ptr(table), _ptr(lens), _ptr(scores), _ptr(table_out), _ptr(lens_out), _ptr(scores_out),
+                                    _ptr(kept), b, h_kv, num_pages, page_size, max_pages, max_pages_out, k, v, dt, kept.shape[-1], int(recent), _stream(stream))
+    if rc != 0:
+        raise MqaError("mqa_paged_evict_kv", rc)
+    return kept
+
+
 def mqa_stream_read(src, sink, stream=None):
     lib = load_library()
     rc = lib.mqa_stream_read(_ptr(src), src.numel() * src.element_size(), _ptr(sink), _stream(stream))
@@ -822,3 +956,40 @@ def mqa_stack_argmax(x, out=None, stream=None):
         out = torch.empty((rows,), dtype=torch.int32, device=x.device)
     _rc("mqa_stack_argmax", load_library().mqa_stack_argmax(_ptr(x), _ptr(out), rows, n, _stream(stream)))
     return out
+
+
+def mqa_stack_verify_workspace_bytes(b, n, vocab) -> int:
+    """Scratch bytes that mqa_stack_verify_drafts uses (0: unsupported sizes)."""
+    return int(load_library().mqa_stack_verify_workspace_bytes(b, n, vocab))
+
+
+def mqa_stack_verify_drafts(logits, drafts, u, draft_logits=None, counts=None, temperature=1.0, tokens=None, accepted=None, workspace=None, stream=None):
+    """logits [b,n+1,vocab] of the target, drafts [b,n] int32 (None: n = 0), u [b,n+1] float32 random numbers of [0,1) (None with temperature 0), draft_logits
+    [b,n,vocab] or None (every draft was certain), counts [b] int32 or None (n drafts each) -> tokens [b,n+1] int32, the drafts that stand and the
+    token behind them, then -1, and accepted [b] int32, how many stand.  Workspace: a block of the call's own unless given."""
+    lib = load_library()
+    _check(logits, "logits", torch.float32)
+    for name, t, dtype in (("drafts", drafts, torch.int32), ("u", u, torch.float32), ("draft_logits", draft_logits, torch.float32),
+                           ("counts", counts, torch.int32), ("tokens", tokens, torch.int32), ("accepted", accepted, torch.int32)):
+        if t is not None:
+            _check(t, name, dtype)
+    if logits.dim() != 3:
+        raise ValueError(f"logits must be [b,n+1,vocab], not {tuple(logits.shape)}")
+    b, n, vocab = logits.shape[0], logits.shape[1] - 1, logits.shape[2]
+    for name, t, shape in (("drafts", drafts, (b, n)), ("u", u, (b, n + 1)), ("draft_logits", draft_logits, (b, n, vocab)), ("counts", counts, (b,)),
+                           ("tokens", tokens, (b, n + 1)), ("accepted", accepted, (b,))):
+        if t is not None and t.shape != shape:
+            raise ValueError(f"{name} must be {shape}, not {tuple(t.shape)}")
+    device = _one_device(logits, drafts, u, draft_logits, counts, tokens, accepted, workspace)
+    with _on(device, stream):
+        if tokens is None:
+            tokens = torch.empty((b, n + 1), dtype=torch.int32, device=device)
+        if accepted is None:
+            accepted = torch.empty((b,), dtype=torch.int32, device=device)
+        if workspace is None:
+            workspace, nbytes = _call_workspace(mqa_stack_verify_workspace_bytes(b, n, vocab), device, stream)
+        else:
+            nbytes = workspace.numel() * workspace.element_size()
+        _rc("mqa_stack_verify_drafts", lib.mqa_stack_verify_drafts(_ptr(logits), _ptr(draft_logits), _ptr(drafts), _ptr(counts), _ptr(u), _ptr(tokens),
+                                                                   _ptr(accepted), b, n, vocab, float(temperature), _ptr(workspace), nbytes, _stream(stream)))
+    return tokens, accepted

@@ -1,0 +1,404 @@
+"""Paged caches on the GPU against the float64 oracle (oracle/paged.py)."""
+import numpy as np
+import pytest
+
+import mqa_inputs as mi
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+EPS = 2.0 ** -24          # half a step of float32
+
+
+@pytest.fixture(scope="module")
+def m():
+    import paper_1911_02150_amd as mod
+    mod.load_library()
+    return mod
+
+
+def rounded(x, dtype):
+    """x as a cache of this type holds it, in float64."""
+    x = np.asarray(x, dtype=np.float32)
+    return mi.bf16_bits_to_f64(mi.f32_to_bf16_bits(x)) if dtype == "bf16" else x.astype(np.float64)
+
+
+def pool(rng, num_pages, h_kv, page_size, width, dtype):
+    return rounded(rng.standard_normal((num_pages, h_kv, page_size, width)), dtype)
+
+
+def on_gpu(x, dtype=None, one_head=False):
+    """A numpy array as a device tensor; a pool of one head without the heads' axis."""
+    t = torch.from_numpy(np.ascontiguousarray(x))
+    if dtype:
+        t = t.to(torch.bfloat16 if dtype == "bf16" else torch.float32)
+    elif t.dtype == torch.float64:
+        t = t.float()
+    elif t.dtype == torch.int64:
+        t = t.to(torch.int32)
+    return (t[:, 0] if one_head else t).contiguous().to(DEV)
+
+
+def tables(rng, b, each, first=0):
+    return first + rng.permutation(b * each).reshape(b, each)
+
+
+def tolerance(q, K, size, scale, length):
+    """Half a step for each of: k products and their sum (a logit, at most scale * |q| |K|), the exponential and its argument, as many sums as there are positions, each
+    over rounding errors that do not know of one another (eight standard deviations)."""
+    k = q.shape[-1]
+    logit = abs(scale) * np.abs(q).max() * np.abs(K[np.isfinite(K)]).max() * k ** 0.5 * 4      # (4: a sum of k products of normal numbers)
+    return EPS * (2 * (8 + 4) * logit + 16 + 8 * length ** 0.5) * size + 1e-30
+
+
+# b, n, h, h_kv, k, v, page size, dtype, lengths
+ATTEND = [
+    (1, 1, 1, 1, 8, 8, 1, "f32", [1]),
+    (3, 1, 8, 1, 128, 128, 16, "bf16", [0, 1, 33]),
+    (4, 1, 8, 1, 128, 128, 16, "bf16", [511, 512, 513, 700]),
+    (2, 1, 32, 1, 128, 128, 64, "bf16", [1500, 31]),
+    (2, 1, 64, 1, 128, 128, 16, "bf16", [300, 900]),
+    (2, 1, 20, 1, 128, 128, 7, "bf16", [129, 257]),
+    (2, 5, 8, 1, 128, 128, 16, "bf16", [5, 400]),
+    (2, 3, 8, 8, 128, 128, 16, "bf16", [2, 350]),
+    (3, 1, 8, 8, 64, 64, 16, "f32", [1, 128, 600]),
+    (2, 4, 8, 2, 64, 64, 5, "f32", [3, 77]),
+    (2, 2, 12, 3, 64, 64, 16, "bf16", [290, 33]),
+    (2, 1, 8, 1, 128, 128, 16, "f32", [1025, 64]),
+    (2, 2, 24, 1, 128, 128, 100, "f32", [99, 301]),
+    (2, 2, 6, 2, 40, 24, 3, "bf16", [100, 350]),
+    (2, 1, 3, 1, 256, 256, 16, "f32", [513, 17]),
+    (1, 1, 9, 1, 16, 256, 16, "bf16", [400]),
+    (1, 1, 70, 1, 256, 8, 11, "f32", [290]),
+    (1, 128, 8, 1, 128, 128, 16, "bf16", [300]),
+    (5, 1, 1, 1, 128, 128, 32, "bf16", [0, 0, 0, 0, 0]),
+]
+
+
+@pytest.mark.parametrize("scored", [False, True])
+@pytest.mark.parametrize("b,n,h,h_kv,k,v,page,dtype,lens", ATTEND)
+def test_attention(m, b, n, h, h_kv, k, v, page, dtype, lens, scored):
+    from oracle import paged
+    rng = np.random.default_rng(b + 7 * n + 11 * h + k + len(lens))
+    each = -(-max(max(lens), 1) // page) + 3
+    K, V = (pool(rng, b * each, h_kv, page, w, dtype) for w in (k, v))
+    table, lens = tables(rng, b, each), np.array(lens)
+    q = rng.standard_normal((b, n, h, k)).astype(np.float32)
+    scores = rng.random((b, h_kv, each * page)).astype(np.float32) if scored else None
+    scale = 2 / k ** 0.5
+    want, total, size = paged.attend(q.astype(np.float64), K, V, table, lens, float(np.float32(scale)), scores)
+    one = h_kv == 1
+    args = on_gpu(q[:, 0] if n == 1 else q), on_gpu(K, dtype, one), on_gpu(V, dtype, one), on_gpu(table), on_gpu(lens)
+    kw = {}
+    if scored:
+        kw["scores"] = on_gpu(scores, one_head=one)
+        kw["scores_out"] = torch.full_like(kw["scores"], 777.0)
+    got = m.mqa_paged_decode_step(*args, scale=scale, **kw)
+    again = m.mqa_paged_decode_step(*args, scale=scale, **kw)
+    assert got.shape == ((b, h, v) if n == 1 else (b, n, h, v)) and torch.equal(got, again)
+    off = np.abs(got.cpu().numpy().reshape(want.shape) - want)
+    assert (off <= tolerance(q, K, size, scale, max(lens))).all(), off.max()
+    if scored:
+        out = kw["scores_out"].cpu().numpy().reshape(total.shape)
+        left = np.isnan(total)
+        assert (out[left] == 777).all()
+        bound = tolerance(q, K, 1, scale, max(lens)) * total + EPS * (2 + n * h / h_kv) * total
+        assert (np.abs(out - total)[~left] <= bound[~left]).all()
+        before = kw["scores"].clone()
+        m.mqa_paged_decode_step(*args, scale=scale, scores=before)                # in place
+        assert torch.equal(before.view(-1)[torch.from_numpy(~left.reshape(-1)).to(DEV)], kw["scores_out"].view(-1)[torch.from_numpy(~left.reshape(-1)).to(DEV)])
+        m.mqa_paged_decode_step(*args, scale=scale, scores_out=before)            # from nothing
+        _, zero, _ = paged.attend(q.astype(np.float64), K, V, table, lens, float(np.float32(scale)), np.zeros_like(scores))
+        assert (np.abs(before.cpu().numpy().reshape(total.shape) - zero)[~left] <= bound[~left]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("n,h,h_kv,k", [(1, 8, 1, 128), (4, 8, 1, 128), (3, 4, 4, 64), (2, 40, 1, 128), (2, 4, 2, 24)])
+def test_what_is_not_seen_may_hold_anything(m, n, h, h_kv, k, dtype):
+    """NaN and infinities behind the length, on missing pages, and at the places of later queries; lengths out of range; pages that hold nothing."""
+    from oracle import paged
+    rng = np.random.default_rng(n * h + k)
+    b, page, each = 5, 16, 6
+    K, V = (pool(rng, b * each, h_kv, page, k, dtype) for _ in range(2))
+    table, lens = tables(rng, b, each), np.array([40, -3, 1000, 65, 96])
+    clean_K, clean_V = K.copy(), V.copy()
+    table[0, 1], table[3, 0], table[3, 1], table[4] = -1, b * each, 2 ** 31 - 1, -5
+    for i in range(b):
+        length = min(max(int(lens[i]), 0), page * each)
+        for p in range(length, page * each):
+            at = paged.where(table, i, p, b * each, page)
+            if at is not None:
+                K[at[0], :, at[1]], V[at[0], :, at[1]] = np.nan, np.inf
+        for j in range(1, n):                                                 # seen by the later queries alone
+            at = paged.where(table, i, length - j, b * each, page) if length - j >= 0 else None
+            if at is not None:
+                V[at[0], :, at[1], : k // 2] = (np.inf, -np.inf, np.nan)[j % 3]
+    q = rng.standard_normal((b, n, h, k)).astype(np.float32)
+    one = h_kv == 1
+    want, total, size = paged.attend(q.astype(np.float64), K, V, table, lens, 0.25)
+    scores = torch.zeros((b, each * page) if one else (b, h_kv, each * page), device=DEV)
+    got = m.mqa_paged_decode_step(on_gpu(q), on_gpu(K, dtype, one), on_gpu(V, dtype, one), on_gpu(table), on_gpu(lens), scale=0.25, scores=scores)
+    got = got.cpu().numpy().astype(np.float64)
+    assert not got[1].any() and not got[4].any() and np.isfinite(got[:, 0]).all()
+    finite = np.isfinite(want)
+    assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(got[~finite & ~np.isnan(want)], want[~finite & ~np.isnan(want)])
+    assert (np.abs(got - want)[finite] <= tolerance(q, clean_K, size, 0.25, 96)[finite]).all()
+    there = ~np.isnan(total)
+    assert (np.abs(scores.cpu().numpy().reshape(total.shape) - total)[there] <= tolerance(q, clean_K, 1, 0.25, 96) + EPS * (n * h + 2)).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("k", [128, 64, 40])
+def test_infinite_keys(m, k, dtype):
+    """A key of -infinity that is seen has weight 0 where q is positive, and the row stays finite."""
+    rng = np.random.default_rng(k)
+    from oracle import paged
+    K, V, table, lens = pool(rng, 4, 1, 16, k, dtype), pool(rng, 4, 1, 16, k, dtype), np.array([[2, 0, 3, 1]]), np.array([50])
+    K[0, 0, 3] = K[3, 0, 15] = -np.inf
+    q = np.abs(rng.standard_normal((1, 1, 4, k))).astype(np.float32)
+    want, _, size = paged.attend(q.astype(np.float64), K, V, table, lens, 0.25)
+    assert np.isfinite(want).all()
+    got = m.mqa_paged_decode_step(on_gpu(q), on_gpu(K, dtype, True), on_gpu(V, dtype, True), on_gpu(table), on_gpu(lens), scale=0.25).cpu().numpy()
+    assert (np.abs(got - want) <= tolerance(q, K, size, 0.25, 50)).all()
+
+
+def test_large_logits(m):
+    """Logits of hundreds: one position takes all the weight, others none."""
+    from oracle import paged
+    rng = np.random.default_rng(5)
+    K, V, table, lens = pool(rng, 40, 1, 16, 128, "bf16"), pool(rng, 40, 1, 16, 128, "bf16"), tables(rng, 1, 40), np.array([640])
+    q = (20 * rng.standard_normal((1, 1, 8, 128))).astype(np.float32)
+    want, _, size = paged.attend(q.astype(np.float64), K, V, table, lens)
+    got = m.mqa_paged_decode_step(on_gpu(q[:, 0]), on_gpu(K, "bf16", True), on_gpu(V, "bf16", True), on_gpu(table), on_gpu(lens)).cpu().numpy()
+    assert (np.abs(got - want[:, 0]) <= tolerance(q, K, size, 1.0, 640)[:, 0]).all()
+
+
+def test_many_short_sequences_and_one_long(m):
+    """More sequences than a workgroup has threads, empty ones among them, against the contiguous call."""
+    g = torch.Generator(device=DEV).manual_seed(1)
+    b, each, page = 700, 40, 16
+    lens = torch.randint(0, 60, (b,), generator=g, device=DEV, dtype=torch.int32)
+    lens[::7], lens[333] = 0, each * page
+    used = torch.randn((b, each * page, 128), generator=g, device=DEV).bfloat16()
+    table = torch.randperm(b * each, generator=g, device=DEV).to(torch.int32).view(b, each)
+    K = torch.empty((b * each, page, 128), dtype=torch.bfloat16, device=DEV)
+    K[table.long()] = used.view(b, each, page, 128)
+    q = torch.randn((b, 8, 128), generator=g, device=DEV)
+    got = m.mqa_paged_decode_step(q, K, K, table, lens, scale=0.1)
+    want = m.mqa_decode_step(q, used, used, lens, scale=0.1)
+    assert not got[lens == 0].any()
+    # (the contiguous call's q and weights are two bfloat16 terms each: 2^-17 of a logit's products and of a weight)
+    assert (got - want).abs().max().item() <= 2 ** -15 * used.abs().max().item()
+
+
+@pytest.mark.parametrize("b,n,h_kv,k,v,page,dtype", [(3, 1, 1, 128, 128, 16, "bf16"), (4, 9, 3, 24, 40, 5, "f32"), (2, 40, 1, 64, 8, 7, "bf16"), (1, 1, 8, 64, 64, 1, "f32")])
+def test_append(m, b, n, h_kv, k, v, page, dtype):
+    from oracle import paged
+    rng = np.random.default_rng(n)
+    each = 12
+    K, V = (pool(rng, b * each + 1, h_kv, page, w, dtype) for w in (k, v))
+    table = tables(rng, b, each)
+    table[0, 1] = -1                                                           # a page that holds nothing: its rows are dropped
+    lens = np.array([page, page * each - n + 1, 0, -1])[:b]                    # (the second has no room for n, the fourth no length)
+    for counts in (None, np.array([n, max(0, n - 1), -2, n + 5])[:b]):
+        k_new, v_new = (rng.standard_normal((b, n, h_kv, w)).astype(np.float32) for w in (k, v))
+        wK, wV = K.copy(), V.copy()
+        want = paged.append(wK, wV, table, k_new, v_new, lens, counts, lambda x: rounded(x, dtype))
+        one = h_kv == 1
+        gK, gV, out = on_gpu(K, dtype, one), on_gpu(V, dtype, one), torch.zeros(b, dtype=torch.int32, device=DEV)
+        new = [on_gpu(x[:, :, 0] if one else x) for x in (k_new, v_new)]
+        assert m.mqa_paged_append_kv_rows(gK, gV, on_gpu(table), *new, on_gpu(lens), out, counts=None if counts is None else on_gpu(counts)) is out
+        assert out.tolist() == want.tolist()
+        assert np.array_equal(gK.double().cpu().numpy().reshape(K.shape), wK) and np.array_equal(gV.double().cpu().numpy().reshape(V.shape), wV)
+
+
+def test_append_rounds_as_the_contiguous_call(m):
+    """Halfway cases, NaN, infinities, denormals and negative zero."""
+    bits = np.array([0x3f808000, 0x3f818000, 0x3f807fff, 0x7fc00001, 0x7f800000, 0xff800000, 0x00000001, 0x80000000, 0x7f7fffff, 0x00008000, 0x807fffff, 0x7f800001],
+                    dtype=np.uint32)
+    row = torch.from_numpy(np.resize(bits, 64).view(np.float32).copy()).view(1, 1, 64).to(DEV)
+    K, lens = torch.zeros((1, 16, 64), dtype=torch.bfloat16, device=DEV), torch.zeros(1, dtype=torch.int32, device=DEV)
+    pages, table = torch.zeros((2, 16, 64), dtype=torch.bfloat16, device=DEV), torch.ones((1, 1), dtype=torch.int32, device=DEV)
+    m.mqa_paged_append_kv_rows(pages, torch.zeros_like(pages), table, row, row, lens, torch.empty_like(lens))
+    m.mqa_append_kv(K, torch.zeros_like(K), row[:, 0].contiguous(), row[:, 0].contiguous(), lens)
+    a, b = pages[1, 0].view(torch.int16), K[0, 0].view(torch.int16)
+    nan = torch.isnan(K[0, 0])
+    assert torch.equal(a[~nan], b[~nan]) and torch.isnan(pages[1, 0][nan]).all()
+
+
+EVICT = [
+    (1, 1, 8, 8, 1, "f32", [1], 1, 0),
+    (3, 1, 128, 128, 16, "bf16", [0, 40, 700], 64, 16),
+    (2, 4, 24, 40, 5, "f32", [33, 60], 20, 20),
+    (2, 2, 64, 64, 16, "bf16", [3000, 1025], 1024, 0),
+    (2, 1, 64, 8, 16, "f32", [100, 16], 100, 3),
+    (1, 1, 16, 16, 16, "f32", [5000], 77, 7),
+]
+
+
+@pytest.mark.parametrize("kind", ["random", "ties", "odd"])
+@pytest.mark.parametrize("b,h_kv,k,v,page,dtype,lens,budget,recent", EVICT)
+def test_evict(m, b, h_kv, k, v, page, dtype, lens, budget, recent, kind):
+    from oracle import paged
+    rng = np.random.default_rng(budget + len(kind))
+    each, out_each = -(-max(lens) // page) + 1, -(-budget // page) + 1
+    K, V = (pool(rng, b * (each + out_each), h_kv, page, w, dtype) for w in (k, v))
+    table, table_out = tables(rng, b, each), tables(rng, b, out_each, b * each)
+    lens = np.array(lens)
+    scores = rng.random((b, h_kv, each * page)).astype(np.float32)
+    if kind == "ties":
+        scores = np.floor(scores * 4).astype(np.float32) * np.where(rng.random(scores.shape) < 0.1, -0.0, 1).astype(np.float32)
+    if kind == "odd":                                                          # NaN, infinities, negative and tiny ones; pages that hold nothing
+        scores = np.where(rng.random(scores.shape) < 0.3, rng.choice([np.nan, np.inf, -np.inf, -1.5, 1e-42, -1e-42], scores.shape), scores - 0.5).astype(np.float32)
+        table[-1, 0], table_out[0, 0] = -1, 2 ** 31 - 1
+        lens[0] = 10 ** 9 if b > 1 else lens[0]
+    wK, wV = K.copy(), V.copy()
+    want_lens, want_kept, want_scores = paged.evict(wK, wV, table, lens, scores, table_out, budget, recent)
+    one = h_kv == 1
+    gK, gV = on_gpu(K, dtype, one), on_gpu(V, dtype, one)
+    lead = (b,) if one else (b, h_kv)
+    lens_out, kept = torch.full((b,), 9, dtype=torch.int32, device=DEV), torch.full((*lead, budget), 9, dtype=torch.int32, device=DEV)
+    scores_out = torch.full((*lead, out_each * page), 777.0, device=DEV)
+    assert m.mqa_paged_evict_kv(gK, gV, on_gpu(table), on_gpu(lens), on_gpu(scores, one_head=one), on_gpu(table_out), lens_out, scores_out, kept, recent) is kept
+    assert lens_out.tolist() == want_lens.tolist()
+    assert np.array_equal(kept.cpu().numpy().reshape(want_kept.shape), want_kept)
+    got = scores_out.cpu().numpy().reshape(want_scores.shape)
+    slots = np.arange(want_scores.shape[2]) < want_lens[:, None, None]
+    slots = np.broadcast_to(slots, got.shape)
+    assert np.array_equal(got[slots], want_scores[slots].astype(np.float32), equal_nan=True) and (got[~slots] == 777).all()
+    assert np.array_equal(gK.double().cpu().numpy().reshape(K.shape), wK) and np.array_equal(gV.double().cpu().numpy().reshape(V.shape), wV)
+
+
+def test_a_cache_on_its_way(m):
+    """Prompts appended, steps with scores, an eviction, more steps: as the oracle does them, in one captured graph and without."""
+    from oracle import paged
+    rng = np.random.default_rng(8)
+    b, h, k, page, n = 3, 8, 128, 16, 50
+    each, out_each, budget, recent = 5, 4, 40, 8
+    prompt, counts = rng.standard_normal((2, b, n, 1, k)).astype(np.float32), np.array([50, 7, 33])
+    table, table_out = tables(rng, b, each), tables(rng, b, out_each, b * each)
+    new = rng.standard_normal((4, 2, b, 1, 1, k)).astype(np.float32)
+    qs = rng.standard_normal((4, b, 1, h, k)).astype(np.float32)
+    scale = 0.125
+    K, V = (np.zeros((b * (each + out_each), 1, page, k)) for _ in range(2))
+    bf = lambda x: rounded(x, "bf16")  # noqa: E731
+    lens = paged.append(K, V, table, prompt[0], prompt[1], np.zeros(b, dtype=np.int64), counts, bf)
+    scores, outs = np.zeros((b, 1, each * page)), []
+    for t in range(2):
+        lens = paged.append(K, V, table, new[t, 0], new[t, 1], lens, rounded=bf)
+        o, scores, size = paged.attend(qs[t].astype(np.float64), K, V, table, lens, scale, np.nan_to_num(scores))
+        outs.append((o, size))
+    gpu = [on_gpu(np.zeros_like(K), "bf16", True) for _ in range(2)]
+    t_in, t_out, first = on_gpu(table), on_gpu(table_out), on_gpu(counts)
+    p, x, queries = [on_gpu(y[:, :, 0]) for y in prompt], [[on_gpu(y[:, :, 0]) for y in z] for z in new], [on_gpu(y[:, 0]) for y in qs]
+    ints = lambda *s: torch.zeros(s, dtype=torch.int32, device=DEV)  # noqa: E731
+    ls, s_in, s_out, kept, results = [ints(b) for _ in range(6)], torch.zeros((b, each * page), device=DEV), torch.zeros((b, out_each * page), device=DEV), ints(b, budget), {}
+
+    def whole():
+        s_in.zero_()
+        s_out.zero_()
+        ls[0].zero_()
+        m.mqa_paged_append_kv_rows(*gpu, t_in, *p, ls[0], ls[1], counts=first)
+        for t in range(2):
+            m.mqa_paged_append_kv_rows(*gpu, t_in, *x[t], ls[1 + t], ls[2 + t])
+            results[t] = m.mqa_paged_decode_step(queries[t], *gpu, t_in, ls[2 + t], scale=scale, scores=s_in)
+        m.mqa_paged_evict_kv(*gpu, t_in, ls[3], s_in, t_out, ls[4], s_out, kept, recent)
+        for t in range(2, 4):
+            m.mqa_paged_append_kv_rows(*gpu, t_out, *x[t], ls[2 + t], ls[3 + t]) if t == 2 else m.mqa_paged_append_kv_rows(*gpu, t_out, *x[t], ls[5], ls[0])
+            results[t] = m.mqa_paged_decode_step(queries[t], *gpu, t_out, ls[5] if t == 2 else ls[0], scale=scale, scores=s_out)
+
+    whole()
+    torch.cuda.synchronize()
+    eager = [results[t].clone() for t in range(4)]
+    got_scores = s_in.cpu().numpy().astype(np.float64)[:, None]
+    assert ls[3].tolist() == lens.tolist()
+    for t in range(2):
+        assert (np.abs(eager[t].cpu().numpy()[:, None] - outs[t][0]) <= tolerance(qs, np.concatenate([prompt[0].ravel(), new.ravel()]), outs[t][1], scale, 60)).all()
+    # from here on by the scores that the GPU has (a near tie may go either way)
+    lens, want_kept, scores = paged.evict(K, V, table, lens, got_scores, table_out, budget, recent)
+    assert np.array_equal(kept.cpu().numpy()[:, None], want_kept)
+    for t in range(2, 4):
+        lens = paged.append(K, V, table_out, new[t, 0], new[t, 1], lens, rounded=bf)
+        o, scores, size = paged.attend(qs[t].astype(np.float64), K, V, table_out, lens, scale, np.nan_to_num(scores))
+        assert (np.abs(eager[t].cpu().numpy()[:, None] - o) <= tolerance(qs, np.concatenate([prompt[0].ravel(), new.ravel()]), size, scale, 60)).all()
+    assert np.array_equal(gpu[0].double().cpu().numpy()[:, None], K)
+    graph, side = torch.cuda.CUDAGraph(), torch.cuda.Stream()
+    with torch.cuda.graph(graph, stream=side):
+        whole()
+    for _ in range(3):
+        for t in range(4):
+            results[t].zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for t in range(4):
+            assert torch.equal(results[t], eager[t])
+
+
+def test_on_another_stream_and_from_two_threads(m):
+    """Calls on streams of their own, at the same time, on workspaces of their own."""
+    import threading
+    g = torch.Generator(device=DEV).manual_seed(2)
+    K = torch.randn((256, 16, 128), generator=g, device=DEV).bfloat16()
+    table = torch.randperm(256, generator=g, device=DEV).to(torch.int32).view(2, 128)
+    lens = torch.tensor([2000, 1500], dtype=torch.int32, device=DEV)
+    qs = [torch.randn((2, 8, 128), generator=g, device=DEV) for _ in range(2)]
+    want = [m.mqa_paged_decode_step(q, K, K, table, lens) for q in qs]
+    torch.cuda.synchronize()
+    bad = []
+
+    def many(x):
+        stream = torch.cuda.Stream()
+        for r in range(50):
+            if r % 2:
+                got = m.mqa_paged_decode_step(qs[x], K, K, table, lens, stream=stream)
+            else:
+                with torch.cuda.stream(stream):
+                    got = m.mqa_paged_decode_step(qs[x], K, K, table, lens)
+            stream.synchronize()
+            if not torch.equal(got, want[x]):
+                bad.append((x, r))
+
+    threads = [threading.Thread(target=many, args=(x,)) for x in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert not bad
+
+
+def test_a_given_workspace(m):
+    g = torch.Generator(device=DEV).manual_seed(3)
+    K = torch.randn((256, 16, 128), generator=g, device=DEV).bfloat16()
+    table, lens = torch.arange(256, dtype=torch.int32, device=DEV).view(2, 128), torch.tensor([2000, 1500], dtype=torch.int32, device=DEV)
+    q = torch.randn((2, 8, 128), generator=g, device=DEV)
+    need = m.mqa_paged_decode_workspace_bytes(2, 1, 8, 1, 16, 128, 128, 128, m.MQA_BF16)
+    guard = torch.full((need + 4096,), 0x5a, dtype=torch.uint8, device=DEV)
+    o = torch.empty((2, 8, 128), device=DEV)
+    assert m.mqa_paged_decode_step(q, K, K, table, lens, o=o, workspace=guard[:need]) is o
+    assert (guard[need:] == 0x5a).all() and torch.equal(o, m.mqa_paged_decode_step(q, K, K, table, lens))
+    with pytest.raises(m.MqaError, match="workspace"):
+        m.mqa_paged_decode_step(q, K, K, table, lens, workspace=guard[:need - 16])
+
+
+def test_wrong_tensors_are_refused(m):
+    K, table = torch.zeros((8, 16, 128), dtype=torch.bfloat16, device=DEV), torch.zeros((2, 4), dtype=torch.int32, device=DEV)
+    lens, q = torch.ones(2, dtype=torch.int32, device=DEV), torch.zeros((2, 8, 128), device=DEV)
+    call = m.mqa_paged_decode_step
+    for bad in (dict(q=q[:, :, :64].contiguous()), dict(lens=lens[:1]), dict(table=table[:1]), dict(table=table.view(-1)), dict(o=torch.zeros((2, 8, 64), device=DEV)),
+                dict(scores=torch.zeros((2, 63), device=DEV)), dict(V_pages=K[:, :8].contiguous()), dict(q=q.transpose(1, 2)), dict(q=q.view(-1)),
+                dict(lens=lens.cpu()), dict(q=q[None, None])):
+        with pytest.raises(ValueError):
+            call(**{**dict(q=q, K_pages=K, V_pages=K, table=table, lens=lens), **bad})
+    for bad in (dict(q=q.double()), dict(V_pages=K.float()), dict(table=table.long()), dict(lens=lens.long()), dict(K_pages=K.half(), V_pages=K.half())):
+        with pytest.raises(TypeError):
+            call(**{**dict(q=q, K_pages=K, V_pages=K, table=table, lens=lens), **bad})
+    new = torch.zeros((2, 1, 128), device=DEV)
+    with pytest.raises(ValueError):
+        m.mqa_paged_append_kv_rows(K, K, table, new, new[:, :, :64].contiguous(), lens, lens.clone())
+    with pytest.raises(m.MqaError):
+        m.mqa_paged_append_kv_rows(K, K, table, new, new, lens, lens)
+    s, kept = torch.zeros((2, 64), device=DEV), torch.zeros((2, 8), dtype=torch.int32, device=DEV)
+    with pytest.raises(ValueError):
+        m.mqa_paged_evict_kv(K, K, table, lens, s, table.clone(), lens.clone(), s[:, :32].contiguous(), kept, 0)
+    with pytest.raises(m.MqaError):
+        m.mqa_paged_evict_kv(K, K, table, lens, s, table.clone(), lens.clone(), s.clone(), kept, 9)
