@@ -6,6 +6,8 @@
 // Positions on pages that hold nothing have weight 0, and a row that sees nothing is 0.
 #include "paged.hpp"
 
+#include <type_traits>
+
 namespace mqa {
 namespace {
 
@@ -231,69 +233,70 @@ __device__ __forceinline__ void for_segments(const PagedDecode& p, Work&& work) 
   __shared__ int s_at[2];
   const int tid = threadIdx.x;
   const long long units = (long long)p.c.h_kv * p.blocks;       // of a sequence
-  if (!p.split) {                                               // a unit each
-    const long long u = blockIdx.x;
-    Segment s;
-    s.i = (int)(u / units);
-    s.e = (int)(u % units) / p.blocks;
-    s.row0 = (int)(u % p.blocks) * p.block_rows;
-    s.L = paged_length(p.c, p.lens[s.i]);
-    s.begin = 0;
-    s.end = s.L;
-    s.slot = -1;
-    work(s);
-    return;
-  }
-  const int per = (p.b + kThreads - 1) / kThreads;
-  int tiles, mine;
-  const int before = tiles_before_me(p, per, s_waves, &tiles, &mine);
-  if (blockIdx.x == 0) {                                        // for the merge
-    int at = before;
-    for (int x = 0; x < per; ++x) {
-      const long long i = (long long)tid * per + x;
-      if (i > p.b) break;
-      p.starts[i] = at;
-      if (i < p.b) at += tiles_of(p, (int)i);
-    }
-    if (tid == 0) p.starts[p.b] = tiles;
-  }
-  const long long total = tiles * units, W = sharing(p, total), w = blockIdx.x;
-  if (w >= W || total == 0) return;
-  long long at = w * total / W;
-  const long long end = (w + 1) * total / W;
-  if (before * units <= at && at < (before + mine) * units) {   // one thread: its sequences hold the first tile
-    int b0 = before;
-    for (int x = 0; x < per; ++x) {
-      const int i = tid * per + x, t = tiles_of(p, i);
-      if (at < (b0 + t) * units) {
-        s_at[0] = i;
-        s_at[1] = b0;
-        break;
+  long long at = 0, end = 1;
+  int i = 0, first = 0;
+  if (p.split) {
+    const int per = (p.b + kThreads - 1) / kThreads;
+    int tiles, mine;
+    const int before = tiles_before_me(p, per, s_waves, &tiles, &mine);
+    if (blockIdx.x == 0) {                                      // for the merge
+      int from = before;
+      for (int x = 0; x < per; ++x) {
+        const long long seq = (long long)tid * per + x;
+        if (seq > p.b) break;
+        p.starts[seq] = from;
+        if (seq < p.b) from += tiles_of(p, (int)seq);
       }
-      b0 += t;
+      if (tid == 0) p.starts[p.b] = tiles;
     }
+    const long long total = tiles * units, W = sharing(p, total), w = blockIdx.x;
+    if (w >= W || total == 0) return;
+    at = w * total / W;
+    end = (w + 1) * total / W;
+    if (before * units <= at && at < (before + mine) * units) { // one thread: its sequences hold the first tile
+      int from = before;
+      for (int x = 0; x < per; ++x) {
+        const int seq = tid * per + x, t = tiles_of(p, seq);
+        if (at < (from + t) * units) {
+          s_at[0] = seq;
+          s_at[1] = from;
+          break;
+        }
+        from += t;
+      }
+    }
+    __syncthreads();
+    i = s_at[0];
+    first = s_at[1];
+  } else {
+    i = (int)(blockIdx.x / units);
   }
-  __syncthreads();
-  int i = s_at[0], first = s_at[1];
   while (at < end) {
-    const int L = paged_length(p.c, p.lens[i]), t = (L + kPagedTile - 1) / kPagedTile;
-    const long long off = at - first * units;
-    if (off >= t * units) {                                     // the next sequence
-      first += t;
-      ++i;
-      continue;
-    }
-    const int u = (int)(off / t), tile0 = (int)(off - (long long)u * t), count = (int)min((long long)(t - tile0), end - at);
     Segment s;
+    s.L = paged_length(p.c, p.lens[i]);
+    const int t = (s.L + kPagedTile - 1) / kPagedTile;
+    int u = (int)(blockIdx.x % units), tile0 = 0, count = t;
+    if (p.split) {
+      const long long off = at - first * units;
+      if (off >= t * units) {                                   // the next sequence
+        first += t;
+        ++i;
+        continue;
+      }
+      u = (int)(off / t);
+      tile0 = (int)(off - (long long)u * t);
+      count = (int)min((long long)(t - tile0), end - at);
+      at += count;
+    } else {
+      at = end;
+    }
     s.i = i;
     s.e = u / p.blocks;
     s.row0 = (u % p.blocks) * p.block_rows;
-    s.L = L;
     s.begin = tile0 * kPagedTile;
-    s.end = min(L, (tile0 + count) * kPagedTile);
-    s.slot = count == t ? -1 : 2 * (int)w + (tile0 > 0 ? 0 : 1);
+    s.end = min(s.L, (tile0 + count) * kPagedTile);
+    s.slot = count == t ? -1 : 2 * (int)blockIdx.x + (tile0 > 0 ? 0 : 1);
     work(s);
-    at += count;
   }
 }
 
@@ -302,6 +305,358 @@ __global__ __launch_bounds__(kThreads)
 void paged_scalar_kernel(PagedDecode p) {
   extern __shared__ __align__(16) float smem[];
   for_segments(p, [&](const Segment& s) { scalar_segment<T>(p, s, s.row0, min(p.R - s.row0, kScalarRows), smem); });
+}
+
+// ---------------------------------------------------------------- matrix instructions
+// Caches of k = v = D = 64 or 128.  A workgroup is four waves; wave w has the tiles w, w + 4, ... of a segment, for all rows of the block (16 or 32), and keeps
+// their running maximum, sum and outputs; at the end the four states are merged through LDS.  Rows go from memory straight into the operands:
+//   logits^T[32 pos x 16 rows] = K_tile . q^T: lane (i, g) = (lane % 16, lane / 16) has 16-byte pieces g, g + 4, ... of two K rows.  Row i of product u is position
+//     8 (i / 4) + 4u + i % 4 of the tile, so that lane (row, g) ends up with positions 8g .. 8g + 7: the weights are the second product's operand as they are.
+//   out^T[D cols x 16 rows] += V_tile^T . weights^T: lane (c, g) has 1/16 of the columns of rows 8g .. 8g + 7.
+// bf16: v_mfma_f32_16x16x32_bf16, q and the weights as three bf16 terms (24 bits: the float32 itself), V transposed 8 x 8 inside the lane.  float32:
+// v_mfma_f32_16x16x4_f32.  The rows' places are looked up a tile ahead: a lane has a position's table entry, the wave's 32 rows pass through LDS.
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+typedef __attribute__((ext_vector_type(4))) float floatx4;
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
+constexpr float kSlack = 8.f;        // log2 of the largest weight kept before the running maximum is moved (all rows of a wave together)
+
+__device__ __forceinline__ floatx4 mfma_bf16(const u32x4& a, const u32x4& b, const floatx4& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
+}
+// a pair of floats as three bf16 pairs whose sums are the floats
+__device__ __forceinline__ void split3(float a, float b, uint32_t (&t)[3]) {
+  t[0] = pack_bf16_pair(a, b);
+  a -= __uint_as_float(t[0] << 16);
+  b -= __uint_as_float(t[0] & 0xffff0000u);
+  t[1] = pack_bf16_pair(a, b);
+  t[2] = pack_bf16_pair(a - __uint_as_float(t[1] << 16), b - __uint_as_float(t[1] & 0xffff0000u));
+}
+
+template <typename T, int D> struct Form;
+template <int D> struct Form<uint16_t, D> {
+  static constexpr int kPieces = D / 32;                   // 16-byte pieces of a K row in a lane
+  static constexpr int kTerms = 3;
+  static constexpr int kColumns = D / 16;                  // columns of a lane
+  typedef typename std::conditional<D == 128, u32x4, u32x2>::type VRow;
+  static __device__ __forceinline__ int column(int i, int j4) { return kColumns * i + 4 * j4; }      // of the products 4 j4 ..: row i
+};
+template <int D> struct Form<float, D> {
+  static constexpr int kPieces = D / 16;
+  static constexpr int kTerms = 1;
+  static constexpr int kColumns = D / 16;
+  struct VRow { floatx4 x[D / 64]; };
+  static __device__ __forceinline__ int column(int i, int j4) { return 64 * j4 + 4 * i; }
+};
+
+constexpr int kWaves = 4;
+template <typename T, int D, int HB> constexpr size_t matrix_lds_bytes() {
+  const size_t q = (size_t)Form<T, D>::kTerms * HB * Form<T, D>::kPieces * 64 * 16, merge = ((size_t)kWaves * 16 * HB * (D + 4) + 2 * kWaves * 16 * HB) * 4;
+  const size_t plain = scalar_lds_floats(D, D) * sizeof(float), most = q > merge ? q : merge;
+  return most > plain ? most : plain;
+}
+
+template <typename T, int D, int HB>
+__device__ __forceinline__ void matrix_segment(const PagedDecode& p, const Segment& s, unsigned char* smem, int (*s_rows)[2][32], int* s_bad) {
+  typedef Form<T, D> F;
+  constexpr int NH = 16 * HB, KP = F::kPieces, KT = F::kTerms, NJ = F::kColumns, QOPS = HB * KP * 64;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i16 = lane & 15, g = lane >> 4;
+  const int32_t* table = p.c.table + (size_t)s.i * p.c.max_pages;
+  const unsigned char* Kp = static_cast<const unsigned char*>(p.c.K);
+  const unsigned char* Vp = static_cast<const unsigned char*>(p.c.V);
+  const int ntiles = (s.end - s.begin + kPagedTile - 1) / kPagedTile;
+
+  // ---- where a tile's rows are
+  int entry = -1, inside = 0;
+  auto look_up = [&](int t) {                              // lane: position lane % 32
+    const int pos = s.begin + kPagedTile * t + (lane & 31);
+    entry = -1;
+    if (pos < s.end) {
+      const unsigned page = (unsigned)pos / (unsigned)p.c.page_size;
+      inside = pos - (int)page * p.c.page_size;
+      entry = table[page];
+    }
+  };
+  struct Tile { u32x4 kr[2][KP]; typename F::VRow vr[8]; uint32_t bad; } tl;      // bad: bit e: position 8g + e is not there
+  auto publish = [&](int buf) {
+    const int row = (unsigned)entry < (unsigned)p.c.num_pages ? (entry * p.c.h_kv + s.e) * p.c.page_size + inside : -1;
+    if (lane < 32) s_rows[wave][buf][lane] = row;
+    asm volatile("" ::: "memory");
+  };
+  auto load_k = [&](int buf) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int row = s_rows[wave][buf][8 * (i16 >> 2) + 4 * u + (i16 & 3)];
+      const u32x4* src = reinterpret_cast<const u32x4*>(Kp + (size_t)max(row, 0) * (D * sizeof(T))) + g;
+#pragma unroll
+      for (int x = 0; x < KP; ++x) tl.kr[u][x] = __builtin_nontemporal_load(src + 4 * x);
+    }
+  };
+  auto load_v = [&](int buf) {
+    int rows[8];
+    *reinterpret_cast<int4*>(rows) = reinterpret_cast<const int4*>(s_rows[wave][buf])[2 * g];
+    *reinterpret_cast<int4*>(rows + 4) = reinterpret_cast<const int4*>(s_rows[wave][buf])[2 * g + 1];
+    tl.bad = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      tl.bad |= (uint32_t)(rows[e] < 0) << e;
+      const unsigned char* src = Vp + (size_t)max(rows[e], 0) * (D * sizeof(T));
+      if constexpr (sizeof(T) == 2) {
+        tl.vr[e] = __builtin_nontemporal_load(reinterpret_cast<const typename F::VRow*>(src) + i16);
+      } else {
+#pragma unroll
+        for (int x = 0; x < D / 64; ++x) tl.vr[e].x[x] = __builtin_nontemporal_load(reinterpret_cast<const floatx4*>(src) + 16 * x + i16);
+      }
+    }
+  };
+
+  __syncthreads();                                         // the LDS of the segment before is read
+  if (tid == 0) *s_bad = 0;
+  const bool any = wave < ntiles;
+  if (any) look_up(wave);
+
+  // ---- q: operands of the first product
+  u32x4* qs = reinterpret_cast<u32x4*>(smem);              // [term][block of 16 rows][piece][lane]
+  constexpr int EACH = 16 / sizeof(T);                     // values of a piece
+  for (int idx = tid; idx < NH * (D / EACH); idx += kThreads) {
+    const int r = idx / (D / EACH), c = idx - r * (D / EACH);
+    float x[EACH];
+#pragma unroll
+    for (int y = 0; y < EACH / 4; ++y) {
+      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (s.row0 + r < p.R) v = reinterpret_cast<const float4*>(p.q + row_offset(p, s.i, s.e, s.row0 + r) * D + EACH * c)[y];
+      x[4 * y] = v.x * p.qscale; x[4 * y + 1] = v.y * p.qscale; x[4 * y + 2] = v.z * p.qscale; x[4 * y + 3] = v.w * p.qscale;
+    }
+    const int slot = ((r >> 4) * KP + (c >> 2)) * 64 + (r & 15) + 16 * (c & 3);
+    if constexpr (sizeof(T) == 2) {
+      u32x4 t[3];
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        uint32_t w[3];
+        split3(x[2 * y], x[2 * y + 1], w);
+        t[0][y] = w[0]; t[1][y] = w[1]; t[2][y] = w[2];
+      }
+#pragma unroll
+      for (int y = 0; y < 3; ++y) qs[y * QOPS + slot] = t[y];
+    } else {
+      qs[slot] = u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
+    }
+  }
+  if (any) {
+    publish(0);
+    if (wave + kWaves < ntiles) look_up(wave + kWaves);
+    load_k(0);
+    load_v(0);
+  }
+  __syncthreads();
+
+  floatx4 acc[HB][NJ];
+  float m_run[HB], l_run[HB];
+  int lim[HB];
+#pragma unroll
+  for (int hb = 0; hb < HB; ++hb) {
+    m_run[hb] = -INFINITY;
+    l_run[hb] = 0.f;
+    lim[hb] = row_limit(p, s.L, min(s.row0 + 16 * hb + i16, p.R - 1));
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) acc[hb][j] = floatx4{0.f, 0.f, 0.f, 0.f};
+  }
+  const int lim_min = row_limit(p, s.L, s.row0);           // positions from here on are not seen by all rows
+
+  int buf = 0;
+  for (int t = wave; t < ntiles; t += kWaves) {
+    const int p0 = s.begin + kPagedTile * t;
+    const bool more = t + kWaves < ntiles;
+    buf ^= 1;
+    if (more) {
+      publish(buf);
+      if (t + 2 * kWaves < ntiles) look_up(t + 2 * kWaves);
+    }
+    floatx4 sc[2][HB];
+#pragma unroll
+    for (int hb = 0; hb < HB; ++hb) {
+      sc[0][hb] = sc[1][hb] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int x = 0; x < KP; ++x)
+#pragma unroll
+        for (int term = 0; term < KT; ++term) {
+          const u32x4 b = qs[term * QOPS + (hb * KP + x) * 64 + lane];
+#pragma unroll
+          for (int u = 0; u < 2; ++u) {
+            if constexpr (sizeof(T) == 2) {
+              sc[u][hb] = mfma_bf16(tl.kr[u][x], b, sc[u][hb]);
+            } else {
+#pragma unroll
+              for (int y = 0; y < 4; ++y)
+                sc[u][hb] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(tl.kr[u][x][y]), __uint_as_float(b[y]), sc[u][hb], 0, 0, 0);
+            }
+          }
+        }
+    }
+    const uint32_t bad = tl.bad;
+    if (more) load_k(buf);                                 // its registers are free
+
+    if (__any(bad != 0) || p0 + kPagedTile > lim_min) {    // what is not there, or not seen
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const bool gone = bad >> e & 1;
+#pragma unroll
+        for (int hb = 0; hb < HB; ++hb)
+          if (gone || p0 + 8 * g + e >= lim[hb]) sc[e >> 2][hb][e & 3] = -INFINITY;
+        if (gone) tl.vr[e] = typename F::VRow{};
+      }
+    }
+    if (p.logits) {
+      const size_t pitch = logits_pitch(p);
+#pragma unroll
+      for (int hb = 0; hb < HB; ++hb)
+        if (s.row0 + 16 * hb + i16 < p.R) {
+          float* at = p.logits + (((size_t)s.i * p.c.h_kv + s.e) * p.R + s.row0 + 16 * hb + i16) * pitch + p0 + 8 * g;
+          reinterpret_cast<floatx4*>(at)[0] = sc[0][hb];
+          reinterpret_cast<floatx4*>(at)[1] = sc[1][hb];
+        }
+    }
+    // ---- softmax: the running maximum is moved when a row's has grown by more than kSlack (any reference will do for the sums)
+    float w[HB][8];
+#pragma unroll
+    for (int hb = 0; hb < HB; ++hb) {
+      float mx = fmaxf(fmaxf(fmaxf(sc[0][hb][0], sc[0][hb][1]), fmaxf(sc[0][hb][2], sc[0][hb][3])),
+                       fmaxf(fmaxf(sc[1][hb][0], sc[1][hb][1]), fmaxf(sc[1][hb][2], sc[1][hb][3])));
+      mx = fmaxf(mx, __shfl_xor(mx, 16));
+      mx = fmaxf(mx, __shfl_xor(mx, 32));
+      const float mnew = fmaxf(m_run[hb], mx);
+      if (__any(mnew > m_run[hb] + kSlack)) {
+        const float alpha = __builtin_amdgcn_exp2f(m_run[hb] - (mnew == -INFINITY ? 0.f : mnew));
+        l_run[hb] *= alpha;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[hb][j] *= alpha;
+        m_run[hb] = mnew;
+      }
+      const float mref = m_run[hb] == -INFINITY ? 0.f : m_run[hb];
+      float sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        w[hb][e] = __builtin_amdgcn_exp2f(sc[e >> 2][hb][e & 3] - mref);
+        sum += w[hb][e];
+      }
+      l_run[hb] += sum;
+    }
+    // ---- outputs
+    if constexpr (sizeof(T) == 2) {
+      u32x4 wt[HB][3];
+#pragma unroll
+      for (int hb = 0; hb < HB; ++hb)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          uint32_t x[3];
+          split3(w[hb][2 * y], w[hb][2 * y + 1], x);
+          wt[hb][0][y] = x[0]; wt[hb][1][y] = x[1]; wt[hb][2][y] = x[2];
+        }
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        u32x4 a;
+#pragma unroll
+        for (int x = 0; x < 4; ++x) a[x] = __builtin_amdgcn_perm(tl.vr[2 * x + 1][j >> 1], tl.vr[2 * x][j >> 1], j & 1 ? 0x07060302u : 0x05040100u);
+#pragma unroll
+        for (int term = 0; term < 3; ++term)
+#pragma unroll
+          for (int hb = 0; hb < HB; ++hb) acc[hb][j] = mfma_bf16(a, wt[hb][term], acc[hb][j]);
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+          for (int hb = 0; hb < HB; ++hb)
+            acc[hb][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(tl.vr[e].x[j >> 2][j & 3], w[hb][e], acc[hb][j], 0, 0, 0);
+    }
+    if (more) load_v(buf);
+  }
+
+  // ---- a weight of 0 times an infinity, or one term of a product against another, is NaN: such a segment is done again in the plain form, which multiplies what is seen only
+  float odd = 0.f;
+#pragma unroll
+  for (int hb = 0; hb < HB; ++hb) {
+    odd += 0.f * l_run[hb];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j)
+#pragma unroll
+      for (int r = 0; r < 4; ++r) odd += 0.f * acc[hb][j][r];
+  }
+  if (odd != odd) *s_bad = 1;
+  __syncthreads();                                         // (the q operands are read)
+  if (*s_bad) {
+    for (int r0 = s.row0; r0 < min(p.R, s.row0 + NH); r0 += kScalarRows)
+      scalar_segment<T>(p, s, r0, min(p.R - r0, kScalarRows), reinterpret_cast<float*>(smem));
+    return;
+  }
+
+  // ---- the four waves' states
+  constexpr int PITCH = D + 4;
+  float* so = reinterpret_cast<float*>(smem);              // [wave][NH][PITCH]
+  float* sm = so + kWaves * NH * PITCH;                    // [NH][wave]
+  float* sl = sm + kWaves * NH;
+#pragma unroll
+  for (int hb = 0; hb < HB; ++hb) {
+    float* row = so + ((size_t)wave * NH + 16 * hb + i16) * PITCH;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+      for (int j4 = 0; j4 < NJ / 4; ++j4)
+        *reinterpret_cast<float4*>(row + F::column(4 * g + r, j4)) =
+            make_float4(acc[hb][4 * j4][r], acc[hb][4 * j4 + 1][r], acc[hb][4 * j4 + 2][r], acc[hb][4 * j4 + 3][r]);
+    float l = l_run[hb];                                   // the four lanes of a row share its maximum and have a part of its sum each
+    l += __shfl_xor(l, 16);
+    l += __shfl_xor(l, 32);
+    if (g == 0) {
+      sm[(16 * hb + i16) * kWaves + wave] = m_run[hb];
+      sl[(16 * hb + i16) * kWaves + wave] = l;
+    }
+  }
+  __syncthreads();
+  for (int idx = tid; idx < NH * (D / 4); idx += kThreads) {
+    const int r = idx / (D / 4), c4 = idx - r * (D / 4);
+    if (s.row0 + r >= p.R) break;
+    const float4 m4 = reinterpret_cast<const float4*>(sm)[r], l4 = reinterpret_cast<const float4*>(sl)[r];
+    const float ms[4] = {m4.x, m4.y, m4.z, m4.w}, ls[4] = {l4.x, l4.y, l4.z, l4.w};
+    const float M = fmaxf(fmaxf(ms[0], ms[1]), fmaxf(ms[2], ms[3])), ref = M == -INFINITY ? 0.f : M;
+    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+    float l = 0.f;
+#pragma unroll
+    for (int x = 0; x < kWaves; ++x) {
+      const float f = __builtin_amdgcn_exp2f(ms[x] - ref);
+      const float4 o = reinterpret_cast<const float4*>(so + ((size_t)x * NH + r) * PITCH)[c4];
+      a.x += f * o.x; a.y += f * o.y; a.z += f * o.z; a.w += f * o.w;
+      l += f * ls[x];
+    }
+    if (s.slot < 0) {
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      a.x *= inv; a.y *= inv; a.z *= inv; a.w *= inv;
+      reinterpret_cast<float4*>(p.o + row_offset(p, s.i, s.e, s.row0 + r) * D)[c4] = a;
+      if (p.stats && c4 == 0) {
+        float* stat = p.stats + (((size_t)s.i * p.c.h_kv + s.e) * p.R + s.row0 + r) * 2;
+        stat[0] = ref;
+        stat[1] = inv;
+      }
+    } else {
+      const size_t at = (size_t)s.slot * p.block_rows + r;
+      reinterpret_cast<float4*>(p.part_o + at * D)[c4] = a;
+      if (c4 == 0) {
+        p.part_m[at] = M;
+        p.part_l[at] = l;
+      }
+    }
+  }
+}
+
+template <typename T, int D, int HB>
+__global__ __launch_bounds__(kThreads, 2)
+void paged_matrix_kernel(PagedDecode p) {
+  extern __shared__ __align__(16) unsigned char smem_raw[];
+  __shared__ __align__(16) int s_rows[kWaves][2][32];
+  __shared__ int s_bad;
+  for_segments(p, [&](const Segment& s) { matrix_segment<T, D, HB>(p, s, smem_raw, s_rows, &s_bad); });
 }
 
 // ---------------------------------------------------------------- merge
@@ -436,8 +791,8 @@ static size_t lay_out(PagedDecode* p, const PagedPlan& pl, float* at) {
 PagedPlan paged_plan(int b, int n, int h, int h_kv, int page_size, int max_pages, int k, int v, int is_bf16, int with_scores) {
   PagedPlan pl = {};
   const long long R = (long long)n * (h / h_kv), positions = (long long)max_pages * page_size, tiles = (positions + kPagedTile - 1) / kPagedTile;
-  pl.mfma = false;
-  pl.block_rows = kScalarRows;
+  pl.mfma = k == v && (k == 64 || k == 128);
+  pl.block_rows = !pl.mfma ? kScalarRows : R <= 16 ? 16 : 32;
   pl.blocks = (int)((R + pl.block_rows - 1) / pl.block_rows);
   const long long units = (long long)b * h_kv * pl.blocks;
   pl.split = tiles > 8;
@@ -453,12 +808,40 @@ PagedPlan paged_plan(int b, int n, int h, int h_kv, int page_size, int max_pages
 
 void paged_workspace(PagedDecode* p, const PagedPlan& pl, void* workspace) { lay_out(p, pl, static_cast<float*>(workspace)); }
 
-hipError_t launch_paged_decode(const PagedDecode& p_in, const PagedPlan& pl, int is_bf16, hipStream_t st) {
-  PagedDecode p = p_in;
-  const size_t lds = scalar_lds_floats(p.c.k, p.c.v) * sizeof(float);
-  if (is_bf16) hipLaunchKernelGGL(paged_scalar_kernel<uint16_t>, dim3((unsigned)pl.W), dim3(kThreads), lds, st, p);
-  else hipLaunchKernelGGL(paged_scalar_kernel<float>, dim3((unsigned)pl.W), dim3(kThreads), lds, st, p);
-  hipError_t e = hipGetLastError();
+template <typename T, int D, int HB>
+static hipError_t launch_matrix(const PagedDecode& p, hipStream_t st) {
+  constexpr size_t lds = matrix_lds_bytes<T, D, HB>();
+  if (lds > 62 * 1024) {      // (of the 64 KiB that need no asking the kernel's own arrays are part) opt in, once per device
+    static bool done[64] = {};
+    int dev = 0;
+    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) dev = 0;
+    if (!done[dev]) {
+      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(paged_matrix_kernel<T, D, HB>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+      if (e != hipSuccess) return e;
+      done[dev] = true;
+    }
+  }
+  hipLaunchKernelGGL((paged_matrix_kernel<T, D, HB>), dim3((unsigned)p.W), dim3(kThreads), lds, st, p);
+  return hipGetLastError();
+}
+
+hipError_t launch_paged_decode(const PagedDecode& p, const PagedPlan& pl, int is_bf16, hipStream_t st) {
+  hipError_t e = hipErrorInvalidValue;
+  if (pl.mfma) {
+    const bool wide = pl.block_rows == 32;
+    if (p.c.k == 128) {
+      if (is_bf16) e = wide ? launch_matrix<uint16_t, 128, 2>(p, st) : launch_matrix<uint16_t, 128, 1>(p, st);
+      else e = wide ? launch_matrix<float, 128, 2>(p, st) : launch_matrix<float, 128, 1>(p, st);
+    } else {
+      if (is_bf16) e = wide ? launch_matrix<uint16_t, 64, 2>(p, st) : launch_matrix<uint16_t, 64, 1>(p, st);
+      else e = wide ? launch_matrix<float, 64, 2>(p, st) : launch_matrix<float, 64, 1>(p, st);
+    }
+  } else {
+    const size_t lds = scalar_lds_floats(p.c.k, p.c.v) * sizeof(float);
+    if (is_bf16) hipLaunchKernelGGL(paged_scalar_kernel<uint16_t>, dim3((unsigned)p.W), dim3(kThreads), lds, st, p);
+    else hipLaunchKernelGGL(paged_scalar_kernel<float>, dim3((unsigned)p.W), dim3(kThreads), lds, st, p);
+    e = hipGetLastError();
+  }
   if (e != hipSuccess) return e;
   const long long groups = (long long)p.b * p.c.h_kv;
   if (pl.split) {
