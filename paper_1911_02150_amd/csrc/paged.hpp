@@ -27,9 +27,10 @@ struct PagedAppend {
   int b, n;
 };
 
-// A decode launch's work is a list of units, (sequence, K/V head, block of query rows), each as many tiles of 32 positions as the sequence is long, one
-// behind the other; workgroup w of W takes an equal share of the tiles.  A unit that one workgroup has whole is finished there, of the others partial
-// softmax states are left in slots 2w (the unit was begun before) and 2w + 1 (it goes on behind), which a second launch merges.
+// A decode launch's work is cut into pieces: every group (sequence, K/V head) into as many, of equal length, as make them no longer than a share of all groups'
+// tiles of 32 positions; `blocks` workgroups have a piece, one for every block of query rows.  A group in one piece is finished by it; the others' pieces leave
+// partial softmax states, which a second launch merges.  (Pieces that run on from one group into the next, all of the same length, were slower: a
+// workgroup's start and end, 5 us, are then paid twice in a row.)
 struct PagedDecode {
   PagedCache c;
   const float* q;          // [b, n, h, k]
@@ -37,17 +38,17 @@ struct PagedDecode {
   float* o;                // [b, n, h, v]
   const float* scores_in;  // [b, h_kv, positions], or null: zeros
   float* scores_out;       // the same, or null
-  float* part_o;           // [slots, rows of a block, v]
-  float* part_m;           // [slots, rows of a block], log2 domain
+  float* part_o;           // [pieces, R, v]
+  float* part_m;           // [pieces, R], log2 domain
   float* part_l;
-  int32_t* starts;         // [b + 1]: tiles of the sequences before
+  int2* spans;             // [b, h_kv]: a group's first piece, and how many it has
   float* logits;           // with scores: [b, h_kv, R, positions rounded up to 32], log2 domain
-  float* stats;            // with scores: [b, h_kv, R, 2]: maximum, 1 / sum
+  float2* stats;           // with scores: [b, h_kv, R]: maximum, 1 / sum, of groups in one piece
   int b, n, h;
   int R;                   // query rows of a group: n * h / h_kv, query-major
   int block_rows, blocks;  // R in blocks
-  int W;                   // workgroups
-  int split;               // 0: workgroup w takes unit w whole
+  int shares;              // of all tiles, of which a piece has one at most
+  int split;               // 0: piece g is group g
   float qscale;            // scale * log2(e)
 };
 
@@ -65,7 +66,7 @@ struct PagedEvict {
 
 struct PagedPlan {
   bool mfma;
-  int block_rows, blocks, W, split;
+  int block_rows, blocks, shares, split, pieces;      // pieces: at most
   size_t bytes;
 };
 constexpr int kPagedTile = 32;

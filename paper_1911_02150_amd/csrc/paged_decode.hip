@@ -14,12 +14,12 @@ namespace {
 constexpr int kThreads = 256;
 constexpr int kScalarRows = 8;            // query rows of a pass of the scalar form
 
-// A run of tiles of one unit.
+// A run of tiles of one group, for one block of its query rows.
 struct Segment {
   int i, e, row0;          // sequence, head, first query row of the block
   int L;                   // the sequence's length
   int begin, end;          // positions
-  int slot;                // where its partial states go; -1: the segment is the whole unit
+  int piece;               // where its partial states go; -1: the segment is the whole group
 };
 
 __device__ __forceinline__ size_t row_offset(const PagedDecode& p, int i, int e, int r) {      // of q and o, in rows
@@ -30,6 +30,9 @@ __device__ __forceinline__ int row_limit(const PagedDecode& p, int L, int r) {  
   return max(0, L - (p.n - 1 - r / (p.h / p.c.h_kv)));
 }
 __device__ __forceinline__ size_t logits_pitch(const PagedDecode& p) { return (size_t)((p.c.positions() + kPagedTile - 1) / kPagedTile) * kPagedTile; }
+
+// What a row's weights are taken from: 2^(logit - x) y.  A row that sees nothing: weights of 0.
+__device__ __forceinline__ float2 state_of(float m, float l) { return make_float2(m == -INFINITY ? 0.f : m, l == 0.f ? 0.f : 1.f / l); }
 
 // The plain form of a segment, rows r0 .. r0 + nr - 1 of the group (nr <= 8): float32 products, any widths.  What is not seen is never multiplied, so that
 // it may hold infinities and NaN.  LDS in floats: q, one tile of K or V rows (at the end the parts of the outputs), weights, states.
@@ -170,44 +173,31 @@ __device__ void scalar_segment(const PagedDecode& p, const Segment& s, int r0, i
     for (int j = 0; j < kScalarRows; ++j) {
       if (j >= nr) break;
       float4 a = sums[j];
-      if (s.slot < 0) {
-        const float inv = s_m[j] == -INFINITY && s_l[j] == 0.f ? 0.f : 1.f / s_l[j];
+      if (s.piece < 0) {
+        const float inv = state_of(s_m[j], s_l[j]).y;
         a.x *= inv; a.y *= inv; a.z *= inv; a.w *= inv;
         reinterpret_cast<float4*>(p.o + row_offset(p, s.i, s.e, r0 + j) * v)[tid] = a;
       } else {
-        reinterpret_cast<float4*>(p.part_o + ((size_t)s.slot * p.block_rows + r0 + j - s.row0) * v)[tid] = a;
+        reinterpret_cast<float4*>(p.part_o + ((size_t)s.piece * p.R + r0 + j) * v)[tid] = a;
       }
     }
   if (tid < nr) {
-    if (s.slot >= 0) {
-      p.part_m[(size_t)s.slot * p.block_rows + r0 + tid - s.row0] = s_m[tid];
-      p.part_l[(size_t)s.slot * p.block_rows + r0 + tid - s.row0] = s_l[tid];
+    if (s.piece >= 0) {
+      p.part_m[(size_t)s.piece * p.R + r0 + tid] = s_m[tid];
+      p.part_l[(size_t)s.piece * p.R + r0 + tid] = s_l[tid];
     } else if (p.stats) {
-      float* stat = p.stats + (((size_t)s.i * p.c.h_kv + s.e) * p.R + r0 + tid) * 2;
-      stat[0] = s_m[tid] == -INFINITY ? 0.f : s_m[tid];
-      stat[1] = s_m[tid] == -INFINITY && s_l[tid] == 0.f ? 0.f : 1.f / s_l[tid];
+      p.stats[((size_t)s.i * p.c.h_kv + s.e) * p.R + r0 + tid] = state_of(s_m[tid], s_l[tid]);
     }
   }
 }
 
 // ---------------------------------------------------------------- the list of work
-__device__ __forceinline__ int tiles_of(const PagedDecode& p, int i) { return (paged_length(p.c, p.lens[i]) + kPagedTile - 1) / kPagedTile; }
+__device__ __forceinline__ int tiles_of(const PagedDecode& p, int len) { return (paged_length(p.c, len) + kPagedTile - 1) / kPagedTile; }
 
-// The workgroups that share `total` tiles: as many as have kLeastTiles each, one at least.
-constexpr int kLeastTiles = 4;
-__device__ __forceinline__ long long sharing(const PagedDecode& p, long long total) { return max(1ll, min((long long)p.W, total / kLeastTiles)); }
-// Workgroup w of W has the tiles w * total / W up to the next one's; this is the one that has tile g.
-__device__ __forceinline__ int workgroup_of(long long g, long long total, long long W) { return (int)(((g + 1) * W - 1) / total); }
-
-// Tiles of the sequences before each one, all threads of the workgroup together: thread t has sequences t * per up to the next one's.
-__device__ __forceinline__ int tiles_before_me(const PagedDecode& p, int per, int* s_waves, int* total, int* mine) {
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  int sum = 0;
-  for (int x = 0; x < per; ++x) {
-    const long long i = (long long)tid * per + x;
-    if (i < p.b) sum += tiles_of(p, (int)i);
-  }
-  int incl = sum;
+// Sum of x over the threads before this one; *all: over all.
+__device__ __forceinline__ int before_me(int x, int* s_waves, int* all) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int incl = x;
 #pragma unroll
   for (int off = 1; off < 64; off <<= 1) {
     const int y = __shfl_up(incl, off);
@@ -215,96 +205,87 @@ __device__ __forceinline__ int tiles_before_me(const PagedDecode& p, int per, in
   }
   if (lane == 63) s_waves[wave] = incl;
   __syncthreads();
-  int before = 0, all = 0;
+  int before = incl - x, sum = 0;
 #pragma unroll
   for (int w = 0; w < kThreads / 64; ++w) {
     if (w < wave) before += s_waves[w];
-    all += s_waves[w];
+    sum += s_waves[w];
   }
-  *total = all;
-  *mine = sum;
-  return before + incl - sum;
+  *all = sum;
+  return before;
 }
 
-// Runs `work` over the segments of this workgroup.
-template <typename Work>
-__device__ __forceinline__ void for_segments(const PagedDecode& p, Work&& work) {
-  __shared__ int s_waves[kThreads / 64];
-  __shared__ int s_at[2];
-  const int tid = threadIdx.x;
-  const long long units = (long long)p.c.h_kv * p.blocks;       // of a sequence
-  long long at = 0, end = 1;
-  int i = 0, first = 0;
-  if (p.split) {
-    const int per = (p.b + kThreads - 1) / kThreads;
-    int tiles, mine;
-    const int before = tiles_before_me(p, per, s_waves, &tiles, &mine);
-    if (blockIdx.x == 0) {                                      // for the merge
-      int from = before;
-      for (int x = 0; x < per; ++x) {
-        const long long seq = (long long)tid * per + x;
-        if (seq > p.b) break;
-        p.starts[seq] = from;
-        if (seq < p.b) from += tiles_of(p, (int)seq);
-      }
-      if (tid == 0) p.starts[p.b] = tiles;
-    }
-    const long long total = tiles * units, W = sharing(p, total), w = blockIdx.x;
-    if (w >= W || total == 0) return;
-    at = w * total / W;
-    end = (w + 1) * total / W;
-    if (before * units <= at && at < (before + mine) * units) { // one thread: its sequences hold the first tile
-      int from = before;
-      for (int x = 0; x < per; ++x) {
-        const int seq = tid * per + x, t = tiles_of(p, seq);
-        if (at < (from + t) * units) {
-          s_at[0] = seq;
-          s_at[1] = from;
-          break;
-        }
-        from += t;
-      }
-    }
-    __syncthreads();
-    i = s_at[0];
-    first = s_at[1];
-  } else {
-    i = (int)(blockIdx.x / units);
+// This workgroup's segment; false: there is none.  Every workgroup looks at all lengths: thread t has sequences t * each up to the next one's.
+__device__ __forceinline__ bool find_segment(const PagedDecode& p, Segment* s) {
+  __shared__ int s_waves[2][kThreads / 64];
+  __shared__ int s_at[4];
+  const int tid = threadIdx.x, heads = p.c.h_kv;
+  int piece = blockIdx.x, block = 0;
+  if (p.blocks > 1) {
+    piece = (int)(blockIdx.x / (unsigned)p.blocks);
+    block = (int)blockIdx.x - piece * p.blocks;
   }
-  while (at < end) {
-    Segment s;
-    s.L = paged_length(p.c, p.lens[i]);
-    const int t = (s.L + kPagedTile - 1) / kPagedTile;
-    int u = (int)(blockIdx.x % units), tile0 = 0, count = t;
-    if (p.split) {
-      const long long off = at - first * units;
-      if (off >= t * units) {                                   // the next sequence
-        first += t;
-        ++i;
-        continue;
-      }
-      u = (int)(off / t);
-      tile0 = (int)(off - (long long)u * t);
-      count = (int)min((long long)(t - tile0), end - at);
-      at += count;
-    } else {
-      at = end;
-    }
-    s.i = i;
-    s.e = u / p.blocks;
-    s.row0 = (u % p.blocks) * p.block_rows;
-    s.begin = tile0 * kPagedTile;
-    s.end = min(s.L, (tile0 + count) * kPagedTile);
-    s.slot = count == t ? -1 : 2 * (int)blockIdx.x + (tile0 > 0 ? 0 : 1);
-    work(s);
+  s->row0 = block * p.block_rows;
+  if (!p.split) {
+    s->i = piece / heads;
+    s->e = piece - s->i * heads;
+    s->L = paged_length(p.c, p.lens[s->i]);
+    s->begin = 0;
+    s->end = s->L;
+    s->piece = -1;
+    return true;
   }
+  const int each = (p.b + kThreads - 1) / kThreads, from = tid * each, to = min(p.b, from + each);
+  const int len = from < to ? p.lens[from] : 0;            // (up to 256 sequences: read once)
+  int mine = tiles_of(p, len);
+  for (int x = from + 1; x < to; ++x) mine += tiles_of(p, p.lens[x]);
+  int total;
+  before_me(mine, s_waves[0], &total);
+  total *= heads;
+  // tiles of a piece, at most: a whole number for each of the workgroup's four waves
+  const int per = max(1, (int)((unsigned)(total + p.shares - 1) / (unsigned)p.shares + 3) >> 2) * 4;
+  auto pieces_of = [&](int t) { return max(1, (int)((unsigned)(t + per - 1) / (unsigned)per)); };
+  int count = from < to ? pieces_of(tiles_of(p, len)) : 0;
+  for (int x = from + 1; x < to; ++x) count += pieces_of(tiles_of(p, p.lens[x]));
+  int all;
+  int before = before_me(count, s_waves[1], &all);
+  if (piece >= all * heads) return false;
+  if (before * heads <= piece && piece < (before + count) * heads) {      // one thread
+    int x = from, L = len, c = pieces_of(tiles_of(p, len));
+    while (piece >= (before + c) * heads) {
+      before += c;
+      L = p.lens[++x];
+      c = pieces_of(tiles_of(p, L));
+    }
+    s_at[0] = x;
+    s_at[1] = piece - before * heads;
+    s_at[2] = L;
+    s_at[3] = c;
+  }
+  __syncthreads();
+  s->i = __builtin_amdgcn_readfirstlane(s_at[0]);
+  const int off = __builtin_amdgcn_readfirstlane(s_at[1]), c = __builtin_amdgcn_readfirstlane(s_at[3]);
+  s->L = paged_length(p.c, __builtin_amdgcn_readfirstlane(s_at[2]));
+  s->e = heads == 1 ? 0 : off / c;
+  const int x = off - s->e * c, t = (s->L + kPagedTile - 1) / kPagedTile;
+  s->begin = 0;
+  s->end = s->L;
+  s->piece = -1;
+  if (c > 1) {
+    s->begin = (int)((unsigned)(x * t) / (unsigned)c) * kPagedTile;
+    s->end = min(s->L, (int)((unsigned)((x + 1) * t) / (unsigned)c) * kPagedTile);
+    s->piece = piece;
+  }
+  if (x == 0 && block == 0 && tid == 0) p.spans[(size_t)s->i * heads + s->e] = make_int2(piece, c);
+  return true;
 }
 
 template <typename T>
 __global__ __launch_bounds__(kThreads)
 void paged_scalar_kernel(PagedDecode p) {
   extern __shared__ __align__(16) float smem[];
-  for_segments(p, [&](const Segment& s) { scalar_segment<T>(p, s, s.row0, min(p.R - s.row0, kScalarRows), smem); });
+  Segment s;
+  if (find_segment(p, &s)) scalar_segment<T>(p, s, s.row0, min(p.R - s.row0, kScalarRows), smem);
 }
 
 // ---------------------------------------------------------------- matrix instructions
@@ -410,21 +391,37 @@ __device__ __forceinline__ void matrix_segment(const PagedDecode& p, const Segme
     }
   };
 
-  __syncthreads();                                         // the LDS of the segment before is read
   if (tid == 0) *s_bad = 0;
   const bool any = wave < ntiles;
   if (any) look_up(wave);
 
-  // ---- q: operands of the first product
-  u32x4* qs = reinterpret_cast<u32x4*>(smem);              // [term][block of 16 rows][piece][lane]
-  constexpr int EACH = 16 / sizeof(T);                     // values of a piece
-  for (int idx = tid; idx < NH * (D / EACH); idx += kThreads) {
-    const int r = idx / (D / EACH), c = idx - r * (D / EACH);
+  // ---- q, on its way before the first tile and converted while that is
+  u32x4* qs = reinterpret_cast<u32x4*>(smem);              // operands of the first product: [term][block of 16 rows][piece][lane]
+  constexpr int EACH = 16 / sizeof(T), ALL = NH * (D / EACH), ITEMS = (ALL + kThreads - 1) / kThreads;      // values of a piece; pieces of a thread
+  float4 qv[ITEMS][EACH / 4];
+#pragma unroll
+  for (int it = 0; it < ITEMS; ++it) {
+    const int idx = tid + it * kThreads, r = idx / (D / EACH), c = idx - r * (D / EACH);
+#pragma unroll
+    for (int y = 0; y < EACH / 4; ++y) {
+      qv[it][y] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (idx < ALL && s.row0 + r < p.R) qv[it][y] = reinterpret_cast<const float4*>(p.q + row_offset(p, s.i, s.e, s.row0 + r) * D + EACH * c)[y];
+    }
+  }
+  if (any) {
+    publish(0);
+    if (wave + kWaves < ntiles) look_up(wave + kWaves);
+    load_k(0);
+    load_v(0);
+  }
+#pragma unroll
+  for (int it = 0; it < ITEMS; ++it) {
+    const int idx = tid + it * kThreads, r = idx / (D / EACH), c = idx - r * (D / EACH);
+    if (idx >= ALL) break;
     float x[EACH];
 #pragma unroll
     for (int y = 0; y < EACH / 4; ++y) {
-      float4 v = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (s.row0 + r < p.R) v = reinterpret_cast<const float4*>(p.q + row_offset(p, s.i, s.e, s.row0 + r) * D + EACH * c)[y];
+      const float4 v = qv[it][y];
       x[4 * y] = v.x * p.qscale; x[4 * y + 1] = v.y * p.qscale; x[4 * y + 2] = v.z * p.qscale; x[4 * y + 3] = v.w * p.qscale;
     }
     const int slot = ((r >> 4) * KP + (c >> 2)) * 64 + (r & 15) + 16 * (c & 3);
@@ -441,12 +438,6 @@ __device__ __forceinline__ void matrix_segment(const PagedDecode& p, const Segme
     } else {
       qs[slot] = u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
     }
-  }
-  if (any) {
-    publish(0);
-    if (wave + kWaves < ntiles) look_up(wave + kWaves);
-    load_k(0);
-    load_v(0);
   }
   __syncthreads();
 
@@ -630,17 +621,13 @@ __device__ __forceinline__ void matrix_segment(const PagedDecode& p, const Segme
       a.x += f * o.x; a.y += f * o.y; a.z += f * o.z; a.w += f * o.w;
       l += f * ls[x];
     }
-    if (s.slot < 0) {
-      const float inv = l == 0.f ? 0.f : 1.f / l;
-      a.x *= inv; a.y *= inv; a.z *= inv; a.w *= inv;
+    if (s.piece < 0) {
+      const float2 state = state_of(M, l);
+      a.x *= state.y; a.y *= state.y; a.z *= state.y; a.w *= state.y;
       reinterpret_cast<float4*>(p.o + row_offset(p, s.i, s.e, s.row0 + r) * D)[c4] = a;
-      if (p.stats && c4 == 0) {
-        float* stat = p.stats + (((size_t)s.i * p.c.h_kv + s.e) * p.R + s.row0 + r) * 2;
-        stat[0] = ref;
-        stat[1] = inv;
-      }
+      if (p.stats && c4 == 0) p.stats[((size_t)s.i * p.c.h_kv + s.e) * p.R + s.row0 + r] = state;
     } else {
-      const size_t at = (size_t)s.slot * p.block_rows + r;
+      const size_t at = (size_t)s.piece * p.R + s.row0 + r;
       reinterpret_cast<float4*>(p.part_o + at * D)[c4] = a;
       if (c4 == 0) {
         p.part_m[at] = M;
@@ -656,49 +643,29 @@ void paged_matrix_kernel(PagedDecode p) {
   extern __shared__ __align__(16) unsigned char smem_raw[];
   __shared__ __align__(16) int s_rows[kWaves][2][32];
   __shared__ int s_bad;
-  for_segments(p, [&](const Segment& s) { matrix_segment<T, D, HB>(p, s, smem_raw, s_rows, &s_bad); });
+  Segment s;
+  if (find_segment(p, &s)) matrix_segment<T, D, HB>(p, s, smem_raw, s_rows, &s_bad);
 }
 
 // ---------------------------------------------------------------- merge
-// The slots of a unit that several workgroups had: the first one's second, then the others' first.
-struct Slots { int w0, w1; };
-__device__ __forceinline__ Slots slots_of(const PagedDecode& p, int i, int e, int block, bool* empty) {
-  const int t0 = p.starts[i], t = p.starts[i + 1] - t0;
-  const long long units = (long long)p.c.h_kv * p.blocks, total = p.starts[p.b] * units;
-  *empty = t == 0;
-  if (t == 0) return Slots{0, 0};
-  const long long W = sharing(p, total), g = t0 * units + ((long long)e * p.blocks + block) * t;
-  return Slots{workgroup_of(g, total, W), workgroup_of(g + t - 1, total, W)};
-}
-__device__ __forceinline__ size_t slot_of(const Slots& s, int x) { return (size_t)(x == 0 ? 2 * s.w0 + 1 : 2 * (s.w0 + x)); }
-
-// With (m_s, l_s, acc_s) the partial states: M = max m_s, l = sum l_s 2^(m_s - M), o = sum acc_s 2^(m_s - M) / l.  A workgroup has `rows` rows of a unit,
-// thread = (four columns, row, slot group).
-__global__ __launch_bounds__(256)
-void paged_merge_kernel(PagedDecode p, int rows) {
-  __shared__ float s_m[256], s_l[256];
-  __shared__ float4 s_a[256];
-  const int v4 = p.c.v >> 2, tid = threadIdx.x;
-  const int pieces = (p.block_rows + rows - 1) / rows;
-  const long long u = (long long)blockIdx.x / pieces;
-  const int block = (int)(u % p.blocks), e = (int)(u / p.blocks % p.c.h_kv), i = (int)(u / p.blocks / p.c.h_kv);
-  const int groups = 256 / (v4 * rows);
-  const int c4 = tid % v4, row = tid / v4 % rows, sg = tid / v4 / rows;
-  const int rb = (int)(blockIdx.x % pieces) * rows + row, r = block * p.block_rows + rb;      // in the block, and in the group
-  bool empty;
-  const Slots s = slots_of(p, i, e, block, &empty);
-  if (!empty && s.w0 == s.w1) return;                    // finished by its workgroup
-  const bool mine = sg < groups && rb < p.block_rows && r < p.R;
+// With (m_s, l_s, acc_s) the partial states: M = max m_s, l = sum l_s 2^(m_s - M), o = sum acc_s 2^(m_s - M) / l.  A workgroup has `rows` rows of a group,
+// thread = (four columns, row, every `parts`-th piece).
+__device__ __forceinline__ void merge_rows(const PagedDecode& p, int g, int row0, int rows, float (&s_m)[256], float (&s_l)[256], float4 (&s_a)[256]) {
+  const int2 span = p.spans[g];
+  if (span.y == 1) return;                               // finished by its piece
+  const int v4 = p.c.v >> 2, tid = threadIdx.x, parts = 256 / (v4 * rows);
+  const int line = tid / v4, c4 = tid - line * v4, part = line / rows, r = row0 + line - part * rows;
+  const bool mine = part < parts && r < p.R;
   float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
   float M = -INFINITY, l = 0.f;
-  const int count = empty ? 0 : s.w1 - s.w0 + 1;
+  const int count = span.y;
   if (mine)
-    for (int x0 = sg; x0 < count; x0 += 4 * groups) {
+    for (int x0 = part; x0 < count; x0 += 4 * parts) {
       float pm[4], pl[4];
       float4 po[4];
 #pragma unroll
       for (int x = 0; x < 4; ++x) {
-        const size_t at = slot_of(s, min(x0 + x * groups, count - 1)) * p.block_rows + rb;
+        const size_t at = ((size_t)span.x + min(x0 + x * parts, count - 1)) * p.R + r;
         pm[x] = p.part_m[at];
         pl[x] = p.part_l[at];
         po[x] = reinterpret_cast<const float4*>(p.part_o + at * p.c.v)[c4];
@@ -706,60 +673,107 @@ void paged_merge_kernel(PagedDecode p, int rows) {
       float Mn = M;
 #pragma unroll
       for (int x = 0; x < 4; ++x)
-        if (x0 + x * groups < count) Mn = fmaxf(Mn, pm[x]);
+        if (x0 + x * parts < count) Mn = fmaxf(Mn, pm[x]);
       const float ref = Mn == -INFINITY ? 0.f : Mn, f0 = __builtin_amdgcn_exp2f(M - ref);
       a.x *= f0; a.y *= f0; a.z *= f0; a.w *= f0;
       l *= f0;
 #pragma unroll
       for (int x = 0; x < 4; ++x)
-        if (x0 + x * groups < count) {
+        if (x0 + x * parts < count) {
           const float f = __builtin_amdgcn_exp2f(pm[x] - ref);
           a.x += f * po[x].x; a.y += f * po[x].y; a.z += f * po[x].z; a.w += f * po[x].w;
           l += f * pl[x];
         }
       M = Mn;
     }
-  if (groups > 1) {
+  if (parts > 1) {
     s_m[tid] = M;
     s_l[tid] = l;
     s_a[tid] = a;
     __syncthreads();
-    if (sg != 0) return;
-    const int per = v4 * rows;
-    for (int g = 1; g < groups; ++g) M = fmaxf(M, s_m[g * per + tid]);
+    if (part != 0) return;
+    const int all = v4 * rows;
+    for (int x = 1; x < parts; ++x) M = fmaxf(M, s_m[x * all + tid]);
     const float ref = M == -INFINITY ? 0.f : M;
     a = make_float4(0.f, 0.f, 0.f, 0.f);
     l = 0.f;
-    for (int g = 0; g < groups; ++g) {
-      const float f = __builtin_amdgcn_exp2f(s_m[g * per + tid] - ref);
-      const float4 x = s_a[g * per + tid];
-      a.x += f * x.x; a.y += f * x.y; a.z += f * x.z; a.w += f * x.w;
-      l += f * s_l[g * per + tid];
+    for (int x = 0; x < parts; ++x) {
+      const float f = __builtin_amdgcn_exp2f(s_m[x * all + tid] - ref);
+      const float4 o = s_a[x * all + tid];
+      a.x += f * o.x; a.y += f * o.y; a.z += f * o.z; a.w += f * o.w;
+      l += f * s_l[x * all + tid];
     }
   }
-  if (!mine || sg != 0) return;
-  const float inv = M == -INFINITY && l == 0.f ? 0.f : 1.f / l;
+  if (!mine) return;
+  const float inv = state_of(M, l).y;
   a.x *= inv; a.y *= inv; a.z *= inv; a.w *= inv;
-  reinterpret_cast<float4*>(p.o + row_offset(p, i, e, r) * p.c.v)[c4] = a;
-  if (p.stats && c4 == 0) {
-    float* stat = p.stats + (((size_t)i * p.c.h_kv + e) * p.R + r) * 2;
-    stat[0] = M == -INFINITY ? 0.f : M;
-    stat[1] = inv;
-  }
+  const int heads = p.c.h_kv, i = g / heads;
+  reinterpret_cast<float4*>(p.o + row_offset(p, i, g - i * heads, r) * p.c.v)[c4] = a;
 }
 
-// scores_out[p] = (p is older than this step's tokens ? scores_in[p] : 0) + sum over the rows of their weights at p.  A thread has a position.
-__global__ __launch_bounds__(256)
-void paged_scores_kernel(PagedDecode p, int chunks) {
-  const int g = blockIdx.x / chunks, pos = (int)(blockIdx.x % chunks) * 256 + threadIdx.x, i = g / p.c.h_kv;
-  const int L = paged_length(p.c, p.lens[i]);
+// scores_out[p] = (p is older than this step's tokens ? scores_in[p] : 0) + sum over the rows of their weights at p.  A thread has four positions.
+__device__ __forceinline__ void add_scores(const PagedDecode& p, int g, int chunk, float2* s_state) {
+  const int tid = threadIdx.x, i = g / p.c.h_kv, L = paged_length(p.c, p.lens[i]);
+  if (chunk * 1024 >= L) return;
+  int2 span = make_int2(0, 1);
+  if (p.split) span = p.spans[g];
+  if (span.y == 1) {
+    for (int r = tid; r < p.R; r += 256) s_state[r] = p.stats[(size_t)g * p.R + r];
+  } else {                                               // the rows' states from their parts': `parts` neighbouring threads a row
+    int parts = 64;
+    while (parts > 1 && parts * p.R > 256) parts >>= 1;
+    const int count = span.y, part = tid % parts;
+    for (int r = tid / parts; r < p.R; r += 256 / parts) {
+      float M = -INFINITY, l = 0.f;
+      for (int x = part; x < count; x += parts) {
+        const size_t at = ((size_t)span.x + x) * p.R + r;
+        const float m = p.part_m[at], Mn = fmaxf(M, m), ref = Mn == -INFINITY ? 0.f : Mn;
+        l = l * __builtin_amdgcn_exp2f(M - ref) + p.part_l[at] * __builtin_amdgcn_exp2f(m - ref);
+        M = Mn;
+      }
+      for (int off = 1; off < parts; off <<= 1) {
+        const float m = __shfl_xor(M, off), y = __shfl_xor(l, off), Mn = fmaxf(M, m), ref = Mn == -INFINITY ? 0.f : Mn;
+        l = l * __builtin_amdgcn_exp2f(M - ref) + y * __builtin_amdgcn_exp2f(m - ref);
+        M = Mn;
+      }
+      if (part == 0) s_state[r] = state_of(M, l);
+    }
+  }
+  __syncthreads();
+  const int pos = chunk * 1024 + 4 * tid;
   if (pos >= L) return;
-  const size_t pitch = logits_pitch(p), at = (size_t)g * p.c.positions() + pos;
+  const size_t pitch = logits_pitch(p);
   const float* z = p.logits + (size_t)g * p.R * pitch + pos;
-  const float* stat = p.stats + (size_t)g * p.R * 2;
-  float sum = 0.f;
-  for (int r = 0; r < p.R; ++r) sum += __builtin_amdgcn_exp2f(z[r * pitch] - stat[2 * r]) * stat[2 * r + 1];
-  p.scores_out[at] = (p.scores_in && pos < L - p.n ? p.scores_in[at] : 0.f) + sum;
+  float sum[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+  for (int r = 0; r < p.R; ++r) {
+    const floatx4 x = __builtin_nontemporal_load(reinterpret_cast<const floatx4*>(z + r * pitch));
+    const float2 state = s_state[r];
+#pragma unroll
+    for (int y = 0; y < 4; ++y) sum[y] += __builtin_amdgcn_exp2f(x[y] - state.x) * state.y;
+  }
+  const size_t at = (size_t)g * p.c.positions() + pos;
+#pragma unroll
+  for (int y = 0; y < 4; ++y)
+    if (pos + y < L) p.scores_out[at + y] = (p.scores_in && pos + y < L - p.n ? p.scores_in[at + y] : 0.f) + sum[y];
+}
+
+// Workgroups of merge_rows, `pieces` a group, then of add_scores, `chunks` a group.
+__global__ __launch_bounds__(256)
+void paged_finish_kernel(PagedDecode p, int rows, int pieces, int chunks) {
+  __shared__ union Shared {
+    struct { float m[256], l[256]; float4 a[256]; } merge;
+    float2 state[kPagedMaxRows];
+    __device__ Shared() {}
+  } s;
+  const unsigned merging = (unsigned)pieces * p.b * p.c.h_kv;
+  if (blockIdx.x < merging) {
+    const int g = (int)(blockIdx.x / (unsigned)pieces);
+    merge_rows(p, g, ((int)blockIdx.x - g * pieces) * rows, rows, s.merge.m, s.merge.l, s.merge.a);
+  } else {
+    const int g = (int)((blockIdx.x - merging) / (unsigned)chunks);
+    add_scores(p, g, (int)(blockIdx.x - merging) - g * chunks, s.state);
+  }
 }
 
 }  // namespace
@@ -774,16 +788,16 @@ static size_t lay_out(PagedDecode* p, const PagedPlan& pl, float* at) {
     floats += (count + 3) & ~(size_t)3;
     return here;
   };
-  const size_t slots = (size_t)2 * pl.W * pl.block_rows, rows = (size_t)p->b * p->c.h_kv * p->R;
+  const size_t states = (size_t)pl.pieces * p->R, groups = (size_t)p->b * p->c.h_kv;
   if (pl.split) {
-    p->part_o = take(slots * p->c.v);
-    p->part_m = take(slots);
-    p->part_l = take(slots);
-    p->starts = reinterpret_cast<int32_t*>(take((size_t)p->b + 1));
+    p->part_o = take(states * p->c.v);
+    p->part_m = take(states);
+    p->part_l = take(states);
+    p->spans = reinterpret_cast<int2*>(take(groups * 2));
   }
   if (p->scores_out) {
-    p->stats = take(rows * 2);
-    p->logits = take(rows * (((size_t)p->c.positions() + kPagedTile - 1) / kPagedTile * kPagedTile));
+    p->stats = reinterpret_cast<float2*>(take(groups * p->R * 2));
+    p->logits = take(groups * p->R * (((size_t)p->c.positions() + kPagedTile - 1) / kPagedTile * kPagedTile));
   }
   return floats * sizeof(float);
 }
@@ -794,10 +808,11 @@ PagedPlan paged_plan(int b, int n, int h, int h_kv, int page_size, int max_pages
   pl.mfma = k == v && (k == 64 || k == 128);
   pl.block_rows = !pl.mfma ? kScalarRows : R <= 16 ? 16 : 32;
   pl.blocks = (int)((R + pl.block_rows - 1) / pl.block_rows);
-  const long long units = (long long)b * h_kv * pl.blocks;
+  const long long groups = (long long)b * h_kv;
   pl.split = tiles > 8;
-  pl.W = pl.split ? kPagedWorkgroups : (int)units;
-  if (pl.split && units * tiles / kLeastTiles < pl.W) pl.W = (int)(units * tiles / kLeastTiles);
+  pl.shares = pl.blocks < kPagedWorkgroups ? kPagedWorkgroups / pl.blocks : 1;
+  const long long least = groups * ((tiles + 3) / 4), most = groups + pl.shares;      // (pieces of four tiles; a last, shorter one in every group)
+  pl.pieces = (int)(!pl.split ? groups : least < most ? least : most);
   PagedDecode p = {};
   p.b = b; p.R = (int)R;
   p.c.h_kv = h_kv; p.c.v = v; p.c.page_size = page_size; p.c.max_pages = max_pages;
@@ -809,7 +824,7 @@ PagedPlan paged_plan(int b, int n, int h, int h_kv, int page_size, int max_pages
 void paged_workspace(PagedDecode* p, const PagedPlan& pl, void* workspace) { lay_out(p, pl, static_cast<float*>(workspace)); }
 
 template <typename T, int D, int HB>
-static hipError_t launch_matrix(const PagedDecode& p, hipStream_t st) {
+static hipError_t launch_matrix(const PagedDecode& p, const PagedPlan& pl, hipStream_t st) {
   constexpr size_t lds = matrix_lds_bytes<T, D, HB>();
   if (lds > 62 * 1024) {      // (of the 64 KiB that need no asking the kernel's own arrays are part) opt in, once per device
     static bool done[64] = {};
@@ -821,7 +836,7 @@ static hipError_t launch_matrix(const PagedDecode& p, hipStream_t st) {
       done[dev] = true;
     }
   }
-  hipLaunchKernelGGL((paged_matrix_kernel<T, D, HB>), dim3((unsigned)p.W), dim3(kThreads), lds, st, p);
+  hipLaunchKernelGGL((paged_matrix_kernel<T, D, HB>), dim3((unsigned)pl.pieces * pl.blocks), dim3(kThreads), lds, st, p);
   return hipGetLastError();
 }
 
@@ -830,34 +845,30 @@ hipError_t launch_paged_decode(const PagedDecode& p, const PagedPlan& pl, int is
   if (pl.mfma) {
     const bool wide = pl.block_rows == 32;
     if (p.c.k == 128) {
-      if (is_bf16) e = wide ? launch_matrix<uint16_t, 128, 2>(p, st) : launch_matrix<uint16_t, 128, 1>(p, st);
-      else e = wide ? launch_matrix<float, 128, 2>(p, st) : launch_matrix<float, 128, 1>(p, st);
+      if (is_bf16) e = wide ? launch_matrix<uint16_t, 128, 2>(p, pl, st) : launch_matrix<uint16_t, 128, 1>(p, pl, st);
+      else e = wide ? launch_matrix<float, 128, 2>(p, pl, st) : launch_matrix<float, 128, 1>(p, pl, st);
     } else {
-      if (is_bf16) e = wide ? launch_matrix<uint16_t, 64, 2>(p, st) : launch_matrix<uint16_t, 64, 1>(p, st);
-      else e = wide ? launch_matrix<float, 64, 2>(p, st) : launch_matrix<float, 64, 1>(p, st);
+      if (is_bf16) e = wide ? launch_matrix<uint16_t, 64, 2>(p, pl, st) : launch_matrix<uint16_t, 64, 1>(p, pl, st);
+      else e = wide ? launch_matrix<float, 64, 2>(p, pl, st) : launch_matrix<float, 64, 1>(p, pl, st);
     }
   } else {
     const size_t lds = scalar_lds_floats(p.c.k, p.c.v) * sizeof(float);
-    if (is_bf16) hipLaunchKernelGGL(paged_scalar_kernel<uint16_t>, dim3((unsigned)p.W), dim3(kThreads), lds, st, p);
-    else hipLaunchKernelGGL(paged_scalar_kernel<float>, dim3((unsigned)p.W), dim3(kThreads), lds, st, p);
+    if (is_bf16) hipLaunchKernelGGL(paged_scalar_kernel<uint16_t>, dim3((unsigned)pl.pieces * pl.blocks), dim3(kThreads), lds, st, p);
+    else hipLaunchKernelGGL(paged_scalar_kernel<float>, dim3((unsigned)pl.pieces * pl.blocks), dim3(kThreads), lds, st, p);
     e = hipGetLastError();
   }
   if (e != hipSuccess) return e;
   const long long groups = (long long)p.b * p.c.h_kv;
-  if (pl.split) {
-    const int v4 = p.c.v >> 2, together = 256 / v4;
-    const int rows = groups * pl.blocks >= 64 ? (together < pl.block_rows ? together : pl.block_rows) : 1;
-    const long long pieces = (pl.block_rows + rows - 1) / rows;
-    hipLaunchKernelGGL(paged_merge_kernel, dim3((unsigned)(groups * pl.blocks * pieces)), dim3(256), 0, st, p, rows);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
+  int rows = 1, pieces = 0, chunks = 0;
+  if (p.split) {
+    const int together = 256 / (p.c.v >> 2);
+    rows = groups * p.R >= 512 ? (together < p.R ? together : p.R) : 1;
+    pieces = (p.R + rows - 1) / rows;
   }
-  if (p.scores_out) {
-    const long long chunks = (p.c.positions() + 255) / 256;
-    hipLaunchKernelGGL(paged_scores_kernel, dim3((unsigned)(groups * chunks)), dim3(256), 0, st, p, (int)chunks);
-    e = hipGetLastError();
-  }
-  return e;
+  if (p.scores_out) chunks = (p.c.positions() + 1023) / 1024;
+  if (pieces + chunks == 0) return hipSuccess;
+  hipLaunchKernelGGL(paged_finish_kernel, dim3((unsigned)(groups * (pieces + chunks))), dim3(256), 0, st, p, rows, pieces, chunks);
+  return hipGetLastError();
 }
 
 }  // namespace mqa
