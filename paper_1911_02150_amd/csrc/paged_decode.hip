@@ -194,7 +194,7 @@ __device__ void scalar_segment(const PagedDecode& p, const Segment& s, int r0, i
 // ---------------------------------------------------------------- the list of work
 __device__ __forceinline__ int tiles_of(const PagedDecode& p, int len) { return (paged_length(p.c, len) + kPagedTile - 1) / kPagedTile; }
 
-// Sum of x over the threads before this one; *all: over all.
+// Sum of x over the threads before this one, of the workgroup's first 256; *all: over those.
 __device__ __forceinline__ int before_me(int x, int* s_waves, int* all) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int incl = x;
@@ -203,7 +203,7 @@ __device__ __forceinline__ int before_me(int x, int* s_waves, int* all) {
     const int y = __shfl_up(incl, off);
     if (lane >= off) incl += y;
   }
-  if (lane == 63) s_waves[wave] = incl;
+  if (lane == 63 && wave < kThreads / 64) s_waves[wave] = incl;
   __syncthreads();
   int before = incl - x, sum = 0;
 #pragma unroll
@@ -283,9 +283,9 @@ __device__ __forceinline__ bool find_segment(const PagedDecode& p, Segment* s) {
 template <typename T>
 __global__ __launch_bounds__(kThreads)
 void paged_scalar_kernel(PagedDecode p) {
-  extern __shared__ __align__(16) float smem[];
+  extern __shared__ __align__(16) unsigned char smem[];
   Segment s;
-  if (find_segment(p, &s)) scalar_segment<T>(p, s, s.row0, min(p.R - s.row0, kScalarRows), smem);
+  if (find_segment(p, &s)) scalar_segment<T>(p, s, s.row0, min(p.R - s.row0, kScalarRows), reinterpret_cast<float*>(smem));
 }
 
 // ---------------------------------------------------------------- matrix instructions
@@ -330,163 +330,118 @@ template <int D> struct Form<float, D> {
   static __device__ __forceinline__ int column(int i, int j4) { return 64 * j4 + 4 * i; }
 };
 
-constexpr int kWaves = 4;
-template <typename T, int D, int HB> constexpr size_t matrix_lds_bytes() {
-  const size_t q = (size_t)Form<T, D>::kTerms * HB * Form<T, D>::kPieces * 64 * 16, merge = ((size_t)kWaves * 16 * HB * (D + 4) + 2 * kWaves * 16 * HB) * 4;
-  const size_t plain = scalar_lds_floats(D, D) * sizeof(float), most = q > merge ? q : merge;
-  return most > plain ? most : plain;
-}
+constexpr int kWaves = 4;            // that share a block of rows
+template <typename T, int D, int HB> struct Lds {
+  static constexpr size_t q = (size_t)Form<T, D>::kTerms * HB * Form<T, D>::kPieces * 64 * 16;                                   // operands
+  static constexpr size_t merge = ((size_t)kWaves * 16 * HB * (D + 4) + 2 * kWaves * 16 * HB) * 4;                             // the waves' states
+  static constexpr size_t plain = scalar_lds_floats(D, D) * sizeof(float);
+  static constexpr size_t alone = q > merge ? (q > plain ? q : plain) : (merge > plain ? merge : plain);
+};
 
-template <typename T, int D, int HB>
-__device__ __forceinline__ void matrix_segment(const PagedDecode& p, const Segment& s, unsigned char* smem, int (*s_rows)[2][32], int* s_bad) {
+template <typename T, int D> struct Tile {
+  u32x4 kr[2][Form<T, D>::kPieces];
+  typename Form<T, D>::VRow vr[8];
+};
+
+// A wave's rows, 16 HB of a group from row0 on, and what they have seen.
+template <typename T, int D, int HB, bool SCORED>
+struct Rows {
   typedef Form<T, D> F;
-  constexpr int NH = 16 * HB, KP = F::kPieces, KT = F::kTerms, NJ = F::kColumns, QOPS = HB * KP * 64;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i16 = lane & 15, g = lane >> 4;
-  const int32_t* table = p.c.table + (size_t)s.i * p.c.max_pages;
-  const unsigned char* Kp = static_cast<const unsigned char*>(p.c.K);
-  const unsigned char* Vp = static_cast<const unsigned char*>(p.c.V);
-  const int ntiles = (s.end - s.begin + kPagedTile - 1) / kPagedTile;
-
-  // ---- where a tile's rows are
-  int entry = -1, inside = 0;
-  auto look_up = [&](int t) {                              // lane: position lane % 32
-    const int pos = s.begin + kPagedTile * t + (lane & 31);
-    entry = -1;
-    if (pos < s.end) {
-      const unsigned page = (unsigned)pos / (unsigned)p.c.page_size;
-      inside = pos - (int)page * p.c.page_size;
-      entry = table[page];
-    }
-  };
-  struct Tile { u32x4 kr[2][KP]; typename F::VRow vr[8]; uint32_t bad; } tl;      // bad: bit e: position 8g + e is not there
-  auto publish = [&](int buf) {
-    const int row = (unsigned)entry < (unsigned)p.c.num_pages ? (entry * p.c.h_kv + s.e) * p.c.page_size + inside : -1;
-    if (lane < 32) s_rows[wave][buf][lane] = row;
-    asm volatile("" ::: "memory");
-  };
-  auto load_k = [&](int buf) {
-#pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int row = s_rows[wave][buf][8 * (i16 >> 2) + 4 * u + (i16 & 3)];
-      const u32x4* src = reinterpret_cast<const u32x4*>(Kp + (size_t)max(row, 0) * (D * sizeof(T))) + g;
-#pragma unroll
-      for (int x = 0; x < KP; ++x) tl.kr[u][x] = __builtin_nontemporal_load(src + 4 * x);
-    }
-  };
-  auto load_v = [&](int buf) {
-    int rows[8];
-    *reinterpret_cast<int4*>(rows) = reinterpret_cast<const int4*>(s_rows[wave][buf])[2 * g];
-    *reinterpret_cast<int4*>(rows + 4) = reinterpret_cast<const int4*>(s_rows[wave][buf])[2 * g + 1];
-    tl.bad = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      tl.bad |= (uint32_t)(rows[e] < 0) << e;
-      const unsigned char* src = Vp + (size_t)max(rows[e], 0) * (D * sizeof(T));
-      if constexpr (sizeof(T) == 2) {
-        tl.vr[e] = __builtin_nontemporal_load(reinterpret_cast<const typename F::VRow*>(src) + i16);
-      } else {
-#pragma unroll
-        for (int x = 0; x < D / 64; ++x) tl.vr[e].x[x] = __builtin_nontemporal_load(reinterpret_cast<const floatx4*>(src) + 16 * x + i16);
-      }
-    }
-  };
-
-  if (tid == 0) *s_bad = 0;
-  const bool any = wave < ntiles;
-  if (any) look_up(wave);
-
-  // ---- q, on its way before the first tile and converted while that is
-  u32x4* qs = reinterpret_cast<u32x4*>(smem);              // operands of the first product: [term][block of 16 rows][piece][lane]
-  constexpr int EACH = 16 / sizeof(T), ALL = NH * (D / EACH), ITEMS = (ALL + kThreads - 1) / kThreads;      // values of a piece; pieces of a thread
-  float4 qv[ITEMS][EACH / 4];
-#pragma unroll
-  for (int it = 0; it < ITEMS; ++it) {
-    const int idx = tid + it * kThreads, r = idx / (D / EACH), c = idx - r * (D / EACH);
-#pragma unroll
-    for (int y = 0; y < EACH / 4; ++y) {
-      qv[it][y] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (idx < ALL && s.row0 + r < p.R) qv[it][y] = reinterpret_cast<const float4*>(p.q + row_offset(p, s.i, s.e, s.row0 + r) * D + EACH * c)[y];
-    }
-  }
-  if (any) {
-    publish(0);
-    if (wave + kWaves < ntiles) look_up(wave + kWaves);
-    load_k(0);
-    load_v(0);
-  }
-#pragma unroll
-  for (int it = 0; it < ITEMS; ++it) {
-    const int idx = tid + it * kThreads, r = idx / (D / EACH), c = idx - r * (D / EACH);
-    if (idx >= ALL) break;
-    float x[EACH];
-#pragma unroll
-    for (int y = 0; y < EACH / 4; ++y) {
-      const float4 v = qv[it][y];
-      x[4 * y] = v.x * p.qscale; x[4 * y + 1] = v.y * p.qscale; x[4 * y + 2] = v.z * p.qscale; x[4 * y + 3] = v.w * p.qscale;
-    }
-    const int slot = ((r >> 4) * KP + (c >> 2)) * 64 + (r & 15) + 16 * (c & 3);
-    if constexpr (sizeof(T) == 2) {
-      u32x4 t[3];
-#pragma unroll
-      for (int y = 0; y < 4; ++y) {
-        uint32_t w[3];
-        split3(x[2 * y], x[2 * y + 1], w);
-        t[0][y] = w[0]; t[1][y] = w[1]; t[2][y] = w[2];
-      }
-#pragma unroll
-      for (int y = 0; y < 3; ++y) qs[y * QOPS + slot] = t[y];
-    } else {
-      qs[slot] = u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
-    }
-  }
-  __syncthreads();
-
+  static constexpr int NH = 16 * HB, KP = F::kPieces, KT = F::kTerms, NJ = F::kColumns, QOPS = HB * KP * 64;
+  static constexpr int EACH = 16 / sizeof(T), ALL = NH * (D / EACH), ITEMS = (ALL + kThreads - 1) / kThreads;      // values of a piece of q; pieces of a thread
   floatx4 acc[HB][NJ];
   float m_run[HB], l_run[HB];
-  int lim[HB];
-#pragma unroll
-  for (int hb = 0; hb < HB; ++hb) {
-    m_run[hb] = -INFINITY;
-    l_run[hb] = 0.f;
-    lim[hb] = row_limit(p, s.L, min(s.row0 + 16 * hb + i16, p.R - 1));
-#pragma unroll
-    for (int j = 0; j < NJ; ++j) acc[hb][j] = floatx4{0.f, 0.f, 0.f, 0.f};
-  }
-  const int lim_min = row_limit(p, s.L, s.row0);           // positions from here on are not seen by all rows
+  int lim[HB], lim_min;                // the first position that a lane's row does not see, and the first that not all rows see
 
-  int buf = 0;
-  for (int t = wave; t < ntiles; t += kWaves) {
-    const int p0 = s.begin + kPagedTile * t;
-    const bool more = t + kWaves < ntiles;
-    buf ^= 1;
-    if (more) {
-      publish(buf);
-      if (t + 2 * kWaves < ntiles) look_up(t + 2 * kWaves);
+  // q: on its way, and (tid: of the 256 threads that share the rows) as operands of the first product, [term][block of 16 rows][piece][lane]
+  struct Query { float4 v[ITEMS][EACH / 4]; };
+  static __device__ __forceinline__ void load_q(const PagedDecode& p, const Segment& s, int row0, int tid, Query* q) {
+#pragma unroll
+    for (int it = 0; it < ITEMS; ++it) {
+      const int idx = tid + it * kThreads, r = idx / (D / EACH), c = idx - r * (D / EACH);
+#pragma unroll
+      for (int y = 0; y < EACH / 4; ++y) {
+        q->v[it][y] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (idx < ALL && row0 + r < p.R) q->v[it][y] = reinterpret_cast<const float4*>(p.q + row_offset(p, s.i, s.e, row0 + r) * D + EACH * c)[y];
+      }
     }
-    floatx4 sc[2][HB];
+  }
+  static __device__ __forceinline__ void store_q(const PagedDecode& p, int tid, const Query& q, u32x4* qs) {
+#pragma unroll
+    for (int it = 0; it < ITEMS; ++it) {
+      const int idx = tid + it * kThreads, r = idx / (D / EACH), c = idx - r * (D / EACH);
+      if (idx >= ALL) break;
+      float x[EACH];
+#pragma unroll
+      for (int y = 0; y < EACH / 4; ++y) {
+        const float4 v = q.v[it][y];
+        x[4 * y] = v.x * p.qscale; x[4 * y + 1] = v.y * p.qscale; x[4 * y + 2] = v.z * p.qscale; x[4 * y + 3] = v.w * p.qscale;
+      }
+      const int slot = ((r >> 4) * KP + (c >> 2)) * 64 + (r & 15) + 16 * (c & 3);
+      if constexpr (sizeof(T) == 2) {
+        u32x4 t[3];
+#pragma unroll
+        for (int y = 0; y < 4; ++y) {
+          uint32_t w[3];
+          split3(x[2 * y], x[2 * y + 1], w);
+          t[0][y] = w[0]; t[1][y] = w[1]; t[2][y] = w[2];
+        }
+#pragma unroll
+        for (int y = 0; y < 3; ++y) qs[y * QOPS + slot] = t[y];
+      } else {
+        qs[slot] = u32x4{__float_as_uint(x[0]), __float_as_uint(x[1]), __float_as_uint(x[2]), __float_as_uint(x[3])};
+      }
+    }
+  }
+
+  __device__ __forceinline__ void begin(const PagedDecode& p, const Segment& s, int row0, int lane) {
 #pragma unroll
     for (int hb = 0; hb < HB; ++hb) {
-      sc[0][hb] = sc[1][hb] = floatx4{0.f, 0.f, 0.f, 0.f};
+      m_run[hb] = -INFINITY;
+      l_run[hb] = 0.f;
+      lim[hb] = row_limit(p, s.L, min(row0 + 16 * hb + (lane & 15), p.R - 1));
 #pragma unroll
-      for (int x = 0; x < KP; ++x)
-#pragma unroll
-        for (int term = 0; term < KT; ++term) {
-          const u32x4 b = qs[term * QOPS + (hb * KP + x) * 64 + lane];
-#pragma unroll
-          for (int u = 0; u < 2; ++u) {
-            if constexpr (sizeof(T) == 2) {
-              sc[u][hb] = mfma_bf16(tl.kr[u][x], b, sc[u][hb]);
-            } else {
-#pragma unroll
-              for (int y = 0; y < 4; ++y)
-                sc[u][hb] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(tl.kr[u][x][y]), __uint_as_float(b[y]), sc[u][hb], 0, 0, 0);
-            }
-          }
-        }
+      for (int j = 0; j < NJ; ++j) acc[hb][j] = floatx4{0.f, 0.f, 0.f, 0.f};
     }
-    const uint32_t bad = tl.bad;
-    if (more) load_k(buf);                                 // its registers are free
+    lim_min = row_limit(p, s.L, min(row0, p.R - 1));
+  }
 
+  // logits of a tile, from its K rows
+  static __device__ __forceinline__ void first_product(const Tile<T, D>& tl, const u32x4* qs, int lane, floatx4 (&sc)[2][HB]) {
+    u32x4 b[2][KT][HB];                // q of a piece, read while the one before is multiplied
+    auto read = [&](int x) {
+#pragma unroll
+      for (int term = 0; term < KT; ++term)
+#pragma unroll
+        for (int hb = 0; hb < HB; ++hb) b[x & 1][term][hb] = qs[term * QOPS + (hb * KP + x) * 64 + lane];
+    };
+    read(0);
+#pragma unroll
+    for (int hb = 0; hb < HB; ++hb) sc[0][hb] = sc[1][hb] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int x = 0; x < KP; ++x) {
+      if (x + 1 < KP) read(x + 1);
+      __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+      for (int term = 0; term < KT; ++term)
+#pragma unroll
+        for (int y = 0; y < (sizeof(T) == 2 ? 1 : 4); ++y)
+#pragma unroll
+          for (int hb = 0; hb < HB; ++hb)
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              if constexpr (sizeof(T) == 2)
+                sc[u][hb] = mfma_bf16(tl.kr[u][x], b[x & 1][term][hb], sc[u][hb]);
+              else
+                sc[u][hb] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(tl.kr[u][x][y]), __uint_as_float(b[x & 1][term][hb][y]), sc[u][hb], 0, 0, 0);
+            }
+      __builtin_amdgcn_sched_barrier(0);
+    }
+  }
+
+  // the softmax of a tile from position p0 on, and its V rows; bad: bit e: position p0 + 8g + e is not there
+  __device__ __forceinline__ void second_product(const PagedDecode& p, const Segment& s, int row0, int lane, int p0, uint32_t bad, floatx4 (&sc)[2][HB], Tile<T, D>& tl) {
+    const int i16 = lane & 15, g = lane >> 4;
     if (__any(bad != 0) || p0 + kPagedTile > lim_min) {    // what is not there, or not seen
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
@@ -497,26 +452,26 @@ __device__ __forceinline__ void matrix_segment(const PagedDecode& p, const Segme
         if (gone) tl.vr[e] = typename F::VRow{};
       }
     }
-    if (p.logits) {
+    if constexpr (SCORED) {
       const size_t pitch = logits_pitch(p);
 #pragma unroll
       for (int hb = 0; hb < HB; ++hb)
-        if (s.row0 + 16 * hb + i16 < p.R) {
-          float* at = p.logits + (((size_t)s.i * p.c.h_kv + s.e) * p.R + s.row0 + 16 * hb + i16) * pitch + p0 + 8 * g;
+        if (row0 + 16 * hb + i16 < p.R) {
+          float* at = p.logits + (((size_t)s.i * p.c.h_kv + s.e) * p.R + row0 + 16 * hb + i16) * pitch + p0 + 8 * g;
           reinterpret_cast<floatx4*>(at)[0] = sc[0][hb];
           reinterpret_cast<floatx4*>(at)[1] = sc[1][hb];
         }
     }
-    // ---- softmax: the running maximum is moved when a row's has grown by more than kSlack (any reference will do for the sums)
+    // the running maximum is moved when a row's has grown by more than kSlack (any reference will do for the sums)
     float w[HB][8];
 #pragma unroll
     for (int hb = 0; hb < HB; ++hb) {
       float mx = fmaxf(fmaxf(fmaxf(sc[0][hb][0], sc[0][hb][1]), fmaxf(sc[0][hb][2], sc[0][hb][3])),
                        fmaxf(fmaxf(sc[1][hb][0], sc[1][hb][1]), fmaxf(sc[1][hb][2], sc[1][hb][3])));
-      mx = fmaxf(mx, __shfl_xor(mx, 16));
-      mx = fmaxf(mx, __shfl_xor(mx, 32));
-      const float mnew = fmaxf(m_run[hb], mx);
-      if (__any(mnew > m_run[hb] + kSlack)) {
+      if (__any(mx > m_run[hb] + kSlack)) {
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        const float mnew = fmaxf(m_run[hb], mx);
         const float alpha = __builtin_amdgcn_exp2f(m_run[hb] - (mnew == -INFINITY ? 0.f : mnew));
         l_run[hb] *= alpha;
 #pragma unroll
@@ -532,7 +487,6 @@ __device__ __forceinline__ void matrix_segment(const PagedDecode& p, const Segme
       }
       l_run[hb] += sum;
     }
-    // ---- outputs
     if constexpr (sizeof(T) == 2) {
       u32x4 wt[HB][3];
 #pragma unroll
@@ -543,16 +497,17 @@ __device__ __forceinline__ void matrix_segment(const PagedDecode& p, const Segme
           split3(w[hb][2 * y], w[hb][2 * y + 1], x);
           wt[hb][0][y] = x[0]; wt[hb][1][y] = x[1]; wt[hb][2][y] = x[2];
         }
+      u32x4 a[NJ];                                         // (all of V first: then the products of a sum are far apart)
 #pragma unroll
-      for (int j = 0; j < NJ; ++j) {
-        u32x4 a;
+      for (int j = 0; j < NJ; ++j)
 #pragma unroll
-        for (int x = 0; x < 4; ++x) a[x] = __builtin_amdgcn_perm(tl.vr[2 * x + 1][j >> 1], tl.vr[2 * x][j >> 1], j & 1 ? 0x07060302u : 0x05040100u);
+        for (int x = 0; x < 4; ++x) a[j][x] = __builtin_amdgcn_perm(tl.vr[2 * x + 1][j >> 1], tl.vr[2 * x][j >> 1], j & 1 ? 0x07060302u : 0x05040100u);
 #pragma unroll
-        for (int term = 0; term < 3; ++term)
+      for (int term = 0; term < 3; ++term)
 #pragma unroll
-          for (int hb = 0; hb < HB; ++hb) acc[hb][j] = mfma_bf16(a, wt[hb][term], acc[hb][j]);
-      }
+        for (int j = 0; j < NJ; ++j)
+#pragma unroll
+          for (int hb = 0; hb < HB; ++hb) acc[hb][j] = mfma_bf16(a[j], wt[hb][term], acc[hb][j]);
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
@@ -562,89 +517,186 @@ __device__ __forceinline__ void matrix_segment(const PagedDecode& p, const Segme
           for (int hb = 0; hb < HB; ++hb)
             acc[hb][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(tl.vr[e].x[j >> 2][j & 3], w[hb][e], acc[hb][j], 0, 0, 0);
     }
-    if (more) load_v(buf);
   }
 
-  // ---- a weight of 0 times an infinity, or one term of a product against another, is NaN: such a segment is done again in the plain form, which multiplies what is seen only
-  float odd = 0.f;
+  // A weight of 0 times an infinity, or one term of a product against another, is NaN: such a segment is done again in the plain form, which multiplies what is seen only.
+  __device__ __forceinline__ bool odd() const {
+    float x = 0.f;
 #pragma unroll
-  for (int hb = 0; hb < HB; ++hb) {
-    odd += 0.f * l_run[hb];
+    for (int hb = 0; hb < HB; ++hb) {
+      x += 0.f * l_run[hb];
 #pragma unroll
-    for (int j = 0; j < NJ; ++j)
+      for (int j = 0; j < NJ; ++j)
 #pragma unroll
-      for (int r = 0; r < 4; ++r) odd += 0.f * acc[hb][j][r];
-  }
-  if (odd != odd) *s_bad = 1;
-  __syncthreads();                                         // (the q operands are read)
-  if (*s_bad) {
-    for (int r0 = s.row0; r0 < min(p.R, s.row0 + NH); r0 += kScalarRows)
-      scalar_segment<T>(p, s, r0, min(p.R - r0, kScalarRows), reinterpret_cast<float*>(smem));
-    return;
+        for (int r = 0; r < 4; ++r) x += 0.f * acc[hb][j][r];
+    }
+    return x != x;
   }
 
-  // ---- the four waves' states
-  constexpr int PITCH = D + 4;
-  float* so = reinterpret_cast<float*>(smem);              // [wave][NH][PITCH]
-  float* sm = so + kWaves * NH * PITCH;                    // [NH][wave]
-  float* sl = sm + kWaves * NH;
+  // The four waves' states in one (all 256 threads that share the rows; `lds` is theirs), and where it goes.
+  static constexpr int PITCH = D + 4;
+  __device__ __forceinline__ void put(float* lds, int wave, int lane) const {
+    const int i16 = lane & 15, g = lane >> 4;
+    float *sm = lds + kWaves * NH * PITCH, *sl = sm + kWaves * NH;
 #pragma unroll
-  for (int hb = 0; hb < HB; ++hb) {
-    float* row = so + ((size_t)wave * NH + 16 * hb + i16) * PITCH;
+    for (int hb = 0; hb < HB; ++hb) {
+      float* row = lds + ((size_t)wave * NH + 16 * hb + i16) * PITCH;
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
+      for (int r = 0; r < 4; ++r)
 #pragma unroll
-      for (int j4 = 0; j4 < NJ / 4; ++j4)
-        *reinterpret_cast<float4*>(row + F::column(4 * g + r, j4)) =
-            make_float4(acc[hb][4 * j4][r], acc[hb][4 * j4 + 1][r], acc[hb][4 * j4 + 2][r], acc[hb][4 * j4 + 3][r]);
-    float l = l_run[hb];                                   // the four lanes of a row share its maximum and have a part of its sum each
-    l += __shfl_xor(l, 16);
-    l += __shfl_xor(l, 32);
-    if (g == 0) {
-      sm[(16 * hb + i16) * kWaves + wave] = m_run[hb];
-      sl[(16 * hb + i16) * kWaves + wave] = l;
-    }
-  }
-  __syncthreads();
-  for (int idx = tid; idx < NH * (D / 4); idx += kThreads) {
-    const int r = idx / (D / 4), c4 = idx - r * (D / 4);
-    if (s.row0 + r >= p.R) break;
-    const float4 m4 = reinterpret_cast<const float4*>(sm)[r], l4 = reinterpret_cast<const float4*>(sl)[r];
-    const float ms[4] = {m4.x, m4.y, m4.z, m4.w}, ls[4] = {l4.x, l4.y, l4.z, l4.w};
-    const float M = fmaxf(fmaxf(ms[0], ms[1]), fmaxf(ms[2], ms[3])), ref = M == -INFINITY ? 0.f : M;
-    float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
-    float l = 0.f;
-#pragma unroll
-    for (int x = 0; x < kWaves; ++x) {
-      const float f = __builtin_amdgcn_exp2f(ms[x] - ref);
-      const float4 o = reinterpret_cast<const float4*>(so + ((size_t)x * NH + r) * PITCH)[c4];
-      a.x += f * o.x; a.y += f * o.y; a.z += f * o.z; a.w += f * o.w;
-      l += f * ls[x];
-    }
-    if (s.piece < 0) {
-      const float2 state = state_of(M, l);
-      a.x *= state.y; a.y *= state.y; a.z *= state.y; a.w *= state.y;
-      reinterpret_cast<float4*>(p.o + row_offset(p, s.i, s.e, s.row0 + r) * D)[c4] = a;
-      if (p.stats && c4 == 0) p.stats[((size_t)s.i * p.c.h_kv + s.e) * p.R + s.row0 + r] = state;
-    } else {
-      const size_t at = (size_t)s.piece * p.R + s.row0 + r;
-      reinterpret_cast<float4*>(p.part_o + at * D)[c4] = a;
-      if (c4 == 0) {
-        p.part_m[at] = M;
-        p.part_l[at] = l;
+        for (int j4 = 0; j4 < NJ / 4; ++j4)
+          *reinterpret_cast<float4*>(row + F::column(4 * g + r, j4)) =
+              make_float4(acc[hb][4 * j4][r], acc[hb][4 * j4 + 1][r], acc[hb][4 * j4 + 2][r], acc[hb][4 * j4 + 3][r]);
+      float l = l_run[hb];                                 // the four lanes of a row share its maximum and have a part of its sum each
+      l += __shfl_xor(l, 16);
+      l += __shfl_xor(l, 32);
+      if (g == 0) {
+        sm[(16 * hb + i16) * kWaves + wave] = m_run[hb];
+        sl[(16 * hb + i16) * kWaves + wave] = l;
       }
     }
   }
+  static __device__ __forceinline__ void finish(const PagedDecode& p, const Segment& s, int row0, const float* lds, int tid) {
+    const float *sm = lds + kWaves * NH * PITCH, *sl = sm + kWaves * NH;
+    for (int idx = tid; idx < NH * (D / 4); idx += kThreads) {
+      const int r = idx / (D / 4), c4 = idx - r * (D / 4);
+      if (row0 + r >= p.R) break;
+      const float4 m4 = reinterpret_cast<const float4*>(sm)[r], l4 = reinterpret_cast<const float4*>(sl)[r];
+      const float ms[4] = {m4.x, m4.y, m4.z, m4.w}, ls[4] = {l4.x, l4.y, l4.z, l4.w};
+      const float M = fmaxf(fmaxf(ms[0], ms[1]), fmaxf(ms[2], ms[3])), ref = M == -INFINITY ? 0.f : M;
+      float4 a = make_float4(0.f, 0.f, 0.f, 0.f);
+      float l = 0.f;
+#pragma unroll
+      for (int x = 0; x < kWaves; ++x) {
+        const float f = __builtin_amdgcn_exp2f(ms[x] - ref);
+        const float4 o = reinterpret_cast<const float4*>(lds + ((size_t)x * NH + r) * PITCH)[c4];
+        a.x += f * o.x; a.y += f * o.y; a.z += f * o.z; a.w += f * o.w;
+        l += f * ls[x];
+      }
+      if (s.piece < 0) {
+        const float2 state = state_of(M, l);
+        a.x *= state.y; a.y *= state.y; a.z *= state.y; a.w *= state.y;
+        reinterpret_cast<float4*>(p.o + row_offset(p, s.i, s.e, row0 + r) * D)[c4] = a;
+        if (p.stats && c4 == 0) p.stats[((size_t)s.i * p.c.h_kv + s.e) * p.R + row0 + r] = state;
+      } else {
+        const size_t at = (size_t)s.piece * p.R + row0 + r;
+        reinterpret_cast<float4*>(p.part_o + at * D)[c4] = a;
+        if (c4 == 0) {
+          p.part_m[at] = M;
+          p.part_l[at] = l;
+        }
+      }
+    }
+  }
+};
+
+template <typename T>
+__device__ __forceinline__ void in_plain_form(const PagedDecode& p, const Segment& s, int rows, unsigned char* smem) {
+  for (int r0 = s.row0; r0 < min(p.R, s.row0 + rows); r0 += kScalarRows) scalar_segment<T>(p, s, r0, min(p.R - r0, kScalarRows), reinterpret_cast<float*>(smem));
 }
 
-template <typename T, int D, int HB>
-__global__ __launch_bounds__(kThreads, 2)
+// TEAMS: two (of four waves, 32 rows each) for up to 64 query rows: the waves that have the same tiles read them at about the same time, from memory once and
+// for the other from L2.
+template <typename T, int D, int HB, int TEAMS, bool SCORED>
+__global__ __launch_bounds__(TEAMS * kThreads, 2)
 void paged_matrix_kernel(PagedDecode p) {
-  extern __shared__ __align__(16) unsigned char smem_raw[];
-  __shared__ __align__(16) int s_rows[kWaves][2][32];
-  __shared__ int s_bad;
+  typedef Rows<T, D, HB, SCORED> R;
+  typedef Form<T, D> F;
+  extern __shared__ __align__(16) unsigned char smem[];
+  __shared__ __align__(16) int s_rows[TEAMS * kWaves][2][32];
+  __shared__ int s_odd;
   Segment s;
-  if (find_segment(p, &s)) matrix_segment<T, D, HB>(p, s, smem_raw, s_rows, &s_bad);
+  if (!find_segment(p, &s)) return;
+  const int team = TEAMS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads) : 0, tid = threadIdx.x - team * kThreads, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), i16 = lane & 15, g = lane >> 4, row0 = s.row0 + team * R::NH;
+  int (&places)[2][32] = s_rows[team * kWaves + wave];
+  unsigned char* const lds = smem + team * Lds<T, D, HB>::alone;
+  const int32_t* table = p.c.table + (size_t)s.i * p.c.max_pages;
+  const unsigned char* Kp = static_cast<const unsigned char*>(p.c.K);
+  const unsigned char* Vp = static_cast<const unsigned char*>(p.c.V);
+  const int ntiles = (s.end - s.begin + kPagedTile - 1) / kPagedTile;
+
+  // ---- where a tile's rows are: a lane asks for position lane % 32's.  (A tile past the end is none of the cache's, and is read as the pool's first row: without a
+  // branch around them the loads stay in order, and a wait is for those that are needed.)
+  struct Place { int entry, inside; };                     // inside: of the page; -1: past the end
+  auto look_up = [&](int t) {
+    const int pos = s.begin + kPagedTile * t + (lane & 31), inside = min(pos, max(s.end - 1, 0));
+    const unsigned page = (unsigned)inside / (unsigned)p.c.page_size;
+    return Place{table[page], pos < s.end ? inside - (int)page * p.c.page_size : -1};
+  };
+  Tile<T, D> tl;
+  uint32_t bad;                                            // bit e: position 8g + e of the tile is not there
+  auto publish = [&](const Place& x, int buf) {
+    const bool there = (unsigned)x.entry < (unsigned)p.c.num_pages && x.inside >= 0;
+    places[buf][lane & 31] = there ? (x.entry * p.c.h_kv + s.e) * p.c.page_size + x.inside : -1;
+    asm volatile("" ::: "memory");
+  };
+  auto read = [](const auto* at) {                         // once, or by both teams
+    if constexpr (TEAMS == 1) return __builtin_nontemporal_load(at);
+    else return *at;
+  };
+  auto load_k = [&](int buf) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int row = places[buf][8 * (i16 >> 2) + 4 * u + (i16 & 3)];
+      const u32x4* src = reinterpret_cast<const u32x4*>(Kp + (size_t)max(row, 0) * (D * sizeof(T))) + g;
+#pragma unroll
+      for (int x = 0; x < F::kPieces; ++x) tl.kr[u][x] = read(src + 4 * x);
+    }
+  };
+  auto load_v = [&](int buf) {
+    int rows[8];
+    *reinterpret_cast<int4*>(rows) = reinterpret_cast<const int4*>(places[buf])[2 * g];
+    *reinterpret_cast<int4*>(rows + 4) = reinterpret_cast<const int4*>(places[buf])[2 * g + 1];
+    bad = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      bad |= (uint32_t)(rows[e] < 0) << e;
+      const unsigned char* src = Vp + (size_t)max(rows[e], 0) * (D * sizeof(T));
+      if constexpr (sizeof(T) == 2) {
+        tl.vr[e] = read(reinterpret_cast<const typename F::VRow*>(src) + i16);
+      } else {
+#pragma unroll
+        for (int x = 0; x < D / 64; ++x) tl.vr[e].x[x] = read(reinterpret_cast<const floatx4*>(src) + 16 * x + i16);
+      }
+    }
+  };
+
+  if (threadIdx.x == 0) s_odd = 0;
+  Place next = look_up(wave);
+  typename R::Query q;                                     // requested before the first tile and converted while that is on its way
+  R::load_q(p, s, row0, tid, &q);
+  publish(next, 0);
+  load_k(0);
+  load_v(0);
+  next = look_up(wave + kWaves);
+  u32x4* qs = reinterpret_cast<u32x4*>(lds);
+  R::store_q(p, tid, q, qs);
+  __syncthreads();
+
+  R rows;
+  rows.begin(p, s, row0, lane);
+  int buf = 0;
+  for (int t = wave; t < ntiles; t += kWaves) {
+    buf ^= 1;
+    publish(next, buf);
+    next = look_up(t + 2 * kWaves);
+    floatx4 sc[2][HB];
+    R::first_product(tl, qs, lane, sc);
+    load_k(buf);                                           // its registers are free
+    rows.second_product(p, s, row0, lane, s.begin + kPagedTile * t, bad, sc, tl);
+    load_v(buf);
+  }
+
+  if (rows.odd()) s_odd = 1;
+  __syncthreads();                                         // (and the q operands are read)
+  if (s_odd) {
+    in_plain_form<T>(p, s, TEAMS * R::NH, smem);
+    return;
+  }
+  rows.put(reinterpret_cast<float*>(lds), wave, lane);
+  __syncthreads();
+  R::finish(p, s, row0, reinterpret_cast<const float*>(lds), tid);
 }
 
 // ---------------------------------------------------------------- merge
@@ -806,7 +858,7 @@ PagedPlan paged_plan(int b, int n, int h, int h_kv, int page_size, int max_pages
   PagedPlan pl = {};
   const long long R = (long long)n * (h / h_kv), positions = (long long)max_pages * page_size, tiles = (positions + kPagedTile - 1) / kPagedTile;
   pl.mfma = k == v && (k == 64 || k == 128);
-  pl.block_rows = !pl.mfma ? kScalarRows : R <= 16 ? 16 : 32;
+  pl.block_rows = !pl.mfma ? kScalarRows : R <= 16 ? 16 : R <= 32 ? 32 : 64;
   pl.blocks = (int)((R + pl.block_rows - 1) / pl.block_rows);
   const long long groups = (long long)b * h_kv;
   pl.split = tiles > 8;
@@ -823,39 +875,42 @@ PagedPlan paged_plan(int b, int n, int h, int h_kv, int page_size, int max_pages
 
 void paged_workspace(PagedDecode* p, const PagedPlan& pl, void* workspace) { lay_out(p, pl, static_cast<float*>(workspace)); }
 
-template <typename T, int D, int HB>
-static hipError_t launch_matrix(const PagedDecode& p, const PagedPlan& pl, hipStream_t st) {
-  constexpr size_t lds = matrix_lds_bytes<T, D, HB>();
-  if (lds > 62 * 1024) {      // (of the 64 KiB that need no asking the kernel's own arrays are part) opt in, once per device
-    static bool done[64] = {};
-    int dev = 0;
-    if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) dev = 0;
-    if (!done[dev]) {
-      const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(paged_matrix_kernel<T, D, HB>), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
-      if (e != hipSuccess) return e;
-      done[dev] = true;
-    }
+// More than 64 KiB of LDS has to be asked for, once per device and kernel.
+template <void (*kernel)(PagedDecode)>
+static hipError_t launch_form(int threads, size_t lds, const PagedDecode& p, const PagedPlan& pl, hipStream_t st) {
+  static bool done[64] = {};
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) dev = 0;
+  if (lds > 60 * 1024 && !done[dev]) {
+    const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+    if (e != hipSuccess) return e;
+    done[dev] = true;
   }
-  hipLaunchKernelGGL((paged_matrix_kernel<T, D, HB>), dim3((unsigned)pl.pieces * pl.blocks), dim3(kThreads), lds, st, p);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)pl.pieces * pl.blocks), dim3(threads), lds, st, p);
   return hipGetLastError();
+}
+template <typename T, int D, int HB, int TEAMS>
+static hipError_t launch_matrix(const PagedDecode& p, const PagedPlan& pl, hipStream_t st) {
+  if (p.scores_out) return launch_form<paged_matrix_kernel<T, D, HB, TEAMS, true>>(TEAMS * kThreads, TEAMS * Lds<T, D, HB>::alone, p, pl, st);
+  return launch_form<paged_matrix_kernel<T, D, HB, TEAMS, false>>(TEAMS * kThreads, TEAMS * Lds<T, D, HB>::alone, p, pl, st);
+}
+template <typename T, int D>
+static hipError_t launch_rows(const PagedDecode& p, const PagedPlan& pl, hipStream_t st) {
+  switch (pl.block_rows) {
+    case 16: return launch_matrix<T, D, 1, 1>(p, pl, st);
+    case 32: return launch_matrix<T, D, 2, 1>(p, pl, st);
+    default: return launch_matrix<T, D, 2, 2>(p, pl, st);
+  }
 }
 
 hipError_t launch_paged_decode(const PagedDecode& p, const PagedPlan& pl, int is_bf16, hipStream_t st) {
   hipError_t e = hipErrorInvalidValue;
   if (pl.mfma) {
-    const bool wide = pl.block_rows == 32;
-    if (p.c.k == 128) {
-      if (is_bf16) e = wide ? launch_matrix<uint16_t, 128, 2>(p, pl, st) : launch_matrix<uint16_t, 128, 1>(p, pl, st);
-      else e = wide ? launch_matrix<float, 128, 2>(p, pl, st) : launch_matrix<float, 128, 1>(p, pl, st);
-    } else {
-      if (is_bf16) e = wide ? launch_matrix<uint16_t, 64, 2>(p, pl, st) : launch_matrix<uint16_t, 64, 1>(p, pl, st);
-      else e = wide ? launch_matrix<float, 64, 2>(p, pl, st) : launch_matrix<float, 64, 1>(p, pl, st);
-    }
+    if (p.c.k == 128) e = is_bf16 ? launch_rows<uint16_t, 128>(p, pl, st) : launch_rows<float, 128>(p, pl, st);
+    else e = is_bf16 ? launch_rows<uint16_t, 64>(p, pl, st) : launch_rows<float, 64>(p, pl, st);
   } else {
     const size_t lds = scalar_lds_floats(p.c.k, p.c.v) * sizeof(float);
-    if (is_bf16) hipLaunchKernelGGL(paged_scalar_kernel<uint16_t>, dim3((unsigned)pl.pieces * pl.blocks), dim3(kThreads), lds, st, p);
-    else hipLaunchKernelGGL(paged_scalar_kernel<float>, dim3((unsigned)pl.pieces * pl.blocks), dim3(kThreads), lds, st, p);
-    e = hipGetLastError();
+    e = is_bf16 ? launch_form<paged_scalar_kernel<uint16_t>>(kThreads, lds, p, pl, st) : launch_form<paged_scalar_kernel<float>>(kThreads, lds, p, pl, st);
   }
   if (e != hipSuccess) return e;
   const long long groups = (long long)p.b * p.c.h_kv;
