@@ -47,7 +47,6 @@ struct PagedDecode {
   int b, n, h;
   int R;                   // query rows of a group: n * h / h_kv, query-major
   int block_rows, blocks;  // R in blocks
-  int shares;              // of all tiles, of which a piece has one at most
   int split;               // 0: piece g is group g
   float qscale;            // scale * log2(e)
 };
@@ -66,7 +65,7 @@ struct PagedEvict {
 
 struct PagedPlan {
   bool mfma;
-  int block_rows, blocks, shares, split, pieces;      // pieces: at most
+  int block_rows, blocks, split, pieces;      // pieces: at most
   size_t bytes;
 };
 constexpr int kPagedTile = 32;

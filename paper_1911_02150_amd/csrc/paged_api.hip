@@ -77,7 +77,7 @@ int mqa_paged_decode_step(const float* q, const void* K_pages, const void* V_pag
   p.c = cache_of(K_pages, V_pages, table, h_kv, num_pages, page_size, max_pages, k, v);
   p.q = q; p.lens = lens; p.o = o; p.scores_in = scores_in; p.scores_out = scores_out;
   p.b = b; p.n = n; p.h = h; p.R = n * (h / h_kv);
-  p.block_rows = pl.block_rows; p.blocks = pl.blocks; p.shares = pl.shares; p.split = pl.split;
+  p.block_rows = pl.block_rows; p.blocks = pl.blocks; p.split = pl.split;
   p.qscale = scale * kLog2e;
   paged_workspace(&p, pl, workspace);
   return launch_paged_decode(p, pl, dt == MQA_BF16, static_cast<hipStream_t>(stream)) == hipSuccess ? MQA_OK : MQA_ERR_LAUNCH;

@@ -194,7 +194,7 @@ __device__ void scalar_segment(const PagedDecode& p, const Segment& s, int r0, i
 // ---------------------------------------------------------------- the list of work
 __device__ __forceinline__ int tiles_of(const PagedDecode& p, int len) { return (paged_length(p.c, len) + kPagedTile - 1) / kPagedTile; }
 
-// Sum of x over the threads before this one, of the workgroup's first 256; *all: over those.
+// Sum of x over the threads before this one; *all: over all.
 __device__ __forceinline__ int before_me(int x, int* s_waves, int* all) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int incl = x;
@@ -203,7 +203,7 @@ __device__ __forceinline__ int before_me(int x, int* s_waves, int* all) {
     const int y = __shfl_up(incl, off);
     if (lane >= off) incl += y;
   }
-  if (lane == 63 && wave < kThreads / 64) s_waves[wave] = incl;
+  if (lane == 63) s_waves[wave] = incl;
   __syncthreads();
   int before = incl - x, sum = 0;
 #pragma unroll
@@ -215,18 +215,22 @@ __device__ __forceinline__ int before_me(int x, int* s_waves, int* all) {
   return before;
 }
 
+constexpr int kComputeUnits = 256, kShares = 768;
+
 // This workgroup's segment; false: there is none.  Every workgroup looks at all lengths: thread t has sequences t * each up to the next one's.
 __device__ __forceinline__ bool find_segment(const PagedDecode& p, Segment* s) {
-  __shared__ int s_waves[2][kThreads / 64];
+  __shared__ int s_waves[5][kThreads / 64];
   __shared__ int s_at[4];
   const int tid = threadIdx.x, heads = p.c.h_kv;
   int piece = blockIdx.x, block = 0;
-  if (p.blocks > 1) {
-    piece = (int)(blockIdx.x / (unsigned)p.blocks);
-    block = (int)blockIdx.x - piece * p.blocks;
+  if (p.blocks > 1) {                    // (workgroups go to the eight XCDs in turn: a piece's are neighbours on one)
+    const unsigned turn = blockIdx.x >> 3;
+    block = (int)(turn % (unsigned)p.blocks);
+    piece = (int)(turn / (unsigned)p.blocks) * 8 + (int)(blockIdx.x & 7);
   }
   s->row0 = block * p.block_rows;
   if (!p.split) {
+    if (piece >= p.b * heads) return false;
     s->i = piece / heads;
     s->e = piece - s->i * heads;
     s->L = paged_length(p.c, p.lens[s->i]);
@@ -242,13 +246,23 @@ __device__ __forceinline__ bool find_segment(const PagedDecode& p, Segment* s) {
   int total;
   before_me(mine, s_waves[0], &total);
   total *= heads;
-  // tiles of a piece, at most: a whole number for each of the workgroup's four waves
-  const int per = max(1, (int)((unsigned)(total + p.shares - 1) / (unsigned)p.shares + 3) >> 2) * 4;
+  // Tiles of a piece, at most: a whole number for each of the workgroup's four waves.  As many as leave a workgroup for every compute unit at most, if that
+  // is not too uneven (64 sequences of 8192, 32 heads: 53 us, in 512 pieces 58); else shares so small that a compute unit has several in turn (512 sequences
+  // of up to 4096, 32 heads: 126, in shares of a 512th 137, of a 1536th 133).
+  int per = 0, count = 0, before = 0, all = 0, turn = 0;
   auto pieces_of = [&](int t) { return max(1, (int)((unsigned)(t + per - 1) / (unsigned)per)); };
-  int count = from < to ? pieces_of(tiles_of(p, len)) : 0;
-  for (int x = from + 1; x < to; ++x) count += pieces_of(tiles_of(p, p.lens[x]));
-  int all;
-  int before = before_me(count, s_waves[1], &all);
+  auto cut = [&](int tiles) {
+    per = max(1, (tiles + 3) >> 2) * 4;
+    count = from < to ? pieces_of(tiles_of(p, len)) : 0;
+    for (int x = from + 1; x < to; ++x) count += pieces_of(tiles_of(p, p.lens[x]));
+    before = before_me(count, s_waves[++turn], &all);
+    return (long long)all * heads * p.blocks <= kComputeUnits;
+  };
+  const int units = kComputeUnits / p.blocks;
+  bool fits = false;
+  if ((long long)p.b * heads * p.blocks <= kComputeUnits)
+    for (int x = 8; x <= 10 && !fits; ++x) fits = cut((int)(((long long)total * x + 8 * units - 1) / (8 * units)));
+  if (!fits) cut((total + kShares - 1) / kShares);
   if (piece >= all * heads) return false;
   if (before * heads <= piece && piece < (before + count) * heads) {      // one thread
     int x = from, L = len, c = pieces_of(tiles_of(p, len));
@@ -342,6 +356,9 @@ template <typename T, int D> struct Tile {
   u32x4 kr[2][Form<T, D>::kPieces];
   typename Form<T, D>::VRow vr[8];
 };
+// V as the second product wants it: bf16, transposed (its rows' registers are then free for the next tile's).
+template <typename T, int D> struct Turned {};
+template <int D> struct Turned<uint16_t, D> { u32x4 a[D / 16]; };
 
 // A wave's rows, 16 HB of a group from row0 on, and what they have seen.
 template <typename T, int D, int HB, bool SCORED>
@@ -406,51 +423,58 @@ struct Rows {
     lim_min = row_limit(p, s.L, min(row0, p.R - 1));
   }
 
-  // logits of a tile, from its K rows
-  static __device__ __forceinline__ void first_product(const Tile<T, D>& tl, const u32x4* qs, int lane, floatx4 (&sc)[2][HB]) {
-    u32x4 b[2][KT][HB];                // q of a piece, read while the one before is multiplied
-    auto read = [&](int x) {
+  // logits of a tile, from its K rows; after(x): the multiplications of piece x are under way and its registers free
+  template <typename After>
+  static __device__ __forceinline__ void first_product(const Tile<T, D>& tl, const u32x4* qs, int lane, floatx4 (&sc)[2][HB], After&& after) {
+    constexpr int STEPS = KP * KT, DEEP = 3;               // q of a step (piece, term): read while the two before are multiplied
+    u32x4 b[DEEP][HB];
+    auto read = [&](int n) {
 #pragma unroll
-      for (int term = 0; term < KT; ++term)
-#pragma unroll
-        for (int hb = 0; hb < HB; ++hb) b[x & 1][term][hb] = qs[term * QOPS + (hb * KP + x) * 64 + lane];
+      for (int hb = 0; hb < HB; ++hb) b[n % DEEP][hb] = qs[n % KT * QOPS + (hb * KP + n / KT) * 64 + lane];
     };
-    read(0);
+#pragma unroll
+    for (int n = 0; n < DEEP - 1; ++n) read(n);
 #pragma unroll
     for (int hb = 0; hb < HB; ++hb) sc[0][hb] = sc[1][hb] = floatx4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int x = 0; x < KP; ++x) {
-      if (x + 1 < KP) read(x + 1);
+    for (int n = 0; n < STEPS; ++n) {
+      if (n + DEEP - 1 < STEPS) read(n + DEEP - 1);
       __builtin_amdgcn_sched_barrier(0);
+      const int x = n / KT;
 #pragma unroll
-      for (int term = 0; term < KT; ++term)
+      for (int y = 0; y < (sizeof(T) == 2 ? 1 : 4); ++y)
 #pragma unroll
-        for (int y = 0; y < (sizeof(T) == 2 ? 1 : 4); ++y)
+        for (int hb = 0; hb < HB; ++hb)
 #pragma unroll
-          for (int hb = 0; hb < HB; ++hb)
+          for (int u = 0; u < 2; ++u) {
+            if constexpr (sizeof(T) == 2)
+              sc[u][hb] = mfma_bf16(tl.kr[u][x], b[n % DEEP][hb], sc[u][hb]);
+            else
+              sc[u][hb] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(tl.kr[u][x][y]), __uint_as_float(b[n % DEEP][hb][y]), sc[u][hb], 0, 0, 0);
+          }
+      if (n % KT == KT - 1) after(x);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  // V's part of piece x: NJ / KP of its column groups
+  static __device__ __forceinline__ void turn(const Tile<T, D>& tl, int x, Turned<T, D>& v) {
+    if constexpr (sizeof(T) == 2) {
 #pragma unroll
-            for (int u = 0; u < 2; ++u) {
-              if constexpr (sizeof(T) == 2)
-                sc[u][hb] = mfma_bf16(tl.kr[u][x], b[x & 1][term][hb], sc[u][hb]);
-              else
-                sc[u][hb] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(tl.kr[u][x][y]), __uint_as_float(b[x & 1][term][hb][y]), sc[u][hb], 0, 0, 0);
-            }
-      __builtin_amdgcn_sched_barrier(0);
+      for (int j = x * NJ / KP; j < (x + 1) * NJ / KP; ++j)
+#pragma unroll
+        for (int y = 0; y < 4; ++y) v.a[j][y] = __builtin_amdgcn_perm(tl.vr[2 * y + 1][j >> 1], tl.vr[2 * y][j >> 1], j & 1 ? 0x07060302u : 0x05040100u);
     }
   }
 
-  // the softmax of a tile from position p0 on, and its V rows; bad: bit e: position p0 + 8g + e is not there
-  __device__ __forceinline__ void second_product(const PagedDecode& p, const Segment& s, int row0, int lane, int p0, uint32_t bad, floatx4 (&sc)[2][HB], Tile<T, D>& tl) {
+  // the softmax of a tile from position p0 on; bad: bit e: position p0 + 8g + e is not there
+  __device__ __forceinline__ void weights(const PagedDecode& p, const Segment& s, int row0, int lane, int p0, uint32_t bad, floatx4 (&sc)[2][HB], float (&w)[HB][8]) {
     const int i16 = lane & 15, g = lane >> 4;
     if (__any(bad != 0) || p0 + kPagedTile > lim_min) {    // what is not there, or not seen
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const bool gone = bad >> e & 1;
+      for (int e = 0; e < 8; ++e)
 #pragma unroll
         for (int hb = 0; hb < HB; ++hb)
-          if (gone || p0 + 8 * g + e >= lim[hb]) sc[e >> 2][hb][e & 3] = -INFINITY;
-        if (gone) tl.vr[e] = typename F::VRow{};
-      }
+          if ((bad >> e & 1) || p0 + 8 * g + e >= lim[hb]) sc[e >> 2][hb][e & 3] = -INFINITY;
     }
     if constexpr (SCORED) {
       const size_t pitch = logits_pitch(p);
@@ -463,7 +487,6 @@ struct Rows {
         }
     }
     // the running maximum is moved when a row's has grown by more than kSlack (any reference will do for the sums)
-    float w[HB][8];
 #pragma unroll
     for (int hb = 0; hb < HB; ++hb) {
       float mx = fmaxf(fmaxf(fmaxf(sc[0][hb][0], sc[0][hb][1]), fmaxf(sc[0][hb][2], sc[0][hb][3])),
@@ -487,6 +510,10 @@ struct Rows {
       }
       l_run[hb] += sum;
     }
+  }
+  // after(e): the registers of V row e are free
+  template <typename After>
+  __device__ __forceinline__ void second_product(const float (&w)[HB][8], const Tile<T, D>& tl, const Turned<T, D>& v, After&& after) {
     if constexpr (sizeof(T) == 2) {
       u32x4 wt[HB][3];
 #pragma unroll
@@ -497,25 +524,28 @@ struct Rows {
           split3(w[hb][2 * y], w[hb][2 * y + 1], x);
           wt[hb][0][y] = x[0]; wt[hb][1][y] = x[1]; wt[hb][2][y] = x[2];
         }
-      u32x4 a[NJ];                                         // (all of V first: then the products of a sum are far apart)
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int j = 0; j < NJ; ++j)
+      for (int j = 0; j < NJ; ++j) {
 #pragma unroll
-        for (int x = 0; x < 4; ++x) a[j][x] = __builtin_amdgcn_perm(tl.vr[2 * x + 1][j >> 1], tl.vr[2 * x][j >> 1], j & 1 ? 0x07060302u : 0x05040100u);
+        for (int term = 0; term < 3; ++term)
 #pragma unroll
-      for (int term = 0; term < 3; ++term)
+          for (int hb = 0; hb < HB; ++hb) acc[hb][j] = mfma_bf16(v.a[j], wt[hb][term], acc[hb][j]);
 #pragma unroll
-        for (int j = 0; j < NJ; ++j)
-#pragma unroll
-          for (int hb = 0; hb < HB; ++hb) acc[hb][j] = mfma_bf16(a[j], wt[hb][term], acc[hb][j]);
+        for (int e = 8 / NJ * j; e < 8 / NJ * (j + 1); ++e) after(e);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
+      for (int e = 0; e < 8; ++e) {
 #pragma unroll
         for (int j = 0; j < NJ; ++j)
 #pragma unroll
           for (int hb = 0; hb < HB; ++hb)
             acc[hb][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(tl.vr[e].x[j >> 2][j & 3], w[hb][e], acc[hb][j], 0, 0, 0);
+        after(e);
+        __builtin_amdgcn_sched_barrier(0);
+      }
     }
   }
 
@@ -595,22 +625,21 @@ __device__ __forceinline__ void in_plain_form(const PagedDecode& p, const Segmen
   for (int r0 = s.row0; r0 < min(p.R, s.row0 + rows); r0 += kScalarRows) scalar_segment<T>(p, s, r0, min(p.R - r0, kScalarRows), reinterpret_cast<float*>(smem));
 }
 
-// TEAMS: two (of four waves, 32 rows each) for up to 64 query rows: the waves that have the same tiles read them at about the same time, from memory once and
-// for the other from L2.
-template <typename T, int D, int HB, int TEAMS, bool SCORED>
-__global__ __launch_bounds__(TEAMS * kThreads, 2)
+// CACHED: several blocks of rows read the same tiles, neighbours on an XCD at about the same time: from memory once and else from L2.  (64 heads of 512
+// sequences of up to 4096: 185 us.  Two teams of four waves in a workgroup 207: a workgroup to a compute unit, whose start and end nothing covers; that with
+// the tiles in LDS 300; all 64 rows in a wave, two tiles on their way, 260.)
+template <typename T, int D, int HB, bool SCORED, bool CACHED>
+__global__ __launch_bounds__(kThreads, 2)
 void paged_matrix_kernel(PagedDecode p) {
   typedef Rows<T, D, HB, SCORED> R;
   typedef Form<T, D> F;
   extern __shared__ __align__(16) unsigned char smem[];
-  __shared__ __align__(16) int s_rows[TEAMS * kWaves][2][32];
+  __shared__ __align__(16) int s_rows[kWaves][2][32];
   __shared__ int s_odd;
   Segment s;
   if (!find_segment(p, &s)) return;
-  const int team = TEAMS > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x / kThreads) : 0, tid = threadIdx.x - team * kThreads, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), i16 = lane & 15, g = lane >> 4, row0 = s.row0 + team * R::NH;
-  int (&places)[2][32] = s_rows[team * kWaves + wave];
-  unsigned char* const lds = smem + team * Lds<T, D, HB>::alone;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i16 = lane & 15, g = lane >> 4;
+  int (&places)[2][32] = s_rows[wave];
   const int32_t* table = p.c.table + (size_t)s.i * p.c.max_pages;
   const unsigned char* Kp = static_cast<const unsigned char*>(p.c.K);
   const unsigned char* Vp = static_cast<const unsigned char*>(p.c.V);
@@ -625,78 +654,97 @@ void paged_matrix_kernel(PagedDecode p) {
     return Place{table[page], pos < s.end ? inside - (int)page * p.c.page_size : -1};
   };
   Tile<T, D> tl;
-  uint32_t bad;                                            // bit e: position 8g + e of the tile is not there
+  int k_row[2], v_row[8];                                  // of the tile that is loaded next
   auto publish = [&](const Place& x, int buf) {
     const bool there = (unsigned)x.entry < (unsigned)p.c.num_pages && x.inside >= 0;
     places[buf][lane & 31] = there ? (x.entry * p.c.h_kv + s.e) * p.c.page_size + x.inside : -1;
     asm volatile("" ::: "memory");
   };
-  auto read = [](const auto* at) {                         // once, or by both teams
-    if constexpr (TEAMS == 1) return __builtin_nontemporal_load(at);
-    else return *at;
+  auto take = [&](int buf) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) k_row[u] = places[buf][8 * (i16 >> 2) + 4 * u + (i16 & 3)];
+    *reinterpret_cast<int4*>(v_row) = reinterpret_cast<const int4*>(places[buf])[2 * g];
+    *reinterpret_cast<int4*>(v_row + 4) = reinterpret_cast<const int4*>(places[buf])[2 * g + 1];
   };
-  auto load_k = [&](int buf) {
+  auto read = [](const auto* at) {
+    if constexpr (CACHED) return *at;
+    else return __builtin_nontemporal_load(at);
+  };
+  auto load_k = [&](int x) {
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-      const int row = places[buf][8 * (i16 >> 2) + 4 * u + (i16 & 3)];
-      const u32x4* src = reinterpret_cast<const u32x4*>(Kp + (size_t)max(row, 0) * (D * sizeof(T))) + g;
+    for (int u = 0; u < 2; ++u) tl.kr[u][x] = read(reinterpret_cast<const u32x4*>(Kp + (size_t)max(k_row[u], 0) * (D * sizeof(T))) + g + 4 * x);
+  };
+  auto load_v = [&](int e) {
+    const unsigned char* src = Vp + (size_t)max(v_row[e], 0) * (D * sizeof(T));
+    if constexpr (sizeof(T) == 2) {
+      tl.vr[e] = read(reinterpret_cast<const typename F::VRow*>(src) + i16);
+    } else {
 #pragma unroll
-      for (int x = 0; x < F::kPieces; ++x) tl.kr[u][x] = read(src + 4 * x);
+      for (int x = 0; x < D / 64; ++x) tl.vr[e].x[x] = read(reinterpret_cast<const floatx4*>(src) + 16 * x + i16);
     }
   };
-  auto load_v = [&](int buf) {
-    int rows[8];
-    *reinterpret_cast<int4*>(rows) = reinterpret_cast<const int4*>(places[buf])[2 * g];
-    *reinterpret_cast<int4*>(rows + 4) = reinterpret_cast<const int4*>(places[buf])[2 * g + 1];
-    bad = 0;
+  auto missing = [&]() {                                   // bit e: position 8g + e of the tile is not there
+    uint32_t bits = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      bad |= (uint32_t)(rows[e] < 0) << e;
-      const unsigned char* src = Vp + (size_t)max(rows[e], 0) * (D * sizeof(T));
-      if constexpr (sizeof(T) == 2) {
-        tl.vr[e] = read(reinterpret_cast<const typename F::VRow*>(src) + i16);
-      } else {
-#pragma unroll
-        for (int x = 0; x < D / 64; ++x) tl.vr[e].x[x] = read(reinterpret_cast<const floatx4*>(src) + 16 * x + i16);
-      }
-    }
+    for (int e = 0; e < 8; ++e) bits |= (uint32_t)(v_row[e] < 0) << e;
+    return bits;
   };
 
-  if (threadIdx.x == 0) s_odd = 0;
+  if (tid == 0) s_odd = 0;
   Place next = look_up(wave);
   typename R::Query q;                                     // requested before the first tile and converted while that is on its way
-  R::load_q(p, s, row0, tid, &q);
+  R::load_q(p, s, s.row0, tid, &q);
   publish(next, 0);
-  load_k(0);
-  load_v(0);
   next = look_up(wave + kWaves);
-  u32x4* qs = reinterpret_cast<u32x4*>(lds);
+  take(0);
+#pragma unroll
+  for (int x = 0; x < F::kPieces; ++x) load_k(x);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) load_v(e);
+  uint32_t bad = missing();
+  u32x4* qs = reinterpret_cast<u32x4*>(smem);
   R::store_q(p, tid, q, qs);
   __syncthreads();
 
   R rows;
-  rows.begin(p, s, row0, lane);
-  int buf = 0;
+  rows.begin(p, s, s.row0, lane);
+  publish(next, 1);
+  next = look_up(wave + 2 * kWaves);
+  take(1);
+  int buf = 1;
   for (int t = wave; t < ntiles; t += kWaves) {
-    buf ^= 1;
-    publish(next, buf);
-    next = look_up(t + 2 * kWaves);
+    const int p0 = s.begin + kPagedTile * t;
+    const uint32_t now = bad;
+    if (__any(now != 0)) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (now >> e & 1) tl.vr[e] = typename F::VRow{};
+    }
     floatx4 sc[2][HB];
-    R::first_product(tl, qs, lane, sc);
-    load_k(buf);                                           // its registers are free
-    rows.second_product(p, s, row0, lane, s.begin + kPagedTile * t, bad, sc, tl);
-    load_v(buf);
+    Turned<T, D> v;
+    R::first_product(tl, qs, lane, sc, [&](int x) {
+      load_k(x);
+      R::turn(tl, x, v);
+    });
+    bad = missing();
+    buf ^= 1;
+    publish(next, buf);                                    // places of the tile after the next one
+    next = look_up(t + 3 * kWaves);
+    float w[HB][8];
+    rows.weights(p, s, s.row0, lane, p0, now, sc, w);
+    rows.second_product(w, tl, v, load_v);
+    take(buf);
   }
 
   if (rows.odd()) s_odd = 1;
   __syncthreads();                                         // (and the q operands are read)
   if (s_odd) {
-    in_plain_form<T>(p, s, TEAMS * R::NH, smem);
+    in_plain_form<T>(p, s, R::NH, smem);
     return;
   }
-  rows.put(reinterpret_cast<float*>(lds), wave, lane);
+  rows.put(reinterpret_cast<float*>(smem), wave, lane);
   __syncthreads();
-  R::finish(p, s, row0, reinterpret_cast<const float*>(lds), tid);
+  R::finish(p, s, s.row0, reinterpret_cast<const float*>(smem), tid);
 }
 
 // ---------------------------------------------------------------- merge
@@ -830,8 +878,6 @@ void paged_finish_kernel(PagedDecode p, int rows, int pieces, int chunks) {
 
 }  // namespace
 
-constexpr int kPagedWorkgroups = 512;
-
 // The parts of a call's workspace, each on 16 bytes; their size in all.
 static size_t lay_out(PagedDecode* p, const PagedPlan& pl, float* at) {
   size_t floats = 0;
@@ -858,12 +904,11 @@ PagedPlan paged_plan(int b, int n, int h, int h_kv, int page_size, int max_pages
   PagedPlan pl = {};
   const long long R = (long long)n * (h / h_kv), positions = (long long)max_pages * page_size, tiles = (positions + kPagedTile - 1) / kPagedTile;
   pl.mfma = k == v && (k == 64 || k == 128);
-  pl.block_rows = !pl.mfma ? kScalarRows : R <= 16 ? 16 : R <= 32 ? 32 : 64;
+  pl.block_rows = !pl.mfma ? kScalarRows : R <= 16 || (k == 128 && !is_bf16) ? 16 : 32;      // (float32 rows of 128: 32 query rows do not fit a wave's registers beside a tile)
   pl.blocks = (int)((R + pl.block_rows - 1) / pl.block_rows);
   const long long groups = (long long)b * h_kv;
   pl.split = tiles > 8;
-  pl.shares = pl.blocks < kPagedWorkgroups ? kPagedWorkgroups / pl.blocks : 1;
-  const long long least = groups * ((tiles + 3) / 4), most = groups + pl.shares;      // (pieces of four tiles; a last, shorter one in every group)
+  const long long least = groups * ((tiles + 3) / 4), most = groups + kShares;      // (pieces of four tiles; a last, shorter one in every group)
   pl.pieces = (int)(!pl.split ? groups : least < most ? least : most);
   PagedDecode p = {};
   p.b = b; p.R = (int)R;
@@ -877,7 +922,7 @@ void paged_workspace(PagedDecode* p, const PagedPlan& pl, void* workspace) { lay
 
 // More than 64 KiB of LDS has to be asked for, once per device and kernel.
 template <void (*kernel)(PagedDecode)>
-static hipError_t launch_form(int threads, size_t lds, const PagedDecode& p, const PagedPlan& pl, hipStream_t st) {
+static hipError_t launch_form(size_t lds, const PagedDecode& p, const PagedPlan& pl, hipStream_t st) {
   static bool done[64] = {};
   int dev = 0;
   if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) dev = 0;
@@ -886,21 +931,22 @@ static hipError_t launch_form(int threads, size_t lds, const PagedDecode& p, con
     if (e != hipSuccess) return e;
     done[dev] = true;
   }
-  hipLaunchKernelGGL(kernel, dim3((unsigned)pl.pieces * pl.blocks), dim3(threads), lds, st, p);
+  hipLaunchKernelGGL(kernel, dim3((unsigned)(pl.blocks > 1 ? (pl.pieces + 7) / 8 * 8 : pl.pieces) * pl.blocks), dim3(kThreads), lds, st, p);
   return hipGetLastError();
 }
-template <typename T, int D, int HB, int TEAMS>
+template <typename T, int D, int HB>
 static hipError_t launch_matrix(const PagedDecode& p, const PagedPlan& pl, hipStream_t st) {
-  if (p.scores_out) return launch_form<paged_matrix_kernel<T, D, HB, TEAMS, true>>(TEAMS * kThreads, TEAMS * Lds<T, D, HB>::alone, p, pl, st);
-  return launch_form<paged_matrix_kernel<T, D, HB, TEAMS, false>>(TEAMS * kThreads, TEAMS * Lds<T, D, HB>::alone, p, pl, st);
+  constexpr size_t lds = Lds<T, D, HB>::alone;
+  if constexpr (HB > 1 || sizeof(T) * D > 256)             // (else more rows would be of another kind)
+    if (pl.blocks > 1)
+      return p.scores_out ? launch_form<paged_matrix_kernel<T, D, HB, true, true>>(lds, p, pl, st) : launch_form<paged_matrix_kernel<T, D, HB, false, true>>(lds, p, pl, st);
+  return p.scores_out ? launch_form<paged_matrix_kernel<T, D, HB, true, false>>(lds, p, pl, st) : launch_form<paged_matrix_kernel<T, D, HB, false, false>>(lds, p, pl, st);
 }
 template <typename T, int D>
 static hipError_t launch_rows(const PagedDecode& p, const PagedPlan& pl, hipStream_t st) {
-  switch (pl.block_rows) {
-    case 16: return launch_matrix<T, D, 1, 1>(p, pl, st);
-    case 32: return launch_matrix<T, D, 2, 1>(p, pl, st);
-    default: return launch_matrix<T, D, 2, 2>(p, pl, st);
-  }
+  if constexpr (sizeof(T) * D <= 256)
+    if (pl.block_rows == 32) return launch_matrix<T, D, 2>(p, pl, st);
+  return launch_matrix<T, D, 1>(p, pl, st);
 }
 
 hipError_t launch_paged_decode(const PagedDecode& p, const PagedPlan& pl, int is_bf16, hipStream_t st) {
@@ -910,7 +956,7 @@ hipError_t launch_paged_decode(const PagedDecode& p, const PagedPlan& pl, int is
     else e = is_bf16 ? launch_rows<uint16_t, 64>(p, pl, st) : launch_rows<float, 64>(p, pl, st);
   } else {
     const size_t lds = scalar_lds_floats(p.c.k, p.c.v) * sizeof(float);
-    e = is_bf16 ? launch_form<paged_scalar_kernel<uint16_t>>(kThreads, lds, p, pl, st) : launch_form<paged_scalar_kernel<float>>(kThreads, lds, p, pl, st);
+    e = is_bf16 ? launch_form<paged_scalar_kernel<uint16_t>>(lds, p, pl, st) : launch_form<paged_scalar_kernel<float>>(lds, p, pl, st);
   }
   if (e != hipSuccess) return e;
   const long long groups = (long long)p.b * p.c.h_kv;
