@@ -47,6 +47,8 @@ _NATIVE_FUNCTIONS = [
     "mqa_decode_step", "mha_decode_step", "mqa_decode_step_window", "mha_decode_step_window", "mqa_project_append_qkv", "mqa_project_qkvo_ex",
     "mqa_project_add_layernorm", "mqa_project_memory_kv", "mqa_project_memory_kv_ws", "mqa_memory_decode_step", "mqa_decode_step_beams",
     "mqa_beam_reorder_kv", "mqa_prefill_attention", "mha_prefill_attention",
+    "mqa_paged_append_kv_rows", "mqa_paged_decode_workspace_bytes", "mqa_paged_decode_step", "mqa_paged_evict_kv",
+    "mqa_stack_verify_workspace_bytes", "mqa_stack_verify_drafts",
 ]
 
 
@@ -786,6 +788,10 @@ def mqa_paged_append_kv_rows(K_pages, V_pages, table, k_new, v_new, lens, lens_o
     """K_pages [num_pages,page_size,k] (multi-query) or [num_pages,h_kv,page_size,k], V_pages likewise (float32 or bfloat16), table
     [b,max_pages] int32: rows k_new [b,n,k] or [b,n,h_kv,k] / v_new, of sequence i the first counts[i] (None: all), go behind the lens[i] rows it has.
     lens_out [b] int32, another tensor than lens, receives the new lengths and is returned."""
+    if stream is None and _native is not None:
+        done = _native.paged_append(K_pages, V_pages, table, k_new, v_new, lens, lens_out, counts)
+        if done is not None:
+            return done
     lib = load_library()
     _check(k_new, "k_new", torch.float32), _check(v_new, "v_new", torch.float32)
     _check(lens, "lens", torch.int32), _check(lens_out, "lens_out", torch.int32)
@@ -816,6 +822,10 @@ def mqa_paged_decode_step(q, K_pages, V_pages, table, lens, o=None, scale=1.0, s
     int32 (behind their append) -> o [b,h,v] or [b,n,h,v].  scores [b,positions] (multi-query) or [b,h_kv,positions], positions = max_pages * page_size: the
     attention weight that each position has received; scores_out receives it with this step's added (None: scores itself; scores None: from 0).
     Workspace: a block of the call's own unless given."""
+    if stream is None and _native is not None:
+        done = _native.paged_decode(q, K_pages, V_pages, table, lens, o, scale, scores, scores_out, workspace)
+        if done is not None:
+            return done
     lib = load_library()
     _check(q, "q", torch.float32), _check(lens, "lens", torch.int32)
     if q.dim() not in (3, 4):
@@ -856,6 +866,10 @@ def mqa_paged_evict_kv(K_pages, V_pages, table, lens, scores, table_out, lens_ou
     """Of every sequence (and K/V head) the latest `recent` positions and those with the largest scores, budget = kept.shape[-1] in all, are copied in their order to
     the pages of table_out [b,max_pages_out]; lens_out [b], scores_out (as scores, for table_out's positions) and kept [b,budget] or
     [b,h_kv,budget] int32 receive their number, their scores and which they were (-1 behind them).  Returns kept."""
+    if stream is None and _native is not None:
+        done = _native.paged_evict(K_pages, V_pages, table, lens, scores, table_out, lens_out, scores_out, kept, recent)
+        if done is not None:
+            return done
     lib = load_library()
     i32 = torch.int32
     _check(lens, "lens", i32), _check(lens_out, "lens_out", i32), _check(table_out, "table_out", i32), _check(kept, "kept", i32)
@@ -870,7 +884,8 @@ def mqa_paged_evict_kv(K_pages, V_pages, table, lens, scores, table_out, lens_ou
     dt = _cache_dtype(K_pages)
     with _on(_one_device(K_pages, V_pages, table, lens, scores, table_out, lens_out, scores_out, kept), stream):
         rc = lib.mqa_paged_evict_kv(_ptr(K_pages), _ptr(V_pages), _ptr(table), _ptr(lens), _ptr(scores), _ptr(table_out), _ptr(lens_out), _ptr(scores_out),
-                                    _ptr(kept), b, h_kv, num_pages, page_size, max_pages, max_pages_out, k, v, dt, kept.shape[-1], int(recent), _stream(stream))
+                                    _ptr(kept), b, h_kv, num_pages, page_size, max_pages, max_pages_out, k, v, dt, kept.shape[-1],
+                                    max(-1, min(int(recent), 2 ** 31 - 1)), _stream(stream))
     if rc != 0:
         raise MqaError("mqa_paged_evict_kv", rc)
     return kept
@@ -967,6 +982,10 @@ def mqa_stack_verify_drafts(logits, drafts, u, draft_logits=None, counts=None, t
     """logits [b,n+1,vocab] of the target, drafts [b,n] int32 (None: n = 0), u [b,n+1] float32 random numbers of [0,1) (None with temperature 0), draft_logits
     [b,n,vocab] or None (every draft was certain), counts [b] int32 or None (n drafts each) -> tokens [b,n+1] int32, the drafts that stand and the
     token behind them, then -1, and accepted [b] int32, how many stand.  Workspace: a block of the call's own unless given."""
+    if stream is None and _native is not None:
+        done = _native.verify(logits, drafts, u, draft_logits, counts, temperature, tokens, accepted, workspace)
+        if done is not None:
+            return done
     lib = load_library()
     _check(logits, "logits", torch.float32)
     for name, t, dtype in (("drafts", drafts, torch.int32), ("u", u, torch.float32), ("draft_logits", draft_logits, torch.float32),

@@ -13,6 +13,7 @@
 #include <ATen/PythonTorchFunctionTLS.h>
 #include <c10/core/impl/TorchDispatchModeTLS.h>
 #include <c10/hip/HIPFunctions.h>
+#include <c10/hip/HIPGraphsC10Utils.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -33,6 +34,12 @@ struct Functions {
   decltype(&mqa_decode_step_beams) beams;
   decltype(&mqa_beam_reorder_kv) reorder;
   decltype(&mqa_prefill_attention) mqa_prefill, mha_prefill;
+  decltype(&mqa_paged_append_kv_rows) paged_append;
+  decltype(&mqa_paged_decode_workspace_bytes) paged_workspace;
+  decltype(&mqa_paged_decode_step) paged_decode;
+  decltype(&mqa_paged_evict_kv) paged_evict;
+  decltype(&mqa_stack_verify_workspace_bytes) verify_workspace;
+  decltype(&mqa_stack_verify_drafts) verify;
 } fn;
 PyObject* error_class = nullptr;
 PyObject* parameter_class = nullptr;
@@ -318,6 +325,143 @@ MQA_CALL(reorder, 7) {
   return result(WITHOUT_GIL(fn.reorder(Ksp, Vsp, lsp, pp, Kdp, Vdp, ldp, n, h_kv, cap, k, v, (mqa_dtype)dt, st)), "mqa_beam_reorder_kv", Py_True);
 }
 
+// A tensor of this type or None; false: neither.
+bool maybe(PyObject* o, at::ScalarType type, const at::Tensor** t) {
+  *t = nullptr;
+  return o == Py_None || (*t = plain(o, type)) != nullptr;
+}
+
+// The sizes of a paged cache; false: not these
+struct Paged { int64_t h_kv, pages, size, each, k, v; int dt; };
+bool paged_of(const at::Tensor* K, const at::Tensor* V, const at::Tensor* table, int64_t b, Paged* c) {
+  if (!K || !V || !table || K->dim() < 3 || K->dim() > 4 || V->dim() != K->dim() || table->dim() != 2 || table->size(0) != b || V->scalar_type() != K->scalar_type() ||
+      V->sizes().slice(0, V->dim() - 1) != K->sizes().slice(0, K->dim() - 1) || !fits(*K) || !fits(*V) || !fits(*table))
+    return false;
+  *c = Paged{K->dim() == 4 ? K->size(1) : 1, K->size(0), K->size(-2), table->size(1), K->size(-1), V->size(-1), cache_type(*K)};
+  return c->dt >= 0 && c->size > 0;
+}
+// [b, (h_kv,) last], as the cache has its heads
+bool per_head(const at::Tensor& t, const at::Tensor& K, int64_t b, int64_t last) {
+  return K.dim() == 4 ? shape_is(t, {b, K.size(1), last}) : shape_is(t, {b, last});
+}
+
+// Scratch memory for a call: the caller's (held until the call has been made), or a block of the allocator, the current stream's.  false: the general path's matter
+// (a stream that is captured, another kind of memory).
+struct Scratch { at::Tensor own; void* at = nullptr; size_t bytes = 0; };
+bool scratch(PyObject* given, size_t need, const at::Tensor& like, Scratch* s) {
+  if (given != Py_None) {
+    const at::Tensor* t = plain(given);
+    if (!t) return false;
+    s->at = t->data_ptr();
+    s->bytes = bytes_of(*t);
+    return true;
+  }
+  if (need == 0) return true;
+  if (c10::hip::currentStreamCaptureStatusMayInitCtx() != c10::hip::CaptureStatus::None) return false;
+  s->own = at::empty({(int64_t)need}, like.options().dtype(at::kByte).requires_grad(false));
+  s->at = s->own.data_ptr();
+  s->bytes = need;
+  return true;
+}
+
+// (K_pages, V_pages, table, k_new, v_new, lens, lens_out, counts)
+MQA_CALL(paged_append, 8) {
+  const at::Tensor *K = plain(a[0]), *V = plain(a[1]), *table = i32(a[2]), *kn = f32(a[3]), *vn = f32(a[4]), *lens = i32(a[5]), *out = i32(a[6]), *counts;
+  Paged c;
+  if (!kn || !vn || !lens || !out || !maybe(a[7], at::kInt, &counts) || kn->dim() < 3 || !fits(*kn) || !paged_of(K, V, table, kn->size(0), &c)) NOT_HERE;
+  const int64_t b = kn->size(0), n = kn->size(1);
+  if (!(K->dim() == 4 ? shape_is(*kn, {b, n, c.h_kv, c.k}) && shape_is(*vn, {b, n, c.h_kv, c.v}) : shape_is(*kn, {b, n, c.k}) && shape_is(*vn, {b, n, c.v})) ||
+      lens->numel() != b || out->numel() != b || (counts && counts->numel() != b))
+    NOT_HERE;
+  const float *kp = at_of<float>(kn), *vp = at_of<float>(vn);
+  const int32_t *cp = at_of<int32_t>(counts), *tp = at_of<int32_t>(table), *lp = at_of<int32_t>(lens);
+  int32_t* op = at_of<int32_t>(out);
+  void *Kp = K->data_ptr(), *Vp = V->data_ptr(), *st = current_stream();
+  Py_INCREF(a[6]);
+  return result(WITHOUT_GIL(fn.paged_append(kp, vp, cp, Kp, Vp, tp, lp, op, b, n, c.h_kv, c.pages, c.size, c.each, c.k, c.v, (mqa_dtype)c.dt, st)),
+                "mqa_paged_append_kv_rows", a[6]);
+}
+
+// (q, K_pages, V_pages, table, lens, o, scale, scores, scores_out, workspace)
+MQA_CALL(paged_decode, 10) {
+  const at::Tensor *q = f32(a[0]), *K = plain(a[1]), *V = plain(a[2]), *table = i32(a[3]), *lens = i32(a[4]), *in, *out, *o;
+  float scale;
+  Paged c;
+  if (!q || !lens || q->dim() < 3 || q->dim() > 4 || !fits(*q) || !number(a[6], &scale) || !maybe(a[7], at::kFloat, &in) || !maybe(a[8], at::kFloat, &out) ||
+      !paged_of(K, V, table, q->size(0), &c))
+    NOT_HERE;
+  const int64_t b = q->size(0), n = q->dim() == 4 ? q->size(1) : 1, h = q->size(-2);
+  if (!out) out = in;
+  if (q->size(-1) != c.k || lens->numel() != b || c.each > INT32_MAX / c.size || (in && !per_head(*in, *K, b, c.each * c.size)) ||
+      (out && !per_head(*out, *K, b, c.each * c.size)))
+    NOT_HERE;
+  at::Tensor own;
+  Held res{q->dim() == 4 ? output(a[5], *q, {b, n, h, c.v}, &o, &own) : output(a[5], *q, {b, h, c.v}, &o, &own)};
+  if (!res.p) NOT_HERE;
+  Scratch ws;
+  if (!scratch(a[9], a[9] == Py_None ? fn.paged_workspace(b, n, h, c.h_kv, c.size, c.each, c.k, c.v, (mqa_dtype)c.dt, out != nullptr) : 0, *q, &ws)) NOT_HERE;
+  const float *qp = at_of<float>(q), *ip = at_of<float>(in);
+  float *op = at_of<float>(o), *sp = at_of<float>(out);
+  const int32_t *tp = at_of<int32_t>(table), *lp = at_of<int32_t>(lens);
+  const void *Kp = K->data_ptr(), *Vp = V->data_ptr();
+  void* st = current_stream();
+  return result(WITHOUT_GIL(fn.paged_decode(qp, Kp, Vp, tp, lp, op, ip, sp, b, n, h, c.h_kv, c.pages, c.size, c.each, c.k, c.v, (mqa_dtype)c.dt, scale, ws.at, ws.bytes, st)),
+                "mqa_paged_decode_step", res.take());
+}
+
+// (K_pages, V_pages, table, lens, scores, table_out, lens_out, scores_out, kept, recent)
+MQA_CALL(paged_evict, 10) {
+  const at::Tensor *K = plain(a[0]), *V = plain(a[1]), *table = i32(a[2]), *lens = i32(a[3]), *scores = f32(a[4]), *table_out = i32(a[5]), *lens_out = i32(a[6]),
+                   *scores_out = f32(a[7]), *kept = i32(a[8]);
+  int recent;
+  Paged c, d;
+  if (!lens || !scores || !lens_out || !scores_out || !kept || kept->dim() < 1 || !fits(*kept) || !integer(a[9], &recent) || !paged_of(K, V, table, lens->numel(), &c) ||
+      !paged_of(K, V, table_out, lens->numel(), &d))
+    NOT_HERE;
+  const int64_t b = lens->numel(), budget = kept->size(-1);
+  if (c.each > INT32_MAX / c.size || d.each > INT32_MAX / c.size || !per_head(*scores, *K, b, c.each * c.size) || !per_head(*scores_out, *K, b, d.each * c.size) ||
+      !per_head(*kept, *K, b, budget) || lens_out->numel() != b)
+    NOT_HERE;
+  void *Kp = K->data_ptr(), *Vp = V->data_ptr(), *st = current_stream();
+  const int32_t *tp = at_of<int32_t>(table), *lp = at_of<int32_t>(lens), *up = at_of<int32_t>(table_out);
+  const float* sp = at_of<float>(scores);
+  int32_t *mp = at_of<int32_t>(lens_out), *kp = at_of<int32_t>(kept);
+  float* rp = at_of<float>(scores_out);
+  Py_INCREF(a[8]);
+  return result(WITHOUT_GIL(fn.paged_evict(Kp, Vp, tp, lp, sp, up, mp, rp, kp, b, c.h_kv, c.pages, c.size, c.each, d.each, c.k, c.v, (mqa_dtype)c.dt, budget, recent, st)),
+                "mqa_paged_evict_kv", a[8]);
+}
+
+// (logits, drafts, u, draft_logits, counts, temperature, tokens, accepted, workspace)
+MQA_CALL(verify, 9) {
+  const at::Tensor *logits = f32(a[0]), *drafts, *u, *draft_logits, *counts, *tokens, *accepted;
+  float temperature;
+  if (!logits || logits->dim() != 3 || !fits(*logits) || !maybe(a[1], at::kInt, &drafts) || !maybe(a[2], at::kFloat, &u) || !maybe(a[3], at::kFloat, &draft_logits) ||
+      !maybe(a[4], at::kInt, &counts) || !number(a[5], &temperature) || !maybe(a[6], at::kInt, &tokens) || !maybe(a[7], at::kInt, &accepted))
+    NOT_HERE;
+  const int64_t b = logits->size(0), n = logits->size(1) - 1, vocab = logits->size(2);
+  if (n < 0 || (drafts && !shape_is(*drafts, {b, n})) || (u && !shape_is(*u, {b, n + 1})) || (draft_logits && !shape_is(*draft_logits, {b, n, vocab})) ||
+      (counts && !shape_is(*counts, {b})) || (tokens && !shape_is(*tokens, {b, n + 1})) || (accepted && !shape_is(*accepted, {b})))
+    NOT_HERE;
+  Scratch ws;
+  if (!scratch(a[8], a[8] == Py_None ? fn.verify_workspace(b, n, vocab) : 0, *logits, &ws)) NOT_HERE;
+  const auto ints = logits->options().dtype(at::kInt).requires_grad(false);
+  at::Tensor new_tokens, new_accepted;
+  Held t{nullptr}, c{nullptr};
+  if (tokens) Py_INCREF(a[6]), t.p = a[6];
+  else new_tokens = at::empty({b, n + 1}, ints), tokens = &new_tokens, t.p = THPVariable_Wrap(new_tokens);
+  if (accepted) Py_INCREF(a[7]), c.p = a[7];
+  else new_accepted = at::empty({b}, ints), accepted = &new_accepted, c.p = THPVariable_Wrap(new_accepted);
+  if (!t.p || !c.p) NOT_HERE;
+  const float *lp = at_of<float>(logits), *qp = at_of<float>(draft_logits), *up = at_of<float>(u);
+  const int32_t *dp = at_of<int32_t>(drafts), *np = at_of<int32_t>(counts);
+  int32_t *tp = at_of<int32_t>(tokens), *ap = at_of<int32_t>(accepted);
+  void* st = current_stream();
+  PyObject* both = PyTuple_Pack(2, t.p, c.p);
+  if (!both) NOT_HERE;
+  return result(WITHOUT_GIL(fn.verify(lp, qp, dp, np, up, tp, ap, b, n, vocab, temperature, ws.at, ws.bytes, st)), "mqa_stack_verify_drafts", both);
+}
+
 // (the error's class, torch.nn.Parameter, addresses in the order of Functions)
 PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n) {
   constexpr Py_ssize_t count = sizeof(Functions) / sizeof(void*);
@@ -342,7 +486,7 @@ PyObject* torch_version(PyObject*, PyObject* const*, Py_ssize_t) { return PyUnic
 
 #define ENTRY(NAME) {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(NAME)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ENTRY(init), ENTRY(torch_version), ENTRY(decode), ENTRY(append_qkv), ENTRY(project), ENTRY(add_layernorm), ENTRY(memory_kv), ENTRY(attend_rows), ENTRY(beams),
-                         ENTRY(reorder), {nullptr, nullptr, 0, nullptr}};
+                         ENTRY(reorder), ENTRY(paged_append), ENTRY(paged_decode), ENTRY(paged_evict), ENTRY(verify), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", "Native argument marshalling of binding.py", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -402,3 +402,78 @@ def test_wrong_tensors_are_refused(m):
         m.mqa_paged_evict_kv(K, K, table, lens, s, table.clone(), lens.clone(), s[:, :32].contiguous(), kept, 0)
     with pytest.raises(m.MqaError):
         m.mqa_paged_evict_kv(K, K, table, lens, s, table.clone(), lens.clone(), s.clone(), kept, 9)
+
+
+class _Watch:
+    """The native calls, with what they returned; or (off) ones that take nothing."""
+
+    def __init__(self, native, on):
+        self.native, self.on, self.took = native, on, []
+
+    def __getattr__(self, name):
+        def call(*args):
+            done = getattr(self.native, name)(*args) if self.on else None
+            self.took.append((name, done is not None))
+            return done
+        return call
+
+
+@pytest.mark.parametrize("heads", [0, 2])
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_native_calls(heads, dtype, monkeypatch):
+    """Plain arguments are taken by the native calls, with the general path's results, a captured stream is left to it."""
+    import paper_1911_02150_amd.binding as m
+    m.load_library()
+    g = torch.Generator(device=DEV).manual_seed(9)
+    b, n, page, each, k = 3, 2, 16, 40, 64
+    lead, per = ((b * each * 2, page) if heads == 0 else (b * each * 2, heads, page)), ((b,) if heads == 0 else (b, heads))
+    K, V = (torch.randn((*lead, k), generator=g, device=DEV).to(dtype) for _ in range(2))
+    table, out = (torch.randperm(b * each, generator=g, device=DEV).to(torch.int32).view(b, each) + x for x in (0, b * each))
+    lens, scores = torch.tensor([600, 7, 0], dtype=torch.int32, device=DEV), torch.rand((*per, each * page), generator=g, device=DEV)
+    q, new = torch.randn((b, n, 4, k), generator=g, device=DEV), torch.randn((b, n, *per[1:], k), generator=g, device=DEV)
+    logits, drafts, u = torch.randn((b, n + 1, 50), generator=g, device=DEV), torch.ones((b, n), dtype=torch.int32, device=DEV), torch.rand((b, n + 1), generator=g, device=DEV)
+    ws = torch.empty(1 << 24, dtype=torch.uint8, device=DEV)
+
+    def append(counts):
+        Kc, Vc, after = K.clone(), V.clone(), torch.zeros_like(lens)
+        assert m.mqa_paged_append_kv_rows(Kc, Vc, table, new, new, lens, after, counts=counts) is after
+        return Kc, Vc, after
+
+    def scored(**kw):
+        s = torch.zeros_like(scores)
+        return m.mqa_paged_decode_step(q, K, V, table, lens, scores=scores, scores_out=s, **kw), s
+
+    def evict():
+        Kc, Vc, kept, after, s = K.clone(), V.clone(), torch.zeros((*per, 30), dtype=torch.int32, device=DEV), torch.zeros_like(lens), torch.zeros_like(scores)
+        assert m.mqa_paged_evict_kv(Kc, Vc, table, lens, scores, out, after, s, kept, 5) is kept
+        return Kc, Vc, kept, after, s
+
+    calls = [("paged_append", lambda: append(None)), ("paged_append", lambda: append(torch.tensor([1, 0, 2], dtype=torch.int32, device=DEV))),
+             ("paged_decode", lambda: m.mqa_paged_decode_step(q[:, 0].contiguous(), K, V, table, lens)),
+             ("paged_decode", lambda: m.mqa_paged_decode_step(q, K, V, table, lens, o=torch.zeros_like(q), scale=0.5, workspace=ws)),
+             ("paged_decode", scored), ("paged_decode", lambda: scored(workspace=ws)), ("paged_evict", evict),
+             ("verify", lambda: m.mqa_stack_verify_drafts(logits, drafts, u)),
+             ("verify", lambda: m.mqa_stack_verify_drafts(logits, drafts, u, draft_logits=logits[:, :n].contiguous(), counts=lens, temperature=0.5, workspace=ws,
+                                                          tokens=torch.zeros_like(drafts[:, :1]).repeat(1, n + 1), accepted=torch.zeros_like(lens)))]
+    native = m._native
+    for name, call in calls:
+        got = []
+        for on in (True, False):
+            watch = _Watch(native, on)
+            monkeypatch.setattr(m, "_native", watch)
+            got.append(call())
+            assert watch.took == [(name, on)], name
+        x, y = ((r if isinstance(r, tuple) else (r,)) for r in got)
+        assert len(x) == len(y) and all(torch.equal(c, d) and c.dtype == d.dtype and c.shape == d.shape for c, d in zip(x, y)), name
+    watch = _Watch(native, True)
+    monkeypatch.setattr(m, "_native", watch)
+    want, graph = m.mqa_paged_decode_step(q, K, V, table, lens), torch.cuda.CUDAGraph()
+    watch.took.clear()
+    with torch.cuda.graph(graph):
+        got = m.mqa_paged_decode_step(q, K, V, table, lens)
+    assert watch.took == [("paged_decode", False)]
+    graph.replay()
+    assert torch.equal(got, want)
+    for bad in (dict(q=q.transpose(1, 2)), dict(lens=lens[:2]), dict(scores=scores[..., 1:].contiguous()), dict(o=q[:, :1].contiguous()), dict(K_pages=K[..., :0], V_pages=V[..., :0, :])):
+        with pytest.raises((ValueError, m.MqaError)):
+            m.mqa_paged_decode_step(**{**dict(q=q, K_pages=K, V_pages=V, table=table, lens=lens), **bad})
