@@ -5,7 +5,8 @@
 // where no draft was refused): the lowest index at which the running sum exceeds u[n] times the whole.
 //
 // The indices are what comes out, so that everything between is held in float64: a running sum over 32768 probabilities in float32 is off by more than many of
-// them are.  Its exponential is the Taylor series of 2^x on [-1/2, 1/2]; the sums of the rows cost about as long as reading them.
+// them are.  An exponential is some twenty float64 instructions, 2^x by its Taylor series around the nearest integer.  Three launches: the rows' sums
+// (what reads, all but the drafts behind the count); the sums of what is left of the row that decides, in chunks; the chunk that holds the goal, element by element.
 #include "paged.hpp"
 
 namespace mqa {
@@ -15,34 +16,37 @@ constexpr int kThreads = 256;
 constexpr int kEach = 16;                          // logits of a thread
 constexpr int kChunk = kThreads * kEach;           // of a workgroup
 
-// What a chunk of a row of logits adds up to.
-struct ChunkStats { double sum; float most; int at; };       // sum of e^((x - most) / temperature); the largest logit and its lowest index
+// What a chunk of a row of logits adds up to: the sum of e^((x - most) / temperature); the largest logit and (temperature 0) its lowest index.
+struct ChunkStats { double sum; float most; int at; };
+struct RowStats { double sum; float most; int at; };
 
 // -inf for NaN, and +inf as the largest number: a row always has a distribution unless it is -inf throughout.
 __device__ __forceinline__ float tame(float x) { return x != x ? -INFINITY : fminf(x, 3.402823466e+38f); }
 
-// 2^x for x <= 0: the series sum (x ln 2)^k / k! to k = 13 (the next term is below 2^-54 of the sum on [-1/2, 1/2])
+// 2^x for x <= 0: with n the nearest integer (left in the low word by an addition that rounds to integers) and y = x - n the series sum (y ln 2)^k / k!
+// to k = 12, whose next term is below 2^-52 of the sum; below 2^-1000 nothing.
 __device__ __forceinline__ double exp2_of(double x) {
-  if (!(x > -1000.)) return 0.;                    // (2^-1000 of the largest: nothing in any sum; -inf)
-  const double whole = rint(x), y = (x - whole) * 0.6931471805599453094;
-  double s = 1. / 6227020800.;
-  s = fma(s, y, 1. / 479001600.);
-  s = fma(s, y, 1. / 39916800.);
-  s = fma(s, y, 1. / 3628800.);
-  s = fma(s, y, 1. / 362880.);
-  s = fma(s, y, 1. / 40320.);
-  s = fma(s, y, 1. / 5040.);
-  s = fma(s, y, 1. / 720.);
-  s = fma(s, y, 1. / 120.);
-  s = fma(s, y, 1. / 24.);
-  s = fma(s, y, 1. / 6.);
-  s = fma(s, y, 0.5);
+  const double shift = 6755399441055744.;          // 1.5 * 2^52
+  const double n = x + shift, y = x - (n - shift);
+  double s = 2.5678435993488205e-11;               // ln(2)^12 / 12! and so on
+  s = fma(s, y, 4.4455382718708115e-10);
+  s = fma(s, y, 7.0549116208011233e-9);
+  s = fma(s, y, 1.0178086009239700e-7);
+  s = fma(s, y, 1.3215486790144309e-6);
+  s = fma(s, y, 1.5252733804059840e-5);
+  s = fma(s, y, 1.5403530393381610e-4);
+  s = fma(s, y, 1.3333558146428443e-3);
+  s = fma(s, y, 9.6181291076284772e-3);
+  s = fma(s, y, 5.5504108664821580e-2);
+  s = fma(s, y, 0.24022650695910071);
+  s = fma(s, y, 0.69314718055994531);
   s = fma(s, y, 1.);
-  s = fma(s, y, 1.);
-  return ldexp(s, (int)whole);
+  const double z = __hiloint2double(__double2hiint(s) + (__double2loint(n) << 20), __double2loint(s));
+  return x > -1000. ? z : 0.;                      // (-inf, and what a row of -inf throughout gives, NaN, are here)
 }
 // e^((x - most) / temperature), `per` = log2(e) / temperature
-__device__ __forceinline__ double weight(float x, float most, double per) { return most == -INFINITY ? 0. : exp2_of(((double)x - (double)most) * per); }
+__device__ __forceinline__ double weight(float x, float most, double per) { return exp2_of(((double)x - (double)most) * per); }
+__device__ __forceinline__ double per_of(const Verify& p) { return 1.4426950408889634074 / (double)p.temperature; }
 
 __device__ __forceinline__ void better(float& x, int& i, float y, int j) {
   if (y > x || (y == x && j < i)) { x = y; i = j; }
@@ -51,7 +55,6 @@ __device__ __forceinline__ void better(float& x, int& i, float y, int j) {
 __device__ __forceinline__ double block_sum(double x, double* red) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) x += __shfl_xor(x, o);
-  __syncthreads();
   if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = x;
   __syncthreads();
   return (red[0] + red[1]) + (red[2] + red[3]);
@@ -59,105 +62,158 @@ __device__ __forceinline__ double block_sum(double x, double* red) {
 
 __device__ __forceinline__ int drafts_of(const Verify& p, int i) { return p.counts ? min(max(p.counts[i], 0), p.n) : p.n; }
 
+// A thread's 16 logits of a chunk: 16 bytes at a time where rows are aligned; past the end -inf.  at(e): the index of the e-th.
+struct Logits {
+  float x[kEach];
+  int first, step;
+  __device__ __forceinline__ Logits(const float* row, int chunk, int vocab, bool aligned) {
+    if (aligned) {
+      first = chunk * kChunk + 4 * (int)threadIdx.x;
+      step = 4 * kThreads;
+#pragma unroll
+      for (int e = 0; e < kEach / 4; ++e) {
+        float4 v = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+        if (first + e * step < vocab) v = *reinterpret_cast<const float4*>(row + first + e * step);
+        x[4 * e] = v.x; x[4 * e + 1] = v.y; x[4 * e + 2] = v.z; x[4 * e + 3] = v.w;
+      }
+    } else {
+      first = chunk * kChunk + (int)threadIdx.x;
+      step = 0;
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) x[e] = first + e * kThreads < vocab ? row[first + e * kThreads] : -INFINITY;
+    }
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) x[e] = tame(x[e]);
+  }
+  __device__ __forceinline__ int at(int e) const { return step ? first + (e >> 2) * step + (e & 3) : first + e * kThreads; }
+};
+
 // rows of a sequence: n + 1 of the target, then n of the draft
+template <bool GREEDY>
 __global__ __launch_bounds__(kThreads)
 void verify_stats_kernel(Verify p, int chunks, int rows, ChunkStats* stats) {
   __shared__ double red[4];
   __shared__ float s_most[4];
   __shared__ int s_at[4];
-  const int chunk = blockIdx.x % chunks, row = blockIdx.x / chunks % rows, i = blockIdx.x / chunks / rows;
+  const unsigned line = blockIdx.x / (unsigned)chunks;
+  const int chunk = (int)(blockIdx.x - line * chunks), i = (int)(line / (unsigned)rows), row = (int)line - i * rows;
   const int count = drafts_of(p, i);
   const bool drafted = row > p.n;
   const int j = drafted ? row - p.n - 1 : row;
   if (drafted ? j >= count : j > count) return;
-  const float* x = drafted ? p.draft_logits + ((size_t)i * p.n + j) * p.vocab : p.logits + ((size_t)i * (p.n + 1) + j) * p.vocab;
-  const int first = chunk * kChunk;
-  float val[kEach];
+  const Logits v(drafted ? p.draft_logits + ((size_t)i * p.n + j) * p.vocab : p.logits + ((size_t)i * (p.n + 1) + j) * p.vocab, chunk, p.vocab, (p.vocab & 3) == 0);
   float most = -INFINITY;
   int at = 0x7fffffff;
 #pragma unroll
   for (int e = 0; e < kEach; ++e) {
-    const int idx = first + e * kThreads + threadIdx.x;
-    val[e] = idx < p.vocab ? tame(x[idx]) : -INFINITY;
+    if constexpr (GREEDY) {
+      if (v.at(e) < p.vocab) better(most, at, v.x[e], v.at(e));
+    } else {
+      most = fmaxf(most, v.x[e]);
+    }
   }
 #pragma unroll
-  for (int e = 0; e < kEach; ++e) {
-    const int idx = first + e * kThreads + threadIdx.x;
-    if (idx < p.vocab) better(most, at, val[e], idx);
+  for (int o = 32; o > 0; o >>= 1) {
+    if constexpr (GREEDY) better(most, at, __shfl_xor(most, o), __shfl_xor(at, o));
+    else most = fmaxf(most, __shfl_xor(most, o));
   }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) better(most, at, __shfl_xor(most, o), __shfl_xor(at, o));
   if ((threadIdx.x & 63) == 0) { s_most[threadIdx.x >> 6] = most; s_at[threadIdx.x >> 6] = at; }
   __syncthreads();
 #pragma unroll
-  for (int w = 0; w < 4; ++w) better(most, at, s_most[w], s_at[w]);
+  for (int w = 0; w < 4; ++w) {
+    if constexpr (GREEDY) better(most, at, s_most[w], s_at[w]);
+    else most = fmaxf(most, s_most[w]);
+  }
   double sum = 0.;
-  if (p.temperature > 0.f) {
-    const double per = 1.4426950408889634074 / (double)p.temperature;
+  if constexpr (!GREEDY) {
+    const double per = per_of(p);
 #pragma unroll
-    for (int e = 0; e < kEach; ++e) sum += weight(val[e], most, per);
+    for (int e = 0; e < kEach; ++e) sum += weight(v.x[e], most, per);
     sum = block_sum(sum, red);
   }
-  if (threadIdx.x == 0) stats[((size_t)i * rows + row) * chunks + chunk] = ChunkStats{sum, most, at};
+  if (threadIdx.x == 0) stats[(size_t)line * chunks + chunk] = ChunkStats{sum, most, at};
 }
 
-struct RowStats { double sum; float most; int at; };
-__device__ __forceinline__ RowStats row_stats(const ChunkStats* s, int chunks, double per) {
+// A row's statistics from its chunks', by a group of `lanes` neighbouring threads (a power of two up to 64), of which this is the x-th; all get them.
+template <bool GREEDY>
+__device__ __forceinline__ RowStats row_stats(const ChunkStats* s, int chunks, double per, int x, int lanes) {
   RowStats r{0., -INFINITY, 0x7fffffff};
-  for (int c = 0; c < chunks; ++c) better(r.most, r.at, s[c].most, s[c].at);
-  if (per > 0.)
-    for (int c = 0; c < chunks; ++c) r.sum += s[c].sum * weight(s[c].most, r.most, per);
+  for (int c = x; c < chunks; c += lanes) {
+    const ChunkStats y = s[c];
+    if constexpr (GREEDY) {
+      better(r.most, r.at, y.most, y.at);
+    } else {
+      const float most = fmaxf(r.most, y.most);
+      r.sum = r.sum * weight(r.most, most, per) + y.sum * weight(y.most, most, per);
+      r.most = most;
+    }
+  }
+  for (int o = 1; o < lanes; o <<= 1) {
+    const float most = __shfl_xor(r.most, o);
+    if constexpr (GREEDY) {
+      better(r.most, r.at, most, __shfl_xor(r.at, o));
+    } else {
+      const float both = fmaxf(r.most, most);
+      r.sum = r.sum * weight(r.most, both, per) + __shfl_xor(r.sum, o) * weight(most, both, per);
+      r.most = both;
+    }
+  }
   return r;
 }
 
 // How many drafts stand, and the distribution of the token behind them: all threads of the workgroup together.
-struct Choice { int accepted; bool refused; int drafted; RowStats p, q; };
+struct Choice { int accepted, drafted; bool refused; RowStats p, q; };
+template <bool GREEDY>
 __device__ __forceinline__ Choice choose(const Verify& p, int i, int chunks, int rows, const ChunkStats* stats, int* s_first) {
-  const int count = drafts_of(p, i);
-  const double per = p.temperature > 0.f ? 1.4426950408889634074 / (double)p.temperature : 0.;
+  const int count = drafts_of(p, i), tid = threadIdx.x;
+  const double per = GREEDY ? 0. : per_of(p);
   const ChunkStats* mine = stats + (size_t)i * rows * chunks;
-  if (threadIdx.x == 0) *s_first = count;
+  int lanes = 64;
+  while (lanes > 1 && lanes / 2 >= chunks) lanes >>= 1;
+  const int x = tid & (lanes - 1), group = tid / lanes, groups = kThreads / lanes;
+  if (tid == 0) *s_first = count;
   __syncthreads();
-  for (int j = threadIdx.x; j < count; j += kThreads) {
-    const int t = p.drafts[(size_t)i * p.n + j];
-    const RowStats a = row_stats(mine + (size_t)j * chunks, chunks, per);
+  for (int j0 = 0; j0 < count; j0 += groups) {             // (all threads of a group, so that they can exchange)
+    const int j = min(j0 + group, count - 1), t = p.drafts[(size_t)i * p.n + j];
+    const RowStats a = row_stats<GREEDY>(mine + (size_t)j * chunks, chunks, per, x, lanes);
     bool stands = false;
-    if (t >= 0 && t < p.vocab) {
-      if (per == 0.) {
-        stands = t == (a.at < p.vocab ? a.at : 0);
+    const bool token = t >= 0 && t < p.vocab;
+    if constexpr (GREEDY) {
+      stands = token && t == (a.at < p.vocab && a.most > -INFINITY ? a.at : 0);
+    } else {
+      const double u = p.u[(size_t)i * (p.n + 1) + j];
+      const double pt = weight(token ? tame(p.logits[((size_t)i * (p.n + 1) + j) * p.vocab + t]) : -INFINITY, a.most, per);
+      if (p.draft_logits) {
+        const RowStats d = row_stats<false>(mine + (size_t)(p.n + 1 + j) * chunks, chunks, per, x, lanes);
+        const double qt = weight(token ? tame(p.draft_logits[((size_t)i * p.n + j) * p.vocab + t]) : -INFINITY, d.most, per);
+        stands = pt > 0. && u * qt * a.sum < pt * d.sum;
+        if (d.sum == 0.) stands = pt > 0.;                 // (a draft row of -inf throughout: probabilities of 0)
       } else {
-        const double u = p.u[(size_t)i * (p.n + 1) + j];
-        const double pt = weight(tame(p.logits[((size_t)i * (p.n + 1) + j) * p.vocab + t]), a.most, per);
-        if (p.draft_logits) {
-          const RowStats d = row_stats(mine + (size_t)(p.n + 1 + j) * chunks, chunks, per);
-          const double qt = weight(tame(p.draft_logits[((size_t)i * p.n + j) * p.vocab + t]), d.most, per);
-          stands = u * qt * a.sum < pt * d.sum;
-        } else {
-          stands = u * a.sum < pt;
-        }
+        stands = pt > 0. && u * a.sum < pt;
       }
     }
-    if (!stands) atomicMin(s_first, j);
+    if (!stands && x == 0) atomicMin(s_first, j);
   }
   __syncthreads();
   Choice c;
   c.accepted = *s_first;
   c.refused = c.accepted < count;
   c.drafted = c.refused ? p.drafts[(size_t)i * p.n + c.accepted] : -1;
-  c.p = row_stats(mine + (size_t)c.accepted * chunks, chunks, per);
+  c.p = row_stats<GREEDY>(mine + (size_t)c.accepted * chunks, chunks, per, x, lanes);
   c.q = RowStats{0., -INFINITY, 0};
-  if (c.refused && p.draft_logits && per > 0.) c.q = row_stats(mine + (size_t)(p.n + 1 + c.accepted) * chunks, chunks, per);
+  if constexpr (!GREEDY)
+    if (c.refused && p.draft_logits) c.q = row_stats<false>(mine + (size_t)(p.n + 1 + c.accepted) * chunks, chunks, per, x, lanes);
   return c;
 }
 
-// What p has over q at index v, times the sum of p's row.
+// What p has over q, times the sum of p's row.
 struct Rest {
-  const float *x, *y;
-  float most_p, most_q;
+  const float *x, *y;      // the rows of logits; y null: nothing is taken off but the drafted token
   double per, scale_q;
+  float most_p, most_q;
   int drafted;
   __device__ __forceinline__ Rest(const Verify& p, int i, const Choice& c) {
-    per = 1.4426950408889634074 / (double)p.temperature;
+    per = per_of(p);
     x = p.logits + ((size_t)i * (p.n + 1) + c.accepted) * p.vocab;
     y = c.refused && p.draft_logits ? p.draft_logits + ((size_t)i * p.n + c.accepted) * p.vocab : nullptr;
     most_p = c.p.most;
@@ -165,11 +221,10 @@ struct Rest {
     scale_q = c.q.sum > 0. ? c.p.sum / c.q.sum : 0.;
     drafted = y ? -1 : c.drafted;
   }
-  __device__ __forceinline__ double at(int v) const {
+  __device__ __forceinline__ double of(int v, float lp, float lq) const {
     if (v == drafted) return 0.;
-    double r = weight(tame(x[v]), most_p, per);
-    if (y) r = fmax(r - weight(tame(y[v]), most_q, per) * scale_q, 0.);
-    return r;
+    const double r = weight(lp, most_p, per);
+    return y ? fmax(r - weight(lq, most_q, per) * scale_q, 0.) : r;
   }
 };
 
@@ -177,27 +232,34 @@ __global__ __launch_bounds__(kThreads)
 void verify_rest_kernel(Verify p, int chunks, int rows, const ChunkStats* stats, double* rest) {
   __shared__ double red[4];
   __shared__ int s_first;
-  const int chunk = blockIdx.x % chunks, i = blockIdx.x / chunks;
-  const Choice c = choose(p, i, chunks, rows, stats, &s_first);
+  const int i = (int)(blockIdx.x / (unsigned)chunks), chunk = (int)blockIdx.x - i * chunks;
+  const Choice c = choose<false>(p, i, chunks, rows, stats, &s_first);
   const Rest r(p, i, c);
+  const bool aligned = (p.vocab & 3) == 0;
+  const Logits lp(r.x, chunk, p.vocab, aligned);
   double sum = 0.;
-#pragma unroll 4
-  for (int e = 0; e < kEach; ++e) {
-    const int v = chunk * kChunk + e * kThreads + threadIdx.x;
-    if (v < p.vocab) sum += r.at(v);
+  if (r.y) {
+    const Logits lq(r.y, chunk, p.vocab, aligned);
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) sum += r.of(lp.at(e), lp.x[e], lq.x[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) sum += r.of(lp.at(e), lp.x[e], 0.f);
   }
   sum = block_sum(sum, red);
   if (threadIdx.x == 0) rest[(size_t)i * chunks + chunk] = sum;
 }
 
+template <bool GREEDY>
 __global__ __launch_bounds__(kThreads)
 void verify_draw_kernel(Verify p, int chunks, int rows, const ChunkStats* stats, const double* rest) {
-  __shared__ int s_first, s_token, s_last;
+  __shared__ int s_first, s_token, s_last, s_at[4];
   __shared__ double s_waves[4];
+  __shared__ float s_most[4];
   const int i = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const Choice c = choose(p, i, chunks, rows, stats, &s_first);
-  int token = c.p.at < p.vocab ? c.p.at : 0;             // the most probable (a row of -inf throughout: 0)
-  if (p.temperature > 0.f) {
+  const Choice c = choose<GREEDY>(p, i, chunks, rows, stats, &s_first);
+  int token = c.p.at < p.vocab && c.p.most > -INFINITY ? c.p.at : 0;      // (a row of -inf throughout: 0)
+  if constexpr (!GREEDY) {
     const Rest r(p, i, c);
     double total = 0.;
     for (int x = 0; x < chunks; ++x) total += rest[(size_t)i * chunks + x];
@@ -216,10 +278,16 @@ void verify_draw_kernel(Verify p, int chunks, int rows, const ChunkStats* stats,
       if (!inside) chunk = last;
       if (tid == 0) { s_token = 0x7fffffff; s_last = -1; }
       double val[kEach], mine = 0.;
-      const int v0 = chunk * kChunk + tid * kEach;
+      const int v0 = chunk * kChunk + tid * kEach;         // (neighbouring elements: the order counts)
+      float lp[kEach], lq[kEach];
 #pragma unroll
       for (int e = 0; e < kEach; ++e) {
-        val[e] = v0 + e < p.vocab ? r.at(v0 + e) : 0.;
+        lp[e] = v0 + e < p.vocab ? r.x[v0 + e] : -INFINITY;
+        lq[e] = r.y && v0 + e < p.vocab ? r.y[v0 + e] : -INFINITY;
+      }
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) {
+        val[e] = r.of(v0 + e, tame(lp[e]), tame(lq[e]));
         mine += val[e];
       }
       double incl = mine;
@@ -246,6 +314,17 @@ void verify_draw_kernel(Verify p, int chunks, int rows, const ChunkStats* stats,
       __syncthreads();
       if (s_token != 0x7fffffff) token = s_token;
       else if (s_last >= 0) token = s_last;
+    } else {                                               // nothing to draw from: the largest logit
+      float most = -INFINITY;
+      int at = 0x7fffffff;
+      for (int v = tid; v < p.vocab; v += kThreads) better(most, at, tame(r.x[v]), v);
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) better(most, at, __shfl_xor(most, o), __shfl_xor(at, o));
+      if (lane == 0) { s_most[wave] = most; s_at[wave] = at; }
+      __syncthreads();
+#pragma unroll
+      for (int w = 0; w < 4; ++w) better(most, at, s_most[w], s_at[w]);
+      token = most > -INFINITY ? at : 0;
     }
   }
   for (int j = tid; j <= p.n; j += kThreads)
@@ -266,15 +345,20 @@ hipError_t launch_verify(const Verify& p, void* workspace, hipStream_t st) {
   const int chunks = verify_chunks(p.vocab), rows = p.draft_logits && p.temperature > 0.f ? 2 * p.n + 1 : p.n + 1;
   ChunkStats* stats = static_cast<ChunkStats*>(workspace);
   double* rest = reinterpret_cast<double*>(stats + (size_t)p.b * rows * chunks);
-  hipLaunchKernelGGL(verify_stats_kernel, dim3((unsigned)((size_t)p.b * rows * chunks)), dim3(kThreads), 0, st, p, chunks, rows, stats);
+  const dim3 all((unsigned)((size_t)p.b * rows * chunks)), rests((unsigned)((size_t)p.b * chunks)), each((unsigned)p.b), block(kThreads);
+  const bool greedy = !(p.temperature > 0.f);
+  if (greedy) hipLaunchKernelGGL(verify_stats_kernel<true>, all, block, 0, st, p, chunks, rows, stats);
+  else hipLaunchKernelGGL(verify_stats_kernel<false>, all, block, 0, st, p, chunks, rows, stats);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  if (p.temperature > 0.f) {
-    hipLaunchKernelGGL(verify_rest_kernel, dim3((unsigned)((size_t)p.b * chunks)), dim3(kThreads), 0, st, p, chunks, rows, stats, rest);
-    e = hipGetLastError();
-    if (e != hipSuccess) return e;
+  if (greedy) {
+    hipLaunchKernelGGL(verify_draw_kernel<true>, each, block, 0, st, p, chunks, rows, stats, rest);
+    return hipGetLastError();
   }
-  hipLaunchKernelGGL(verify_draw_kernel, dim3((unsigned)p.b), dim3(kThreads), 0, st, p, chunks, rows, stats, rest);
+  hipLaunchKernelGGL(verify_rest_kernel, rests, block, 0, st, p, chunks, rows, stats, rest);
+  e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  hipLaunchKernelGGL(verify_draw_kernel<false>, each, block, 0, st, p, chunks, rows, stats, rest);
   return hipGetLastError();
 }
 
