@@ -76,13 +76,18 @@ __device__ __forceinline__ int before_me(int x, int* waves, int* total) {
 
 // Which positions of (sequence, head) stay: the latest `recent`, and of the older ones the largest scores up to the budget, the lower position among
 // equals.  A radix selection over the keys, 11 + 11 + 10 bits from the top: a histogram of the keys that agree with the threshold so far, and the bin in
-// which the wanted rank lies.  One workgroup per (sequence, head).
+// which the wanted rank lies.  One workgroup per (sequence, head), which is bound by the latency of its steps: a thread's KEEP positions (tid, tid + 1024, ...) are
+// read once and stay in registers, and what stays is put in order by two sums over all of them, not two for every 1024 (8192 positions: 36 -> 12.7 us).  Capacities
+// beyond (KEEP = 0) are gone over again for every step.
+template <int KEEP>
 __global__ __launch_bounds__(kSelectThreads)
 void evict_select_kernel(PagedEvict p) {
+  constexpr int kWaves = kSelectThreads / 64;
   __shared__ int bins[kBins];
-  __shared__ int waves[kSelectThreads / 64];
+  __shared__ int waves[kWaves];
   __shared__ int s_bin, s_above;
-  const int tid = threadIdx.x;
+  __shared__ int s_count[2][(KEEP > 0 ? KEEP : 1) * kWaves + 1];      // of a wave's 64 positions: those at the threshold, those that stay
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int g = blockIdx.x, i = g / p.c.h_kv;
   const int L = paged_length(p.c, p.lens_in[i]);
   const int32_t* table = p.c.table + (size_t)i * p.c.max_pages;
@@ -90,20 +95,44 @@ void evict_select_kernel(PagedEvict p) {
   const int old = max(0, L - p.recent);
   auto there = [&](int pos) { return (unsigned)table[(unsigned)pos / (unsigned)p.c.page_size] < (unsigned)p.c.num_pages; };
   auto key_of = [&](int pos) -> uint32_t { return pos < old && there(pos) ? score_key(score[pos]) : 0u; };      // 0: not one of the older ones
+  uint32_t keys[KEEP > 0 ? KEEP : 1];
+  float values[KEEP > 0 ? KEEP : 1];
+  uint32_t late = 0;                   // bit u: the thread's u-th position is one of the latest, and there
   int n_old = 0, n_recent = 0;
-  for (int pos = tid; pos < L; pos += kSelectThreads)
-    if (there(pos)) (pos < old ? n_old : n_recent) += 1;
+  if constexpr (KEEP > 0) {
+    const unsigned size = p.c.page_size, step = kSelectThreads / size, more = kSelectThreads % size;
+    unsigned page = (unsigned)tid / size, inside = (unsigned)tid % size;      // of position tid + u * 1024
+#pragma unroll
+    for (int u = 0; u < KEEP; ++u) {   // (past the length: the first entry and score, which are there)
+      const int pos = tid + u * kSelectThreads;
+      keys[u] = (uint32_t)table[pos < L ? page : 0u];
+      values[u] = score[pos < L ? pos : 0];
+      page += step;
+      inside += more;
+      if (inside >= size) { inside -= size; ++page; }
+    }
+#pragma unroll
+    for (int u = 0; u < KEEP; ++u) {
+      const int pos = tid + u * kSelectThreads;
+      const bool is = pos < L && keys[u] < (unsigned)p.c.num_pages;
+      keys[u] = is && pos < old ? score_key(values[u]) : 0u;
+      late |= (uint32_t)(is && pos >= old) << u;
+      n_old += keys[u] != 0;
+    }
+    n_recent = __popc(late);
+  } else {
+    for (int pos = tid; pos < L; pos += kSelectThreads)
+      if (there(pos)) (pos < old ? n_old : n_recent) += 1;
+  }
   int all_old, all_recent;
   before_me(n_old, waves, &all_old);
   before_me(n_recent, waves, &all_recent);
-  int want = min(all_old, p.budget - min(all_recent, p.budget));
+  const int want = min(all_old, p.budget - min(all_recent, p.budget));
   uint32_t threshold = 0;              // keys above it stay, and of those equal to it the first `ties`
   int ties = 0;
-  if (want == all_old) {
-    threshold = 0;                     // (every one: their keys are above 0)
-  } else if (want == 0) {
+  if (want == 0) {
     threshold = 0xffffffffu;
-  } else {
+  } else if (want < all_old) {         // (else every one: their keys are above 0)
     int rank = want;                   // the rank of the threshold among the keys that agree with its upper bits
     const int shifts[3] = {21, 10, 0}, sizes[3] = {11, 11, 10};
 #pragma unroll
@@ -112,9 +141,14 @@ void evict_select_kernel(PagedEvict p) {
       const uint32_t agree = pass == 0 ? 0u : ~0u << (shift + sizes[pass]);
       for (int x = tid; x < count; x += kSelectThreads) bins[x] = 0;
       __syncthreads();
-      for (int pos = tid; pos < old; pos += kSelectThreads) {
-        const uint32_t key = key_of(pos);
+      auto add = [&](uint32_t key) {
         if (key != 0 && (key & agree) == (threshold & agree)) atomicAdd(&bins[(key >> shift) & (count - 1)], 1);
+      };
+      if constexpr (KEEP > 0) {
+#pragma unroll
+        for (int u = 0; u < KEEP; ++u) add(keys[u]);
+      } else {
+        for (int pos = tid; pos < old; pos += kSelectThreads) add(key_of(pos));
       }
       __syncthreads();
       // bins from the top: thread t has the two (or the one) from count - 1 - 2t down
@@ -134,20 +168,71 @@ void evict_select_kernel(PagedEvict p) {
   // the positions that stay, in order
   int32_t* kept = p.kept + (size_t)g * p.budget;
   float* score_out = p.scores_out + (size_t)g * p.max_pages_out * p.c.page_size;
-  int done = 0, tied = 0;
-  for (int base = 0; base < L; base += kSelectThreads) {
-    const int pos = base + tid;
-    const uint32_t key = pos < old ? key_of(pos) : 0u;
-    const bool equal = key != 0 && key == threshold;
-    int total;
-    const int equals_before = tied + before_me(equal ? 1 : 0, waves, &total);
-    tied += total;
-    const bool stays = pos < L && (pos < old ? key > threshold || (equal && equals_before < ties) : there(pos));
-    const int slot = done + before_me(stays ? 1 : 0, waves, &total);
-    done += total;
-    if (stays && slot < p.budget) {
-      kept[slot] = pos;
-      score_out[slot] = score[pos];
+  int done = 0;
+  if constexpr (KEEP > 0) {
+    // in order: by u, then by wave, then by lane
+    const unsigned long long below = (1ull << lane) - 1;
+    auto in_order = [&](int which) {   // the counts of all waves in the place of their running sum; the last: of all
+      constexpr int all = KEEP * kWaves;
+      static_assert(all <= kSelectThreads, "a count a thread");
+      __syncthreads();
+      int total;
+      const int before = before_me(tid < all ? s_count[which][tid] : 0, waves, &total);
+      if (tid < all) s_count[which][tid] = before;
+      if (tid == 0) s_count[which][all] = total;
+      __syncthreads();
+    };
+    uint32_t equal = 0, stays = late;
+#pragma unroll
+    for (int u = 0; u < KEEP; ++u) {
+      equal |= (uint32_t)(keys[u] != 0 && keys[u] == threshold) << u;
+      stays |= (uint32_t)(keys[u] > threshold) << u;
+    }
+    if (ties > 0) {
+#pragma unroll
+      for (int u = 0; u < KEEP; ++u) {
+        const unsigned long long those = __ballot(equal >> u & 1);
+        if (lane == 0) s_count[0][u * kWaves + wave] = __popcll(those);
+      }
+      in_order(0);
+#pragma unroll
+      for (int u = 0; u < KEEP; ++u) {
+        const unsigned long long those = __ballot(equal >> u & 1);
+        if ((equal >> u & 1) && s_count[0][u * kWaves + wave] + __popcll(those & below) < ties) stays |= 1u << u;
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < KEEP; ++u) {
+      const unsigned long long those = __ballot(stays >> u & 1);
+      if (lane == 0) s_count[1][u * kWaves + wave] = __popcll(those);
+    }
+    in_order(1);
+#pragma unroll
+    for (int u = 0; u < KEEP; ++u) {
+      const unsigned long long those = __ballot(stays >> u & 1);
+      const int slot = s_count[1][u * kWaves + wave] + __popcll(those & below);
+      if ((stays >> u & 1) && slot < p.budget) {
+        kept[slot] = tid + u * kSelectThreads;
+        score_out[slot] = values[u];
+      }
+    }
+    done = s_count[1][KEEP * kWaves];
+  } else {
+    int tied = 0;
+    for (int base = 0; base < L; base += kSelectThreads) {
+      const int pos = base + tid;
+      const uint32_t key = pos < old ? key_of(pos) : 0u;
+      const bool equal = key != 0 && key == threshold;
+      int total;
+      const int equals_before = tied + before_me(equal ? 1 : 0, waves, &total);
+      tied += total;
+      const bool stays = pos < L && (pos < old ? key > threshold || (equal && equals_before < ties) : there(pos));
+      const int slot = done + before_me(stays ? 1 : 0, waves, &total);
+      done += total;
+      if (stays && slot < p.budget) {
+        kept[slot] = pos;
+        score_out[slot] = score[pos];
+      }
     }
   }
   done = min(done, p.budget);
@@ -155,24 +240,26 @@ void evict_select_kernel(PagedEvict p) {
   if (g % p.c.h_kv == 0 && tid == 0) p.lens_out[i] = done;
 }
 
-// The rows that stay, 16 bytes a thread.
+// The rows that stay: 16 lanes a row, a word of K and one of V of each on their way together.  A row costs a chain (kept position -> two table entries -> row)
+// that other waves cover: 56000 rows of 512 bytes 13 us (4.6 TB/s read and written), where a thread with two rows takes 24 and one with a single word 19.
+// (Without branches around the loads, which would wait for one another: what is not to be copied is read from the pool's first row.)
+constexpr int kCopyLanes = 16, kCopyEach = 256 / kCopyLanes;      // lanes of a row, rows of a workgroup
 __global__ __launch_bounds__(256)
-void evict_copy_kernel(PagedEvict p, int k16, int v16) {
-  const int w16 = k16 + v16;
-  const size_t idx = (size_t)blockIdx.x * 256 + threadIdx.x;
-  const size_t line = idx / w16;                                  // (sequence, head, slot)
-  const size_t g = line / p.budget;
-  if (g >= (size_t)p.b * p.c.h_kv) return;
-  const int x = (int)(idx - line * w16), slot = (int)(line - g * p.budget);
-  const int i = (int)(g / p.c.h_kv), e = (int)(g - (size_t)i * p.c.h_kv);
-  const int pos = p.kept[line];
-  if (pos < 0) return;
-  const int from = paged_row(p.c, p.c.table + (size_t)i * p.c.max_pages, e, pos);
+void evict_copy_kernel(PagedEvict p, int k16, int v16, int pieces) {
+  const int g = (int)(blockIdx.x / (unsigned)pieces), piece = (int)blockIdx.x - g * pieces;
+  const int i = g / p.c.h_kv, e = g - i * p.c.h_kv;
+  const int mine = piece * kCopyEach + (int)threadIdx.x / kCopyLanes, slot = min(mine, p.budget - 1);
+  const int pos = p.kept[(size_t)g * p.budget + slot];
+  const int from = paged_row(p.c, p.c.table + (size_t)i * p.c.max_pages, e, max(pos, 0));
   const int to = paged_row(p.c, p.table_out + (size_t)i * p.max_pages_out, e, slot);
-  if (from < 0 || to < 0) return;
-  uint4* pool = static_cast<uint4*>(x < k16 ? p.c.K : p.c.V);
-  const int width = x < k16 ? k16 : v16, at = x < k16 ? x : x - k16;
-  pool[(size_t)to * width + at] = pool[(size_t)from * width + at];
+  const bool copied = mine < p.budget && pos >= 0 && from >= 0 && to >= 0;
+  const size_t src = max(from, 0), dst = max(to, 0);
+  uint4 *K = static_cast<uint4*>(p.c.K), *V = static_cast<uint4*>(p.c.V);
+  for (int x = threadIdx.x & (kCopyLanes - 1); x < max(k16, v16); x += kCopyLanes) {
+    const uint4 kw = K[src * k16 + min(x, k16 - 1)], vw = V[src * v16 + min(x, v16 - 1)];
+    if (copied && x < k16) K[dst * k16 + x] = kw;
+    if (copied && x < v16) V[dst * v16 + x] = vw;
+  }
 }
 
 }  // namespace
@@ -186,13 +273,16 @@ hipError_t launch_paged_append(const PagedAppend& p, int is_bf16, hipStream_t st
 }
 
 hipError_t launch_paged_evict(const PagedEvict& p, int is_bf16, hipStream_t st) {
-  const int groups = p.b * p.c.h_kv, esz = is_bf16 ? 2 : 4;
-  hipLaunchKernelGGL(evict_select_kernel, dim3((unsigned)groups), dim3(kSelectThreads), 0, st, p);
-  hipError_t e = hipGetLastError();
+  const int groups = p.b * p.c.h_kv, esz = is_bf16 ? 2 : 4, each = (p.c.positions() + kSelectThreads - 1) / kSelectThreads;
+  const dim3 grid((unsigned)groups), block(kSelectThreads);
+  if (each <= 3) hipLaunchKernelGGL(evict_select_kernel<3>, grid, block, 0, st, p);
+  else if (each <= 10) hipLaunchKernelGGL(evict_select_kernel<10>, grid, block, 0, st, p);
+  else if (each <= 24) hipLaunchKernelGGL(evict_select_kernel<24>, grid, block, 0, st, p);
+  else hipLaunchKernelGGL(evict_select_kernel<0>, grid, block, 0, st, p);
+  const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const int k16 = p.c.k * esz / 16, v16 = p.c.v * esz / 16;
-  const size_t threads = (size_t)groups * p.budget * (k16 + v16);
-  hipLaunchKernelGGL(evict_copy_kernel, dim3((unsigned)((threads + 255) / 256)), dim3(256), 0, st, p, k16, v16);
+  const int pieces = (p.budget + kCopyEach - 1) / kCopyEach;
+  hipLaunchKernelGGL(evict_copy_kernel, dim3((unsigned)groups * pieces), dim3(256), 0, st, p, p.c.k * esz / 16, p.c.v * esz / 16, pieces);
   return hipGetLastError();
 }
 

@@ -6,7 +6,8 @@
 //
 // The indices are what comes out, so that everything between is held in float64: a running sum over 32768 probabilities in float32 is off by more than many of
 // them are.  An exponential is some twenty float64 instructions, 2^x by its Taylor series around the nearest integer.  Three launches: the rows' sums
-// (what reads, all but the drafts behind the count); the sums of what is left of the row that decides, in chunks; the chunk that holds the goal, element by element.
+// (what reads, all but the drafts behind the count); the choice of the row that decides, and what is left of it in segments of 256 tokens; the segment that
+// holds the goal, token by token.
 #include "paged.hpp"
 
 namespace mqa {
@@ -24,13 +25,11 @@ struct RowStats { double sum; float most; int at; };
 __device__ __forceinline__ float tame(float x) { return x != x ? -INFINITY : fminf(x, 3.402823466e+38f); }
 
 // 2^x for x <= 0: with n the nearest integer (left in the low word by an addition that rounds to integers) and y = x - n the series sum (y ln 2)^k / k!
-// to k = 12, whose next term is below 2^-52 of the sum; below 2^-1000 nothing.
+// to k = 10, whose next term is below 2^-42 of the sum (an index goes wrong where the goal is that near a border); below 2^-1000 nothing.
 __device__ __forceinline__ double exp2_of(double x) {
   const double shift = 6755399441055744.;          // 1.5 * 2^52
   const double n = x + shift, y = x - (n - shift);
-  double s = 2.5678435993488205e-11;               // ln(2)^12 / 12! and so on
-  s = fma(s, y, 4.4455382718708115e-10);
-  s = fma(s, y, 7.0549116208011233e-9);
+  double s = 7.0549116208011233e-9;                // ln(2)^10 / 10! and so on
   s = fma(s, y, 1.0178086009239700e-7);
   s = fma(s, y, 1.3215486790144309e-6);
   s = fma(s, y, 1.5252733804059840e-5);
@@ -138,6 +137,21 @@ void verify_stats_kernel(Verify p, int chunks, int rows, ChunkStats* stats) {
 template <bool GREEDY>
 __device__ __forceinline__ RowStats row_stats(const ChunkStats* s, int chunks, double per, int x, int lanes) {
   RowStats r{0., -INFINITY, 0x7fffffff};
+  if (chunks <= lanes) {                                   // a chunk each: the largest first, then one exponential
+    ChunkStats y{0., -INFINITY, 0x7fffffff};
+    if (x < chunks) y = s[x];
+    r.most = y.most;
+    r.at = y.at;
+    for (int o = 1; o < lanes; o <<= 1) {
+      if constexpr (GREEDY) better(r.most, r.at, __shfl_xor(r.most, o), __shfl_xor(r.at, o));
+      else r.most = fmaxf(r.most, __shfl_xor(r.most, o));
+    }
+    if constexpr (!GREEDY) {
+      r.sum = y.sum * weight(y.most, r.most, per);
+      for (int o = 1; o < lanes; o <<= 1) r.sum += __shfl_xor(r.sum, o);
+    }
+    return r;
+  }
   for (int c = x; c < chunks; c += lanes) {
     const ChunkStats y = s[c];
     if constexpr (GREEDY) {
@@ -162,47 +176,58 @@ __device__ __forceinline__ RowStats row_stats(const ChunkStats* s, int chunks, d
 }
 
 // How many drafts stand, and the distribution of the token behind them: all threads of the workgroup together.
-struct Choice { int accepted, drafted; bool refused; RowStats p, q; };
+struct Choice { RowStats p, q; int accepted, drafted; };      // drafted: the refused token; -1: none was refused
+constexpr int kKept = 32;
+struct ChooseLds { RowStats p[kKept], q[kKept]; int first; };
 template <bool GREEDY>
-__device__ __forceinline__ Choice choose(const Verify& p, int i, int chunks, int rows, const ChunkStats* stats, int* s_first) {
+__device__ __forceinline__ Choice choose(const Verify& p, int i, int chunks, int rows, const ChunkStats* stats, ChooseLds* lds) {
   const int count = drafts_of(p, i), tid = threadIdx.x;
   const double per = GREEDY ? 0. : per_of(p);
   const ChunkStats* mine = stats + (size_t)i * rows * chunks;
   int lanes = 64;
   while (lanes > 1 && lanes / 2 >= chunks) lanes >>= 1;
   const int x = tid & (lanes - 1), group = tid / lanes, groups = kThreads / lanes;
-  if (tid == 0) *s_first = count;
+  if (tid == 0) lds->first = count;
   __syncthreads();
-  for (int j0 = 0; j0 < count; j0 += groups) {             // (all threads of a group, so that they can exchange)
-    const int j = min(j0 + group, count - 1), t = p.drafts[(size_t)i * p.n + j];
-    const RowStats a = row_stats<GREEDY>(mine + (size_t)j * chunks, chunks, per, x, lanes);
-    bool stands = false;
+  for (int j0 = 0; j0 <= count; j0 += groups) {            // (all threads of a group, so that they can exchange; row `count` is behind the last draft)
+    const int j = min(j0 + group, count), t = j < count ? p.drafts[(size_t)i * p.n + j] : -1;
     const bool token = t >= 0 && t < p.vocab;
+    const float lp = token ? p.logits[((size_t)i * (p.n + 1) + j) * p.vocab + t] : -INFINITY;
+    const RowStats a = row_stats<GREEDY>(mine + (size_t)j * chunks, chunks, per, x, lanes);
+    RowStats d{0., -INFINITY, 0};
+    bool stands = false;
     if constexpr (GREEDY) {
       stands = token && t == (a.at < p.vocab && a.most > -INFINITY ? a.at : 0);
-    } else {
+    } else if (j < count) {                                // (the same j, and draft_logits, in all of a group)
       const double u = p.u[(size_t)i * (p.n + 1) + j];
-      const double pt = weight(token ? tame(p.logits[((size_t)i * (p.n + 1) + j) * p.vocab + t]) : -INFINITY, a.most, per);
+      const double pt = weight(tame(lp), a.most, per);
       if (p.draft_logits) {
-        const RowStats d = row_stats<false>(mine + (size_t)(p.n + 1 + j) * chunks, chunks, per, x, lanes);
-        const double qt = weight(token ? tame(p.draft_logits[((size_t)i * p.n + j) * p.vocab + t]) : -INFINITY, d.most, per);
-        stands = pt > 0. && u * qt * a.sum < pt * d.sum;
-        if (d.sum == 0.) stands = pt > 0.;                 // (a draft row of -inf throughout: probabilities of 0)
+        const float lq = token ? p.draft_logits[((size_t)i * p.n + j) * p.vocab + t] : -INFINITY;
+        d = row_stats<false>(mine + (size_t)(p.n + 1 + j) * chunks, chunks, per, x, lanes);
+        // (a draft row of -inf throughout: probabilities of 0)
+        stands = pt > 0. && (d.sum == 0. || u * weight(tame(lq), d.most, per) * a.sum < pt * d.sum);
       } else {
         stands = pt > 0. && u * a.sum < pt;
       }
     }
-    if (!stands && x == 0) atomicMin(s_first, j);
+    if (x == 0 && j < kKept) { lds->p[j] = a; lds->q[j] = d; }
+    if (x == 0 && !stands && j < count) atomicMin(&lds->first, j);
   }
   __syncthreads();
   Choice c;
-  c.accepted = *s_first;
-  c.refused = c.accepted < count;
-  c.drafted = c.refused ? p.drafts[(size_t)i * p.n + c.accepted] : -1;
-  c.p = row_stats<GREEDY>(mine + (size_t)c.accepted * chunks, chunks, per, x, lanes);
-  c.q = RowStats{0., -INFINITY, 0};
-  if constexpr (!GREEDY)
-    if (c.refused && p.draft_logits) c.q = row_stats<false>(mine + (size_t)(p.n + 1 + c.accepted) * chunks, chunks, per, x, lanes);
+  c.accepted = lds->first;
+  c.drafted = c.accepted < count ? p.drafts[(size_t)i * p.n + c.accepted] : -1;
+  if (c.accepted < kKept) {
+    c.p = lds->p[c.accepted];
+    c.q = lds->q[c.accepted];
+  } else {
+    c.p = row_stats<GREEDY>(mine + (size_t)c.accepted * chunks, chunks, per, x, lanes);
+    c.q = RowStats{0., -INFINITY, 0};
+    if constexpr (!GREEDY)
+      if (c.accepted < count && p.draft_logits) c.q = row_stats<false>(mine + (size_t)(p.n + 1 + c.accepted) * chunks, chunks, per, x, lanes);
+  }
+  if (c.accepted >= count) c.drafted = -1;
+  else if (c.drafted < 0) c.drafted = 0x7fffffff;          // (refused, and no token)
   return c;
 }
 
@@ -215,7 +240,7 @@ struct Rest {
   __device__ __forceinline__ Rest(const Verify& p, int i, const Choice& c) {
     per = per_of(p);
     x = p.logits + ((size_t)i * (p.n + 1) + c.accepted) * p.vocab;
-    y = c.refused && p.draft_logits ? p.draft_logits + ((size_t)i * p.n + c.accepted) * p.vocab : nullptr;
+    y = c.drafted >= 0 && p.draft_logits ? p.draft_logits + ((size_t)i * p.n + c.accepted) * p.vocab : nullptr;
     most_p = c.p.most;
     most_q = c.q.most;
     scale_q = c.q.sum > 0. ? c.p.sum / c.q.sum : 0.;
@@ -228,108 +253,152 @@ struct Rest {
   }
 };
 
-__global__ __launch_bounds__(kThreads)
-void verify_rest_kernel(Verify p, int chunks, int rows, const ChunkStats* stats, double* rest) {
-  __shared__ double red[4];
-  __shared__ int s_first;
-  const int i = (int)(blockIdx.x / (unsigned)chunks), chunk = (int)blockIdx.x - i * chunks;
-  const Choice c = choose<false>(p, i, chunks, rows, stats, &s_first);
-  const Rest r(p, i, c);
-  const bool aligned = (p.vocab & 3) == 0;
-  const Logits lp(r.x, chunk, p.vocab, aligned);
-  double sum = 0.;
-  if (r.y) {
-    const Logits lq(r.y, chunk, p.vocab, aligned);
+constexpr int kSegment = 256, kSegments = kChunk / kSegment;      // tokens; of a chunk
+
+// Sum of x over the threads up to this one; *all: over all.
+__device__ __forceinline__ double up_to_me(double x, double* s_waves, double* all) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
 #pragma unroll
-    for (int e = 0; e < kEach; ++e) sum += r.of(lp.at(e), lp.x[e], lq.x[e]);
-  } else {
-#pragma unroll
-    for (int e = 0; e < kEach; ++e) sum += r.of(lp.at(e), lp.x[e], 0.f);
+  for (int off = 1; off < 64; off <<= 1) {
+    const double y = __shfl_up(x, off);
+    if (lane >= off) x += y;
   }
-  sum = block_sum(sum, red);
-  if (threadIdx.x == 0) rest[(size_t)i * chunks + chunk] = sum;
+  __syncthreads();
+  if (lane == 63) s_waves[wave] = x;
+  __syncthreads();
+  double before = 0.;
+  for (int w = 0; w < wave; ++w) before += s_waves[w];
+  *all = (s_waves[0] + s_waves[1]) + (s_waves[2] + s_waves[3]);
+  return x + before;
 }
 
-template <bool GREEDY>
+// draft: the thread's own, of the first 256
+__device__ __forceinline__ void write_tokens(const Verify& p, int i, int accepted, int token, int draft) {
+  for (int j = threadIdx.x; j <= p.n; j += kThreads)
+    p.tokens[(size_t)i * (p.n + 1) + j] = j < accepted ? (j < kThreads ? draft : p.drafts[(size_t)i * p.n + j]) : j == accepted ? token : -1;
+  if (threadIdx.x == 0) p.accepted[i] = accepted;
+}
+
 __global__ __launch_bounds__(kThreads)
-void verify_draw_kernel(Verify p, int chunks, int rows, const ChunkStats* stats, const double* rest) {
-  __shared__ int s_first, s_token, s_last, s_at[4];
-  __shared__ double s_waves[4];
-  __shared__ float s_most[4];
-  const int i = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const Choice c = choose<GREEDY>(p, i, chunks, rows, stats, &s_first);
-  int token = c.p.at < p.vocab && c.p.most > -INFINITY ? c.p.at : 0;      // (a row of -inf throughout: 0)
-  if constexpr (!GREEDY) {
-    const Rest r(p, i, c);
-    double total = 0.;
-    for (int x = 0; x < chunks; ++x) total += rest[(size_t)i * chunks + x];
-    if (total > 0.) {
-      const double goal = (double)p.u[(size_t)i * (p.n + 1) + p.n] * total;
-      // the chunk in which the running sum exceeds the goal; past all of them (u is not below 1): the last that has anything
-      int chunk = -1, last = 0;
-      double before = 0., sum = 0.;
-      for (int x = 0; x < chunks; ++x) {
-        const double add = rest[(size_t)i * chunks + x];
-        if (add > 0.) last = x;
-        if (chunk < 0 && sum + add > goal) { chunk = x; before = sum; }
-        sum += add;
+void verify_greedy_kernel(Verify p, int chunks, int rows, const ChunkStats* stats) {
+  __shared__ ChooseLds lds;
+  const int draft = (int)threadIdx.x < p.n ? p.drafts[(size_t)blockIdx.x * p.n + threadIdx.x] : -1;
+  const Choice c = choose<true>(p, blockIdx.x, chunks, rows, stats, &lds);
+  write_tokens(p, blockIdx.x, c.accepted, c.p.at < p.vocab && c.p.most > -INFINITY ? c.p.at : 0, draft);      // (a row of -inf throughout: 0)
+}
+
+// What is left of the row that decides, a chunk a workgroup, in segments.  (With the draw in the same launch, by the last of a sequence's workgroups, 19 us in
+// the place of 9 and 9: what orders writes and reads across the XCDs costs more than a launch.)
+__global__ __launch_bounds__(kThreads)
+void verify_rest_kernel(Verify p, int chunks, int rows, const ChunkStats* stats, double* rest, Choice* choice) {
+  __shared__ ChooseLds lds;
+  __shared__ double s_sum[kSegments][4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int i = (int)(blockIdx.x / (unsigned)chunks), chunk = (int)blockIdx.x - i * chunks;
+  const Choice c = choose<false>(p, i, chunks, rows, stats, &lds);
+  if (chunk == 0 && tid == 0) choice[i] = c;
+  const Rest r(p, i, c);
+  const bool aligned = (p.vocab & 3) == 0;
+  double* left = rest + (size_t)i * chunks * kSegments;
+  {
+    const Logits lp(r.x, chunk, p.vocab, aligned);
+    double of[kEach];
+    if (r.y) {
+      const Logits lq(r.y, chunk, p.vocab, aligned);
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) of[e] = r.of(lp.at(e), lp.x[e], lq.x[e]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < kEach; ++e) of[e] = r.of(lp.at(e), lp.x[e], 0.f);
+    }
+    // by 16 bytes a segment is a wave's 256 neighbouring tokens at a time, else a word of each thread
+    if (aligned) {
+#pragma unroll
+      for (int e = 0; e < kEach / 4; ++e) {
+        double sum = (of[4 * e] + of[4 * e + 1]) + (of[4 * e + 2] + of[4 * e + 3]);
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+        if (lane < 4) s_sum[4 * e + wave][lane] = lane == 0 ? sum : 0.;
       }
-      const bool inside = chunk >= 0;
-      if (!inside) chunk = last;
-      if (tid == 0) { s_token = 0x7fffffff; s_last = -1; }
-      double val[kEach], mine = 0.;
-      const int v0 = chunk * kChunk + tid * kEach;         // (neighbouring elements: the order counts)
-      float lp[kEach], lq[kEach];
+    } else {
 #pragma unroll
       for (int e = 0; e < kEach; ++e) {
-        lp[e] = v0 + e < p.vocab ? r.x[v0 + e] : -INFINITY;
-        lq[e] = r.y && v0 + e < p.vocab ? r.y[v0 + e] : -INFINITY;
+        double sum = of[e];
+#pragma unroll
+        for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+        if (lane == 0) s_sum[e][wave] = sum;
       }
-#pragma unroll
-      for (int e = 0; e < kEach; ++e) {
-        val[e] = r.of(v0 + e, tame(lp[e]), tame(lq[e]));
-        mine += val[e];
-      }
-      double incl = mine;
-#pragma unroll
-      for (int off = 1; off < 64; off <<= 1) {
-        const double y = __shfl_up(incl, off);
-        if (lane >= off) incl += y;
-      }
-      if (lane == 63) s_waves[wave] = incl;
-      __syncthreads();
-      double run = before + (incl - mine);
-      for (int w = 0; w < wave; ++w) run += s_waves[w];
-      int found = 0x7fffffff, there = -1;
-#pragma unroll
-      for (int e = 0; e < kEach; ++e) {
-        run += val[e];
-        if (val[e] > 0.) {
-          there = v0 + e;
-          if (inside && run > goal && found == 0x7fffffff) found = v0 + e;
-        }
-      }
-      if (found != 0x7fffffff) atomicMin(&s_token, found);
-      if (there >= 0) atomicMax(&s_last, there);
-      __syncthreads();
-      if (s_token != 0x7fffffff) token = s_token;
-      else if (s_last >= 0) token = s_last;
-    } else {                                               // nothing to draw from: the largest logit
-      float most = -INFINITY;
-      int at = 0x7fffffff;
-      for (int v = tid; v < p.vocab; v += kThreads) better(most, at, tame(r.x[v]), v);
-#pragma unroll
-      for (int o = 32; o > 0; o >>= 1) better(most, at, __shfl_xor(most, o), __shfl_xor(at, o));
-      if (lane == 0) { s_most[wave] = most; s_at[wave] = at; }
-      __syncthreads();
-#pragma unroll
-      for (int w = 0; w < 4; ++w) better(most, at, s_most[w], s_at[w]);
-      token = most > -INFINITY ? at : 0;
     }
   }
-  for (int j = tid; j <= p.n; j += kThreads)
-    p.tokens[(size_t)i * (p.n + 1) + j] = j < c.accepted ? p.drafts[(size_t)i * p.n + j] : j == c.accepted ? token : -1;
-  if (tid == 0) p.accepted[i] = c.accepted;
+  __syncthreads();
+  if (tid < kSegments) left[(size_t)chunk * kSegments + tid] = (s_sum[tid][0] + s_sum[tid][1]) + (s_sum[tid][2] + s_sum[tid][3]);
+}
+
+__global__ __launch_bounds__(kThreads)
+void verify_draw_kernel(Verify p, int chunks, const double* rest, const Choice* choice) {
+  __shared__ double s_waves[4], s_before;
+  __shared__ float s_most[4];
+  __shared__ int s_at[4], s_found, s_last;
+  const int i = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int segments = (p.vocab + kSegment - 1) / kSegment;
+  const double* left = rest + (size_t)i * chunks * kSegments;
+  const double first = tid < segments ? left[tid] : 0.;      // (all there is, up to 65536 tokens)
+  const float u = p.u[(size_t)i * (p.n + 1) + p.n];
+  const int draft = tid < p.n ? p.drafts[(size_t)i * p.n + tid] : -1;
+  const Choice c = choice[i];
+  const Rest r(p, i, c);
+  if (tid == 0) { s_found = 0x7fffffff; s_last = -1; }
+  double sum = first, total;
+  for (int x = tid + kThreads; x < segments; x += kThreads) sum += left[x];
+  const double upto = up_to_me(sum, s_waves, &total);
+  int token;
+  if (total > 0.) {
+    const double goal = (double)u * total;
+    // the segment in which the running sum exceeds the goal; past all of them (u is not below 1): the last that has anything
+    double before = 0.;
+    for (int x0 = 0; x0 < segments; x0 += kThreads) {
+      const bool only = segments <= kThreads;
+      const double add = only ? first : x0 + tid < segments ? left[x0 + tid] : 0.;
+      double all = total, run = upto;
+      if (!only) run = before + up_to_me(add, s_waves, &all);
+      if (add > 0.) {
+        if (run > goal) atomicMin(&s_found, x0 + tid);
+        atomicMax(&s_last, x0 + tid);
+      }
+      __syncthreads();
+      if (s_found == x0 + tid) s_before = run - add;
+      before += all;
+      if (s_found != 0x7fffffff) break;                    // (the same in all threads: written before the barrier)
+    }
+    __syncthreads();
+    const bool inside = s_found != 0x7fffffff;
+    const int v = (inside ? s_found : s_last) * kSegment + tid;
+    before = inside ? s_before : 0.;
+    double mine = 0.;
+    if (v < p.vocab) mine = r.of(v, tame(r.x[v]), r.y ? tame(r.y[v]) : 0.f);
+    __syncthreads();
+    if (tid == 0) { s_found = 0x7fffffff; s_last = -1; }
+    double all;
+    const double run = before + up_to_me(mine, s_waves, &all);
+    if (mine > 0.) {
+      if (inside && run > goal) atomicMin(&s_found, v);
+      atomicMax(&s_last, v);
+    }
+    __syncthreads();
+    token = s_found != 0x7fffffff ? s_found : s_last;
+  } else {                                                 // nothing to draw from: the largest logit
+    float most = -INFINITY;
+    int at = 0x7fffffff;
+    for (int v = tid; v < p.vocab; v += kThreads) better(most, at, tame(r.x[v]), v);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) better(most, at, __shfl_xor(most, o), __shfl_xor(at, o));
+    if (lane == 0) { s_most[wave] = most; s_at[wave] = at; }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < 4; ++w) better(most, at, s_most[w], s_at[w]);
+    token = most > -INFINITY ? at : 0;
+  }
+  write_tokens(p, i, c.accepted, token, draft);
 }
 
 int verify_chunks(int vocab) { return (vocab + kChunk - 1) / kChunk; }
@@ -338,13 +407,14 @@ int verify_chunks(int vocab) { return (vocab + kChunk - 1) / kChunk; }
 
 size_t verify_workspace_bytes(int b, int n, int vocab) {
   const size_t chunks = verify_chunks(vocab);
-  return (size_t)b * (2 * (size_t)n + 1) * chunks * sizeof(ChunkStats) + (size_t)b * chunks * sizeof(double);
+  return (size_t)b * ((2 * (size_t)n + 1) * chunks * sizeof(ChunkStats) + sizeof(Choice) + chunks * kSegments * sizeof(double));
 }
 
 hipError_t launch_verify(const Verify& p, void* workspace, hipStream_t st) {
   const int chunks = verify_chunks(p.vocab), rows = p.draft_logits && p.temperature > 0.f ? 2 * p.n + 1 : p.n + 1;
   ChunkStats* stats = static_cast<ChunkStats*>(workspace);
-  double* rest = reinterpret_cast<double*>(stats + (size_t)p.b * rows * chunks);
+  Choice* choice = reinterpret_cast<Choice*>(stats + (size_t)p.b * rows * chunks);
+  double* rest = reinterpret_cast<double*>(choice + p.b);
   const dim3 all((unsigned)((size_t)p.b * rows * chunks)), rests((unsigned)((size_t)p.b * chunks)), each((unsigned)p.b), block(kThreads);
   const bool greedy = !(p.temperature > 0.f);
   if (greedy) hipLaunchKernelGGL(verify_stats_kernel<true>, all, block, 0, st, p, chunks, rows, stats);
@@ -352,13 +422,13 @@ hipError_t launch_verify(const Verify& p, void* workspace, hipStream_t st) {
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (greedy) {
-    hipLaunchKernelGGL(verify_draw_kernel<true>, each, block, 0, st, p, chunks, rows, stats, rest);
+    hipLaunchKernelGGL(verify_greedy_kernel, each, block, 0, st, p, chunks, rows, stats);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL(verify_rest_kernel, rests, block, 0, st, p, chunks, rows, stats, rest);
+  hipLaunchKernelGGL(verify_rest_kernel, rests, block, 0, st, p, chunks, rows, stats, rest, choice);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(verify_draw_kernel<false>, each, block, 0, st, p, chunks, rows, stats, rest);
+  hipLaunchKernelGGL(verify_draw_kernel, each, block, 0, st, p, chunks, rest, choice);
   return hipGetLastError();
 }
 
