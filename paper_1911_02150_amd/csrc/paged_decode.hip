@@ -294,16 +294,9 @@ __device__ __forceinline__ bool find_segment(const PagedDecode& p, Segment* s) {
   return true;
 }
 
-template <typename T>
-__global__ __launch_bounds__(kThreads)
-void paged_scalar_kernel(PagedDecode p) {
-  extern __shared__ __align__(16) unsigned char smem[];
-  Segment s;
-  if (find_segment(p, &s)) scalar_segment<T>(p, s, s.row0, min(p.R - s.row0, kScalarRows), reinterpret_cast<float*>(smem));
-}
-
 // ---------------------------------------------------------------- matrix instructions
-// Caches of k = v = D = 64 or 128.  A workgroup is four waves; wave w has the tiles w, w + 4, ... of a segment, for all rows of the block (16 or 32), and keeps
+// Caches of k = v = D = 64 or 128, and (EXACT = false) of any widths up to D = 128 or 256: pieces past a width are read as its last, against q's zeros
+// and into columns that nobody wants.  A workgroup is four waves; wave w has the tiles w, w + 4, ... of a segment, for all rows of the block (16 or 32), and keeps
 // their running maximum, sum and outputs; at the end the four states are merged through LDS.  Rows go from memory straight into the operands:
 //   logits^T[32 pos x 16 rows] = K_tile . q^T: lane (i, g) = (lane % 16, lane / 16) has 16-byte pieces g, g + 4, ... of two K rows.  Row i of product u is position
 //     8 (i / 4) + 4u + i % 4 of the tile, so that lane (row, g) ends up with positions 8g .. 8g + 7: the weights are the second product's operand as they are.
@@ -313,6 +306,7 @@ void paged_scalar_kernel(PagedDecode p) {
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) float floatx4;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
+typedef __attribute__((ext_vector_type(8))) uint32_t u32x8;
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
 constexpr float kSlack = 8.f;        // log2 of the largest weight kept before the running maximum is moved (all rows of a wave together)
 
@@ -333,7 +327,7 @@ template <int D> struct Form<uint16_t, D> {
   static constexpr int kPieces = D / 32;                   // 16-byte pieces of a K row in a lane
   static constexpr int kTerms = 3;
   static constexpr int kColumns = D / 16;                  // columns of a lane
-  typedef typename std::conditional<D == 128, u32x4, u32x2>::type VRow;
+  typedef typename std::conditional<D == 256, u32x8, typename std::conditional<D == 128, u32x4, u32x2>::type>::type VRow;
   static __device__ __forceinline__ int column(int i, int j4) { return kColumns * i + 4 * j4; }      // of the products 4 j4 ..: row i
 };
 template <int D> struct Form<float, D> {
@@ -361,7 +355,7 @@ template <typename T, int D> struct Turned {};
 template <int D> struct Turned<uint16_t, D> { u32x4 a[D / 16]; };
 
 // A wave's rows, 16 HB of a group from row0 on, and what they have seen.
-template <typename T, int D, int HB, bool SCORED>
+template <typename T, int D, int HB, bool SCORED, bool EXACT>
 struct Rows {
   typedef Form<T, D> F;
   static constexpr int NH = 16 * HB, KP = F::kPieces, KT = F::kTerms, NJ = F::kColumns, QOPS = HB * KP * 64;
@@ -379,7 +373,8 @@ struct Rows {
 #pragma unroll
       for (int y = 0; y < EACH / 4; ++y) {
         q->v[it][y] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (idx < ALL && row0 + r < p.R) q->v[it][y] = reinterpret_cast<const float4*>(p.q + row_offset(p, s.i, s.e, row0 + r) * D + EACH * c)[y];
+        if (idx < ALL && row0 + r < p.R && (EXACT || EACH * c < p.c.k))
+          q->v[it][y] = reinterpret_cast<const float4*>(p.q + row_offset(p, s.i, s.e, row0 + r) * (EXACT ? D : p.c.k) + EACH * c)[y];
       }
     }
   }
@@ -532,7 +527,7 @@ struct Rows {
 #pragma unroll
           for (int hb = 0; hb < HB; ++hb) acc[hb][j] = mfma_bf16(v.a[j], wt[hb][term], acc[hb][j]);
 #pragma unroll
-        for (int e = 8 / NJ * j; e < 8 / NJ * (j + 1); ++e) after(e);
+        for (int e = 8 * j / NJ; e < 8 * (j + 1) / NJ; ++e) after(e);
         __builtin_amdgcn_sched_barrier(0);
       }
     } else {
@@ -588,9 +583,11 @@ struct Rows {
   }
   static __device__ __forceinline__ void finish(const PagedDecode& p, const Segment& s, int row0, const float* lds, int tid) {
     const float *sm = lds + kWaves * NH * PITCH, *sl = sm + kWaves * NH;
+    const int v = EXACT ? D : p.c.v;
     for (int idx = tid; idx < NH * (D / 4); idx += kThreads) {
       const int r = idx / (D / 4), c4 = idx - r * (D / 4);
       if (row0 + r >= p.R) break;
+      if (!EXACT && 4 * c4 >= v) continue;
       const float4 m4 = reinterpret_cast<const float4*>(sm)[r], l4 = reinterpret_cast<const float4*>(sl)[r];
       const float ms[4] = {m4.x, m4.y, m4.z, m4.w}, ls[4] = {l4.x, l4.y, l4.z, l4.w};
       const float M = fmaxf(fmaxf(ms[0], ms[1]), fmaxf(ms[2], ms[3])), ref = M == -INFINITY ? 0.f : M;
@@ -606,11 +603,11 @@ struct Rows {
       if (s.piece < 0) {
         const float2 state = state_of(M, l);
         a.x *= state.y; a.y *= state.y; a.z *= state.y; a.w *= state.y;
-        reinterpret_cast<float4*>(p.o + row_offset(p, s.i, s.e, row0 + r) * D)[c4] = a;
+        reinterpret_cast<float4*>(p.o + row_offset(p, s.i, s.e, row0 + r) * v)[c4] = a;
         if (p.stats && c4 == 0) p.stats[((size_t)s.i * p.c.h_kv + s.e) * p.R + row0 + r] = state;
       } else {
         const size_t at = (size_t)s.piece * p.R + row0 + r;
-        reinterpret_cast<float4*>(p.part_o + at * D)[c4] = a;
+        reinterpret_cast<float4*>(p.part_o + at * v)[c4] = a;
         if (c4 == 0) {
           p.part_m[at] = M;
           p.part_l[at] = l;
@@ -628,10 +625,10 @@ __device__ __forceinline__ void in_plain_form(const PagedDecode& p, const Segmen
 // CACHED: several blocks of rows read the same tiles, neighbours on an XCD at about the same time: from memory once and else from L2.  (64 heads of 512
 // sequences of up to 4096: 185 us.  Two teams of four waves in a workgroup 207: a workgroup to a compute unit, whose start and end nothing covers; that with
 // the tiles in LDS 300; all 64 rows in a wave, two tiles on their way, 260.)
-template <typename T, int D, int HB, bool SCORED, bool CACHED>
-__global__ __launch_bounds__(kThreads, 2)
+template <typename T, int D, int HB, bool SCORED, bool CACHED, bool EXACT>
+__global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2)
 void paged_matrix_kernel(PagedDecode p) {
-  typedef Rows<T, D, HB, SCORED> R;
+  typedef Rows<T, D, HB, SCORED, EXACT> R;
   typedef Form<T, D> F;
   extern __shared__ __align__(16) unsigned char smem[];
   __shared__ __align__(16) int s_rows[kWaves][2][32];
@@ -670,17 +667,26 @@ void paged_matrix_kernel(PagedDecode p) {
     if constexpr (CACHED) return *at;
     else return __builtin_nontemporal_load(at);
   };
+  const int k = EXACT ? D : p.c.k, v = EXACT ? D : p.c.v;
   auto load_k = [&](int x) {
+    const int piece = EXACT ? g + 4 * x : min(g + 4 * x, k / R::EACH - 1);
 #pragma unroll
-    for (int u = 0; u < 2; ++u) tl.kr[u][x] = read(reinterpret_cast<const u32x4*>(Kp + (size_t)max(k_row[u], 0) * (D * sizeof(T))) + g + 4 * x);
+    for (int u = 0; u < 2; ++u) tl.kr[u][x] = read(reinterpret_cast<const u32x4*>(Kp + (size_t)max(k_row[u], 0) * (k * sizeof(T))) + piece);
   };
   auto load_v = [&](int e) {
-    const unsigned char* src = Vp + (size_t)max(v_row[e], 0) * (D * sizeof(T));
+    const unsigned char* src = Vp + (size_t)max(v_row[e], 0) * (v * sizeof(T));
     if constexpr (sizeof(T) == 2) {
-      tl.vr[e] = read(reinterpret_cast<const typename F::VRow*>(src) + i16);
+      constexpr int C = F::kColumns;
+      if constexpr (EXACT || C <= 8) {
+        tl.vr[e] = read(reinterpret_cast<const typename F::VRow*>(src) + (EXACT ? i16 : min(i16, v / C - 1)));
+      } else {                                             // 16 columns: two pieces
+        const u32x4* at = reinterpret_cast<const u32x4*>(src);
+        const u32x4 lo = read(at + min(2 * i16, v / 8 - 1)), hi = read(at + min(2 * i16 + 1, v / 8 - 1));
+        tl.vr[e] = __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7);
+      }
     } else {
 #pragma unroll
-      for (int x = 0; x < D / 64; ++x) tl.vr[e].x[x] = read(reinterpret_cast<const floatx4*>(src) + 16 * x + i16);
+      for (int x = 0; x < D / 64; ++x) tl.vr[e].x[x] = read(reinterpret_cast<const floatx4*>(src) + (EXACT ? 16 * x + i16 : min(16 * x + i16, v / 4 - 1)));
     }
   };
   auto missing = [&]() {                                   // bit e: position 8g + e of the tile is not there
@@ -721,10 +727,10 @@ void paged_matrix_kernel(PagedDecode p) {
         if (now >> e & 1) tl.vr[e] = typename F::VRow{};
     }
     floatx4 sc[2][HB];
-    Turned<T, D> v;
+    Turned<T, D> turned;
     R::first_product(tl, qs, lane, sc, [&](int x) {
       load_k(x);
-      R::turn(tl, x, v);
+      R::turn(tl, x, turned);
     });
     bad = missing();
     buf ^= 1;
@@ -732,7 +738,7 @@ void paged_matrix_kernel(PagedDecode p) {
     next = look_up(t + 3 * kWaves);
     float w[HB][8];
     rows.weights(p, s, s.row0, lane, p0, now, sc, w);
-    rows.second_product(w, tl, v, load_v);
+    rows.second_product(w, tl, turned, load_v);
     take(buf);
   }
 
@@ -811,10 +817,12 @@ __device__ __forceinline__ void merge_rows(const PagedDecode& p, int g, int row0
   reinterpret_cast<float4*>(p.o + row_offset(p, i, g - i * heads, r) * p.c.v)[c4] = a;
 }
 
-// scores_out[p] = (p is older than this step's tokens ? scores_in[p] : 0) + sum over the rows of their weights at p.  A thread has four positions.
-__device__ __forceinline__ void add_scores(const PagedDecode& p, int g, int chunk, float2* s_state) {
+// scores_out[p] = (p is older than this step's tokens ? scores_in[p] : 0) + sum over the rows of their weights at p.  A workgroup has 256 positions, a wave every
+// fourth row of them (1024 positions, all rows of a thread's four: 32 x 32 rows x 8192 positions 10.2 us, so 9.1).
+constexpr int kScored = 256;
+__device__ __forceinline__ void add_scores(const PagedDecode& p, int g, int chunk, float2* s_state, floatx4 (&s_sum)[4][64]) {
   const int tid = threadIdx.x, i = g / p.c.h_kv, L = paged_length(p.c, p.lens[i]);
-  if (chunk * 1024 >= L) return;
+  if (chunk * kScored >= L) return;
   int2 span = make_int2(0, 1);
   if (p.split) span = p.spans[g];
   if (span.y == 1) {
@@ -840,22 +848,26 @@ __device__ __forceinline__ void add_scores(const PagedDecode& p, int g, int chun
     }
   }
   __syncthreads();
-  const int pos = chunk * 1024 + 4 * tid;
-  if (pos >= L) return;
+  const int lane = tid & 63, wave = tid >> 6, pos = chunk * kScored + 4 * lane;
   const size_t pitch = logits_pitch(p);
-  const float* z = p.logits + (size_t)g * p.R * pitch + pos;
-  float sum[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-  for (int r = 0; r < p.R; ++r) {
+  // (the logits of a tile are there whole: past the length, for its last 31 positions, -inf)
+  const float* z = p.logits + (size_t)g * p.R * pitch + min(pos, (L - 1) / kPagedTile * kPagedTile + kPagedTile - 4);
+  floatx4 sum = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+  for (int r = wave; r < p.R; r += 4) {
     const floatx4 x = __builtin_nontemporal_load(reinterpret_cast<const floatx4*>(z + r * pitch));
     const float2 state = s_state[r];
 #pragma unroll
     for (int y = 0; y < 4; ++y) sum[y] += __builtin_amdgcn_exp2f(x[y] - state.x) * state.y;
   }
-  const size_t at = (size_t)g * p.c.positions() + pos;
-#pragma unroll
-  for (int y = 0; y < 4; ++y)
-    if (pos + y < L) p.scores_out[at + y] = (p.scores_in && pos + y < L - p.n ? p.scores_in[at + y] : 0.f) + sum[y];
+  s_sum[wave][lane] = sum;
+  __syncthreads();
+  const int mine = chunk * kScored + tid;
+  if (mine >= L) return;
+  const float* at0 = reinterpret_cast<const float*>(s_sum);
+  const float here = (at0[tid] + at0[256 + tid]) + (at0[512 + tid] + at0[768 + tid]);
+  const size_t at = (size_t)g * p.c.positions() + mine;
+  p.scores_out[at] = (p.scores_in && mine < L - p.n ? p.scores_in[at] : 0.f) + here;
 }
 
 // Workgroups of merge_rows, `pieces` a group, then of add_scores, `chunks` a group.
@@ -863,7 +875,7 @@ __global__ __launch_bounds__(256)
 void paged_finish_kernel(PagedDecode p, int rows, int pieces, int chunks) {
   __shared__ union Shared {
     struct { float m[256], l[256]; float4 a[256]; } merge;
-    float2 state[kPagedMaxRows];
+    struct { float2 state[kPagedMaxRows]; floatx4 sum[4][64]; } scores;
     __device__ Shared() {}
   } s;
   const unsigned merging = (unsigned)pieces * p.b * p.c.h_kv;
@@ -872,7 +884,7 @@ void paged_finish_kernel(PagedDecode p, int rows, int pieces, int chunks) {
     merge_rows(p, g, ((int)blockIdx.x - g * pieces) * rows, rows, s.merge.m, s.merge.l, s.merge.a);
   } else {
     const int g = (int)((blockIdx.x - merging) / (unsigned)chunks);
-    add_scores(p, g, (int)(blockIdx.x - merging) - g * chunks, s.state);
+    add_scores(p, g, (int)(blockIdx.x - merging) - g * chunks, s.scores.state, s.scores.sum);
   }
 }
 
@@ -903,8 +915,11 @@ static size_t lay_out(PagedDecode* p, const PagedPlan& pl, float* at) {
 PagedPlan paged_plan(int b, int n, int h, int h_kv, int page_size, int max_pages, int k, int v, int is_bf16, int with_scores) {
   PagedPlan pl = {};
   const long long R = (long long)n * (h / h_kv), positions = (long long)max_pages * page_size, tiles = (positions + kPagedTile - 1) / kPagedTile;
-  pl.mfma = k == v && (k == 64 || k == 128);
-  pl.block_rows = !pl.mfma ? kScalarRows : R <= 16 || (k == 128 && !is_bf16) ? 16 : 32;      // (float32 rows of 128: 32 query rows do not fit a wave's registers beside a tile)
+  const int wide = k > v ? k : v;
+  pl.form = k == v && (k == 64 || k == 128) ? k : wide <= 128 ? -128 : -256;
+  // (float32 rows of 128, and bf16 rows of 256: 32 query rows do not fit a wave's registers beside a tile)
+  const int row_bytes = (pl.form < 0 ? -pl.form : pl.form) * (is_bf16 ? 2 : 4);
+  pl.block_rows = R <= 16 || row_bytes > 256 ? 16 : 32;
   pl.blocks = (int)((R + pl.block_rows - 1) / pl.block_rows);
   const long long groups = (long long)b * h_kv;
   pl.split = tiles > 8;
@@ -934,29 +949,34 @@ static hipError_t launch_form(size_t lds, const PagedDecode& p, const PagedPlan&
   hipLaunchKernelGGL(kernel, dim3((unsigned)(pl.blocks > 1 ? (pl.pieces + 7) / 8 * 8 : pl.pieces) * pl.blocks), dim3(kThreads), lds, st, p);
   return hipGetLastError();
 }
-template <typename T, int D, int HB>
+template <typename T, int D, int HB, bool CACHED, bool EXACT>
 static hipError_t launch_matrix(const PagedDecode& p, const PagedPlan& pl, hipStream_t st) {
   constexpr size_t lds = Lds<T, D, HB>::alone;
-  if constexpr (HB > 1 || sizeof(T) * D > 256)             // (else more rows would be of another kind)
-    if (pl.blocks > 1)
-      return p.scores_out ? launch_form<paged_matrix_kernel<T, D, HB, true, true>>(lds, p, pl, st) : launch_form<paged_matrix_kernel<T, D, HB, false, true>>(lds, p, pl, st);
-  return p.scores_out ? launch_form<paged_matrix_kernel<T, D, HB, true, false>>(lds, p, pl, st) : launch_form<paged_matrix_kernel<T, D, HB, false, false>>(lds, p, pl, st);
+  return p.scores_out ? launch_form<paged_matrix_kernel<T, D, HB, true, CACHED, EXACT>>(lds, p, pl, st)
+                      : launch_form<paged_matrix_kernel<T, D, HB, false, CACHED, EXACT>>(lds, p, pl, st);
 }
-template <typename T, int D>
+template <typename T, int D, bool EXACT>
 static hipError_t launch_rows(const PagedDecode& p, const PagedPlan& pl, hipStream_t st) {
-  if constexpr (sizeof(T) * D <= 256)
-    if (pl.block_rows == 32) return launch_matrix<T, D, 2>(p, pl, st);
-  return launch_matrix<T, D, 1>(p, pl, st);
+  constexpr bool narrow = sizeof(T) * D > 256;             // (then never 32 rows)
+  if constexpr (!EXACT) {
+    if constexpr (!narrow)
+      if (pl.block_rows == 32) return launch_matrix<T, D, 2, true, false>(p, pl, st);
+    return launch_matrix<T, D, 1, true, false>(p, pl, st);
+  } else if constexpr (narrow) {
+    return pl.blocks > 1 ? launch_matrix<T, D, 1, true, true>(p, pl, st) : launch_matrix<T, D, 1, false, true>(p, pl, st);
+  } else {
+    if (pl.block_rows == 16) return launch_matrix<T, D, 1, false, true>(p, pl, st);
+    return pl.blocks > 1 ? launch_matrix<T, D, 2, true, true>(p, pl, st) : launch_matrix<T, D, 2, false, true>(p, pl, st);
+  }
 }
 
 hipError_t launch_paged_decode(const PagedDecode& p, const PagedPlan& pl, int is_bf16, hipStream_t st) {
-  hipError_t e = hipErrorInvalidValue;
-  if (pl.mfma) {
-    if (p.c.k == 128) e = is_bf16 ? launch_rows<uint16_t, 128>(p, pl, st) : launch_rows<float, 128>(p, pl, st);
-    else e = is_bf16 ? launch_rows<uint16_t, 64>(p, pl, st) : launch_rows<float, 64>(p, pl, st);
-  } else {
-    const size_t lds = scalar_lds_floats(p.c.k, p.c.v) * sizeof(float);
-    e = is_bf16 ? launch_form<paged_scalar_kernel<uint16_t>>(lds, p, pl, st) : launch_form<paged_scalar_kernel<float>>(lds, p, pl, st);
+  hipError_t e;
+  switch (pl.form) {
+    case 64: e = is_bf16 ? launch_rows<uint16_t, 64, true>(p, pl, st) : launch_rows<float, 64, true>(p, pl, st); break;
+    case 128: e = is_bf16 ? launch_rows<uint16_t, 128, true>(p, pl, st) : launch_rows<float, 128, true>(p, pl, st); break;
+    case -128: e = is_bf16 ? launch_rows<uint16_t, 128, false>(p, pl, st) : launch_rows<float, 128, false>(p, pl, st); break;
+    default: e = is_bf16 ? launch_rows<uint16_t, 256, false>(p, pl, st) : launch_rows<float, 256, false>(p, pl, st); break;
   }
   if (e != hipSuccess) return e;
   const long long groups = (long long)p.b * p.c.h_kv;
@@ -966,7 +986,7 @@ hipError_t launch_paged_decode(const PagedDecode& p, const PagedPlan& pl, int is
     rows = groups * p.R >= 512 ? (together < p.R ? together : p.R) : 1;
     pieces = (p.R + rows - 1) / rows;
   }
-  if (p.scores_out) chunks = (p.c.positions() + 1023) / 1024;
+  if (p.scores_out) chunks = (p.c.positions() + kScored - 1) / kScored;
   if (pieces + chunks == 0) return hipSuccess;
   hipLaunchKernelGGL(paged_finish_kernel, dim3((unsigned)(groups * (pieces + chunks))), dim3(256), 0, st, p, rows, pieces, chunks);
   return hipGetLastError();
