@@ -642,19 +642,19 @@ void paged_matrix_kernel(PagedDecode p) {
   const unsigned char* Vp = static_cast<const unsigned char*>(p.c.V);
   const int ntiles = (s.end - s.begin + kPagedTile - 1) / kPagedTile;
 
-  // ---- where a tile's rows are: a lane asks for position lane % 32's.  (A tile past the end is none of the cache's, and is read as the pool's first row: without a
-  // branch around them the loads stay in order, and a wait is for those that are needed.)
-  struct Place { int entry, inside; };                     // inside: of the page; -1: past the end
+  // ---- where a tile's rows are: a lane asks for position lane % 32's.  (What is past the end is read as the last position, which no row sees twice and which holds
+  // what the caller wrote; a page that holds nothing as the pool's first row: without branches around them the loads stay in order, and a wait is for those that
+  // are needed.)
+  struct Place { int entry, inside; };
   auto look_up = [&](int t) {
-    const int pos = s.begin + kPagedTile * t + (lane & 31), inside = min(pos, max(s.end - 1, 0));
-    const unsigned page = (unsigned)inside / (unsigned)p.c.page_size;
-    return Place{table[page], pos < s.end ? inside - (int)page * p.c.page_size : -1};
+    const int pos = min(s.begin + kPagedTile * t + (lane & 31), max(s.end - 1, 0));
+    const unsigned page = (unsigned)pos / (unsigned)p.c.page_size;
+    return Place{table[page], pos - (int)page * p.c.page_size};
   };
   Tile<T, D> tl;
   int k_row[2], v_row[8];                                  // of the tile that is loaded next
   auto publish = [&](const Place& x, int buf) {
-    const bool there = (unsigned)x.entry < (unsigned)p.c.num_pages && x.inside >= 0;
-    places[buf][lane & 31] = there ? (x.entry * p.c.h_kv + s.e) * p.c.page_size + x.inside : -1;
+    places[buf][lane & 31] = (unsigned)x.entry < (unsigned)p.c.num_pages ? (x.entry * p.c.h_kv + s.e) * p.c.page_size + x.inside : -1;
     asm volatile("" ::: "memory");
   };
   auto take = [&](int buf) {
