@@ -338,6 +338,7 @@ int mqa_beam_reorder_kv(const void* K_src, const void* V_src, const int32_t* len
  * mqa_paged_append_kv_rows: rows k_new [b,n,h_kv,k], v_new [b,n,h_kv,v] (float32) go behind the lens_in[i] rows that sequence i has, rounded as in
  * mqa_append_kv; of a padded batch only the first counts[i] (clamped to [0,n]; NULL: all n); lens_out[i] = lens_in[i] + their number.  A sequence that cannot
  * hold them keeps its rows and its length.  lens_in and lens_out must be different arrays (MQA_ERR_SHAPE if they are the same pointer).
+ * n <= max_pages * page_size, b * n * h_kv * (k + v) <= 2^33.
  */
 int mqa_paged_append_kv_rows(const float* k_new, const float* v_new, const int32_t* counts, void* K_pages, void* V_pages, const int32_t* table,
                              const int32_t* lens_in, int32_t* lens_out, int b, int n, int h_kv, int num_pages, int page_size, int max_pages,
@@ -367,7 +368,7 @@ int mqa_paged_decode_step(const float* q, const void* K_pages, const void* V_pag
  * kept [b,h_kv,budget]: which (-1 behind them); scores_out [b,h_kv,max_pages_out * page_size]: their scores (left as they were behind them).  Attention does not
  * depend on the order of positions, but causal rows and the next eviction's `recent` do: the order is kept.  The pages of table_out must be
  * none of table_in's of any sequence; the source's rows stay as they are (other sequences may share them), its pages are the caller's again.
- * budget <= max_pages_out * page_size; table_in and table_out, lens_in and lens_out, scores_in and scores_out must be different arrays.
+ * budget <= max_pages_out * page_size, b * h_kv < 2^22, b * h_kv * (budget + 15) < 2^28; table_in and table_out, lens_in and lens_out, scores_in and scores_out must be different arrays.
  */
 int mqa_paged_evict_kv(void* K_pages, void* V_pages, const int32_t* table_in, const int32_t* lens_in, const float* scores_in, const int32_t* table_out,
                        int32_t* lens_out, float* scores_out, int32_t* kept, int b, int h_kv, int num_pages, int page_size, int max_pages_in,
@@ -478,7 +479,7 @@ int mqa_stack_feed_forward(const float* W1, const float* W2, float* x, int rows,
  * max(p - q, 0) / sum at the first refused draft, from p behind the last of counts[i]: the lowest index whose running sum exceeds u times the whole; the most probable token
  * where there is nothing to draw from), then -1.  temperature 0: a draft stands where it is mqa_stack_argmax's token, which follows the last that stands (u and draft_logits are not
  * looked at).  n = 0: one token is drawn from logits [b,1,vocab] (drafts may be NULL).  NaN counts as -infinity, +infinity as the largest number; a
- * drafted token outside [0,vocab) is refused.  Probabilities are held in float64.
+ * drafted token outside [0,vocab) is refused.  Probabilities are held in float64.  n <= 65536, vocab <= 2^24, b * (2n + 1) * ceil(vocab / 4096) <= 2^23.
  * The workspace: mqa_stack_verify_workspace_bytes(...) bytes (16-byte aligned; 0 = unsupported sizes).
  */
 size_t mqa_stack_verify_workspace_bytes(int b, int n, int vocab);

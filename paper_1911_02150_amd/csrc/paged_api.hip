@@ -90,7 +90,7 @@ int mqa_paged_evict_kv(void* K_pages, void* V_pages, const int32_t* table_in, co
   if (dt != MQA_F32 && dt != MQA_BF16) return MQA_ERR_DTYPE;
   if (!cache_sizes_ok(b, h_kv, num_pages, page_size, max_pages_in, k, v) || !cache_sizes_ok(b, h_kv, num_pages, page_size, max_pages_out, k, v)) return MQA_ERR_SHAPE;
   if (budget <= 0 || recent < 0 || recent > budget || budget > max_pages_out * page_size) return MQA_ERR_SHAPE;
-  if ((long long)b * h_kv > (1ll << 30) / budget / ((k + v) >> 2)) return MQA_ERR_SHAPE;
+  if ((long long)b * h_kv >= (1 << 22) || (long long)b * h_kv * (budget + 15ll) >= (1 << 28)) return MQA_ERR_SHAPE;      // (grids of less than 2^32 threads)
   if (table_in == table_out || lens_in == lens_out || scores_in == scores_out) return MQA_ERR_SHAPE;      // not an in-place operation
   if (misaligned(K_pages) || misaligned(V_pages) || misaligned(table_in) || misaligned(lens_in) || misaligned(scores_in) || misaligned(table_out) ||
       misaligned(lens_out) || misaligned(scores_out) || misaligned(kept))

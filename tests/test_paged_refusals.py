@@ -90,7 +90,8 @@ def test_evict_refuses():
         assert call([None if y == x else p for y, p in enumerate(places)]) == NULL
         assert call([U if y == x else p for y, p in enumerate(places)]) == ALIGN
     assert call(dt=7) == DTYPE
-    for s in bad_cache_sizes() + [dict(max_pages_out=0), dict(budget=0), dict(budget=33), dict(recent=-1), dict(recent=33), dict(max_pages_out=1 << 21)]:
+    for s in bad_cache_sizes() + [dict(max_pages_out=0), dict(budget=0), dict(budget=33), dict(recent=-1), dict(recent=33), dict(max_pages_out=1 << 21),
+                                 dict(b=1 << 21, max_pages=1), dict(b=1 << 20, max_pages=16, max_pages_out=16, budget=256)]:
         assert call(**s) == SHAPE, s
     for x, y in ((2, 5), (3, 6), (4, 7)):                                      # in place
         assert call([places[x] if z == y else p for z, p in enumerate(places)]) == SHAPE
