@@ -72,6 +72,10 @@ ATTEND = [
     (1, 1, 70, 1, 256, 8, 11, "f32", [290]),
     (1, 128, 8, 1, 128, 128, 16, "bf16", [300]),
     (5, 1, 1, 1, 128, 128, 32, "bf16", [0, 0, 0, 0, 0]),
+    (1, 1, 33, 1, 96, 104, 9, "f32", [500]),
+    (2, 2, 20, 1, 200, 200, 16, "f32", [600, 50]),
+    (2, 1, 40, 1, 200, 248, 16, "bf16", [700, 33]),
+    (3, 3, 4, 2, 120, 72, 32, "bf16", [260, 1, 2000]),
 ]
 
 
@@ -233,6 +237,8 @@ EVICT = [
     (2, 2, 64, 64, 16, "bf16", [3000, 1025], 1024, 0),
     (2, 1, 64, 8, 16, "f32", [100, 16], 100, 3),
     (1, 1, 16, 16, 16, "f32", [5000], 77, 7),
+    (1, 2, 8, 8, 48, "bf16", [16000], 2500, 100),
+    (2, 1, 8, 16, 256, "f32", [26000, 24577], 3000, 1),
 ]
 
 
@@ -364,6 +370,76 @@ def test_on_another_stream_and_from_two_threads(m):
     for t in threads:
         t.join()
     assert not bad
+
+
+def test_replayed_for_other_lengths_and_pages(m):
+    """One captured step, replayed as the lengths grow and pages are exchanged between the replays: what it does is decided on the GPU."""
+    g = torch.Generator(device=DEV).manual_seed(4)
+    b, each, page, heads = 5, 64, 16, 2
+    K, V = (torch.randn((b * each, heads, page, 64), generator=g, device=DEV) for _ in range(2))
+    table, lens = torch.randperm(b * each, generator=g, device=DEV).to(torch.int32).view(b, each), torch.zeros(b, dtype=torch.int32, device=DEV)
+    q, new = torch.randn((b, 2, 4, 64), generator=g, device=DEV), torch.randn((b, 2, heads, 64), generator=g, device=DEV)
+    counts, after = torch.zeros(b, dtype=torch.int32, device=DEV), torch.zeros(b, dtype=torch.int32, device=DEV)
+    scores = torch.rand((b, heads, each * page), generator=g, device=DEV)
+
+    def step(K, V, o, out):
+        m.mqa_paged_append_kv_rows(K, V, table, new, new, lens, after, counts=counts)
+        return m.mqa_paged_decode_step(q, K, V, table, after, o=o, scores=scores, scores_out=out)
+
+    kept = K.clone(), V.clone(), torch.zeros_like(q), torch.zeros_like(scores)
+    step(*(t.clone() for t in kept))                       # (before the capture: once outside)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step(*kept)
+    for lengths, rows in (([0, 1, 31, 500, 1022], [2, 1, 0, 2, 2]), ([1024, 1023, 0, -3, 2 ** 31 - 1], [1, 1, 0, 1, 2]), ([900, 900, 900, 900, 900], [2, 2, 2, 2, 9])):
+        table.copy_(table[:, torch.randperm(each, generator=g, device=DEV)].roll(1, 0))
+        lens.copy_(torch.tensor(lengths, dtype=torch.int32)), counts.copy_(torch.tensor(rows, dtype=torch.int32))
+        here = [t.clone() for t in kept]
+        step(*here)
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(x, y) for x, y in zip(here, kept))
+
+
+def test_a_page_named_twice(m):
+    """Sequences that share pages, and one that has a page twice: to be read as often as it is named."""
+    from oracle import paged
+    rng = np.random.default_rng(12)
+    K, V = (pool(rng, 9, 1, 16, 128, "bf16") for _ in range(2))
+    table = np.array([[3, 3, 5, 3], [3, 5, 8, 0], [7, 7, 7, 7]])
+    lens, q = np.array([60, 37, 64]), rng.standard_normal((3, 1, 8, 128)).astype(np.float32)
+    want, _, size = paged.attend(q.astype(np.float64), K, V, table, lens, 0.125)
+    got = m.mqa_paged_decode_step(on_gpu(q[:, 0]), on_gpu(K, "bf16", True), on_gpu(V, "bf16", True), on_gpu(table), on_gpu(lens), scale=0.125)
+    assert (np.abs(got.cpu().numpy()[:, None] - want) <= tolerance(q, K, size, 0.125, 64)).all()
+
+
+@pytest.mark.parametrize("dtype,width", [(torch.float32, 128), (torch.bfloat16, 256)])
+def test_pools_of_more_than_4_gib(m, dtype, width):
+    """The last pages of a large pool against a small one that holds the same."""
+    page, each, heads, b = 64, 20, 3, 2
+    row = torch.zeros((), dtype=dtype).element_size() * width
+    pages = (5 << 30) // (row * page * heads)
+    big = [torch.empty((pages, heads, page, width), dtype=dtype, device=DEV) for _ in range(2)]
+    small = [torch.zeros((3 * b * each, heads, page, width), dtype=dtype, device=DEV) for _ in range(2)]
+    g = torch.Generator(device=DEV).manual_seed(5)
+    for x, y in zip(big, small):
+        x[:1].zero_(), x[-len(y):].zero_()
+    new = torch.randn((b, 1200, heads, width), generator=g, device=DEV)
+    q, lens = torch.randn((b, 2, 6, width), generator=g, device=DEV), torch.tensor([3, 50], dtype=torch.int32, device=DEV)
+    order = torch.randperm(2 * b * each, generator=g, device=DEV).to(torch.int32).view(2, b, each)
+    results = []
+    for K, V, first in ((*big, pages - 3 * b * each), (*small, 0)):
+        table, out = order + first
+        after, lens_out, kept = torch.zeros_like(lens), torch.zeros_like(lens), torch.zeros((b, heads, 500), dtype=torch.int32, device=DEV)
+        scores, left = torch.zeros((b, heads, each * page), device=DEV), torch.zeros((b, heads, each * page), device=DEV)
+        m.mqa_paged_append_kv_rows(K, V, table, new, new, lens, after)
+        o = m.mqa_paged_decode_step(q, K, V, table, after, scale=0.1, scores=scores)
+        m.mqa_paged_evict_kv(K, V, table, after, scores, out, lens_out, left, kept, 10)
+        results.append((after, o, scores, lens_out, left, kept, K[first:first + 2 * b * each].clone(), V[first:first + 2 * b * each].clone()))
+    assert all(torch.equal(x, y) for x, y in zip(*results))
+    assert results[0][1].abs().max() > 0 and results[0][3].tolist() == [500, 500]
 
 
 def test_a_given_workspace(m):

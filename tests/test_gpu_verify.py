@@ -138,6 +138,16 @@ def test_replayed_and_on_a_stream(m):
             assert torch.equal(out[x], want[x]) and torch.equal(side[x], want[x])
 
 
+def test_more_than_2_to_31_logits(m):
+    """The last rows against a call of their own."""
+    b, vocab = 33000, 65536
+    g = torch.Generator(device=DEV).manual_seed(6)
+    logits, u = torch.empty((b, 1, vocab), device=DEV).normal_(generator=g), torch.rand((b, 1), generator=g, device=DEV)
+    tokens, accepted = m.mqa_stack_verify_drafts(logits, None, u)
+    some, _ = m.mqa_stack_verify_drafts(logits[-64:].contiguous(), None, u[-64:].contiguous())
+    assert torch.equal(tokens[-64:], some) and len(set(tokens[:, 0].tolist())) > 1000 and not accepted.any()
+
+
 def test_wrong_tensors_are_refused(m):
     logits, drafts, u = torch.zeros((2, 4, 10), device=DEV), torch.zeros((2, 3), dtype=torch.int32, device=DEV), torch.zeros((2, 4), device=DEV)
     for bad in (dict(drafts=drafts[:, :2].contiguous()), dict(u=u[:1]), dict(logits=logits[0]), dict(draft_logits=logits), dict(counts=drafts), dict(tokens=drafts),
