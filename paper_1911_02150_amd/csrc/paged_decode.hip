@@ -461,15 +461,15 @@ struct Rows {
     }
   }
 
-  // the softmax of a tile from position p0 on; bad: bit e: position p0 + 8g + e is not there
+  // the softmax of a tile from position p0 on; bad: bit e: position p0 + e is not there
   __device__ __forceinline__ void weights(const PagedDecode& p, const Segment& s, int row0, int lane, int p0, uint32_t bad, floatx4 (&sc)[2][HB], float (&w)[HB][8]) {
     const int i16 = lane & 15, g = lane >> 4;
-    if (__any(bad != 0) || p0 + kPagedTile > lim_min) {    // what is not there, or not seen
+    if (bad || p0 + kPagedTile > lim_min) {    // what is not there, or not seen
 #pragma unroll
       for (int e = 0; e < 8; ++e)
 #pragma unroll
         for (int hb = 0; hb < HB; ++hb)
-          if ((bad >> e & 1) || p0 + 8 * g + e >= lim[hb]) sc[e >> 2][hb][e & 3] = -INFINITY;
+          if ((bad >> (8 * g + e) & 1) || p0 + 8 * g + e >= lim[hb]) sc[e >> 2][hb][e & 3] = -INFINITY;
     }
     if constexpr (SCORED) {
       const size_t pitch = logits_pitch(p);
@@ -653,9 +653,11 @@ void paged_matrix_kernel(PagedDecode p) {
   };
   Tile<T, D> tl;
   int k_row[2], v_row[8];                                  // of the tile that is loaded next
-  auto publish = [&](const Place& x, int buf) {
-    places[buf][lane & 31] = (unsigned)x.entry < (unsigned)p.c.num_pages ? (x.entry * p.c.h_kv + s.e) * p.c.page_size + x.inside : -1;
+  auto publish = [&](const Place& x, int buf) -> uint32_t {      // bit e of what is returned: position e of the tile is not there
+    const bool there = (unsigned)x.entry < (unsigned)p.c.num_pages;
+    places[buf][lane & 31] = there ? (x.entry * p.c.h_kv + s.e) * p.c.page_size + x.inside : 0;
     asm volatile("" ::: "memory");
+    return (uint32_t)__ballot(!there);
   };
   auto take = [&](int buf) {
 #pragma unroll
@@ -671,10 +673,10 @@ void paged_matrix_kernel(PagedDecode p) {
   auto load_k = [&](int x) {
     const int piece = EXACT ? g + 4 * x : min(g + 4 * x, k / R::EACH - 1);
 #pragma unroll
-    for (int u = 0; u < 2; ++u) tl.kr[u][x] = read(reinterpret_cast<const u32x4*>(Kp + (size_t)max(k_row[u], 0) * (k * sizeof(T))) + piece);
+    for (int u = 0; u < 2; ++u) tl.kr[u][x] = read(reinterpret_cast<const u32x4*>(Kp + (size_t)k_row[u] * (k * sizeof(T))) + piece);
   };
   auto load_v = [&](int e) {
-    const unsigned char* src = Vp + (size_t)max(v_row[e], 0) * (v * sizeof(T));
+    const unsigned char* src = Vp + (size_t)v_row[e] * (v * sizeof(T));
     if constexpr (sizeof(T) == 2) {
       constexpr int C = F::kColumns;
       if constexpr (EXACT || C <= 8) {
@@ -689,42 +691,35 @@ void paged_matrix_kernel(PagedDecode p) {
       for (int x = 0; x < D / 64; ++x) tl.vr[e].x[x] = read(reinterpret_cast<const floatx4*>(src) + (EXACT ? 16 * x + i16 : min(16 * x + i16, v / 4 - 1)));
     }
   };
-  auto missing = [&]() {                                   // bit e: position 8g + e of the tile is not there
-    uint32_t bits = 0;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) bits |= (uint32_t)(v_row[e] < 0) << e;
-    return bits;
-  };
 
   if (tid == 0) s_odd = 0;
   Place next = look_up(wave);
   typename R::Query q;                                     // requested before the first tile and converted while that is on its way
   R::load_q(p, s, s.row0, tid, &q);
-  publish(next, 0);
+  uint32_t bad = publish(next, 0);                         // of the tile that is loaded; of the one after it
   next = look_up(wave + kWaves);
   take(0);
 #pragma unroll
   for (int x = 0; x < F::kPieces; ++x) load_k(x);
 #pragma unroll
   for (int e = 0; e < 8; ++e) load_v(e);
-  uint32_t bad = missing();
   u32x4* qs = reinterpret_cast<u32x4*>(smem);
   R::store_q(p, tid, q, qs);
   __syncthreads();
 
   R rows;
   rows.begin(p, s, s.row0, lane);
-  publish(next, 1);
+  uint32_t bad_next = publish(next, 1);
   next = look_up(wave + 2 * kWaves);
   take(1);
   int buf = 1;
   for (int t = wave; t < ntiles; t += kWaves) {
     const int p0 = s.begin + kPagedTile * t;
     const uint32_t now = bad;
-    if (__any(now != 0)) {
+    if (now) {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        if (now >> e & 1) tl.vr[e] = typename F::VRow{};
+        if (now >> (8 * g + e) & 1) tl.vr[e] = typename F::VRow{};
     }
     floatx4 sc[2][HB];
     Turned<T, D> turned;
@@ -732,9 +727,9 @@ void paged_matrix_kernel(PagedDecode p) {
       load_k(x);
       R::turn(tl, x, turned);
     });
-    bad = missing();
+    bad = bad_next;
     buf ^= 1;
-    publish(next, buf);                                    // places of the tile after the next one
+    bad_next = publish(next, buf);                         // places of the tile after the next one
     next = look_up(t + 3 * kWaves);
     float w[HB][8];
     rows.weights(p, s, s.row0, lane, p0, now, sc, w);
