@@ -215,11 +215,11 @@ __device__ __forceinline__ int before_me(int x, int* s_waves, int* all) {
   return before;
 }
 
-constexpr int kComputeUnits = 256, kShares = 768;
+constexpr int kComputeUnits = 256, kShares = 768, kLeast = 16;
 
 // This workgroup's segment; false: there is none.  Every workgroup looks at all lengths: thread t has sequences t * each up to the next one's.
 __device__ __forceinline__ bool find_segment(const PagedDecode& p, Segment* s) {
-  __shared__ int s_waves[5][kThreads / 64];
+  __shared__ int s_waves[8][kThreads / 64];
   __shared__ int s_at[4];
   const int tid = threadIdx.x, heads = p.c.h_kv;
   int piece = blockIdx.x, block = 0;
@@ -246,9 +246,10 @@ __device__ __forceinline__ bool find_segment(const PagedDecode& p, Segment* s) {
   int total;
   before_me(mine, s_waves[0], &total);
   total *= heads;
-  // Tiles of a piece, at most: a whole number for each of the workgroup's four waves.  As many as leave a workgroup for every compute unit at most, if that
-  // is not too uneven (64 sequences of 8192, 32 heads: 53 us, in 512 pieces 58); else shares so small that a compute unit has several in turn (512 sequences
-  // of up to 4096, 32 heads: 126, in shares of a 512th 137, of a 1536th 133).
+  // Tiles of a piece, at most: a whole number for each of the workgroup's four waves.  As many as leave every compute unit one workgroup at most, or else two, if
+  // that is not too uneven (64 sequences of 8192, 32 heads: 53 us, in 512 pieces 58; 128 of up to 1024, 64 heads, two to a unit 33, in shares of a 768th 45); else
+  // shares so small that a compute unit has several in turn (512 sequences of up to 4096, 32 heads: 126, in shares of a 512th 137, of a 1536th 133), though
+  // not below four tiles a wave (256 of 512, 64 heads: 31, else 42).
   int per = 0, count = 0, before = 0, all = 0, turn = 0;
   auto pieces_of = [&](int t) { return max(1, (int)((unsigned)(t + per - 1) / (unsigned)per)); };
   auto cut = [&](int tiles) {
@@ -256,13 +257,17 @@ __device__ __forceinline__ bool find_segment(const PagedDecode& p, Segment* s) {
     count = from < to ? pieces_of(tiles_of(p, len)) : 0;
     for (int x = from + 1; x < to; ++x) count += pieces_of(tiles_of(p, p.lens[x]));
     before = before_me(count, s_waves[++turn], &all);
-    return (long long)all * heads * p.blocks <= kComputeUnits;
   };
-  const int units = kComputeUnits / p.blocks;
   bool fits = false;
-  if ((long long)p.b * heads * p.blocks <= kComputeUnits)
-    for (int x = 8; x <= 10 && !fits; ++x) fits = cut((int)(((long long)total * x + 8 * units - 1) / (8 * units)));
-  if (!fits) cut((total + kShares - 1) / kShares);
+  for (int most = kComputeUnits; most <= 2 * kComputeUnits; most *= 2) {
+    const int units = most / p.blocks;
+    if (p.b * heads <= units)
+      for (int x = 8; x <= 10 && !fits; ++x) {
+        cut((int)(((long long)total * x + 8 * units - 1) / (8 * units)));
+        fits = all * heads <= units;
+      }
+  }
+  if (!fits) cut(max(kLeast, (total + kShares - 1) / kShares));
   if (piece >= all * heads) return false;
   if (before * heads <= piece && piece < (before + count) * heads) {      // one thread
     int x = from, L = len, c = pieces_of(tiles_of(p, len));
@@ -912,11 +917,14 @@ PagedPlan paged_plan(int b, int n, int h, int h_kv, int page_size, int max_pages
   const long long R = (long long)n * (h / h_kv), positions = (long long)max_pages * page_size, tiles = (positions + kPagedTile - 1) / kPagedTile;
   const int wide = k > v ? k : v;
   pl.form = k == v && (k == 64 || k == 128) ? k : wide <= 128 ? -128 : -256;
-  // (float32 rows of 128, and bf16 rows of 256: 32 query rows do not fit a wave's registers beside a tile)
-  const int row_bytes = (pl.form < 0 ? -pl.form : pl.form) * (is_bf16 ? 2 : 4);
-  pl.block_rows = R <= 16 || row_bytes > 256 ? 16 : 32;
-  pl.blocks = (int)((R + pl.block_rows - 1) / pl.block_rows);
   const long long groups = (long long)b * h_kv;
+  // 16 query rows to a workgroup where the work is so little that its latency counts, else 32, whose tiles are read half as often: 16 sequences of 2048, 32 heads
+  // 14.9 us against 18.8, 48 of them 22.6 and 22.5, 512 of up to 4096 with 64 heads 245 and 187; 8 sequences of 200, 64 heads 7.8 and 10.8; 256 wide, 32 heads, 16
+  // sequences of 2048 23.8 and 27.8, 32 of them 31.9 and 31.0.
+  // (float32 rows of more than 64: 32 query rows do not fit a wave's registers beside a tile.)
+  const bool little = groups * tiles * R * (pl.form == -256 ? 4 : 2) <= 3 << 16;
+  pl.block_rows = R <= 16 || little || (!is_bf16 && pl.form != 64) ? 16 : 32;
+  pl.blocks = (int)((R + pl.block_rows - 1) / pl.block_rows);
   pl.split = tiles > 8;
   const long long least = groups * ((tiles + 3) / 4), most = groups + kShares;      // (pieces of four tiles; a last, shorter one in every group)
   pl.pieces = (int)(!pl.split ? groups : least < most ? least : most);
@@ -952,7 +960,7 @@ static hipError_t launch_matrix(const PagedDecode& p, const PagedPlan& pl, hipSt
 }
 template <typename T, int D, bool EXACT>
 static hipError_t launch_rows(const PagedDecode& p, const PagedPlan& pl, hipStream_t st) {
-  constexpr bool narrow = sizeof(T) * D > 256;             // (then never 32 rows)
+  constexpr bool narrow = sizeof(T) == 4 && D > 64;             // (then never 32 rows)
   if constexpr (!EXACT) {
     if constexpr (!narrow)
       if (pl.block_rows == 32) return launch_matrix<T, D, 2, true, false>(p, pl, st);
@@ -960,7 +968,7 @@ static hipError_t launch_rows(const PagedDecode& p, const PagedPlan& pl, hipStre
   } else if constexpr (narrow) {
     return pl.blocks > 1 ? launch_matrix<T, D, 1, true, true>(p, pl, st) : launch_matrix<T, D, 1, false, true>(p, pl, st);
   } else {
-    if (pl.block_rows == 16) return launch_matrix<T, D, 1, false, true>(p, pl, st);
+    if (pl.block_rows == 16) return pl.blocks > 1 ? launch_matrix<T, D, 1, true, true>(p, pl, st) : launch_matrix<T, D, 1, false, true>(p, pl, st);
     return pl.blocks > 1 ? launch_matrix<T, D, 2, true, true>(p, pl, st) : launch_matrix<T, D, 2, false, true>(p, pl, st);
   }
 }
