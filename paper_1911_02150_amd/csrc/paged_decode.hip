@@ -215,11 +215,11 @@ __device__ __forceinline__ int before_me(int x, int* s_waves, int* all) {
   return before;
 }
 
-constexpr int kComputeUnits = 256, kShares = 768, kLeast = 16;
+constexpr int kComputeUnits = 256, kShares = 768, kLeast = 16, kLongest = 64;
 
 // This workgroup's segment; false: there is none.  Every workgroup looks at all lengths: thread t has sequences t * each up to the next one's.
 __device__ __forceinline__ bool find_segment(const PagedDecode& p, Segment* s) {
-  __shared__ int s_waves[8][kThreads / 64];
+  __shared__ int s_waves[8][kThreads / 64], s_longest[kThreads / 64];
   __shared__ int s_at[4];
   const int tid = threadIdx.x, heads = p.c.h_kv;
   int piece = blockIdx.x, block = 0;
@@ -241,12 +241,24 @@ __device__ __forceinline__ bool find_segment(const PagedDecode& p, Segment* s) {
   }
   const int each = (p.b + kThreads - 1) / kThreads, from = tid * each, to = min(p.b, from + each);
   const int len = from < to ? p.lens[from] : 0;            // (up to 256 sequences: read once)
-  int mine = tiles_of(p, len);
-  for (int x = from + 1; x < to; ++x) mine += tiles_of(p, p.lens[x]);
+  int mine = tiles_of(p, len), longest = mine;
+  for (int x = from + 1; x < to; ++x) {
+    const int t = tiles_of(p, p.lens[x]);
+    mine += t;
+    longest = max(longest, t);
+  }
+  const bool many = p.b * heads * p.blocks >= 2 * kComputeUnits;
+  if (many) {
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) longest = max(longest, __shfl_xor(longest, off));
+    if ((tid & 63) == 0) s_longest[tid >> 6] = longest;
+  }
   int total;
   before_me(mine, s_waves[0], &total);
   total *= heads;
-  // Tiles of a piece, at most: a whole number for each of the workgroup's four waves.  As many as leave every compute unit one workgroup at most, or else two, if
+  // Tiles of a piece, at most: a whole number for each of the workgroup's four waves.  Whole groups where there are two for every compute unit, none long and none
+  // more than twice what a workgroup's share would be (512 sequences of up to 1000, 32 heads: 45 us, in shares 56; 64 of up to 2500, 8 heads, which are not cut
+  // by this rule 75, uncut 84).  Else as many as leave every compute unit one workgroup at most, or else two, if
   // that is not too uneven (64 sequences of 8192, 32 heads: 53 us, in 512 pieces 58; 128 of up to 1024, 64 heads, two to a unit 33, in shares of a 768th 45); else
   // shares so small that a compute unit has several in turn (512 sequences of up to 4096, 32 heads: 126, in shares of a 512th 137, of a 1536th 133), though
   // not below four tiles a wave (256 of 512, 64 heads: 31, else 42).
@@ -259,9 +271,14 @@ __device__ __forceinline__ bool find_segment(const PagedDecode& p, Segment* s) {
     before = before_me(count, s_waves[++turn], &all);
   };
   bool fits = false;
+  if (many) {
+    longest = max(max(s_longest[0], s_longest[1]), max(s_longest[2], s_longest[3]));
+    fits = longest <= kLongest && longest * (kComputeUnits / p.blocks) <= total;
+    if (fits) cut(longest);
+  }
   for (int most = kComputeUnits; most <= 2 * kComputeUnits; most *= 2) {
     const int units = most / p.blocks;
-    if (p.b * heads <= units)
+    if (!fits && p.b * heads <= units)
       for (int x = 8; x <= 10 && !fits; ++x) {
         cut((int)(((long long)total * x + 8 * units - 1) / (8 * units)));
         fits = all * heads <= units;
@@ -925,7 +942,10 @@ PagedPlan paged_plan(int b, int n, int h, int h_kv, int page_size, int max_pages
   const bool little = groups * tiles * R * (pl.form == -256 ? 4 : 2) <= 3 << 16;
   pl.block_rows = R <= 16 || little || (!is_bf16 && pl.form != 64) ? 16 : 32;
   pl.blocks = (int)((R + pl.block_rows - 1) / pl.block_rows);
-  pl.split = tiles > 8;
+  // One launch, a workgroup to a group, where cutting and merging would take longer (sequences of 380: 8.3 us, in pieces 10.8; of 800 17.7 and 11.8; float32 of
+  // 380 13.7 and 13.5), and to greater lengths where there is one for every compute unit (256 of up to 760: 18, in pieces 25).
+  const bool heavy = wide > 128 || (!is_bf16 && wide > 64);
+  pl.split = tiles > (groups * pl.blocks >= kComputeUnits ? 32 : heavy ? 12 : 16);
   const long long least = groups * ((tiles + 3) / 4), most = groups + kShares;      // (pieces of four tiles; a last, shorter one in every group)
   pl.pieces = (int)(!pl.split ? groups : least < most ? least : most);
   PagedDecode p = {};
