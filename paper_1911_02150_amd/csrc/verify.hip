@@ -7,7 +7,7 @@
 // The indices are what comes out, so that everything between is held in float64: a running sum over 32768 probabilities in float32 is off by more than many of
 // them are.  An exponential is some twenty float64 instructions, 2^x by its Taylor series around the nearest integer.  Three launches: the rows' sums
 // (what reads, all but the drafts behind the count); the choice of the row that decides, and what is left of it in segments of 256 tokens; the segment that
-// holds the goal, token by token.
+// holds the goal, token by token.  (Shorter rows: what follows the sums in one launch, or all of it.)
 #include "paged.hpp"
 
 namespace mqa {
@@ -61,30 +61,31 @@ __device__ __forceinline__ double block_sum(double x, double* red) {
 
 __device__ __forceinline__ int drafts_of(const Verify& p, int i) { return p.counts ? min(max(p.counts[i], 0), p.n) : p.n; }
 
-// A thread's 16 logits of a chunk: 16 bytes at a time where rows are aligned; past the end -inf.  at(e): the index of the e-th.
+// A thread's logits of a chunk of THREADS * EACH: 16 bytes at a time where rows are aligned; past the end -inf.  at(e): the index of the e-th.
+template <int THREADS = kThreads, int EACH = kEach>
 struct Logits {
-  float x[kEach];
+  float x[EACH];
   int first, step;
   __device__ __forceinline__ Logits(const float* row, int chunk, int vocab, bool aligned) {
     if (aligned) {
-      first = chunk * kChunk + 4 * (int)threadIdx.x;
-      step = 4 * kThreads;
+      first = chunk * THREADS * EACH + 4 * (int)threadIdx.x;
+      step = 4 * THREADS;
 #pragma unroll
-      for (int e = 0; e < kEach / 4; ++e) {
+      for (int e = 0; e < EACH / 4; ++e) {
         float4 v = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
         if (first + e * step < vocab) v = *reinterpret_cast<const float4*>(row + first + e * step);
         x[4 * e] = v.x; x[4 * e + 1] = v.y; x[4 * e + 2] = v.z; x[4 * e + 3] = v.w;
       }
     } else {
-      first = chunk * kChunk + (int)threadIdx.x;
+      first = chunk * THREADS * EACH + (int)threadIdx.x;
       step = 0;
 #pragma unroll
-      for (int e = 0; e < kEach; ++e) x[e] = first + e * kThreads < vocab ? row[first + e * kThreads] : -INFINITY;
+      for (int e = 0; e < EACH; ++e) x[e] = first + e * THREADS < vocab ? row[first + e * THREADS] : -INFINITY;
     }
 #pragma unroll
-    for (int e = 0; e < kEach; ++e) x[e] = tame(x[e]);
+    for (int e = 0; e < EACH; ++e) x[e] = tame(x[e]);
   }
-  __device__ __forceinline__ int at(int e) const { return step ? first + (e >> 2) * step + (e & 3) : first + e * kThreads; }
+  __device__ __forceinline__ int at(int e) const { return step ? first + (e >> 2) * step + (e & 3) : first + e * THREADS; }
 };
 
 // rows of a sequence: n + 1 of the target, then n of the draft
@@ -100,7 +101,7 @@ void verify_stats_kernel(Verify p, int chunks, int rows, ChunkStats* stats) {
   const bool drafted = row > p.n;
   const int j = drafted ? row - p.n - 1 : row;
   if (drafted ? j >= count : j > count) return;
-  const Logits v(drafted ? p.draft_logits + ((size_t)i * p.n + j) * p.vocab : p.logits + ((size_t)i * (p.n + 1) + j) * p.vocab, chunk, p.vocab, (p.vocab & 3) == 0);
+  const Logits<> v(drafted ? p.draft_logits + ((size_t)i * p.n + j) * p.vocab : p.logits + ((size_t)i * (p.n + 1) + j) * p.vocab, chunk, p.vocab, (p.vocab & 3) == 0);
   float most = -INFINITY;
   int at = 0x7fffffff;
 #pragma unroll
@@ -179,14 +180,14 @@ __device__ __forceinline__ RowStats row_stats(const ChunkStats* s, int chunks, d
 struct Choice { RowStats p, q; int accepted, drafted; };      // drafted: the refused token; -1: none was refused
 constexpr int kKept = 32;
 struct ChooseLds { RowStats p[kKept], q[kKept]; int first; };
-template <bool GREEDY>
-__device__ __forceinline__ Choice choose(const Verify& p, int i, int chunks, int rows, const ChunkStats* stats, ChooseLds* lds) {
+// mine: the statistics of the sequence's rows, `chunks` each.
+template <bool GREEDY, int THREADS = kThreads>
+__device__ __forceinline__ Choice choose(const Verify& p, int i, int chunks, const ChunkStats* mine, ChooseLds* lds) {
   const int count = drafts_of(p, i), tid = threadIdx.x;
   const double per = GREEDY ? 0. : per_of(p);
-  const ChunkStats* mine = stats + (size_t)i * rows * chunks;
   int lanes = 64;
   while (lanes > 1 && lanes / 2 >= chunks) lanes >>= 1;
-  const int x = tid & (lanes - 1), group = tid / lanes, groups = kThreads / lanes;
+  const int x = tid & (lanes - 1), group = tid / lanes, groups = THREADS / lanes;
   if (tid == 0) lds->first = count;
   __syncthreads();
   for (int j0 = 0; j0 <= count; j0 += groups) {            // (all threads of a group, so that they can exchange; row `count` is behind the last draft)
@@ -272,10 +273,11 @@ __device__ __forceinline__ double up_to_me(double x, double* s_waves, double* al
   return x + before;
 }
 
-// draft: the thread's own, of the first 256
+// draft: the thread's own, of the first THREADS
+template <int THREADS = kThreads>
 __device__ __forceinline__ void write_tokens(const Verify& p, int i, int accepted, int token, int draft) {
-  for (int j = threadIdx.x; j <= p.n; j += kThreads)
-    p.tokens[(size_t)i * (p.n + 1) + j] = j < accepted ? (j < kThreads ? draft : p.drafts[(size_t)i * p.n + j]) : j == accepted ? token : -1;
+  for (int j = threadIdx.x; j <= p.n; j += THREADS)
+    p.tokens[(size_t)i * (p.n + 1) + j] = j < accepted ? (j < THREADS ? draft : p.drafts[(size_t)i * p.n + j]) : j == accepted ? token : -1;
   if (threadIdx.x == 0) p.accepted[i] = accepted;
 }
 
@@ -283,7 +285,7 @@ __global__ __launch_bounds__(kThreads)
 void verify_greedy_kernel(Verify p, int chunks, int rows, const ChunkStats* stats) {
   __shared__ ChooseLds lds;
   const int draft = (int)threadIdx.x < p.n ? p.drafts[(size_t)blockIdx.x * p.n + threadIdx.x] : -1;
-  const Choice c = choose<true>(p, blockIdx.x, chunks, rows, stats, &lds);
+  const Choice c = choose<true>(p, blockIdx.x, chunks, stats + (size_t)blockIdx.x * rows * chunks, &lds);
   write_tokens(p, blockIdx.x, c.accepted, c.p.at < p.vocab && c.p.most > -INFINITY ? c.p.at : 0, draft);      // (a row of -inf throughout: 0)
 }
 
@@ -295,16 +297,16 @@ void verify_rest_kernel(Verify p, int chunks, int rows, const ChunkStats* stats,
   __shared__ double s_sum[kSegments][4];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int i = (int)(blockIdx.x / (unsigned)chunks), chunk = (int)blockIdx.x - i * chunks;
-  const Choice c = choose<false>(p, i, chunks, rows, stats, &lds);
+  const Choice c = choose<false>(p, i, chunks, stats + (size_t)i * rows * chunks, &lds);
   if (chunk == 0 && tid == 0) choice[i] = c;
   const Rest r(p, i, c);
   const bool aligned = (p.vocab & 3) == 0;
   double* left = rest + (size_t)i * chunks * kSegments;
   {
-    const Logits lp(r.x, chunk, p.vocab, aligned);
+    const Logits<> lp(r.x, chunk, p.vocab, aligned);
     double of[kEach];
     if (r.y) {
-      const Logits lq(r.y, chunk, p.vocab, aligned);
+      const Logits<> lq(r.y, chunk, p.vocab, aligned);
 #pragma unroll
       for (int e = 0; e < kEach; ++e) of[e] = r.of(lp.at(e), lp.x[e], lq.x[e]);
     } else {
@@ -334,12 +336,28 @@ void verify_rest_kernel(Verify p, int chunks, int rows, const ChunkStats* stats,
   if (tid < kSegments) left[(size_t)chunk * kSegments + tid] = (s_sum[tid][0] + s_sum[tid][1]) + (s_sum[tid][2] + s_sum[tid][3]);
 }
 
+// Where there is nothing to draw from: the lowest index of the row's largest logit (all threads together).
+template <int THREADS>
+__device__ __forceinline__ int largest(const float* row, int vocab, float* s_most, int* s_at) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  float most = -INFINITY;
+  int at = 0x7fffffff;
+  for (int v = threadIdx.x; v < vocab; v += THREADS) better(most, at, tame(row[v]), v);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) better(most, at, __shfl_xor(most, o), __shfl_xor(at, o));
+  if (lane == 0) { s_most[wave] = most; s_at[wave] = at; }
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < THREADS / 64; ++w) better(most, at, s_most[w], s_at[w]);
+  return most > -INFINITY ? at : 0;
+}
+
 __global__ __launch_bounds__(kThreads)
 void verify_draw_kernel(Verify p, int chunks, const double* rest, const Choice* choice) {
   __shared__ double s_waves[4], s_before;
   __shared__ float s_most[4];
   __shared__ int s_at[4], s_found, s_last;
-  const int i = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int i = blockIdx.x, tid = threadIdx.x;
   const int segments = (p.vocab + kSegment - 1) / kSegment;
   const double* left = rest + (size_t)i * chunks * kSegments;
   const double first = tid < segments ? left[tid] : 0.;      // (all there is, up to 65536 tokens)
@@ -387,18 +405,160 @@ void verify_draw_kernel(Verify p, int chunks, const double* rest, const Choice* 
     __syncthreads();
     token = s_found != 0x7fffffff ? s_found : s_last;
   } else {                                                 // nothing to draw from: the largest logit
-    float most = -INFINITY;
-    int at = 0x7fffffff;
-    for (int v = tid; v < p.vocab; v += kThreads) better(most, at, tame(r.x[v]), v);
-#pragma unroll
-    for (int o = 32; o > 0; o >>= 1) better(most, at, __shfl_xor(most, o), __shfl_xor(at, o));
-    if (lane == 0) { s_most[wave] = most; s_at[wave] = at; }
-    __syncthreads();
-#pragma unroll
-    for (int w = 0; w < 4; ++w) better(most, at, s_most[w], s_at[w]);
-    token = most > -INFINITY ? at : 0;
+    token = largest<kThreads>(r.x, p.vocab, s_most, s_at);
   }
   write_tokens(p, i, c.accepted, token, draft);
+}
+
+// Rows that one workgroup's threads hold, EACH logits each of the target's and the draft's: what is left of the row that decides stays in registers, and the
+// token is drawn from them.  Of a step of 1024 threads a wave has a segment, 256 tokens or (unaligned rows) 64; the segments' sums in order give the one that
+// holds the goal, and its wave finds the token.  ALONE: the rows' sums as well, a wave a row.
+constexpr int kNear = 1024, kNearEach = 16;        // threads, logits of one at most
+constexpr int kAloneRows = 128;                    // rows of a sequence, at most
+template <bool ALONE, int EACH, bool ALIGNED>
+__global__ __launch_bounds__(kNear)
+void verify_near_kernel(Verify p, int chunks, int rows, const ChunkStats* stats) {
+  constexpr int kWaves = kNear / 64, V = ALIGNED ? 4 : 1, STEPS = EACH / V, kLine = (STEPS * kWaves + 63) / 64;      // kLine: segments of a lane of the wave that searches
+  __shared__ ChooseLds lds;
+  __shared__ ChunkStats s_rows[ALONE ? kAloneRows : 1];
+  __shared__ double s_sum[64 * kLine], s_before, s_total;
+  __shared__ float s_most[kWaves];
+  __shared__ int s_at[kWaves], s_found, s_last, s_token;
+  const int i = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int draft = tid < p.n ? p.drafts[(size_t)i * p.n + tid] : -1;
+  const float u = p.u[(size_t)i * (p.n + 1) + p.n];
+  const ChunkStats* mine = stats + (size_t)i * rows * chunks;
+  if constexpr (ALONE) {
+    const int count = drafts_of(p, i);
+    const double per = per_of(p);
+    for (int row = wave; row < rows; row += kWaves) {
+      const bool drafted = row > p.n;
+      const int j = drafted ? row - p.n - 1 : row;
+      if (drafted ? j >= count : j > count) continue;
+      const float* x = drafted ? p.draft_logits + ((size_t)i * p.n + j) * p.vocab : p.logits + ((size_t)i * (p.n + 1) + j) * p.vocab;
+      auto four = [&](int v0, float (&y)[4]) {             // (loads without branches around them: all on their way at once)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = x[min(v0 + 64 * e, p.vocab - 1)];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) y[e] = v0 + 64 * e < p.vocab ? tame(y[e]) : -INFINITY;
+      };
+      float y[4], most = -INFINITY;
+      for (int v = lane; v < p.vocab; v += 256) {
+        four(v, y);
+        most = fmaxf(most, fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])));
+      }
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) most = fmaxf(most, __shfl_xor(most, o));
+      double sum = 0.;
+      for (int v = lane; v < p.vocab; v += 256) {
+        four(v, y);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum += weight(y[e], most, per);
+      }
+#pragma unroll
+      for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+      if (lane == 0) s_rows[row] = ChunkStats{sum, most, 0};
+    }
+    mine = s_rows;
+    __syncthreads();
+  }
+  const Choice c = choose<false, kNear>(p, i, ALONE ? 1 : chunks, mine, &lds);
+  const Rest r(p, i, c);
+  const Logits<kNear, EACH> lp(r.x, 0, p.vocab, ALIGNED);
+  double of[EACH], upto[STEPS];                            // upto: of the wave's tokens of a step, those up to this lane's last
+  if (r.y) {
+    const Logits<kNear, EACH> lq(r.y, 0, p.vocab, ALIGNED);
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) of[e] = r.of(lp.at(e), lp.x[e], lq.x[e]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) of[e] = r.of(lp.at(e), lp.x[e], 0.f);
+  }
+#pragma unroll
+  for (int q = 0; q < STEPS; ++q) {
+    double x = of[V * q];
+#pragma unroll
+    for (int y = 1; y < V; ++y) x += of[V * q + y];
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const double y = __shfl_up(x, o);
+      if (lane >= o) x += y;
+    }
+    upto[q] = x;
+    if (lane == 63) s_sum[q * kWaves + wave] = x;
+  }
+  if (tid == 0) { s_found = 0x7fffffff; s_last = -1; }
+  __syncthreads();
+  if (wave == 0) {                                         // the segment in which the running sum exceeds the goal, else the last that has anything
+    double add[kLine], mine_all = 0.;
+#pragma unroll
+    for (int x = 0; x < kLine; ++x) {
+      const int at = lane * kLine + x;
+      add[x] = at < STEPS * kWaves ? s_sum[at] : 0.;
+      mine_all += add[x];
+    }
+    double run = mine_all;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const double y = __shfl_up(run, o);
+      if (lane >= o) run += y;
+    }
+    const double total = __shfl(run, 63), goal = (double)u * total;
+    run = __shfl_up(run, 1);
+    if (lane == 0) run = 0.;
+    int found = 0x7fffffff, last = -1;
+    double before = 0.;
+#pragma unroll
+    for (int x = 0; x < kLine; ++x) {
+      if (add[x] > 0.) {
+        if (found == 0x7fffffff && run + add[x] > goal) { found = lane * kLine + x; before = run; }
+        last = lane * kLine + x;
+      }
+      run += add[x];
+    }
+    const unsigned long long those = __ballot(found != 0x7fffffff), any = __ballot(last >= 0);
+    if (those != 0 && lane == __ffsll(those) - 1) { s_found = found; s_before = before; }
+    if (any != 0 && lane == 63 - __clzll(any)) s_last = last;
+    if (lane == 0) s_total = total;
+  }
+  __syncthreads();
+  int token;
+  if (s_total > 0.) {
+    const bool inside = s_found != 0x7fffffff;
+    const int segment = inside ? s_found : s_last;
+    if (segment % kWaves == wave) {                        // its first token that exceeds the goal, else the last that has anything
+      const double goal = inside ? (double)u * s_total : INFINITY;
+      int found = 0x7fffffff, last = -1;
+#pragma unroll
+      for (int q = 0; q < STEPS; ++q) {
+        if (q != segment / kWaves) continue;
+        double run = __shfl_up(upto[q], 1);
+        run = (inside ? s_before : 0.) + (lane == 0 ? 0. : run);
+#pragma unroll
+        for (int y = 0; y < V; ++y) {
+          const double x = of[V * q + y];
+          run += x;
+          if (x > 0.) {
+            if (found == 0x7fffffff && run > goal) found = lp.at(V * q + y);
+            last = lp.at(V * q + y);
+          }
+        }
+      }
+      const unsigned long long those = __ballot(found != 0x7fffffff), any = __ballot(last >= 0);
+      if (lane == (those != 0 ? __ffsll(those) - 1 : 63 - __clzll(any))) s_token = those != 0 ? found : last;
+    }
+    __syncthreads();
+    token = s_token;
+  } else {
+    token = largest<kNear>(r.x, p.vocab, s_most, s_at);
+  }
+  write_tokens<kNear>(p, i, c.accepted, token, draft);
+}
+
+template <bool ALONE, int EACH>
+static void launch_near(const Verify& p, int chunks, int rows, const ChunkStats* stats, hipStream_t st) {
+  if ((p.vocab & 3) == 0) hipLaunchKernelGGL((verify_near_kernel<ALONE, EACH, true>), dim3((unsigned)p.b), dim3(kNear), 0, st, p, chunks, rows, stats);
+  else hipLaunchKernelGGL((verify_near_kernel<ALONE, EACH, false>), dim3((unsigned)p.b), dim3(kNear), 0, st, p, chunks, rows, stats);
 }
 
 int verify_chunks(int vocab) { return (vocab + kChunk - 1) / kChunk; }
@@ -417,12 +577,25 @@ hipError_t launch_verify(const Verify& p, void* workspace, hipStream_t st) {
   double* rest = reinterpret_cast<double*>(choice + p.b);
   const dim3 all((unsigned)((size_t)p.b * rows * chunks)), rests((unsigned)((size_t)p.b * chunks)), each((unsigned)p.b), block(kThreads);
   const bool greedy = !(p.temperature > 0.f);
+  // One launch where the rows that a wave has in turn are short (four drafts, 300 tokens: 8.2 us, in two launches 9.8; of 2000 10.6 and 10.3), and for more
+  // where the sequences are many (256 of two rows of 2000: 11.9 and 13.1; of 4000 19.5 and 14.2).
+  static_assert(2048 <= 4 * kNear, "rows that a thread holds in four");
+  if (!greedy && rows <= kAloneRows && (long long)((rows + 15) / 16) * p.vocab <= (p.b >= 128 ? 2048 : 1024)) {
+    launch_near<true, 4>(p, chunks, rows, stats, st);
+    return hipGetLastError();
+  }
   if (greedy) hipLaunchKernelGGL(verify_stats_kernel<true>, all, block, 0, st, p, chunks, rows, stats);
   else hipLaunchKernelGGL(verify_stats_kernel<false>, all, block, 0, st, p, chunks, rows, stats);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
   if (greedy) {
     hipLaunchKernelGGL(verify_greedy_kernel, each, block, 0, st, p, chunks, rows, stats);
+    return hipGetLastError();
+  }
+  // (two launches for three: four drafts, 4096 tokens 11.1 us for 18.2, 16384 16.2 for 20.6; with twice the logits a thread they do not fit its registers)
+  if (p.vocab <= kNearEach * kNear) {
+    if (p.vocab <= 4 * kNear) launch_near<false, 4>(p, chunks, rows, stats, st);
+    else launch_near<false, kNearEach>(p, chunks, rows, stats, st);
     return hipGetLastError();
   }
   hipLaunchKernelGGL(verify_rest_kernel, rests, block, 0, st, p, chunks, rows, stats, rest, choice);

@@ -35,7 +35,8 @@ def check(m, logits, drafts, u, draft_logits=None, counts=None, temperature=1.0)
 
 @pytest.mark.parametrize("temperature", [1.0, 0.7, 0.0])
 @pytest.mark.parametrize("draft", ["logits", "none"])
-@pytest.mark.parametrize("b,n,vocab", [(1, 1, 1), (2, 3, 2), (7, 4, 100), (3, 5, 4095), (4, 2, 4096), (4, 2, 4097), (8, 4, 32768), (2, 7, 50001), (300, 1, 33), (1, 300, 20)])
+@pytest.mark.parametrize("b,n,vocab", [(1, 1, 1), (2, 3, 2), (7, 4, 100), (3, 5, 4095), (4, 2, 4096), (4, 2, 4097), (8, 4, 32768), (2, 7, 50001), (300, 1, 33), (1, 300, 20),
+                                       (3, 40, 60), (130, 2, 1999), (5, 8, 512), (3, 2, 16384), (2, 3, 9001), (1, 2, 16385)])
 def test_random(m, b, n, vocab, draft, temperature):
     rng = np.random.default_rng(b + n + vocab)
     logits = (3 * rng.standard_normal((b, n + 1, vocab))).astype(np.float32)
@@ -50,7 +51,7 @@ def test_random(m, b, n, vocab, draft, temperature):
         check(m, logits, drafts, u, draft_logits if draft == "logits" else None, c, temperature)
 
 
-@pytest.mark.parametrize("vocab", [64, 5000])
+@pytest.mark.parametrize("vocab", [64, 3000, 5000, 20000])
 def test_masked_logits(m, vocab):
     """-infinity for most tokens, whole rows of it, NaN, +infinity; the largest and the smallest random numbers."""
     rng = np.random.default_rng(vocab)
