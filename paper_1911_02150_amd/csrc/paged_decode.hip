@@ -938,8 +938,9 @@ PagedPlan paged_plan(int b, int n, int h, int h_kv, int page_size, int max_pages
   // 16 query rows to a workgroup where the work is so little that its latency counts, else 32, whose tiles are read half as often: 16 sequences of 2048, 32 heads
   // 14.9 us against 18.8, 48 of them 22.6 and 22.5, 512 of up to 4096 with 64 heads 245 and 187; 8 sequences of 200, 64 heads 7.8 and 10.8; 256 wide, 32 heads, 16
   // sequences of 2048 23.8 and 27.8, 32 of them 31.9 and 31.0.
+  // And only where a compute unit can hold them all, two each, three of 64 wide: 200 sequences of up to 100, 64 heads, 15.9 and 13.4; 64 wide 150 of 40 7.3 and 8.8.
   // (float32 rows of more than 64: 32 query rows do not fit a wave's registers beside a tile.)
-  const bool little = groups * tiles * R * (pl.form == -256 ? 4 : 2) <= 3 << 16;
+  const bool little = groups * tiles * R * (pl.form == -256 ? 4 : 2) <= 3 << 16 && groups * ((R + 15) / 16) <= (pl.form == 64 ? 3 : 2) * kComputeUnits;
   pl.block_rows = R <= 16 || little || (!is_bf16 && pl.form != 64) ? 16 : 32;
   pl.blocks = (int)((R + pl.block_rows - 1) / pl.block_rows);
   // One launch, a workgroup to a group, where cutting and merging would take longer (sequences of 380: 8.3 us, in pieces 10.8; of 800 17.7 and 11.8; float32 of
