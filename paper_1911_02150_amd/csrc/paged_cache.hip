@@ -76,16 +76,17 @@ __device__ __forceinline__ int before_me(int x, int* waves, int* total) {
 
 // Which positions of (sequence, head) stay: the latest `recent`, and of the older ones the largest scores up to the budget, the lower position among
 // equals.  A radix selection over the keys, 11 + 11 + 10 bits from the top: a histogram of the keys that agree with the threshold so far, and the bin in
-// which the wanted rank lies.  One workgroup per (sequence, head), which is bound by the latency of its steps: a thread's KEEP positions (tid, tid + 1024, ...) are
-// read once and stay in registers, and what stays is put in order by two sums over all of them, not two for every 1024 (8192 positions: 36 -> 12.7 us).  Capacities
-// beyond (KEEP = 0) are gone over again for every step.
+// which the wanted rank lies, until all of a bin stays (one sequence of 100 in two passes 8.1 us, in three 10.8).  One workgroup per (sequence, head), which is bound by the latency of its steps: a thread's KEEP positions
+// (tid, tid + 1024, ...) are read once and stay in registers, and what stays is put in order by two sums over all of them, not two
+// for every 1024 (8192 positions: 36 -> 12 us).  Capacities beyond (KEEP = 0) are gone over again for every step, eight positions a thread on their way together
+// (one sequence of 130000: 164 us, one position at a time 379).
 template <int KEEP>
 __global__ __launch_bounds__(kSelectThreads)
 void evict_select_kernel(PagedEvict p) {
   constexpr int kWaves = kSelectThreads / 64;
   __shared__ int bins[kBins];
   __shared__ int waves[kWaves];
-  __shared__ int s_bin, s_above;
+  __shared__ int s_bin, s_above, s_all;
   __shared__ int s_count[2][(KEEP > 0 ? KEEP : 1) * kWaves + 1];      // of a wave's 64 positions: those at the threshold, those that stay
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int g = blockIdx.x, i = g / p.c.h_kv;
@@ -93,23 +94,47 @@ void evict_select_kernel(PagedEvict p) {
   const int32_t* table = p.c.table + (size_t)i * p.c.max_pages;
   const float* score = p.scores_in + (size_t)g * p.c.positions();
   const int old = max(0, L - p.recent);
-  auto there = [&](int pos) { return (unsigned)table[(unsigned)pos / (unsigned)p.c.page_size] < (unsigned)p.c.num_pages; };
-  auto key_of = [&](int pos) -> uint32_t { return pos < old && there(pos) ? score_key(score[pos]) : 0u; };      // 0: not one of the older ones
+  constexpr int kStep = 8 * kSelectThreads;
+  const unsigned size = p.c.page_size, step = kSelectThreads / size, more = kSelectThreads % size;
+  struct Walk { unsigned page, inside; };      // of positions tid, tid + 1024, ...
+  const Walk start{(unsigned)tid / size, (unsigned)tid % size};
+  auto next = [&](Walk& w) {
+    w.page += step;
+    w.inside += more;
+    if (w.inside >= size) { w.inside -= size; ++w.page; }
+  };
+  // see(position, whether it is there, its score) for all positions below `end`, and some that are not, eight on their way at a time
+  auto go_over = [&](int end, auto&& see) {
+    Walk w = start;
+    for (int base = 0; base < end; base += kStep) {
+      int32_t entry[8];
+      float x[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {    // (past the end: the first entry and score, which are there)
+        const int pos = base + u * kSelectThreads + tid;
+        entry[u] = table[pos < end ? w.page : 0u];
+        x[u] = score[pos < end ? pos : 0];
+        next(w);
+      }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const int pos = base + u * kSelectThreads + tid;
+        see(pos, pos < end && (unsigned)entry[u] < (unsigned)p.c.num_pages, x[u]);
+      }
+    }
+  };
   uint32_t keys[KEEP > 0 ? KEEP : 1];
   float values[KEEP > 0 ? KEEP : 1];
   uint32_t late = 0;                   // bit u: the thread's u-th position is one of the latest, and there
   int n_old = 0, n_recent = 0;
   if constexpr (KEEP > 0) {
-    const unsigned size = p.c.page_size, step = kSelectThreads / size, more = kSelectThreads % size;
-    unsigned page = (unsigned)tid / size, inside = (unsigned)tid % size;      // of position tid + u * 1024
+    Walk w = start;
 #pragma unroll
     for (int u = 0; u < KEEP; ++u) {   // (past the length: the first entry and score, which are there)
       const int pos = tid + u * kSelectThreads;
-      keys[u] = (uint32_t)table[pos < L ? page : 0u];
+      keys[u] = (uint32_t)table[pos < L ? w.page : 0u];
       values[u] = score[pos < L ? pos : 0];
-      page += step;
-      inside += more;
-      if (inside >= size) { inside -= size; ++page; }
+      next(w);
     }
 #pragma unroll
     for (int u = 0; u < KEEP; ++u) {
@@ -121,8 +146,10 @@ void evict_select_kernel(PagedEvict p) {
     }
     n_recent = __popc(late);
   } else {
-    for (int pos = tid; pos < L; pos += kSelectThreads)
-      if (there(pos)) (pos < old ? n_old : n_recent) += 1;
+    go_over(L, [&](int pos, bool is, float) {
+      n_old += is && pos < old;
+      n_recent += is && pos >= old;
+    });
   }
   int all_old, all_recent;
   before_me(n_old, waves, &all_old);
@@ -148,7 +175,7 @@ void evict_select_kernel(PagedEvict p) {
 #pragma unroll
         for (int u = 0; u < KEEP; ++u) add(keys[u]);
       } else {
-        for (int pos = tid; pos < old; pos += kSelectThreads) add(key_of(pos));
+        go_over(old, [&](int, bool is, float x) { add(is ? score_key(x) : 0u); });
       }
       __syncthreads();
       // bins from the top: thread t has the two (or the one) from count - 1 - 2t down
@@ -156,11 +183,16 @@ void evict_select_kernel(PagedEvict p) {
       const int x0 = top >= 0 ? bins[top] : 0, x1 = top >= 1 ? bins[top - 1] : 0;
       int total;
       const int above = before_me(x0 + x1, waves, &total);
-      if (above < rank && rank <= above + x0) { s_bin = top; s_above = above; }
-      if (above + x0 < rank && rank <= above + x0 + x1) { s_bin = top - 1; s_above = above + x0; }
+      if (above < rank && rank <= above + x0) { s_bin = top; s_above = above; s_all = x0; }
+      if (above + x0 < rank && rank <= above + x0 + x1) { s_bin = top - 1; s_above = above + x0; s_all = x1; }
       __syncthreads();
       threshold |= (uint32_t)s_bin << shift;
       rank -= s_above;
+      if (rank == s_all) {             // the whole bin stays: every key from its first on  (no key is 0 in the first pass' bits)
+        --threshold;
+        rank = 0;
+        break;
+      }
       __syncthreads();
     }
     ties = rank;
@@ -219,20 +251,48 @@ void evict_select_kernel(PagedEvict p) {
     done = s_count[1][KEEP * kWaves];
   } else {
     int tied = 0;
-    for (int base = 0; base < L; base += kSelectThreads) {
-      const int pos = base + tid;
-      const uint32_t key = pos < old ? key_of(pos) : 0u;
-      const bool equal = key != 0 && key == threshold;
-      int total;
-      const int equals_before = tied + before_me(equal ? 1 : 0, waves, &total);
-      tied += total;
-      const bool stays = pos < L && (pos < old ? key > threshold || (equal && equals_before < ties) : there(pos));
-      const int slot = done + before_me(stays ? 1 : 0, waves, &total);
-      done += total;
-      if (stays && slot < p.budget) {
-        kept[slot] = pos;
-        score_out[slot] = score[pos];
+    for (int base = 0; base < L; base += kStep) {
+      const int first = base + 8 * tid;
+      Walk w{(unsigned)first / size, (unsigned)first % size};
+      float x[8];
+      int32_t entry[8];
+      uint32_t is = 0, stays = 0, equal = 0;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        entry[u] = table[first + u < L ? w.page : 0u];
+        x[u] = score[first + u < L ? first + u : 0];
+        if (++w.inside == size) { w.inside = 0; ++w.page; }
       }
+#pragma unroll
+      for (int u = 0; u < 8; ++u) is |= (uint32_t)(first + u < L && (unsigned)entry[u] < (unsigned)p.c.num_pages) << u;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) {
+        const uint32_t key = score_key(x[u]);
+        const bool late = first + u >= old;
+        stays |= (uint32_t)(late || key > threshold) << u;
+        equal |= (uint32_t)(!late && key == threshold) << u;
+      }
+      stays &= is;
+      equal &= is;
+      int total;
+      if (ties > 0) {                  // (the same in all threads)
+        int rank = tied + before_me(__popc(equal), waves, &total);
+        tied += total;
+#pragma unroll
+        for (int u = 0; u < 8; ++u)
+          if (equal >> u & 1) stays |= (uint32_t)(rank++ < ties) << u;
+      }
+      int slot = done + before_me(__popc(stays), waves, &total);
+      done += total;
+#pragma unroll
+      for (int u = 0; u < 8; ++u)
+        if (stays >> u & 1) {
+          if (slot < p.budget) {
+            kept[slot] = first + u;
+            score_out[slot] = x[u];
+          }
+          ++slot;
+        }
     }
   }
   done = min(done, p.budget);

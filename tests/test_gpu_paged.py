@@ -239,6 +239,8 @@ EVICT = [
     (1, 1, 16, 16, 16, "f32", [5000], 77, 7),
     (1, 2, 8, 8, 48, "bf16", [16000], 2500, 100),
     (2, 1, 8, 16, 256, "f32", [26000, 24577], 3000, 1),
+    (1, 1, 8, 8, 100, "f32", [70001], 5000, 700),
+    (2, 1, 8, 8, 64, "f32", [90000, 8193], 90000, 0),
 ]
 
 
