@@ -64,7 +64,7 @@ struct PagedEvict {
 };
 
 struct PagedPlan {
-  int form;                // the matrix kernel's widths: 64 or 128; -128, -256: up to that
+  int form;                // the matrix kernel's widths: 64 or 128; -64, -128, -256: up to that
   int block_rows, blocks, split, pieces;      // pieces: at most
   size_t bytes;
 };

@@ -317,7 +317,7 @@ __device__ __forceinline__ bool find_segment(const PagedDecode& p, Segment* s) {
 }
 
 // ---------------------------------------------------------------- matrix instructions
-// Caches of k = v = D = 64 or 128, and (EXACT = false) of any widths up to D = 128 or 256: pieces past a width are read as its last, against q's zeros
+// Caches of k = v = D = 64 or 128, and (EXACT = false) of any widths up to D = 64, 128 or 256: pieces past a width are read as its last, against q's zeros
 // and into columns that nobody wants.  A workgroup is four waves; wave w has the tiles w, w + 4, ... of a segment, for all rows of the block (16 or 32), and keeps
 // their running maximum, sum and outputs; at the end the four states are merged through LDS.  Rows go from memory straight into the operands:
 //   logits^T[32 pos x 16 rows] = K_tile . q^T: lane (i, g) = (lane % 16, lane / 16) has 16-byte pieces g, g + 4, ... of two K rows.  Row i of product u is position
@@ -933,15 +933,15 @@ PagedPlan paged_plan(int b, int n, int h, int h_kv, int page_size, int max_pages
   PagedPlan pl = {};
   const long long R = (long long)n * (h / h_kv), positions = (long long)max_pages * page_size, tiles = (positions + kPagedTile - 1) / kPagedTile;
   const int wide = k > v ? k : v;
-  pl.form = k == v && (k == 64 || k == 128) ? k : wide <= 128 ? -128 : -256;
+  pl.form = k == v && (k == 64 || k == 128) ? k : wide <= 64 ? -64 : wide <= 128 ? -128 : -256;
   const long long groups = (long long)b * h_kv;
   // 16 query rows to a workgroup where the work is so little that its latency counts, else 32, whose tiles are read half as often: 16 sequences of 2048, 32 heads
   // 14.9 us against 18.8, 48 of them 22.6 and 22.5, 512 of up to 4096 with 64 heads 245 and 187; 8 sequences of 200, 64 heads 7.8 and 10.8; 256 wide, 32 heads, 16
   // sequences of 2048 23.8 and 27.8, 32 of them 31.9 and 31.0.
   // And only where a compute unit can hold them all, two each, three of 64 wide: 200 sequences of up to 100, 64 heads, 15.9 and 13.4; 64 wide 150 of 40 7.3 and 8.8.
   // (float32 rows of more than 64: 32 query rows do not fit a wave's registers beside a tile.)
-  const bool little = groups * tiles * R * (pl.form == -256 ? 4 : 2) <= 3 << 16 && groups * ((R + 15) / 16) <= (pl.form == 64 ? 3 : 2) * kComputeUnits;
-  pl.block_rows = R <= 16 || little || (!is_bf16 && pl.form != 64) ? 16 : 32;
+  const bool little = groups * tiles * R * (pl.form == -256 ? 4 : 2) <= 3 << 16 && groups * ((R + 15) / 16) <= (wide <= 64 ? 3 : 2) * kComputeUnits;
+  pl.block_rows = R <= 16 || little || (!is_bf16 && wide > 64) ? 16 : 32;
   pl.blocks = (int)((R + pl.block_rows - 1) / pl.block_rows);
   // One launch, a workgroup to a group, where cutting and merging would take longer (sequences of 380: 8.3 us, in pieces 10.8; of 800 17.7 and 11.8; float32 of
   // 380 13.7 and 13.5), and to greater lengths where there is one for every compute unit (256 of up to 760: 18, in pieces 25).
@@ -999,6 +999,7 @@ hipError_t launch_paged_decode(const PagedDecode& p, const PagedPlan& pl, int is
   switch (pl.form) {
     case 64: e = is_bf16 ? launch_rows<uint16_t, 64, true>(p, pl, st) : launch_rows<float, 64, true>(p, pl, st); break;
     case 128: e = is_bf16 ? launch_rows<uint16_t, 128, true>(p, pl, st) : launch_rows<float, 128, true>(p, pl, st); break;
+    case -64: e = is_bf16 ? launch_rows<uint16_t, 64, false>(p, pl, st) : launch_rows<float, 64, false>(p, pl, st); break;
     case -128: e = is_bf16 ? launch_rows<uint16_t, 128, false>(p, pl, st) : launch_rows<float, 128, false>(p, pl, st); break;
     default: e = is_bf16 ? launch_rows<uint16_t, 256, false>(p, pl, st) : launch_rows<float, 256, false>(p, pl, st); break;
   }

@@ -177,6 +177,67 @@ def test_large_logits(m):
     assert (np.abs(got - want[:, 0]) <= tolerance(q, K, size, 1.0, 640)[:, 0]).all()
 
 
+# b, n, h, k, v, dtype, pages of a sequence: so many sequences that a workgroup has 32 rows, in one launch and in two
+MANY = [
+    (300, 1, 20, 128, 128, "bf16", 4),
+    (300, 2, 20, 128, 128, "bf16", 70),
+    (400, 1, 20, 64, 64, "bf16", 70),
+    (400, 2, 20, 64, 64, "f32", 5),
+    (400, 1, 18, 40, 64, "bf16", 70),
+    (400, 1, 18, 64, 24, "f32", 5),
+    (300, 1, 20, 120, 96, "bf16", 70),
+    (300, 1, 40, 200, 256, "bf16", 4),
+    (300, 1, 20, 256, 256, "f32", 70),
+]
+
+
+@pytest.mark.parametrize("scored", [False, True])
+@pytest.mark.parametrize("b,n,h,k,v,dtype,each", MANY)
+def test_many_sequences_of_many_rows(m, b, n, h, k, v, dtype, each, scored):
+    """Pages shared by all sequences, some of them nothing's."""
+    from oracle import paged
+    rng = np.random.default_rng(b + h + k + each)
+    page, pages = 16, 50
+    K, V = (pool(rng, pages, 1, page, w, dtype) for w in (k, v))
+    table = rng.integers(0, pages, (b, each))
+    table[rng.random(table.shape) < 0.1] = -1
+    lens = rng.integers(0, 40, b)
+    lens[5], lens[7], lens[-1] = each * page, each * page - 17, 0
+    q = rng.standard_normal((b, n, h, k)).astype(np.float32)
+    scale = 1 / k ** 0.5
+    scores = np.zeros((b, 1, each * page)) if scored else None
+    want, total, size = paged.attend(q.astype(np.float64), K, V, table, lens, float(np.float32(scale)), scores)
+    kw = dict(scores=torch.zeros((b, each * page), device=DEV)) if scored else {}
+    got = m.mqa_paged_decode_step(on_gpu(q[:, 0] if n == 1 else q), on_gpu(K, dtype, True), on_gpu(V, dtype, True), on_gpu(table), on_gpu(lens), scale=scale, **kw)
+    off = np.abs(got.cpu().numpy().reshape(want.shape) - want)
+    assert (off <= tolerance(q, K, size, scale, lens.max())).all(), off.max()
+    if scored:
+        out, there = kw["scores"].cpu().numpy()[:, None], ~np.isnan(total)
+        bound = tolerance(q, K, 1, scale, lens.max()) * total + EPS * (2 + n * h) * total
+        assert (np.abs(out - total)[there] <= bound[there]).all() and not out[~there].any()
+
+
+@pytest.mark.parametrize("b,k,dtype", [(300, 128, "bf16"), (400, 64, "f32"), (300, 200, "bf16")])
+def test_many_rows_and_a_nan_that_half_of_them_see(m, b, k, dtype):
+    """The newest token's K and V are NaN in every third sequence: of two queries the first does not see them."""
+    from oracle import paged
+    rng = np.random.default_rng(b + k)
+    page, pages, each, n, h = 16, 40, 4, 2, 20
+    K, V = (pool(rng, pages + 1, 1, page, k, dtype) for _ in range(2))
+    clean = K[:pages].copy()
+    K[pages] = V[pages] = np.nan
+    table, lens = rng.integers(0, pages, (b, each)), rng.integers(2, 60, b)
+    lens[::3] = 17 + 16 * rng.integers(0, 3, len(lens[::3]))
+    for i in range(0, b, 3):
+        table[i, lens[i] // page] = pages
+    q = rng.standard_normal((b, n, h, k)).astype(np.float32)
+    want, _, size = paged.attend(q.astype(np.float64), K, V, table, lens, 0.125)
+    got = m.mqa_paged_decode_step(on_gpu(q), on_gpu(K, dtype, True), on_gpu(V, dtype, True), on_gpu(table), on_gpu(lens), scale=0.125).cpu().numpy()
+    finite = np.isfinite(want)
+    assert np.isnan(got[~finite]).all() and finite[:, 0].all() and not finite[::3, 1].any() and finite[1::3].all()
+    assert (np.abs(got - want)[finite] <= tolerance(q, clean, size, 0.125, 60)[finite]).all()
+
+
 def test_many_short_sequences_and_one_long(m):
     """More sequences than a workgroup has threads, empty ones among them, against the contiguous call."""
     g = torch.Generator(device=DEV).manual_seed(1)
