@@ -215,7 +215,7 @@ __device__ __forceinline__ int before_me(int x, int* s_waves, int* all) {
   return before;
 }
 
-constexpr int kComputeUnits = 256, kShares = 768, kLeast = 16, kLongest = 64;
+constexpr int kComputeUnits = 256, kShares = 768, kSharesOfMany = 512, kLeast = 16, kLongest = 64;
 
 // This workgroup's segment; false: there is none.  Every workgroup looks at all lengths: thread t has sequences t * each up to the next one's.
 __device__ __forceinline__ bool find_segment(const PagedDecode& p, Segment* s) {
@@ -260,7 +260,8 @@ __device__ __forceinline__ bool find_segment(const PagedDecode& p, Segment* s) {
   // more than twice what a workgroup's share would be (512 sequences of up to 1000, 32 heads: 45 us, in shares 56; 64 of up to 2500, 8 heads, which are not cut
   // by this rule 75, uncut 84).  Else as many as leave every compute unit one workgroup at most, or else two, if
   // that is not too uneven (64 sequences of 8192, 32 heads: 53 us, in 512 pieces 58; 128 of up to 1024, 64 heads, two to a unit 33, in shares of a 768th 45); else
-  // shares so small that a compute unit has several in turn (512 sequences of up to 4096, 32 heads: 126, in shares of a 512th 137, of a 1536th 133), though
+  // shares so small that a compute unit has several in turn (512 sequences of up to 4096, 32 heads: 126, in shares of a 512th 137, of a 1536th 133; with several
+  // blocks of rows shares of a 512th: 300 of up to 6000, 64 heads 160, of a 768th 166), though
   // not below four tiles a wave (256 of 512, 64 heads: 31, else 42).
   int per = 0, count = 0, before = 0, all = 0, turn = 0;
   auto pieces_of = [&](int t) { return max(1, (int)((unsigned)(t + per - 1) / (unsigned)per)); };
@@ -284,7 +285,8 @@ __device__ __forceinline__ bool find_segment(const PagedDecode& p, Segment* s) {
         fits = all * heads <= units;
       }
   }
-  if (!fits) cut(max(kLeast, (total + kShares - 1) / kShares));
+  const int shares = p.blocks > 1 ? kSharesOfMany : kShares;
+  if (!fits) cut(max(kLeast, (total + shares - 1) / shares));
   if (piece >= all * heads) return false;
   if (before * heads <= piece && piece < (before + count) * heads) {      // one thread
     int x = from, L = len, c = pieces_of(tiles_of(p, len));
