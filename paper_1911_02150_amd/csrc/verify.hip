@@ -61,31 +61,34 @@ __device__ __forceinline__ double block_sum(double x, double* red) {
 
 __device__ __forceinline__ int drafts_of(const Verify& p, int i) { return p.counts ? min(max(p.counts[i], 0), p.n) : p.n; }
 
-// A thread's logits of a chunk of THREADS * EACH: 16 bytes at a time where rows are aligned; past the end -inf.  at(e): the index of the e-th.
+// A thread's logits of a chunk of THREADS * EACH, 16 bytes at a time (of rows that begin at any float: the memory pipe takes them so); past the end -inf.
+// at(e): the index of the e-th.
 template <int THREADS = kThreads, int EACH = kEach>
 struct Logits {
+  typedef __attribute__((ext_vector_type(4), aligned(4))) float Four;
+  static constexpr int kStep = 4 * THREADS;
   float x[EACH];
-  int first, step;
-  __device__ __forceinline__ Logits(const float* row, int chunk, int vocab, bool aligned) {
-    if (aligned) {
-      first = chunk * THREADS * EACH + 4 * (int)threadIdx.x;
-      step = 4 * THREADS;
+  int first;
+  __device__ __forceinline__ Logits(const float* row, int chunk, int vocab) {
+    first = chunk * THREADS * EACH + 4 * (int)threadIdx.x;
 #pragma unroll
-      for (int e = 0; e < EACH / 4; ++e) {
-        float4 v = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
-        if (first + e * step < vocab) v = *reinterpret_cast<const float4*>(row + first + e * step);
-        x[4 * e] = v.x; x[4 * e + 1] = v.y; x[4 * e + 2] = v.z; x[4 * e + 3] = v.w;
+    for (int e = 0; e < EACH / 4; ++e) {
+      const int v = first + e * kStep;
+      Four y = {-INFINITY, -INFINITY, -INFINITY, -INFINITY};
+      if (v + 4 <= vocab) {
+        y = *reinterpret_cast<const Four*>(row + v);
+      } else {
+#pragma unroll
+        for (int z = 0; z < 3; ++z)
+          if (v + z < vocab) y[z] = row[v + z];
       }
-    } else {
-      first = chunk * THREADS * EACH + (int)threadIdx.x;
-      step = 0;
 #pragma unroll
-      for (int e = 0; e < EACH; ++e) x[e] = first + e * THREADS < vocab ? row[first + e * THREADS] : -INFINITY;
+      for (int z = 0; z < 4; ++z) x[4 * e + z] = y[z];
     }
 #pragma unroll
     for (int e = 0; e < EACH; ++e) x[e] = tame(x[e]);
   }
-  __device__ __forceinline__ int at(int e) const { return step ? first + (e >> 2) * step + (e & 3) : first + e * THREADS; }
+  __device__ __forceinline__ int at(int e) const { return first + (e >> 2) * kStep + (e & 3); }
 };
 
 // rows of a sequence: n + 1 of the target, then n of the draft
@@ -101,7 +104,7 @@ void verify_stats_kernel(Verify p, int chunks, int rows, ChunkStats* stats) {
   const bool drafted = row > p.n;
   const int j = drafted ? row - p.n - 1 : row;
   if (drafted ? j >= count : j > count) return;
-  const Logits<> v(drafted ? p.draft_logits + ((size_t)i * p.n + j) * p.vocab : p.logits + ((size_t)i * (p.n + 1) + j) * p.vocab, chunk, p.vocab, (p.vocab & 3) == 0);
+  const Logits<> v(drafted ? p.draft_logits + ((size_t)i * p.n + j) * p.vocab : p.logits + ((size_t)i * (p.n + 1) + j) * p.vocab, chunk, p.vocab);
   float most = -INFINITY;
   int at = 0x7fffffff;
 #pragma unroll
@@ -294,46 +297,34 @@ void verify_greedy_kernel(Verify p, int chunks, int rows, const ChunkStats* stat
 __global__ __launch_bounds__(kThreads)
 void verify_rest_kernel(Verify p, int chunks, int rows, const ChunkStats* stats, double* rest, Choice* choice) {
   __shared__ ChooseLds lds;
-  __shared__ double s_sum[kSegments][4];
+  __shared__ double s_sum[kSegments];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int i = (int)(blockIdx.x / (unsigned)chunks), chunk = (int)blockIdx.x - i * chunks;
   const Choice c = choose<false>(p, i, chunks, stats + (size_t)i * rows * chunks, &lds);
   if (chunk == 0 && tid == 0) choice[i] = c;
   const Rest r(p, i, c);
-  const bool aligned = (p.vocab & 3) == 0;
   double* left = rest + (size_t)i * chunks * kSegments;
   {
-    const Logits<> lp(r.x, chunk, p.vocab, aligned);
+    const Logits<> lp(r.x, chunk, p.vocab);
     double of[kEach];
     if (r.y) {
-      const Logits<> lq(r.y, chunk, p.vocab, aligned);
+      const Logits<> lq(r.y, chunk, p.vocab);
 #pragma unroll
       for (int e = 0; e < kEach; ++e) of[e] = r.of(lp.at(e), lp.x[e], lq.x[e]);
     } else {
 #pragma unroll
       for (int e = 0; e < kEach; ++e) of[e] = r.of(lp.at(e), lp.x[e], 0.f);
     }
-    // by 16 bytes a segment is a wave's 256 neighbouring tokens at a time, else a word of each thread
-    if (aligned) {
 #pragma unroll
-      for (int e = 0; e < kEach / 4; ++e) {
-        double sum = (of[4 * e] + of[4 * e + 1]) + (of[4 * e + 2] + of[4 * e + 3]);
+    for (int e = 0; e < kEach / 4; ++e) {                  // (a segment is a wave's 256 neighbouring tokens)
+      double sum = (of[4 * e] + of[4 * e + 1]) + (of[4 * e + 2] + of[4 * e + 3]);
 #pragma unroll
-        for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-        if (lane < 4) s_sum[4 * e + wave][lane] = lane == 0 ? sum : 0.;
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < kEach; ++e) {
-        double sum = of[e];
-#pragma unroll
-        for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
-        if (lane == 0) s_sum[e][wave] = sum;
-      }
+      for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
+      if (lane == 0) s_sum[4 * e + wave] = sum;
     }
   }
   __syncthreads();
-  if (tid < kSegments) left[(size_t)chunk * kSegments + tid] = (s_sum[tid][0] + s_sum[tid][1]) + (s_sum[tid][2] + s_sum[tid][3]);
+  if (tid < kSegments) left[(size_t)chunk * kSegments + tid] = s_sum[tid];
 }
 
 // Where there is nothing to draw from: the lowest index of the row's largest logit (all threads together).
@@ -411,14 +402,14 @@ void verify_draw_kernel(Verify p, int chunks, const double* rest, const Choice* 
 }
 
 // Rows that one workgroup's threads hold, EACH logits each of the target's and the draft's: what is left of the row that decides stays in registers, and the
-// token is drawn from them.  Of a step of 1024 threads a wave has a segment, 256 tokens or (unaligned rows) 64; the segments' sums in order give the one that
+// token is drawn from them.  Of a step of 1024 threads a wave has a segment of 256 tokens; the segments' sums in order give the one that
 // holds the goal, and its wave finds the token.  ALONE: the rows' sums as well, a wave a row.
 constexpr int kNear = 1024, kNearEach = 16;        // threads, logits of one at most
 constexpr int kAloneRows = 128;                    // rows of a sequence, at most
-template <bool ALONE, int EACH, bool ALIGNED>
+template <bool ALONE, int EACH>
 __global__ __launch_bounds__(kNear)
 void verify_near_kernel(Verify p, int chunks, int rows, const ChunkStats* stats) {
-  constexpr int kWaves = kNear / 64, V = ALIGNED ? 4 : 1, STEPS = EACH / V, kLine = (STEPS * kWaves + 63) / 64;      // kLine: segments of a lane of the wave that searches
+  constexpr int kWaves = kNear / 64, V = 4, STEPS = EACH / V, kLine = (STEPS * kWaves + 63) / 64;      // kLine: segments of a lane of the wave that searches
   __shared__ ChooseLds lds;
   __shared__ ChunkStats s_rows[ALONE ? kAloneRows : 1];
   __shared__ double s_sum[64 * kLine], s_before, s_total;
@@ -464,10 +455,10 @@ void verify_near_kernel(Verify p, int chunks, int rows, const ChunkStats* stats)
   }
   const Choice c = choose<false, kNear>(p, i, ALONE ? 1 : chunks, mine, &lds);
   const Rest r(p, i, c);
-  const Logits<kNear, EACH> lp(r.x, 0, p.vocab, ALIGNED);
+  const Logits<kNear, EACH> lp(r.x, 0, p.vocab);
   double of[EACH], upto[STEPS];                            // upto: of the wave's tokens of a step, those up to this lane's last
   if (r.y) {
-    const Logits<kNear, EACH> lq(r.y, 0, p.vocab, ALIGNED);
+    const Logits<kNear, EACH> lq(r.y, 0, p.vocab);
 #pragma unroll
     for (int e = 0; e < EACH; ++e) of[e] = r.of(lp.at(e), lp.x[e], lq.x[e]);
   } else {
@@ -557,8 +548,7 @@ void verify_near_kernel(Verify p, int chunks, int rows, const ChunkStats* stats)
 
 template <bool ALONE, int EACH>
 static void launch_near(const Verify& p, int chunks, int rows, const ChunkStats* stats, hipStream_t st) {
-  if ((p.vocab & 3) == 0) hipLaunchKernelGGL((verify_near_kernel<ALONE, EACH, true>), dim3((unsigned)p.b), dim3(kNear), 0, st, p, chunks, rows, stats);
-  else hipLaunchKernelGGL((verify_near_kernel<ALONE, EACH, false>), dim3((unsigned)p.b), dim3(kNear), 0, st, p, chunks, rows, stats);
+  hipLaunchKernelGGL((verify_near_kernel<ALONE, EACH>), dim3((unsigned)p.b), dim3(kNear), 0, st, p, chunks, rows, stats);
 }
 
 int verify_chunks(int vocab) { return (vocab + kChunk - 1) / kChunk; }
