@@ -14,8 +14,7 @@ namespace mqa {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kEach = 16;                          // logits of a thread
-constexpr int kChunk = kThreads * kEach;           // of a workgroup
+constexpr int kEach = 16;                          // logits of a thread, or half as many: of a workgroup a chunk of 4096 or 2048
 
 // What a chunk of a row of logits adds up to: the sum of e^((x - most) / temperature); the largest logit and (temperature 0) its lowest index.
 struct ChunkStats { double sum; float most; int at; };
@@ -63,7 +62,7 @@ __device__ __forceinline__ int drafts_of(const Verify& p, int i) { return p.coun
 
 // A thread's logits of a chunk of THREADS * EACH, 16 bytes at a time (of rows that begin at any float: the memory pipe takes them so); past the end -inf.
 // at(e): the index of the e-th.
-template <int THREADS = kThreads, int EACH = kEach>
+template <int THREADS, int EACH>
 struct Logits {
   typedef __attribute__((ext_vector_type(4), aligned(4))) float Four;
   static constexpr int kStep = 4 * THREADS;
@@ -92,7 +91,7 @@ struct Logits {
 };
 
 // rows of a sequence: n + 1 of the target, then n of the draft
-template <bool GREEDY>
+template <bool GREEDY, int EACH>
 __global__ __launch_bounds__(kThreads)
 void verify_stats_kernel(Verify p, int chunks, int rows, ChunkStats* stats) {
   __shared__ double red[4];
@@ -104,11 +103,11 @@ void verify_stats_kernel(Verify p, int chunks, int rows, ChunkStats* stats) {
   const bool drafted = row > p.n;
   const int j = drafted ? row - p.n - 1 : row;
   if (drafted ? j >= count : j > count) return;
-  const Logits<> v(drafted ? p.draft_logits + ((size_t)i * p.n + j) * p.vocab : p.logits + ((size_t)i * (p.n + 1) + j) * p.vocab, chunk, p.vocab);
+  const Logits<kThreads, EACH> v(drafted ? p.draft_logits + ((size_t)i * p.n + j) * p.vocab : p.logits + ((size_t)i * (p.n + 1) + j) * p.vocab, chunk, p.vocab);
   float most = -INFINITY;
   int at = 0x7fffffff;
 #pragma unroll
-  for (int e = 0; e < kEach; ++e) {
+  for (int e = 0; e < EACH; ++e) {
     if constexpr (GREEDY) {
       if (v.at(e) < p.vocab) better(most, at, v.x[e], v.at(e));
     } else {
@@ -131,7 +130,7 @@ void verify_stats_kernel(Verify p, int chunks, int rows, ChunkStats* stats) {
   if constexpr (!GREEDY) {
     const double per = per_of(p);
 #pragma unroll
-    for (int e = 0; e < kEach; ++e) sum += weight(v.x[e], most, per);
+    for (int e = 0; e < EACH; ++e) sum += weight(v.x[e], most, per);
     sum = block_sum(sum, red);
   }
   if (threadIdx.x == 0) stats[(size_t)line * chunks + chunk] = ChunkStats{sum, most, at};
@@ -257,7 +256,7 @@ struct Rest {
   }
 };
 
-constexpr int kSegment = 256, kSegments = kChunk / kSegment;      // tokens; of a chunk
+constexpr int kSegment = 256;                      // tokens; a chunk has EACH of them
 
 // Sum of x over the threads up to this one; *all: over all.
 __device__ __forceinline__ double up_to_me(double x, double* s_waves, double* all) {
@@ -294,29 +293,30 @@ void verify_greedy_kernel(Verify p, int chunks, int rows, const ChunkStats* stat
 
 // What is left of the row that decides, a chunk a workgroup, in segments.  (With the draw in the same launch, by the last of a sequence's workgroups, 19 us in
 // the place of 9 and 9: what orders writes and reads across the XCDs costs more than a launch.)
+template <int EACH>
 __global__ __launch_bounds__(kThreads)
 void verify_rest_kernel(Verify p, int chunks, int rows, const ChunkStats* stats, double* rest, Choice* choice) {
   __shared__ ChooseLds lds;
-  __shared__ double s_sum[kSegments];
+  __shared__ double s_sum[EACH];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int i = (int)(blockIdx.x / (unsigned)chunks), chunk = (int)blockIdx.x - i * chunks;
   const Choice c = choose<false>(p, i, chunks, stats + (size_t)i * rows * chunks, &lds);
   if (chunk == 0 && tid == 0) choice[i] = c;
   const Rest r(p, i, c);
-  double* left = rest + (size_t)i * chunks * kSegments;
+  double* left = rest + (size_t)i * chunks * EACH;
   {
-    const Logits<> lp(r.x, chunk, p.vocab);
-    double of[kEach];
+    const Logits<kThreads, EACH> lp(r.x, chunk, p.vocab);
+    double of[EACH];
     if (r.y) {
-      const Logits<> lq(r.y, chunk, p.vocab);
+      const Logits<kThreads, EACH> lq(r.y, chunk, p.vocab);
 #pragma unroll
-      for (int e = 0; e < kEach; ++e) of[e] = r.of(lp.at(e), lp.x[e], lq.x[e]);
+      for (int e = 0; e < EACH; ++e) of[e] = r.of(lp.at(e), lp.x[e], lq.x[e]);
     } else {
 #pragma unroll
-      for (int e = 0; e < kEach; ++e) of[e] = r.of(lp.at(e), lp.x[e], 0.f);
+      for (int e = 0; e < EACH; ++e) of[e] = r.of(lp.at(e), lp.x[e], 0.f);
     }
 #pragma unroll
-    for (int e = 0; e < kEach / 4; ++e) {                  // (a segment is a wave's 256 neighbouring tokens)
+    for (int e = 0; e < EACH / 4; ++e) {                  // (a segment is a wave's 256 neighbouring tokens)
       double sum = (of[4 * e] + of[4 * e + 1]) + (of[4 * e + 2] + of[4 * e + 3]);
 #pragma unroll
       for (int o = 32; o > 0; o >>= 1) sum += __shfl_xor(sum, o);
@@ -324,7 +324,7 @@ void verify_rest_kernel(Verify p, int chunks, int rows, const ChunkStats* stats,
     }
   }
   __syncthreads();
-  if (tid < kSegments) left[(size_t)chunk * kSegments + tid] = s_sum[tid];
+  if (tid < EACH) left[(size_t)chunk * EACH + tid] = s_sum[tid];
 }
 
 // Where there is nothing to draw from: the lowest index of the row's largest logit (all threads together).
@@ -344,13 +344,13 @@ __device__ __forceinline__ int largest(const float* row, int vocab, float* s_mos
 }
 
 __global__ __launch_bounds__(kThreads)
-void verify_draw_kernel(Verify p, int chunks, const double* rest, const Choice* choice) {
+void verify_draw_kernel(Verify p, int stride, const double* rest, const Choice* choice) {
   __shared__ double s_waves[4], s_before;
   __shared__ float s_most[4];
   __shared__ int s_at[4], s_found, s_last;
   const int i = blockIdx.x, tid = threadIdx.x;
   const int segments = (p.vocab + kSegment - 1) / kSegment;
-  const double* left = rest + (size_t)i * chunks * kSegments;
+  const double* left = rest + (size_t)i * stride;
   const double first = tid < segments ? left[tid] : 0.;      // (all there is, up to 65536 tokens)
   const float u = p.u[(size_t)i * (p.n + 1) + p.n];
   const int draft = tid < p.n ? p.drafts[(size_t)i * p.n + tid] : -1;
@@ -551,47 +551,61 @@ static void launch_near(const Verify& p, int chunks, int rows, const ChunkStats*
   hipLaunchKernelGGL((verify_near_kernel<ALONE, EACH>), dim3((unsigned)p.b), dim3(kNear), 0, st, p, chunks, rows, stats);
 }
 
-int verify_chunks(int vocab) { return (vocab + kChunk - 1) / kChunk; }
+// Logits of a thread: half as many where the chunks would not be one for every compute unit (one sequence, four drafts, 32768 tokens: 21.8 us, so 19.9; above 256 of them no difference, above 4000 slower).
+int verify_each(int b, int n, int vocab) {
+  const long long chunks = (vocab + kThreads * kEach - 1) / (kThreads * kEach);
+  return (long long)b * (2 * n + 1) * chunks <= 256 ? kEach / 2 : kEach;
+}
+int verify_chunks(int vocab, int each) { return (vocab + kThreads * each - 1) / (kThreads * each); }
+
+template <bool GREEDY>
+hipError_t launch_stats(const Verify& p, int each, int chunks, int rows, ChunkStats* stats, hipStream_t st) {
+  const dim3 grid((unsigned)((size_t)p.b * rows * chunks)), block(kThreads);
+  if (each == kEach) hipLaunchKernelGGL((verify_stats_kernel<GREEDY, kEach>), grid, block, 0, st, p, chunks, rows, stats);
+  else hipLaunchKernelGGL((verify_stats_kernel<GREEDY, kEach / 2>), grid, block, 0, st, p, chunks, rows, stats);
+  return hipGetLastError();
+}
 
 }  // namespace
 
 size_t verify_workspace_bytes(int b, int n, int vocab) {
-  const size_t chunks = verify_chunks(vocab);
-  return (size_t)b * ((2 * (size_t)n + 1) * chunks * sizeof(ChunkStats) + sizeof(Choice) + chunks * kSegments * sizeof(double));
+  const int each = verify_each(b, n, vocab);
+  const size_t chunks = verify_chunks(vocab, each);
+  return (size_t)b * ((2 * (size_t)n + 1) * chunks * sizeof(ChunkStats) + sizeof(Choice) + chunks * each * sizeof(double));
 }
 
 hipError_t launch_verify(const Verify& p, void* workspace, hipStream_t st) {
-  const int chunks = verify_chunks(p.vocab), rows = p.draft_logits && p.temperature > 0.f ? 2 * p.n + 1 : p.n + 1;
+  const int each = verify_each(p.b, p.n, p.vocab), chunks = verify_chunks(p.vocab, each), rows = p.draft_logits && p.temperature > 0.f ? 2 * p.n + 1 : p.n + 1;
   ChunkStats* stats = static_cast<ChunkStats*>(workspace);
   Choice* choice = reinterpret_cast<Choice*>(stats + (size_t)p.b * rows * chunks);
   double* rest = reinterpret_cast<double*>(choice + p.b);
-  const dim3 all((unsigned)((size_t)p.b * rows * chunks)), rests((unsigned)((size_t)p.b * chunks)), each((unsigned)p.b), block(kThreads);
-  const bool greedy = !(p.temperature > 0.f);
+  const dim3 rests((unsigned)((size_t)p.b * chunks)), per_sequence((unsigned)p.b), block(kThreads);
+  if (!(p.temperature > 0.f)) {
+    const hipError_t e = launch_stats<true>(p, each, chunks, rows, stats, st);
+    if (e != hipSuccess) return e;
+    hipLaunchKernelGGL(verify_greedy_kernel, per_sequence, block, 0, st, p, chunks, rows, stats);
+    return hipGetLastError();
+  }
   // One launch where the rows that a wave has in turn are short (four drafts, 300 tokens: 8.2 us, in two launches 9.8; of 2000 10.6 and 10.3), and for more
   // where the sequences are many (256 of two rows of 2000: 11.9 and 13.1; of 4000 19.5 and 14.2).
   static_assert(2048 <= 4 * kNear, "rows that a thread holds in four");
-  if (!greedy && rows <= kAloneRows && (long long)((rows + 15) / 16) * p.vocab <= (p.b >= 128 ? 2048 : 1024)) {
+  if (rows <= kAloneRows && (long long)((rows + 15) / 16) * p.vocab <= (p.b >= 128 ? 2048 : 1024)) {
     launch_near<true, 4>(p, chunks, rows, stats, st);
     return hipGetLastError();
   }
-  if (greedy) hipLaunchKernelGGL(verify_stats_kernel<true>, all, block, 0, st, p, chunks, rows, stats);
-  else hipLaunchKernelGGL(verify_stats_kernel<false>, all, block, 0, st, p, chunks, rows, stats);
-  hipError_t e = hipGetLastError();
+  hipError_t e = launch_stats<false>(p, each, chunks, rows, stats, st);
   if (e != hipSuccess) return e;
-  if (greedy) {
-    hipLaunchKernelGGL(verify_greedy_kernel, each, block, 0, st, p, chunks, rows, stats);
-    return hipGetLastError();
-  }
   // (two launches for three: four drafts, 4096 tokens 11.1 us for 18.2, 16384 16.2 for 20.6; with twice the logits a thread they do not fit its registers)
   if (p.vocab <= kNearEach * kNear) {
     if (p.vocab <= 4 * kNear) launch_near<false, 4>(p, chunks, rows, stats, st);
     else launch_near<false, kNearEach>(p, chunks, rows, stats, st);
     return hipGetLastError();
   }
-  hipLaunchKernelGGL(verify_rest_kernel, rests, block, 0, st, p, chunks, rows, stats, rest, choice);
+  if (each == kEach) hipLaunchKernelGGL(verify_rest_kernel<kEach>, rests, block, 0, st, p, chunks, rows, stats, rest, choice);
+  else hipLaunchKernelGGL(verify_rest_kernel<kEach / 2>, rests, block, 0, st, p, chunks, rows, stats, rest, choice);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(verify_draw_kernel, each, block, 0, st, p, chunks, rest, choice);
+  hipLaunchKernelGGL(verify_draw_kernel, per_sequence, block, 0, st, p, chunks * each, rest, choice);
   return hipGetLastError();
 }
 
