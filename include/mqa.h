@@ -331,7 +331,8 @@ int mqa_beam_reorder_kv(const void* K_src, const void* V_src, const int32_t* len
  * h_kv = h: multi-head; anything that divides h between them), of float32 or bfloat16.  table [b,max_pages] (int32) names the pages of a sequence in order:
  * position p is row p % page_size of page table[i, p / page_size]; a sequence holds up to max_pages * page_size positions.  An entry outside [0,num_pages)
  * names a page that holds nothing: rows for it are dropped, and its positions count for nothing in the attention and in an eviction.  Only the entries of
- * positions below a sequence's length (behind an append: its new length) are looked at.  Sequences may share pages (a common prompt); a page that a call writes to
+ * positions below a sequence's length (behind an append: its new length) are looked at; a length below 0 counts as 0, one beyond the capacity as the capacity
+ * (an append leaves both as they are).  Sequences may share pages (a common prompt); a page that a call writes to
  * must not be one that it reads or writes for another sequence.  Limits: k, v multiples of 8 up to 256; max_pages * page_size <= 2^24,
  * b * h_kv * max(256, max_pages * page_size) <= 2^31, num_pages * h_kv * page_size < 2^31.
  *
@@ -355,6 +356,7 @@ int mqa_paged_append_kv_rows(const float* k_new, const float* v_new, const int32
  * Positions at and behind the length are left as they were.
  *
  * The workspace: mqa_paged_decode_workspace_bytes(...) bytes (16-byte aligned; 0 = none, or unsupported sizes), written and read by this call's launches only.
+ * With scores it holds the logits: 4 * b * n * h * max_pages * page_size bytes of it.
  */
 size_t mqa_paged_decode_workspace_bytes(int b, int n, int h, int h_kv, int page_size, int max_pages, int k, int v, mqa_dtype dt, int with_scores);
 int mqa_paged_decode_step(const float* q, const void* K_pages, const void* V_pages, const int32_t* table, const int32_t* lens, float* o,

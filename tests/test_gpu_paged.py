@@ -505,6 +505,32 @@ def test_pools_of_more_than_4_gib(m, dtype, width):
     assert results[0][1].abs().max() > 0 and results[0][3].tolist() == [500, 500]
 
 
+@pytest.mark.parametrize("heads", [None, 2])
+def test_append_and_evict_on_a_stream(m, heads):
+    """On a stream given, and on the current one: one head's pools with and without its axis, too."""
+    g = torch.Generator(device=DEV).manual_seed(11)
+    b, each, page, k = 3, 6, 16, 64
+    lead, per = (2 * b * each, page) if heads is None else (2 * b * each, heads, page), (b,) if heads is None else (b, heads)
+    table, out = (torch.randperm(b * each, generator=g, device=DEV).to(torch.int32).view(b, each) + x for x in (0, b * each))
+    new, scores = torch.randn((b, 70, *per[1:], k), generator=g, device=DEV), torch.rand((*per, each * page), generator=g, device=DEV)
+    results = []
+    for stream in (None, torch.cuda.Stream()):
+        K, V = (torch.zeros((*lead, k), device=DEV) for _ in range(2))
+        lens, after, left = (torch.zeros(b, dtype=torch.int32, device=DEV) for _ in range(3))
+        kept, rest = torch.zeros((*per, 40), dtype=torch.int32, device=DEV), torch.zeros_like(scores)
+        torch.cuda.synchronize()
+        m.mqa_paged_append_kv_rows(K, V, table, new, new, lens, after, stream=stream)
+        m.mqa_paged_evict_kv(K, V, table, after, scores, out, left, rest, kept, 7, stream=stream)
+        torch.cuda.synchronize()
+        results.append((K, V, after, left, kept, rest))
+    assert all(torch.equal(x, y) for x, y in zip(*results)) and results[0][3].tolist() == [40] * b
+    if heads is None:
+        K, V = (torch.zeros((lead[0], 1, page, k), device=DEV) for _ in range(2))
+        m.mqa_paged_append_kv_rows(K, V, table, new[:, :, None].contiguous(), new[:, :, None].contiguous(), lens, after)
+        m.mqa_paged_evict_kv(K, V, table, after, scores[:, None].contiguous(), out, left, torch.zeros_like(scores)[:, None].contiguous(), kept[:, None].contiguous(), 7)
+        assert torch.equal(K[:, 0], results[0][0]) and torch.equal(V[:, 0], results[0][1])
+
+
 def test_a_given_workspace(m):
     g = torch.Generator(device=DEV).manual_seed(3)
     K = torch.randn((256, 16, 128), generator=g, device=DEV).bfloat16()
