@@ -258,23 +258,6 @@ struct Rest {
 
 constexpr int kSegment = 256;                      // tokens; a chunk has EACH of them
 
-// Sum of x over the threads up to this one; *all: over all.
-__device__ __forceinline__ double up_to_me(double x, double* s_waves, double* all) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) {
-    const double y = __shfl_up(x, off);
-    if (lane >= off) x += y;
-  }
-  __syncthreads();
-  if (lane == 63) s_waves[wave] = x;
-  __syncthreads();
-  double before = 0.;
-  for (int w = 0; w < wave; ++w) before += s_waves[w];
-  *all = (s_waves[0] + s_waves[1]) + (s_waves[2] + s_waves[3]);
-  return x + before;
-}
-
 // draft: the thread's own, of the first THREADS
 template <int THREADS = kThreads>
 __device__ __forceinline__ void write_tokens(const Verify& p, int i, int accepted, int token, int draft) {
@@ -343,62 +326,114 @@ __device__ __forceinline__ int largest(const float* row, int vocab, float* s_mos
   return most > -INFINITY ? at : 0;
 }
 
-__global__ __launch_bounds__(kThreads)
+// A wave a sequence, so that nothing waits at a barrier (four waves, the places by atomics in LDS 9.4 us, so 3): the segments, eight neighbouring ones a lane, then the tokens
+// of the one that holds the goal, four a lane.
+constexpr int kLine = 8, kRound = 64 * kLine;      // segments of a lane; gone over at a time, 131072 tokens
+__global__ __launch_bounds__(64)
 void verify_draw_kernel(Verify p, int stride, const double* rest, const Choice* choice) {
-  __shared__ double s_waves[4], s_before;
-  __shared__ float s_most[4];
-  __shared__ int s_at[4], s_found, s_last;
-  const int i = blockIdx.x, tid = threadIdx.x;
+  __shared__ float s_most[1];
+  __shared__ int s_at[1];
+  const int i = blockIdx.x, lane = threadIdx.x;
   const int segments = (p.vocab + kSegment - 1) / kSegment;
   const double* left = rest + (size_t)i * stride;
-  const double first = tid < segments ? left[tid] : 0.;      // (all there is, up to 65536 tokens)
+  double add[kLine], run;                                  // of a round: the lane's segments; those of the lanes up to this one
+  auto load = [&](int x0) {
+#pragma unroll
+    for (int y = 0; y < kLine; ++y) {
+      const int at = x0 + lane * kLine + y;
+      const double x = left[min(at, segments - 1)];
+      add[y] = at < segments ? x : 0.;
+    }
+  };
+  auto scan = [&]() {
+    run = 0.;
+#pragma unroll
+    for (int y = 0; y < kLine; ++y) run += add[y];
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const double y = __shfl_up(run, o);
+      if (lane >= o) run += y;
+    }
+  };
+  load((segments - 1) / kRound * kRound);
   const float u = p.u[(size_t)i * (p.n + 1) + p.n];
-  const int draft = tid < p.n ? p.drafts[(size_t)i * p.n + tid] : -1;
+  const int draft = lane < p.n ? p.drafts[(size_t)i * p.n + lane] : -1;
   const Choice c = choice[i];
   const Rest r(p, i, c);
-  if (tid == 0) { s_found = 0x7fffffff; s_last = -1; }
-  double sum = first, total;
-  for (int x = tid + kThreads; x < segments; x += kThreads) sum += left[x];
-  const double upto = up_to_me(sum, s_waves, &total);
+  scan();
+  double total = __shfl(run, 63);
+  for (int x0 = ((segments - 1) / kRound - 1) * kRound; x0 >= 0; x0 -= kRound) {
+    load(x0);
+    scan();
+    total += __shfl(run, 63);
+  }
   int token;
   if (total > 0.) {
     const double goal = (double)u * total;
     // the segment in which the running sum exceeds the goal; past all of them (u is not below 1): the last that has anything
     double before = 0.;
-    for (int x0 = 0; x0 < segments; x0 += kThreads) {
-      const bool only = segments <= kThreads;
-      const double add = only ? first : x0 + tid < segments ? left[x0 + tid] : 0.;
-      double all = total, run = upto;
-      if (!only) run = before + up_to_me(add, s_waves, &all);
-      if (add > 0.) {
-        if (run > goal) atomicMin(&s_found, x0 + tid);
-        atomicMax(&s_last, x0 + tid);
+    int segment = 0;
+    bool inside = false;
+    for (int x0 = 0;;) {
+      double to = __shfl_up(run, 1), found_before = 0.;
+      to = before + (lane == 0 ? 0. : to);
+      int found = -1, last = -1;
+#pragma unroll
+      for (int y = 0; y < kLine; ++y) {
+        if (add[y] > 0.) {
+          last = x0 + lane * kLine + y;
+          if (found < 0 && to + add[y] > goal) { found = last; found_before = to; }
+        }
+        to += add[y];
       }
-      __syncthreads();
-      if (s_found == x0 + tid) s_before = run - add;
-      before += all;
-      if (s_found != 0x7fffffff) break;                    // (the same in all threads: written before the barrier)
+      const unsigned long long those = __ballot(found >= 0), any = __ballot(last >= 0);
+      if (those != 0) {
+        const int at = __ffsll(those) - 1;
+        segment = __shfl(found, at);
+        before = __shfl(found_before, at);
+        inside = true;
+        break;
+      }
+      if (any != 0) segment = __shfl(last, 63 - __clzll(any));
+      before += __shfl(run, 63);
+      x0 += kRound;
+      if (x0 >= segments) break;
+      load(x0);
+      scan();
     }
-    __syncthreads();
-    const bool inside = s_found != 0x7fffffff;
-    const int v = (inside ? s_found : s_last) * kSegment + tid;
-    before = inside ? s_before : 0.;
-    double mine = 0.;
-    if (v < p.vocab) mine = r.of(v, tame(r.x[v]), r.y ? tame(r.y[v]) : 0.f);
-    __syncthreads();
-    if (tid == 0) { s_found = 0x7fffffff; s_last = -1; }
-    double all;
-    const double run = before + up_to_me(mine, s_waves, &all);
-    if (mine > 0.) {
-      if (inside && run > goal) atomicMin(&s_found, v);
-      atomicMax(&s_last, v);
+    const Logits<64, 4> lp(r.x, segment, p.vocab);       // (a chunk of 64 threads, four logits each)
+    double of[4];
+    if (r.y) {
+      const Logits<64, 4> lq(r.y, segment, p.vocab);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) of[e] = r.of(lp.at(e), lp.x[e], lq.x[e]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) of[e] = r.of(lp.at(e), lp.x[e], 0.f);
     }
-    __syncthreads();
-    token = s_found != 0x7fffffff ? s_found : s_last;
+    double up = (of[0] + of[1]) + (of[2] + of[3]);
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const double y = __shfl_up(up, o);
+      if (lane >= o) up += y;
+    }
+    double to = __shfl_up(up, 1);
+    to = before + (lane == 0 ? 0. : to);
+    int found = -1, last = -1;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      to += of[e];
+      if (of[e] > 0.) {
+        last = lp.at(e);
+        if (found < 0 && to > goal) found = last;
+      }
+    }
+    const unsigned long long those = __ballot(inside && found >= 0), any = __ballot(last >= 0);
+    token = those != 0 ? __shfl(found, __ffsll(those) - 1) : __shfl(last, any != 0 ? 63 - __clzll(any) : 0);
   } else {                                                 // nothing to draw from: the largest logit
-    token = largest<kThreads>(r.x, p.vocab, s_most, s_at);
+    token = largest<64>(r.x, p.vocab, s_most, s_at);
   }
-  write_tokens(p, i, c.accepted, token, draft);
+  write_tokens<64>(p, i, c.accepted, token, draft);
 }
 
 // Rows that one workgroup's threads hold, EACH logits each of the target's and the draft's: what is left of the row that decides stays in registers, and the
@@ -409,10 +444,10 @@ constexpr int kAloneRows = 128;                    // rows of a sequence, at mos
 template <bool ALONE, int EACH>
 __global__ __launch_bounds__(kNear)
 void verify_near_kernel(Verify p, int chunks, int rows, const ChunkStats* stats) {
-  constexpr int kWaves = kNear / 64, V = 4, STEPS = EACH / V, kLine = (STEPS * kWaves + 63) / 64;      // kLine: segments of a lane of the wave that searches
+  constexpr int kWaves = kNear / 64, V = 4, STEPS = EACH / V, kOfLane = (STEPS * kWaves + 63) / 64;      // kOfLane: segments of a lane of the wave that searches
   __shared__ ChooseLds lds;
   __shared__ ChunkStats s_rows[ALONE ? kAloneRows : 1];
-  __shared__ double s_sum[64 * kLine], s_before, s_total;
+  __shared__ double s_sum[64 * kOfLane], s_before, s_total;
   __shared__ float s_most[kWaves];
   __shared__ int s_at[kWaves], s_found, s_last, s_token;
   const int i = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -481,10 +516,10 @@ void verify_near_kernel(Verify p, int chunks, int rows, const ChunkStats* stats)
   if (tid == 0) { s_found = 0x7fffffff; s_last = -1; }
   __syncthreads();
   if (wave == 0) {                                         // the segment in which the running sum exceeds the goal, else the last that has anything
-    double add[kLine], mine_all = 0.;
+    double add[kOfLane], mine_all = 0.;
 #pragma unroll
-    for (int x = 0; x < kLine; ++x) {
-      const int at = lane * kLine + x;
+    for (int x = 0; x < kOfLane; ++x) {
+      const int at = lane * kOfLane + x;
       add[x] = at < STEPS * kWaves ? s_sum[at] : 0.;
       mine_all += add[x];
     }
@@ -500,10 +535,10 @@ void verify_near_kernel(Verify p, int chunks, int rows, const ChunkStats* stats)
     int found = 0x7fffffff, last = -1;
     double before = 0.;
 #pragma unroll
-    for (int x = 0; x < kLine; ++x) {
+    for (int x = 0; x < kOfLane; ++x) {
       if (add[x] > 0.) {
-        if (found == 0x7fffffff && run + add[x] > goal) { found = lane * kLine + x; before = run; }
-        last = lane * kLine + x;
+        if (found == 0x7fffffff && run + add[x] > goal) { found = lane * kOfLane + x; before = run; }
+        last = lane * kOfLane + x;
       }
       run += add[x];
     }
@@ -605,7 +640,7 @@ hipError_t launch_verify(const Verify& p, void* workspace, hipStream_t st) {
   else hipLaunchKernelGGL(verify_rest_kernel<kEach / 2>, rests, block, 0, st, p, chunks, rows, stats, rest, choice);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL(verify_draw_kernel, per_sequence, block, 0, st, p, chunks * each, rest, choice);
+  hipLaunchKernelGGL(verify_draw_kernel, per_sequence, dim3(64), 0, st, p, chunks * each, rest, choice);
   return hipGetLastError();
 }
 
