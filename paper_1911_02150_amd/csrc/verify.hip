@@ -326,6 +326,46 @@ __device__ __forceinline__ int largest(const float* row, int vocab, float* s_mos
   return most > -INFINITY ? at : 0;
 }
 
+// What is left of a wave's 256 tokens, four a lane.
+struct Four {
+  double of[4], upto;      // upto: of the tokens up to this lane's last
+  int first;
+  template <typename L, typename Q>
+  __device__ __forceinline__ Four(const Verify& p, const Rest& r, const L& lp, Q&& drafted) {
+    first = lp.first;
+    if (r.y) {
+      const L lq = drafted();
+#pragma unroll
+      for (int e = 0; e < 4; ++e) of[e] = r.of(lp.at(e), lp.x[e], lq.x[e]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) of[e] = r.of(lp.at(e), lp.x[e], 0.f);
+    }
+    upto = (of[0] + of[1]) + (of[2] + of[3]);
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const double y = __shfl_up(upto, o);
+      if ((int)(threadIdx.x & 63) >= o) upto += y;
+    }
+  }
+  // The first token at which the running sum, `before` in front of the wave's, exceeds the goal, else the last that has anything (there is one).
+  __device__ __forceinline__ int token(double before, double goal) const {
+    double to = __shfl_up(upto, 1);
+    to = before + ((threadIdx.x & 63) == 0 ? 0. : to);
+    int found = -1, last = -1;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      to += of[e];
+      if (of[e] > 0.) {
+        last = first + e;
+        if (found < 0 && to > goal) found = last;
+      }
+    }
+    const unsigned long long those = __ballot(found >= 0), any = __ballot(last >= 0);
+    return those != 0 ? __shfl(found, __ffsll(those) - 1) : __shfl(last, any != 0 ? 63 - __clzll(any) : 0);
+  }
+};
+
 // A wave a sequence, so that nothing waits at a barrier (four waves, the places by atomics in LDS 9.4 us, so 3): the segments, eight neighbouring ones a lane, then the tokens
 // of the one that holds the goal, four a lane.
 constexpr int kLine = 8, kRound = 64 * kLine;      // segments of a lane; gone over at a time, 131072 tokens
@@ -335,13 +375,13 @@ void verify_draw_kernel(Verify p, int stride, const double* rest, const Choice* 
   __shared__ int s_at[1];
   const int i = blockIdx.x, lane = threadIdx.x;
   const int segments = (p.vocab + kSegment - 1) / kSegment;
-  const double* left = rest + (size_t)i * stride;
+  const double* sums = rest + (size_t)i * stride;
   double add[kLine], run;                                  // of a round: the lane's segments; those of the lanes up to this one
   auto load = [&](int x0) {
 #pragma unroll
     for (int y = 0; y < kLine; ++y) {
       const int at = x0 + lane * kLine + y;
-      const double x = left[min(at, segments - 1)];
+      const double x = sums[min(at, segments - 1)];
       add[y] = at < segments ? x : 0.;
     }
   };
@@ -401,55 +441,27 @@ void verify_draw_kernel(Verify p, int stride, const double* rest, const Choice* 
       load(x0);
       scan();
     }
-    const Logits<64, 4> lp(r.x, segment, p.vocab);       // (a chunk of 64 threads, four logits each)
-    double of[4];
-    if (r.y) {
-      const Logits<64, 4> lq(r.y, segment, p.vocab);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) of[e] = r.of(lp.at(e), lp.x[e], lq.x[e]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) of[e] = r.of(lp.at(e), lp.x[e], 0.f);
-    }
-    double up = (of[0] + of[1]) + (of[2] + of[3]);
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const double y = __shfl_up(up, o);
-      if (lane >= o) up += y;
-    }
-    double to = __shfl_up(up, 1);
-    to = before + (lane == 0 ? 0. : to);
-    int found = -1, last = -1;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      to += of[e];
-      if (of[e] > 0.) {
-        last = lp.at(e);
-        if (found < 0 && to > goal) found = last;
-      }
-    }
-    const unsigned long long those = __ballot(inside && found >= 0), any = __ballot(last >= 0);
-    token = those != 0 ? __shfl(found, __ffsll(those) - 1) : __shfl(last, any != 0 ? 63 - __clzll(any) : 0);
+    const Four left(p, r, Logits<64, 4>(r.x, segment, p.vocab), [&]() { return Logits<64, 4>(r.y, segment, p.vocab); });      // (a chunk of 64 threads: a segment)
+    token = left.token(before, inside ? goal : INFINITY);
   } else {                                                 // nothing to draw from: the largest logit
     token = largest<64>(r.x, p.vocab, s_most, s_at);
   }
   write_tokens<64>(p, i, c.accepted, token, draft);
 }
 
-// Rows that one workgroup's threads hold, EACH logits each of the target's and the draft's: what is left of the row that decides stays in registers, and the
-// token is drawn from them.  Of a step of 1024 threads a wave has a segment of 256 tokens; the segments' sums in order give the one that
-// holds the goal, and its wave finds the token.  ALONE: the rows' sums as well, a wave a row.
-constexpr int kNear = 1024, kNearEach = 16;        // threads, logits of one at most
+// Rows that one workgroup's threads hold, four logits each of the target's and the draft's: what is left of the row that decides stays in registers, and the
+// token is drawn from them: the waves' sums in order give the one that holds the goal, and it finds the token.  ALONE: the rows' sums as well, a wave a row.
+constexpr int kNear = 1024, kNearEach = 4;         // threads, logits of one
 constexpr int kAloneRows = 128;                    // rows of a sequence, at most
-template <bool ALONE, int EACH>
+template <bool ALONE>
 __global__ __launch_bounds__(kNear)
 void verify_near_kernel(Verify p, int chunks, int rows, const ChunkStats* stats) {
-  constexpr int kWaves = kNear / 64, V = 4, STEPS = EACH / V, kOfLane = (STEPS * kWaves + 63) / 64;      // kOfLane: segments of a lane of the wave that searches
+  constexpr int kWaves = kNear / 64;
   __shared__ ChooseLds lds;
   __shared__ ChunkStats s_rows[ALONE ? kAloneRows : 1];
-  __shared__ double s_sum[64 * kOfLane], s_before, s_total;
+  __shared__ double s_sum[kWaves];
   __shared__ float s_most[kWaves];
-  __shared__ int s_at[kWaves], s_found, s_last, s_token;
+  __shared__ int s_at[kWaves], s_token;
   const int i = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int draft = tid < p.n ? p.drafts[(size_t)i * p.n + tid] : -1;
   const float u = p.u[(size_t)i * (p.n + 1) + p.n];
@@ -490,88 +502,28 @@ void verify_near_kernel(Verify p, int chunks, int rows, const ChunkStats* stats)
   }
   const Choice c = choose<false, kNear>(p, i, ALONE ? 1 : chunks, mine, &lds);
   const Rest r(p, i, c);
-  const Logits<kNear, EACH> lp(r.x, 0, p.vocab);
-  double of[EACH], upto[STEPS];                            // upto: of the wave's tokens of a step, those up to this lane's last
-  if (r.y) {
-    const Logits<kNear, EACH> lq(r.y, 0, p.vocab);
-#pragma unroll
-    for (int e = 0; e < EACH; ++e) of[e] = r.of(lp.at(e), lp.x[e], lq.x[e]);
-  } else {
-#pragma unroll
-    for (int e = 0; e < EACH; ++e) of[e] = r.of(lp.at(e), lp.x[e], 0.f);
-  }
-#pragma unroll
-  for (int q = 0; q < STEPS; ++q) {
-    double x = of[V * q];
-#pragma unroll
-    for (int y = 1; y < V; ++y) x += of[V * q + y];
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const double y = __shfl_up(x, o);
-      if (lane >= o) x += y;
-    }
-    upto[q] = x;
-    if (lane == 63) s_sum[q * kWaves + wave] = x;
-  }
-  if (tid == 0) { s_found = 0x7fffffff; s_last = -1; }
+  const Four left(p, r, Logits<kNear, kNearEach>(r.x, 0, p.vocab), [&]() { return Logits<kNear, kNearEach>(r.y, 0, p.vocab); });
+  if (lane == 63) s_sum[wave] = left.upto;
   __syncthreads();
-  if (wave == 0) {                                         // the segment in which the running sum exceeds the goal, else the last that has anything
-    double add[kOfLane], mine_all = 0.;
+  const double mine_all = lane < kWaves ? s_sum[lane] : 0.;      // lane w: wave w's
+  double run = mine_all;
 #pragma unroll
-    for (int x = 0; x < kOfLane; ++x) {
-      const int at = lane * kOfLane + x;
-      add[x] = at < STEPS * kWaves ? s_sum[at] : 0.;
-      mine_all += add[x];
-    }
-    double run = mine_all;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-      const double y = __shfl_up(run, o);
-      if (lane >= o) run += y;
-    }
-    const double total = __shfl(run, 63), goal = (double)u * total;
-    run = __shfl_up(run, 1);
-    if (lane == 0) run = 0.;
-    int found = 0x7fffffff, last = -1;
-    double before = 0.;
-#pragma unroll
-    for (int x = 0; x < kOfLane; ++x) {
-      if (add[x] > 0.) {
-        if (found == 0x7fffffff && run + add[x] > goal) { found = lane * kOfLane + x; before = run; }
-        last = lane * kOfLane + x;
-      }
-      run += add[x];
-    }
-    const unsigned long long those = __ballot(found != 0x7fffffff), any = __ballot(last >= 0);
-    if (those != 0 && lane == __ffsll(those) - 1) { s_found = found; s_before = before; }
-    if (any != 0 && lane == 63 - __clzll(any)) s_last = last;
-    if (lane == 0) s_total = total;
+  for (int o = 1; o < kWaves; o <<= 1) {
+    const double y = __shfl_up(run, o);
+    if (lane >= o) run += y;
   }
-  __syncthreads();
+  const double total = __shfl(run, kWaves - 1);
   int token;
-  if (s_total > 0.) {
-    const bool inside = s_found != 0x7fffffff;
-    const int segment = inside ? s_found : s_last;
-    if (segment % kWaves == wave) {                        // its first token that exceeds the goal, else the last that has anything
-      const double goal = inside ? (double)u * s_total : INFINITY;
-      int found = 0x7fffffff, last = -1;
-#pragma unroll
-      for (int q = 0; q < STEPS; ++q) {
-        if (q != segment / kWaves) continue;
-        double run = __shfl_up(upto[q], 1);
-        run = (inside ? s_before : 0.) + (lane == 0 ? 0. : run);
-#pragma unroll
-        for (int y = 0; y < V; ++y) {
-          const double x = of[V * q + y];
-          run += x;
-          if (x > 0.) {
-            if (found == 0x7fffffff && run > goal) found = lp.at(V * q + y);
-            last = lp.at(V * q + y);
-          }
-        }
-      }
-      const unsigned long long those = __ballot(found != 0x7fffffff), any = __ballot(last >= 0);
-      if (lane == (those != 0 ? __ffsll(those) - 1 : 63 - __clzll(any))) s_token = those != 0 ? found : last;
+  if (total > 0.) {
+    // the wave in whose tokens the running sum exceeds the goal; past all of them (u is not below 1): the last that has anything
+    const double goal = (double)u * total;
+    const unsigned long long those = __ballot(mine_all > 0. && run > goal), any = __ballot(mine_all > 0.);
+    const bool inside = those != 0;
+    const int segment = inside ? __ffsll(those) - 1 : 63 - __clzll(any);
+    const double before = __shfl(run - mine_all, segment);
+    if (wave == segment) {
+      token = left.token(before, inside ? goal : INFINITY);
+      if (lane == 0) s_token = token;
     }
     __syncthreads();
     token = s_token;
@@ -581,9 +533,9 @@ void verify_near_kernel(Verify p, int chunks, int rows, const ChunkStats* stats)
   write_tokens<kNear>(p, i, c.accepted, token, draft);
 }
 
-template <bool ALONE, int EACH>
+template <bool ALONE>
 static void launch_near(const Verify& p, int chunks, int rows, const ChunkStats* stats, hipStream_t st) {
-  hipLaunchKernelGGL((verify_near_kernel<ALONE, EACH>), dim3((unsigned)p.b), dim3(kNear), 0, st, p, chunks, rows, stats);
+  hipLaunchKernelGGL(verify_near_kernel<ALONE>, dim3((unsigned)p.b), dim3(kNear), 0, st, p, chunks, rows, stats);
 }
 
 // Logits of a thread: half as many where the chunks would not be one for every compute unit (one sequence, four drafts, 32768 tokens: 21.8 us, so 19.9; above 256 of them no difference, above 4000 slower).
@@ -623,17 +575,16 @@ hipError_t launch_verify(const Verify& p, void* workspace, hipStream_t st) {
   }
   // One launch where the rows that a wave has in turn are short (four drafts, 300 tokens: 8.2 us, in two launches 9.8; of 2000 10.6 and 10.3), and for more
   // where the sequences are many (256 of two rows of 2000: 11.9 and 13.1; of 4000 19.5 and 14.2).
-  static_assert(2048 <= 4 * kNear, "rows that a thread holds in four");
+  static_assert(2048 <= kNear * kNearEach, "rows that the threads hold");
   if (rows <= kAloneRows && (long long)((rows + 15) / 16) * p.vocab <= (p.b >= 128 ? 2048 : 1024)) {
-    launch_near<true, 4>(p, chunks, rows, stats, st);
+    launch_near<true>(p, chunks, rows, stats, st);
     return hipGetLastError();
   }
   hipError_t e = launch_stats<false>(p, each, chunks, rows, stats, st);
   if (e != hipSuccess) return e;
-  // (two launches for three: four drafts, 4096 tokens 11.1 us for 18.2, 16384 16.2 for 20.6; with twice the logits a thread they do not fit its registers)
-  if (p.vocab <= kNearEach * kNear) {
-    if (p.vocab <= 4 * kNear) launch_near<false, 4>(p, chunks, rows, stats, st);
-    else launch_near<false, kNearEach>(p, chunks, rows, stats, st);
+  // (two launches for three: four drafts, 4096 tokens 10.5 us and 12.5, 64 sequences 13.2 and 17.2; 16384 tokens, 16 a thread, 15.6 and 13.2)
+  if (p.vocab <= kNear * kNearEach) {
+    launch_near<false>(p, chunks, rows, stats, st);
     return hipGetLastError();
   }
   if (each == kEach) hipLaunchKernelGGL(verify_rest_kernel<kEach>, rests, block, 0, st, p, chunks, rows, stats, rest, choice);
