@@ -274,8 +274,8 @@ void verify_greedy_kernel(Verify p, int chunks, int rows, const ChunkStats* stat
   write_tokens(p, blockIdx.x, c.accepted, c.p.at < p.vocab && c.p.most > -INFINITY ? c.p.at : 0, draft);      // (a row of -inf throughout: 0)
 }
 
-// What is left of the row that decides, a chunk a workgroup, in segments.  (With the draw in the same launch, by the last of a sequence's workgroups, 19 us in
-// the place of 9 and 9: what orders writes and reads across the XCDs costs more than a launch.)
+// What is left of the row that decides, a chunk a workgroup, in segments.  (With the draw in the same launch, by the last of a sequence's workgroups, 19 us where
+// the two took 9 and 9 (now 7 and 5): what orders writes and reads across the XCDs costs more than a launch.)
 template <int EACH>
 __global__ __launch_bounds__(kThreads)
 void verify_rest_kernel(Verify p, int chunks, int rows, const ChunkStats* stats, double* rest, Choice* choice) {
