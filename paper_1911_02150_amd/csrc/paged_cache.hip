@@ -53,7 +53,7 @@ __device__ __forceinline__ uint32_t score_key(float x) {
 constexpr int kSelectThreads = 1024;
 constexpr int kBins = 2048;
 
-// Sum of x over the workgroup's threads before this one; *total: over all.
+// Sum of x over the workgroup's threads before this one; *total: over all.  `waves` is the call's own until two barriers later.
 __device__ __forceinline__ int before_me(int x, int* waves, int* total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int incl = x;
@@ -62,7 +62,6 @@ __device__ __forceinline__ int before_me(int x, int* waves, int* total) {
     const int y = __shfl_up(incl, off);
     if (lane >= off) incl += y;
   }
-  __syncthreads();
   if (lane == 63) waves[wave] = incl;
   __syncthreads();
   int before = 0, all = 0;
@@ -85,7 +84,7 @@ __global__ __launch_bounds__(kSelectThreads)
 void evict_select_kernel(PagedEvict p) {
   constexpr int kWaves = kSelectThreads / 64;
   __shared__ int bins[kBins];
-  __shared__ int waves[kWaves];
+  __shared__ int waves[8][kWaves];     // a scan's each; those of the loops in turn
   __shared__ int s_bin, s_above, s_all;
   __shared__ int s_count[2][(KEEP > 0 ? KEEP : 1) * kWaves + 1];      // of a wave's 64 positions: those at the threshold, those that stay
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -123,6 +122,7 @@ void evict_select_kernel(PagedEvict p) {
       }
     }
   };
+  for (int x = tid; x < kBins; x += kSelectThreads) bins[x] = 0;
   uint32_t keys[KEEP > 0 ? KEEP : 1];
   float values[KEEP > 0 ? KEEP : 1];
   uint32_t late = 0;                   // bit u: the thread's u-th position is one of the latest, and there
@@ -152,8 +152,15 @@ void evict_select_kernel(PagedEvict p) {
     });
   }
   int all_old, all_recent;
-  before_me(n_old, waves, &all_old);
-  before_me(n_recent, waves, &all_recent);
+  if constexpr (KEEP > 0) {            // (both in one: up to 24576 each)
+    int all;
+    before_me(n_old | n_recent << 16, waves[0], &all);
+    all_old = all & 0xffff;
+    all_recent = (int)((unsigned)all >> 16);
+  } else {
+    before_me(n_old, waves[0], &all_old);
+    before_me(n_recent, waves[1], &all_recent);
+  }
   const int want = min(all_old, p.budget - min(all_recent, p.budget));
   uint32_t threshold = 0;              // keys above it stay, and of those equal to it the first `ties`
   int ties = 0;
@@ -166,8 +173,6 @@ void evict_select_kernel(PagedEvict p) {
     for (int pass = 0; pass < 3; ++pass) {
       const int shift = shifts[pass], count = 1 << sizes[pass];
       const uint32_t agree = pass == 0 ? 0u : ~0u << (shift + sizes[pass]);
-      for (int x = tid; x < count; x += kSelectThreads) bins[x] = 0;
-      __syncthreads();
       auto add = [&](uint32_t key) {
         if (key != 0 && (key & agree) == (threshold & agree)) atomicAdd(&bins[(key >> shift) & (count - 1)], 1);
       };
@@ -180,9 +185,14 @@ void evict_select_kernel(PagedEvict p) {
       __syncthreads();
       // bins from the top: thread t has the two (or the one) from count - 1 - 2t down
       const int top = count - 1 - 2 * tid;
-      const int x0 = top >= 0 ? bins[top] : 0, x1 = top >= 1 ? bins[top - 1] : 0;
+      int x0 = 0, x1 = 0;
+      if (top >= 0) {                  // (count is even)
+        x0 = bins[top];
+        x1 = bins[top - 1];
+        bins[top] = bins[top - 1] = 0; // (for the next pass)
+      }
       int total;
-      const int above = before_me(x0 + x1, waves, &total);
+      const int above = before_me(x0 + x1, waves[2 + pass], &total);
       if (above < rank && rank <= above + x0) { s_bin = top; s_above = above; s_all = x0; }
       if (above + x0 < rank && rank <= above + x0 + x1) { s_bin = top - 1; s_above = above + x0; s_all = x1; }
       __syncthreads();
@@ -193,7 +203,6 @@ void evict_select_kernel(PagedEvict p) {
         rank = 0;
         break;
       }
-      __syncthreads();
     }
     ties = rank;
   }
@@ -209,7 +218,7 @@ void evict_select_kernel(PagedEvict p) {
       static_assert(all <= kSelectThreads, "a count a thread");
       __syncthreads();
       int total;
-      const int before = before_me(tid < all ? s_count[which][tid] : 0, waves, &total);
+      const int before = before_me(tid < all ? s_count[which][tid] : 0, waves[5 + which], &total);
       if (tid < all) s_count[which][tid] = before;
       if (tid == 0) s_count[which][all] = total;
       __syncthreads();
@@ -276,14 +285,15 @@ void evict_select_kernel(PagedEvict p) {
       equal &= is;
       int total;
       if (ties > 0) {                  // (the same in all threads)
-        int rank = tied + before_me(__popc(equal), waves, &total);
+        int rank = tied + before_me(__popc(equal), waves[5], &total);
         tied += total;
 #pragma unroll
         for (int u = 0; u < 8; ++u)
           if (equal >> u & 1) stays |= (uint32_t)(rank++ < ties) << u;
       }
-      int slot = done + before_me(__popc(stays), waves, &total);
+      int slot = done + before_me(__popc(stays), waves[6], &total);
       done += total;
+      __syncthreads();                 // (the scans' places are the next round's)
 #pragma unroll
       for (int u = 0; u < 8; ++u)
         if (stays >> u & 1) {
