@@ -102,8 +102,4 @@ __device__ __forceinline__ int paged_row(const PagedCache& c, const int32_t* tab
 
 __device__ __forceinline__ int paged_length(const PagedCache& c, int len) { return len < 0 ? 0 : min(len, c.positions()); }
 
-template <typename T> __device__ __forceinline__ float cache_value(T x);
-template <> __device__ __forceinline__ float cache_value<float>(float x) { return x; }
-template <> __device__ __forceinline__ float cache_value<uint16_t>(uint16_t x) { return bf16_bits_to_float(x); }
-
 }  // namespace mqa

@@ -331,7 +331,7 @@ struct Four {
   double of[4], upto;      // upto: of the tokens up to this lane's last
   int first;
   template <typename L, typename Q>
-  __device__ __forceinline__ Four(const Verify& p, const Rest& r, const L& lp, Q&& drafted) {
+  __device__ __forceinline__ Four(const Rest& r, const L& lp, Q&& drafted) {
     first = lp.first;
     if (r.y) {
       const L lq = drafted();
@@ -441,7 +441,7 @@ void verify_draw_kernel(Verify p, int stride, const double* rest, const Choice* 
       load(x0);
       scan();
     }
-    const Four left(p, r, Logits<64, 4>(r.x, segment, p.vocab), [&]() { return Logits<64, 4>(r.y, segment, p.vocab); });      // (a chunk of 64 threads: a segment)
+    const Four left(r, Logits<64, 4>(r.x, segment, p.vocab), [&]() { return Logits<64, 4>(r.y, segment, p.vocab); });      // (a chunk of 64 threads: a segment)
     token = left.token(before, inside ? goal : INFINITY);
   } else {                                                 // nothing to draw from: the largest logit
     token = largest<64>(r.x, p.vocab, s_most, s_at);
@@ -502,7 +502,7 @@ void verify_near_kernel(Verify p, int chunks, int rows, const ChunkStats* stats)
   }
   const Choice c = choose<false, kNear>(p, i, ALONE ? 1 : chunks, mine, &lds);
   const Rest r(p, i, c);
-  const Four left(p, r, Logits<kNear, kNearEach>(r.x, 0, p.vocab), [&]() { return Logits<kNear, kNearEach>(r.y, 0, p.vocab); });
+  const Four left(r, Logits<kNear, kNearEach>(r.x, 0, p.vocab), [&]() { return Logits<kNear, kNearEach>(r.y, 0, p.vocab); });
   if (lane == 63) s_sum[wave] = left.upto;
   __syncthreads();
   const double mine_all = lane < kWaves ? s_sum[lane] : 0.;      // lane w: wave w's
