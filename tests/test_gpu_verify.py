@@ -161,3 +161,23 @@ def test_wrong_tensors_are_refused(m):
     for bad in (dict(temperature=-1.0), dict(temperature=float("nan")), dict(u=None), dict(drafts=None)):
         with pytest.raises(m.MqaError):
             m.mqa_stack_verify_drafts(**{**dict(logits=logits, drafts=drafts, u=u), **bad})
+
+
+def test_probabilities_are_float64(m):
+    """Two borders 4e-15 to 1e-13 of the whole away from the goal, which a 2^x of 43 bits puts on the other side of it: three tokens of weights 1, e^-d and e^-d', where
+    1 / u is next to their sum.  (Float64's own errors: u * (1 + w + w'), 3e-16 of the whole.)"""
+    rng = np.random.default_rng(0)
+    d = rng.uniform(0.34, 0.3465, 2_000_000).astype(np.float32)                # (exponents of nearly -1/2, where a series around 0 is least accurate)
+    u = rng.uniform(0.4125, 0.4135, len(d)).astype(np.float32)
+    w = np.exp(-d.astype(np.float64))
+    other = (-np.log(1 / u.astype(np.float64) - 1 - w)).astype(np.float32)
+    left = 1 - u.astype(np.float64) * (1 + w + np.exp(-other.astype(np.float64)))
+    near = (np.abs(left) < 1e-13) & (np.abs(left) > 4e-15) & (other < 0.3465)
+    d, u, other, first = d[near], u[near], other[near], left[near] > 0
+    assert len(d) > 30 and 0 < first.sum() < len(d)
+    rows = np.stack([np.zeros_like(d), -d, -other], axis=1)
+    for vocab in (3, 5000, 20000):                                             # (one launch, two, three)
+        logits = np.full((len(d), 1, vocab), -np.inf, dtype=np.float32)
+        logits[:, 0, :3] = rows
+        tokens, _ = m.mqa_stack_verify_drafts(gpu(logits), None, gpu(u[:, None]))
+        assert ((tokens[:, 0].cpu().numpy() == 0) == first).all()
