@@ -480,7 +480,7 @@ int mqa_stack_feed_forward(const float* W1, const float* W2, float* x, int rows,
  * those before it do and u[i,j] q_j(t) < p_j(t).  tokens [b,n+1]: the accepted[i] drafts that stand, then one token drawn by u[i,n] (from
  * max(p - q, 0) / sum at the first refused draft, from p behind the last of counts[i]: the lowest index whose running sum exceeds u times the whole; the most probable token
  * where there is nothing to draw from), then -1.  temperature 0: a draft stands where it is mqa_stack_argmax's token, which follows the last that stands (u and draft_logits are not
- * looked at).  n = 0: one token is drawn from logits [b,1,vocab] (drafts may be NULL).  NaN counts as -infinity, +infinity as the largest number; a
+ * looked at).  n = 0: one token is drawn from logits [b,1,vocab] (drafts may be NULL).  With a temperature above 0 NaN counts as -infinity, +infinity as the largest number; a
  * drafted token outside [0,vocab) is refused.  Probabilities are held in float64.  n <= 65536, vocab <= 2^24, b * (2n + 1) * ceil(vocab / 4096) <= 2^23.
  * The workspace: mqa_stack_verify_workspace_bytes(...) bytes (16-byte aligned; 0 = unsupported sizes).
  */

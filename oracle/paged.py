@@ -99,6 +99,14 @@ def probabilities(logits, temperature):
     return w / w.sum()
 
 
+def largest(row, temperature):
+    """The lowest index of a row's largest logit, 0 if there is none.  With temperature 0 NaN is no logit at all; else NaN counts as -inf, and +inf as the largest number."""
+    if temperature == 0:
+        there = np.nonzero(~np.isnan(row))[0]
+        return int(there[np.argmax(row[there])]) if len(there) else 0
+    return int(np.argmax(np.where(np.isnan(row), -np.inf, np.minimum(row, np.finfo(np.float32).max))))
+
+
 def verify(logits, drafts, u, draft_logits=None, counts=None, temperature=1.0):
     """(tokens [b,n+1], accepted [b])."""
     b, n, vocab = logits.shape[0], logits.shape[1] - 1, logits.shape[2]
@@ -107,7 +115,7 @@ def verify(logits, drafts, u, draft_logits=None, counts=None, temperature=1.0):
         count = n if counts is None else min(max(int(counts[i]), 0), n)
         rest = None
         for j in range(count + 1):
-            best = int(np.argmax(np.where(np.isnan(logits[i, j]), -np.inf, np.minimum(logits[i, j], np.finfo(np.float32).max))))
+            best = largest(logits[i, j], temperature)
             if temperature > 0:
                 rest = probabilities(logits[i, j], temperature)
             if j == count:

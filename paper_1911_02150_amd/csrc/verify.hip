@@ -17,6 +17,7 @@ constexpr int kThreads = 256;
 constexpr int kEach = 16;                          // logits of a thread, or half as many: of a workgroup a chunk of 4096 or 2048
 
 // What a chunk of a row of logits adds up to: the sum of e^((x - most) / temperature); the largest logit and (temperature 0) its lowest index.
+// (at: not below vocab where nothing is comparable: a row of NaN)
 struct ChunkStats { double sum; float most; int at; };
 struct RowStats { double sum; float most; int at; };
 
@@ -63,8 +64,8 @@ __device__ __forceinline__ double block_sum(double x, double* red) {
 __device__ __forceinline__ int drafts_of(const Verify& p, int i) { return p.counts ? min(max(p.counts[i], 0), p.n) : p.n; }
 
 // A thread's logits of a chunk of THREADS * EACH, 16 bytes at a time (of rows that begin at any float: the memory pipe takes them so); past the end -inf.
-// at(e): the index of the e-th.
-template <int THREADS, int EACH>
+// at(e): the index of the e-th.  RAW: as they are, for the largest one (comparisons pass NaN over, as in argmax_kernel).
+template <int THREADS, int EACH, bool RAW = false>
 struct Logits {
   typedef __attribute__((ext_vector_type(4), aligned(4))) float Four;
   static constexpr int kStep = 4 * THREADS;
@@ -86,8 +87,10 @@ struct Logits {
 #pragma unroll
       for (int z = 0; z < 4; ++z) x[4 * e + z] = y[z];
     }
+    if constexpr (!RAW) {
 #pragma unroll
-    for (int e = 0; e < EACH; ++e) x[e] = tame(x[e]);
+      for (int e = 0; e < EACH; ++e) x[e] = tame(x[e]);
+    }
   }
   __device__ __forceinline__ int at(int e) const { return first + (e >> 2) * kStep + (e & 3); }
 };
@@ -105,7 +108,7 @@ void verify_stats_kernel(Verify p, int chunks, int rows, ChunkStats* stats) {
   const bool drafted = row > p.n;
   const int j = drafted ? row - p.n - 1 : row;
   if (drafted ? j >= count : j > count) return;
-  const Logits<kThreads, EACH> v(drafted ? p.draft_logits + ((size_t)i * p.n + j) * p.vocab : p.logits + ((size_t)i * (p.n + 1) + j) * p.vocab, chunk, p.vocab);
+  const Logits<kThreads, EACH, GREEDY> v(drafted ? p.draft_logits + ((size_t)i * p.n + j) * p.vocab : p.logits + ((size_t)i * (p.n + 1) + j) * p.vocab, chunk, p.vocab);
   float most = -INFINITY;
   int at = 0x7fffffff;
 #pragma unroll
@@ -202,7 +205,7 @@ __device__ __forceinline__ Choice choose(const Verify& p, int i, int chunks, con
     RowStats d{0., -INFINITY, 0};
     bool stands = false;
     if constexpr (GREEDY) {
-      stands = token && t == (a.at < p.vocab && a.most > -INFINITY ? a.at : 0);
+      stands = token && t == (a.at < p.vocab ? a.at : 0);
     } else if (j < count) {                                // (the same j, and draft_logits, in all of a group)
       const double u = p.u[(size_t)i * (p.n + 1) + j];
       const double pt = weight(tame(lp), a.most, per);
@@ -273,7 +276,7 @@ void verify_greedy_kernel(Verify p, int chunks, int rows, const ChunkStats* stat
   __shared__ ChooseLds lds;
   const int draft = (int)threadIdx.x < p.n ? p.drafts[(size_t)blockIdx.x * p.n + threadIdx.x] : -1;
   const Choice c = choose<true>(p, blockIdx.x, chunks, stats + (size_t)blockIdx.x * rows * chunks, &lds);
-  write_tokens(p, blockIdx.x, c.accepted, c.p.at < p.vocab && c.p.most > -INFINITY ? c.p.at : 0, draft);      // (a row of -inf throughout: 0)
+  write_tokens(p, blockIdx.x, c.accepted, c.p.at < p.vocab ? c.p.at : 0, draft);
 }
 
 // What is left of the row that decides, a chunk a workgroup, in segments.  (With the draw in the same launch, by the last of a sequence's workgroups, 19 us where

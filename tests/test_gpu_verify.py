@@ -181,3 +181,21 @@ def test_probabilities_are_float64(m):
         logits[:, 0, :3] = rows
         tokens, _ = m.mqa_stack_verify_drafts(gpu(logits), None, gpu(u[:, None]))
         assert ((tokens[:, 0].cpu().numpy() == 0) == first).all()
+
+
+@pytest.mark.parametrize("vocab", [2, 300, 9000])
+def test_greedy_is_argmax_of_odd_rows_too(m, vocab):
+    """NaN next to -infinity, the largest number next to +infinity, rows of nothing but NaN or -infinity."""
+    top = np.finfo(np.float32).max
+    pairs = [(np.nan, -np.inf), (-np.inf, np.nan), (top, np.inf), (np.inf, top), (np.nan, np.nan), (-np.inf, -np.inf), (np.nan, -3.0), (np.inf, np.inf), (np.nan, np.inf),
+             (-top, -np.inf)]
+    rows = np.full((2 * len(pairs), vocab), np.nan, dtype=np.float32)
+    rows[: len(pairs), :2] = pairs                                             # at the row's beginning, the rest of it NaN ...
+    rows[len(pairs):, vocab - 2:] = pairs                                      # ... and at its end
+    logits = gpu(rows).view(-1, 1, vocab).repeat(1, 3, 1)
+    best = m.mqa_stack_argmax(logits[:, 0].contiguous())
+    drafts = torch.stack([best, (best + 1) % vocab], dim=1)
+    tokens, accepted = m.mqa_stack_verify_drafts(logits, drafts, None, temperature=0.0)
+    assert accepted.tolist() == [1] * len(rows)
+    assert torch.equal(tokens, torch.stack([best, best, torch.full_like(best, -1)], dim=1))
+    check(m, logits.cpu().numpy(), drafts.long().cpu().numpy(), None, temperature=0.0)
