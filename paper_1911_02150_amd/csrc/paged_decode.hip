@@ -879,6 +879,16 @@ __device__ __forceinline__ void add_scores(const PagedDecode& p, int g, int chun
 #pragma unroll
     for (int y = 0; y < 4; ++y) sum[y] += __builtin_amdgcn_exp2f(x[y] - state.x) * state.y;
   }
+  // A row that is NaN makes NaN of 2^-inf as well: a sum that came out so is taken again, over the rows that see the position.
+#pragma unroll
+  for (int y = 0; y < 4; ++y)
+    if (sum[y] != sum[y] && pos + y < L) {
+      float again = 0.f;
+      if (paged_row(p.c, p.c.table + (size_t)i * p.c.max_pages, 0, pos + y) >= 0)
+        for (int r = wave; r < p.R; r += 4)
+          if (pos + y < row_limit(p, L, r)) again += __builtin_amdgcn_exp2f(z[r * pitch + y] - s_state[r].x) * s_state[r].y;
+      sum[y] = again;
+    }
   s_sum[wave][lane] = sum;
   __syncthreads();
   const int mine = chunk * kScored + tid;

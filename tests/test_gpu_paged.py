@@ -642,3 +642,39 @@ def test_native_calls(heads, dtype, monkeypatch):
     for bad in (dict(q=q.transpose(1, 2)), dict(lens=lens[:2]), dict(scores=scores[..., 1:].contiguous()), dict(o=q[:, :1].contiguous()), dict(K_pages=K[..., :0], V_pages=V[..., :0, :])):
         with pytest.raises((ValueError, m.MqaError)):
             m.mqa_paged_decode_step(**{**dict(q=q, K_pages=K, V_pages=V, table=table, lens=lens), **bad})
+
+
+# b, n, h, h_kv, k, dtype, each
+NAN_SCORES = [(3, 3, 8, 1, 128, "bf16", 6), (3, 3, 4, 2, 64, "f32", 6), (3, 2, 20, 1, 128, "bf16", 40), (3, 2, 3, 1, 24, "f32", 40)]
+
+
+@pytest.mark.parametrize("b,n,h,h_kv,k,dtype,each", NAN_SCORES)
+def test_scores_of_a_nan_row(m, b, n, h, h_kv, k, dtype, each):
+    """A row that is NaN (a NaN in its query; an infinite key) adds NaN to what it sees and nothing to what it does not: positions of later tokens and of pages that hold
+    nothing, in one launch and in two."""
+    from oracle import paged
+    rng = np.random.default_rng(k + each)
+    page = 16
+    K, V = (pool(rng, b * each, h_kv, page, k, dtype) for _ in range(2))
+    table, lens = tables(rng, b, each), np.array([each * page - 20, 40, each * page])
+    table[0, 1], table[0, 3], table[2, 0] = -1, 10 ** 6, -7
+    q = rng.standard_normal((b, n, h, k)).astype(np.float32)
+    q[0, 0, h // 2, 3] = np.nan                                               # the first query of sequence 0: the later tokens' positions are not seen by it
+    at = paged.where(table, 1, 5, b * each, page)
+    K[at[0], -1, at[1]] = np.inf                                              # a key of sequence 1, in its last K/V head
+    one = h_kv == 1
+    scores = rng.random((b, h_kv, each * page)).astype(np.float32)
+    with np.errstate(all="ignore"):
+        want, total, _ = paged.attend(q.astype(np.float64), K, V, table, lens, 0.25, scores)
+    written = np.broadcast_to(np.arange(each * page) < lens[:, None, None], total.shape)
+    assert np.isnan(total[written]).any() and np.isfinite(total[0, h // 2 * h_kv // h, lens[0] - n + 1:lens[0]]).all()
+    out = torch.full((b, each * page) if one else (b, h_kv, each * page), 777.0, device=DEV)
+    got = m.mqa_paged_decode_step(on_gpu(q), on_gpu(K, dtype, one), on_gpu(V, dtype, one), on_gpu(table), on_gpu(lens), scale=0.25, scores=on_gpu(scores, one_head=one),
+                                  scores_out=out)
+    assert np.array_equal(np.isnan(got.cpu().numpy()), np.isnan(want))
+    out = out.cpu().numpy().reshape(total.shape)
+    assert (out[~written] == 777).all()
+    assert np.array_equal(np.isnan(out[written]), np.isnan(total[written]))
+    finite = written & ~np.isnan(total)
+    bound = tolerance(np.nan_to_num(q), K, 1, 0.25, lens.max()) + EPS * (n * h + 2)      # (of a weight; there are up to n h of them, at most 1 each)
+    assert (np.abs(out - total)[finite] <= bound * n * h).all()
