@@ -42,6 +42,7 @@ struct PagedDecode {
   float* part_m;           // [pieces, R], log2 domain
   float* part_l;
   int2* spans;             // [b, h_kv]: a group's first piece, and how many it has
+  int4* work;              // [1 + pieces of one head], or null: the list of paged_list_kernel
   float* logits;           // with scores: [b, h_kv, R, positions rounded up to 32], log2 domain
   float2* stats;           // with scores: [b, h_kv, R]: maximum, 1 / sum, of groups in one piece
   int b, n, h;
@@ -66,6 +67,7 @@ struct PagedEvict {
 struct PagedPlan {
   int form;                // the matrix kernel's widths: 64 or 128; -64, -128, -256: up to that
   int block_rows, blocks, split, pieces;      // pieces: at most
+  int listed;              // so many sequences that their pieces are listed first
   size_t bytes;
 };
 constexpr int kPagedTile = 32;

@@ -195,6 +195,7 @@ __device__ void scalar_segment(const PagedDecode& p, const Segment& s, int r0, i
 __device__ __forceinline__ int tiles_of(const PagedDecode& p, int len) { return (paged_length(p.c, len) + kPagedTile - 1) / kPagedTile; }
 
 // Sum of x over the threads before this one; *all: over all.
+template <int THREADS = kThreads>
 __device__ __forceinline__ int before_me(int x, int* s_waves, int* all) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int incl = x;
@@ -207,7 +208,7 @@ __device__ __forceinline__ int before_me(int x, int* s_waves, int* all) {
   __syncthreads();
   int before = incl - x, sum = 0;
 #pragma unroll
-  for (int w = 0; w < kThreads / 64; ++w) {
+  for (int w = 0; w < THREADS / 64; ++w) {
     if (w < wave) before += s_waves[w];
     sum += s_waves[w];
   }
@@ -217,10 +218,139 @@ __device__ __forceinline__ int before_me(int x, int* s_waves, int* all) {
 
 constexpr int kComputeUnits = 256, kShares = 768, kSharesOfMany = 512, kLeast = 16, kLongest = 64;
 
-// This workgroup's segment; false: there is none.  Every workgroup looks at all lengths: thread t has sequences t * each up to the next one's.
-__device__ __forceinline__ bool find_segment(const PagedDecode& p, Segment* s) {
+// Tiles of a piece, at most: a whole number for each of the workgroup's four waves.
+__device__ __forceinline__ int whole_waves(int tiles) { return max(1, (tiles + 3) >> 2) * 4; }
+__device__ __forceinline__ int pieces_of(int tiles, int per) { return max(1, (int)((unsigned)(tiles + per - 1) / (unsigned)per)); }
+// Many groups: are they left whole?  total: of all groups
+__device__ __forceinline__ bool left_whole(const PagedDecode& p, int longest, int total) {
+  return longest <= kLongest && longest * (kComputeUnits / p.blocks) <= total;
+}
+__device__ __forceinline__ int share_of(const PagedDecode& p, int total) {
+  const int shares = p.blocks > 1 ? kSharesOfMany : kShares;
+  return max(kLeast, (total + shares - 1) / shares);
+}
+
+// Thousands of sequences: what look_for finds from all lengths, found once, by one workgroup: p.work[0].x: pieces of one head of all sequences, and behind it for
+// each of them {sequence, pieces before the sequence's, the sequence's, its length}.  Looked for by every workgroup it grows with the square of the sequences: 32768 of up
+// to 20 positions, 8 heads, 5912 us, from the list 397; 2048 54 and 33; of 300 to 1200, 32 heads, 4096 389 and 315, 1024 91 and 92, 300 38 and 47 (a launch more).
+constexpr int kLookedFor = 1024;         // sequences, at most, without it
+constexpr int kListThreads = 1024, kListEach = 8;
+__global__ __launch_bounds__(kListThreads)
+void paged_list_kernel(PagedDecode p) {
+  __shared__ int s_waves[3][kListThreads / 64], s_longest[kListThreads / 64];
+  const int tid = threadIdx.x;
+  int mine = 0, longest = 0;
+  for (int x = tid; x < p.b; x += kListThreads) {
+    const int t = tiles_of(p, p.lens[x]);
+    mine += t;
+    longest = max(longest, t);
+  }
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) longest = max(longest, __shfl_xor(longest, off));
+  if ((tid & 63) == 0) s_longest[tid >> 6] = longest;
+  int total;
+  before_me<kListThreads>(mine, s_waves[2], &total);
+  total *= p.c.h_kv;
+#pragma unroll
+  for (int w = 0; w < kListThreads / 64; ++w) longest = max(longest, s_longest[w]);
+  const int per = whole_waves(left_whole(p, longest, total) ? longest : share_of(p, total));
+  int before = 0;
+  for (int base = 0, turn = 0; base < p.b; base += kListThreads * kListEach, turn ^= 1) {
+    const int first = base + kListEach * tid;
+    int len[kListEach], count[kListEach], sum = 0;
+#pragma unroll
+    for (int x = 0; x < kListEach; ++x) len[x] = p.lens[min(first + x, p.b - 1)];
+#pragma unroll
+    for (int x = 0; x < kListEach; ++x) {
+      count[x] = first + x < p.b ? pieces_of(tiles_of(p, len[x]), per) : 0;
+      sum += count[x];
+    }
+    int all, at = before + before_me<kListThreads>(sum, s_waves[turn], &all);      // (its places are written again two barriers later)
+    before += all;
+#pragma unroll
+    for (int x = 0; x < kListEach; ++x) {
+      const int4 work = make_int4(first + x, at, count[x], len[x]);
+      for (const int end = at + count[x]; at < end; ++at) p.work[1 + at] = work;
+    }
+  }
+  if (tid == 0) p.work[0] = make_int4(before, 0, 0, 0);
+}
+
+// The sequence that a piece is of, which of the sequence's pieces (`off`), and how many a head has (`c`); false: there is no such piece.  Every workgroup looks at all
+// lengths: thread t has sequences t * each up to the next one's.
+__device__ __forceinline__ bool look_for(const PagedDecode& p, int piece, Segment* s, int* off, int* c) {
   __shared__ int s_waves[8][kThreads / 64], s_longest[kThreads / 64];
   __shared__ int s_at[4];
+  const int tid = threadIdx.x, heads = p.c.h_kv;
+  const int each = (p.b + kThreads - 1) / kThreads, from = tid * each, to = min(p.b, from + each);
+  const int len = from < to ? p.lens[from] : 0;            // (up to 256 sequences: read once)
+  int mine = tiles_of(p, len), longest = mine;
+  for (int x = from + 1; x < to; ++x) {
+    const int t = tiles_of(p, p.lens[x]);
+    mine += t;
+    longest = max(longest, t);
+  }
+  const bool many = p.b * heads * p.blocks >= 2 * kComputeUnits;
+  if (many) {
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) longest = max(longest, __shfl_xor(longest, off));
+    if ((tid & 63) == 0) s_longest[tid >> 6] = longest;
+  }
+  int total;
+  before_me(mine, s_waves[0], &total);
+  total *= heads;
+  // Whole groups where there are two for every compute unit, none long and none
+  // more than twice what a workgroup's share would be (512 sequences of up to 1000, 32 heads: 45 us, in shares 56; 64 of up to 2500, 8 heads, which are not cut
+  // by this rule 75, uncut 84).  Else as many as leave every compute unit one workgroup at most, or else two, if
+  // that is not too uneven (64 sequences of 8192, 32 heads: 53 us, in 512 pieces 58; 128 of up to 1024, 64 heads, two to a unit 33, in shares of a 768th 45); else
+  // shares so small that a compute unit has several in turn (512 sequences of up to 4096, 32 heads: 126, in shares of a 512th 137, of a 1536th 133; with several
+  // blocks of rows shares of a 512th: 300 of up to 6000, 64 heads 160, of a 768th 166), though
+  // not below four tiles a wave (256 of 512, 64 heads: 31, else 42).
+  int per = 0, count = 0, before = 0, all = 0, turn = 0;
+  auto cut = [&](int tiles) {
+    per = whole_waves(tiles);
+    count = from < to ? pieces_of(tiles_of(p, len), per) : 0;
+    for (int x = from + 1; x < to; ++x) count += pieces_of(tiles_of(p, p.lens[x]), per);
+    before = before_me(count, s_waves[++turn], &all);
+  };
+  bool fits = false;
+  if (many) {
+    longest = max(max(s_longest[0], s_longest[1]), max(s_longest[2], s_longest[3]));
+    fits = left_whole(p, longest, total);
+    if (fits) cut(longest);
+  }
+  for (int most = kComputeUnits; most <= 2 * kComputeUnits; most *= 2) {
+    const int units = most / p.blocks;
+    if (!fits && p.b * heads <= units)
+      for (int x = 8; x <= 10 && !fits; ++x) {
+        cut((int)(((long long)total * x + 8 * units - 1) / (8 * units)));
+        fits = all * heads <= units;
+      }
+  }
+  if (!fits) cut(share_of(p, total));
+  if (piece >= all * heads) return false;
+  if (before * heads <= piece && piece < (before + count) * heads) {      // one thread
+    int x = from, L = len, mine = pieces_of(tiles_of(p, len), per);
+    while (piece >= (before + mine) * heads) {
+      before += mine;
+      L = p.lens[++x];
+      mine = pieces_of(tiles_of(p, L), per);
+    }
+    s_at[0] = x;
+    s_at[1] = piece - before * heads;
+    s_at[2] = L;
+    s_at[3] = mine;
+  }
+  __syncthreads();
+  s->i = __builtin_amdgcn_readfirstlane(s_at[0]);
+  *off = __builtin_amdgcn_readfirstlane(s_at[1]);
+  *c = __builtin_amdgcn_readfirstlane(s_at[3]);
+  s->L = paged_length(p.c, __builtin_amdgcn_readfirstlane(s_at[2]));
+  return true;
+}
+
+// This workgroup's segment; false: there is none.
+__device__ __forceinline__ bool find_segment(const PagedDecode& p, Segment* s) {
   const int tid = threadIdx.x, heads = p.c.h_kv;
   int piece = blockIdx.x, block = 0;
   if (p.blocks > 1) {                    // (workgroups go to the eight XCDs in turn: a piece's are neighbours on one)
@@ -239,71 +369,17 @@ __device__ __forceinline__ bool find_segment(const PagedDecode& p, Segment* s) {
     s->piece = -1;
     return true;
   }
-  const int each = (p.b + kThreads - 1) / kThreads, from = tid * each, to = min(p.b, from + each);
-  const int len = from < to ? p.lens[from] : 0;            // (up to 256 sequences: read once)
-  int mine = tiles_of(p, len), longest = mine;
-  for (int x = from + 1; x < to; ++x) {
-    const int t = tiles_of(p, p.lens[x]);
-    mine += t;
-    longest = max(longest, t);
+  int off, c;
+  if (p.work) {
+    if (piece >= p.work[0].x * heads) return false;
+    const int4 work = p.work[1 + piece / heads];
+    s->i = work.x;
+    off = piece - work.y * heads;
+    c = work.z;
+    s->L = paged_length(p.c, work.w);
+  } else if (!look_for(p, piece, s, &off, &c)) {
+    return false;
   }
-  const bool many = p.b * heads * p.blocks >= 2 * kComputeUnits;
-  if (many) {
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) longest = max(longest, __shfl_xor(longest, off));
-    if ((tid & 63) == 0) s_longest[tid >> 6] = longest;
-  }
-  int total;
-  before_me(mine, s_waves[0], &total);
-  total *= heads;
-  // Tiles of a piece, at most: a whole number for each of the workgroup's four waves.  Whole groups where there are two for every compute unit, none long and none
-  // more than twice what a workgroup's share would be (512 sequences of up to 1000, 32 heads: 45 us, in shares 56; 64 of up to 2500, 8 heads, which are not cut
-  // by this rule 75, uncut 84).  Else as many as leave every compute unit one workgroup at most, or else two, if
-  // that is not too uneven (64 sequences of 8192, 32 heads: 53 us, in 512 pieces 58; 128 of up to 1024, 64 heads, two to a unit 33, in shares of a 768th 45); else
-  // shares so small that a compute unit has several in turn (512 sequences of up to 4096, 32 heads: 126, in shares of a 512th 137, of a 1536th 133; with several
-  // blocks of rows shares of a 512th: 300 of up to 6000, 64 heads 160, of a 768th 166), though
-  // not below four tiles a wave (256 of 512, 64 heads: 31, else 42).
-  int per = 0, count = 0, before = 0, all = 0, turn = 0;
-  auto pieces_of = [&](int t) { return max(1, (int)((unsigned)(t + per - 1) / (unsigned)per)); };
-  auto cut = [&](int tiles) {
-    per = max(1, (tiles + 3) >> 2) * 4;
-    count = from < to ? pieces_of(tiles_of(p, len)) : 0;
-    for (int x = from + 1; x < to; ++x) count += pieces_of(tiles_of(p, p.lens[x]));
-    before = before_me(count, s_waves[++turn], &all);
-  };
-  bool fits = false;
-  if (many) {
-    longest = max(max(s_longest[0], s_longest[1]), max(s_longest[2], s_longest[3]));
-    fits = longest <= kLongest && longest * (kComputeUnits / p.blocks) <= total;
-    if (fits) cut(longest);
-  }
-  for (int most = kComputeUnits; most <= 2 * kComputeUnits; most *= 2) {
-    const int units = most / p.blocks;
-    if (!fits && p.b * heads <= units)
-      for (int x = 8; x <= 10 && !fits; ++x) {
-        cut((int)(((long long)total * x + 8 * units - 1) / (8 * units)));
-        fits = all * heads <= units;
-      }
-  }
-  const int shares = p.blocks > 1 ? kSharesOfMany : kShares;
-  if (!fits) cut(max(kLeast, (total + shares - 1) / shares));
-  if (piece >= all * heads) return false;
-  if (before * heads <= piece && piece < (before + count) * heads) {      // one thread
-    int x = from, L = len, c = pieces_of(tiles_of(p, len));
-    while (piece >= (before + c) * heads) {
-      before += c;
-      L = p.lens[++x];
-      c = pieces_of(tiles_of(p, L));
-    }
-    s_at[0] = x;
-    s_at[1] = piece - before * heads;
-    s_at[2] = L;
-    s_at[3] = c;
-  }
-  __syncthreads();
-  s->i = __builtin_amdgcn_readfirstlane(s_at[0]);
-  const int off = __builtin_amdgcn_readfirstlane(s_at[1]), c = __builtin_amdgcn_readfirstlane(s_at[3]);
-  s->L = paged_length(p.c, __builtin_amdgcn_readfirstlane(s_at[2]));
   s->e = heads == 1 ? 0 : off / c;
   const int x = off - s->e * c, t = (s->L + kPagedTile - 1) / kPagedTile;
   s->begin = 0;
@@ -933,6 +1009,7 @@ static size_t lay_out(PagedDecode* p, const PagedPlan& pl, float* at) {
     p->part_m = take(states);
     p->part_l = take(states);
     p->spans = reinterpret_cast<int2*>(take(groups * 2));
+    if (pl.listed) p->work = reinterpret_cast<int4*>(take(4 * ((size_t)p->b + kShares + 1)));
   }
   if (p->scores_out) {
     p->stats = reinterpret_cast<float2*>(take(groups * p->R * 2));
@@ -959,6 +1036,7 @@ PagedPlan paged_plan(int b, int n, int h, int h_kv, int page_size, int max_pages
   // 380 13.7 and 13.5), and to greater lengths where there is one for every compute unit (256 of up to 760: 18, in pieces 25).
   const bool heavy = wide > 128 || (!is_bf16 && wide > 64);
   pl.split = tiles > (groups * pl.blocks >= kComputeUnits ? 32 : heavy ? 12 : 16);
+  pl.listed = pl.split && b > kLookedFor;
   const long long least = groups * ((tiles + 3) / 4), most = groups + kShares;      // (pieces of four tiles; a last, shorter one in every group)
   pl.pieces = (int)(!pl.split ? groups : least < most ? least : most);
   PagedDecode p = {};
@@ -1008,6 +1086,11 @@ static hipError_t launch_rows(const PagedDecode& p, const PagedPlan& pl, hipStre
 
 hipError_t launch_paged_decode(const PagedDecode& p, const PagedPlan& pl, int is_bf16, hipStream_t st) {
   hipError_t e;
+  if (pl.listed) {
+    hipLaunchKernelGGL(paged_list_kernel, dim3(1), dim3(kListThreads), 0, st, p);
+    e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
   switch (pl.form) {
     case 64: e = is_bf16 ? launch_rows<uint16_t, 64, true>(p, pl, st) : launch_rows<float, 64, true>(p, pl, st); break;
     case 128: e = is_bf16 ? launch_rows<uint16_t, 128, true>(p, pl, st) : launch_rows<float, 128, true>(p, pl, st); break;

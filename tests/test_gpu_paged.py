@@ -678,3 +678,51 @@ def test_scores_of_a_nan_row(m, b, n, h, h_kv, k, dtype, each):
     finite = written & ~np.isnan(total)
     bound = tolerance(np.nan_to_num(q), K, 1, 0.25, lens.max()) + EPS * (n * h + 2)      # (of a weight; there are up to n h of them, at most 1 each)
     assert (np.abs(out - total)[finite] <= bound * n * h).all()
+
+
+@pytest.mark.parametrize("scored", [False, True])
+@pytest.mark.parametrize("b,h_kv,n,h,longest", [(2100, 1, 1, 3, 40), (5000, 2, 2, 4, 300), (40000, 1, 1, 20, 40), (6000, 1, 2, 18, 4500), (3000, 3, 1, 6, 900)])
+def test_thousands_of_sequences(m, b, h_kv, n, h, longest, scored):
+    """In a table that makes them pieces (more than 1024 positions): against calls for a few hundred sequences each.  Lengths of all kinds, a few far longer than most, or (900)
+    none."""
+    g = torch.Generator(device=DEV).manual_seed(b)
+    page, pages, each, k = 16, 300, 300, 64
+    K, V = (torch.randn((pages, h_kv, page, k), generator=g, device=DEV).bfloat16() for _ in range(2))
+    table = torch.randint(-1, pages, (b, each), generator=g, device=DEV, dtype=torch.int32)
+    lens = torch.randint(0 if longest < 900 else 500, longest, (b,), generator=g, device=DEV, dtype=torch.int32)
+    if longest < 900:
+        lens[b // 2], lens[-1], lens[7] = each * page, each * page - 5, -1
+    q = torch.randn((b, n, h, k), generator=g, device=DEV)
+    scores = torch.zeros((b, h_kv, each * page), device=DEV) if scored else None
+    got = m.mqa_paged_decode_step(q, K, V, table, lens, scale=0.2, scores=scores)
+    again = m.mqa_paged_decode_step(q, K, V, table, lens, scale=0.2)
+    assert scored or torch.equal(got, again)
+    # (cut into other pieces: float32 sums of up to 4800 weights of another order, half a step each, of values up to 5)
+    bound = 2.0 ** -24 * (64 + 8 * 4800 ** 0.5) * 5
+    for i in range(0, b, 700):
+        part = slice(i, min(b, i + 700))
+        s = torch.zeros_like(scores[part]) if scored else None
+        want = m.mqa_paged_decode_step(q[part], K, V, table[part], lens[part], scale=0.2, scores=s)
+        assert (got[part] - want).abs().max().item() <= bound
+        if scored:
+            assert (scores[part] - s).abs().max().item() <= 2.0 ** -24 * (64 + 8 * 4800 ** 0.5) * n * h
+
+
+def test_a_step_grows_with_its_sequences_not_their_square(m):
+    """Four times as many short sequences in a table of more than 1024 positions: four times the time, not sixteen (the shortest of several, with room for what else runs)."""
+    page, each, k = 16, 66, 8
+    K = torch.randn((64, page, k), device=DEV).bfloat16()
+    took = []
+    for b in (1 << 15, 1 << 17):
+        table = torch.zeros((b, each), dtype=torch.int32, device=DEV)
+        lens, q = torch.full((b,), 9, dtype=torch.int32, device=DEV), torch.randn((b, 1, k), device=DEV)
+        o, times = torch.empty_like(q), []
+        for _ in range(6):
+            start, end = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+            start.record()
+            m.mqa_paged_decode_step(q, K, K, table, lens, o=o)
+            end.record()
+            end.synchronize()
+            times.append(start.elapsed_time(end))
+        took.append(min(times))
+    assert took[1] < 8 * took[0], took
