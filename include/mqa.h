@@ -347,13 +347,16 @@ int mqa_paged_append_kv_rows(const float* k_new, const float* v_new, const int32
 
 /*
  * Attention of the newest n tokens of every sequence, n = 1 (a decoding step) or more (drafted tokens, the end of a prompt), after their rows have been
- * appended: q [b,n,h,k] -> o [b,n,h,v].  Query j of sequence i sees the positions below lens[i] - (n - 1 - j); head e of q reads K/V head e / (h / h_kv).  A row that
+ * appended: q [b,n,h,k] -> o [b,n,h,v].  Query j of sequence i sees the positions below lens[i] - (n - 1 - j): of a sequence with fewer new tokens the last rows
+ * of q are theirs, and those before them older positions'.  Head e of q reads K/V head e / (h / h_kv).  A row that
  * sees nothing is 0; what a row does not see may hold anything (infinities and NaN included).  n * h / h_kv <= 1024, b * n * h <= 2^22.
  * Products and sums are float32's (a bfloat16 cache's values are multiplied by three bfloat16 terms of q and of the weights, which together are the float32).
  *
  * scores_out (or NULL), [b,h_kv,max_pages * page_size] float32: the attention weight that each position has received, summed over the n * h / h_kv rows of
  * its head and over the steps: scores_in (NULL: zeros) plus this step's, the newest n positions from 0 on; scores_in and scores_out may be the same array.
- * Positions at and behind the length are left as they were.
+ * Positions at and behind the length are left as they were.  All n tokens' rows are added in every sequence: drafts that may yet be refused, and sequences with
+ * unequal numbers of new tokens, are attended to without scores first; then, with lens as the tokens that stand leave it, a call for each number j of them,
+ * with rows q[:, :j] and scores, and a length of 0 (nothing of that sequence is read, its scores are left as they were) for the sequences with another number.
  *
  * The workspace: mqa_paged_decode_workspace_bytes(...) bytes (16-byte aligned; 0 = none, or unsupported sizes), written and read by this call's launches only.
  * With scores it holds the logits: 4 * b * n * h * max_pages * page_size bytes of it.

@@ -726,3 +726,47 @@ def test_a_step_grows_with_its_sequences_not_their_square(m):
             times.append(start.elapsed_time(end))
         took.append(min(times))
     assert took[1] < 8 * took[0], took
+
+
+@pytest.mark.parametrize("h_kv", [1, 2])
+def test_scores_of_the_tokens_that_stand(m, h_kv):
+    """A loop with drafted tokens: attention without scores, verification, then the scores of the tokens that stand, a call for each number of them; as if only those had ever
+    been queries.  Twice, so that refused drafts' rows are written over, their places scored from 0 again."""
+    from oracle import paged
+    rng = np.random.default_rng(h_kv)
+    b, n, h, k, page, each, vocab = 6, 3, 4, 64, 16, 5, 50
+    one = h_kv == 1
+    K, V = (np.zeros((b * each, h_kv, page, k)) for _ in range(2))
+    table, lens = tables(rng, b, each), np.array([0, 5, 17, 40, 60, 30])
+    first = rng.standard_normal((2, b, 60, h_kv, k)).astype(np.float32)
+    bf = lambda x: rounded(x, "bf16")  # noqa: E731
+    paged.append(K, V, table, *first, np.zeros(b, dtype=np.int64), lens, bf)
+    scores = rng.random((b, h_kv, each * page)).astype(np.float32)
+    gK, gV, g_table, g_lens, g_scores = on_gpu(K, "bf16", one), on_gpu(V, "bf16", one), on_gpu(table), on_gpu(lens), on_gpu(scores, one_head=one)
+    scores, seen = scores.astype(np.float64), set()
+    for _ in range(2):
+        new = rng.standard_normal((2, b, n + 1, h_kv, k)).astype(np.float32)
+        q = rng.standard_normal((b, n + 1, h, k)).astype(np.float32)
+        logits, u = rng.standard_normal((b, n + 1, vocab)).astype(np.float32), rng.random((b, n + 1), dtype=np.float32)
+        drafts = np.where(rng.random((b, n)) < 0.8, logits[:, :n].argmax(-1), 7)
+        g_q, after = on_gpu(q), torch.zeros_like(g_lens)
+        m.mqa_paged_append_kv_rows(gK, gV, g_table, *(on_gpu(x[:, :, 0] if one else x) for x in new), g_lens, after)
+        o = m.mqa_paged_decode_step(g_q, gK, gV, g_table, after, scale=0.25)
+        tokens, accepted = m.mqa_stack_verify_drafts(on_gpu(logits), on_gpu(drafts), on_gpu(u), temperature=0.0)
+        g_lens += accepted + 1
+        for j in range(1, n + 2):
+            m.mqa_paged_decode_step(g_q[:, :j].contiguous(), gK, gV, g_table, g_lens * (accepted + 1 == j), scale=0.25, scores=g_scores)
+        grown = paged.append(K, V, table, *new, lens, rounded=bf)
+        want, _, size = paged.attend(q.astype(np.float64), K, V, table, grown, 0.25)
+        assert (np.abs(o.cpu().numpy() - want) <= tolerance(q, K, size, 0.25, 80)).all()
+        _, stand = paged.verify(logits, drafts, u, temperature=0)
+        assert accepted.tolist() == stand.tolist()
+        seen.update(stand.tolist())
+        lens = lens + stand + 1
+        for i in range(b):
+            rows = stand[i] + 1
+            _, total, _ = paged.attend(q[i:i + 1, :rows].astype(np.float64), K, V, table[i:i + 1], lens[i:i + 1], 0.25, scores[i:i + 1])
+            scores[i] = np.where(np.isnan(total[0]), scores[i], total[0])
+    assert len(seen) > 2 and g_lens.tolist() == lens.tolist()
+    bound = 2 * (tolerance(q, K, 1, 0.25, 80) + EPS * ((n + 1) * h + 2)) * (1 + scores)      # (two steps)
+    assert (np.abs(g_scores.cpu().numpy().reshape(scores.shape) - scores) <= bound).all()
