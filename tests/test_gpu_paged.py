@@ -770,3 +770,29 @@ def test_scores_of_the_tokens_that_stand(m, h_kv):
     assert len(seen) > 2 and g_lens.tolist() == lens.tolist()
     bound = 2 * (tolerance(q, K, 1, 0.25, 80) + EPS * ((n + 1) * h + 2)) * (1 + scores)      # (two steps)
     assert (np.abs(g_scores.cpu().numpy().reshape(scores.shape) - scores) <= bound).all()
+
+
+@pytest.mark.parametrize("scored", [False, True])
+@pytest.mark.parametrize("b,h_kv,n,h,lengths", [(600, 1, 1, 3, "like"), (300, 2, 2, 4, "like"), (260, 1, 1, 40, "like"), (700, 1, 1, 8, "one long"), (1024, 1, 2, 3, "one long")])
+def test_hundreds_of_sequences_in_a_long_table(m, b, h_kv, n, h, lengths, scored):
+    """A table of more than 1024 positions, so that work is looked for by length.  Alike: at most 64 tiles each, the longest no more than twice the average, two workgroups or more
+    for every compute unit: every cache is left whole, and there is nothing to merge.  Or most of them short or empty, and one that is cut."""
+    from oracle import paged
+    rng = np.random.default_rng(b)
+    page, pages, each, k = 16, 60, 70, 64
+    K, V = (pool(rng, pages, h_kv, page, k, "bf16") for _ in range(2))
+    table = rng.integers(0, pages, (b, each))
+    lens = rng.integers(700, 1100, b) if lengths == "like" else rng.integers(0, 60, b) * (np.arange(b) % 7 != 0)
+    if lengths == "one long":
+        lens[b // 2] = each * page
+    q = rng.standard_normal((b, n, h, k)).astype(np.float32)
+    scores = rng.random((b, h_kv, each * page)).astype(np.float32) if scored else None
+    want, total, size = paged.attend(q.astype(np.float64), K, V, table, lens, 0.125, scores)
+    one = h_kv == 1
+    kw = dict(scores=on_gpu(scores, one_head=one), scores_out=torch.full((b, each * page) if one else (b, h_kv, each * page), 777.0, device=DEV)) if scored else {}
+    got = m.mqa_paged_decode_step(on_gpu(q), on_gpu(K, "bf16", one), on_gpu(V, "bf16", one), on_gpu(table), on_gpu(lens), scale=0.125, **kw)
+    assert (np.abs(got.cpu().numpy() - want) <= tolerance(q, K, size, 0.125, lens.max())).all()
+    if scored:
+        out, left = kw["scores_out"].cpu().numpy().reshape(total.shape), np.isnan(total)
+        bound = (tolerance(q, K, 1, 0.125, lens.max()) + EPS * (2 + n * h / h_kv)) * total
+        assert (out[left] == 777).all() and (np.abs(out - total)[~left] <= bound[~left]).all()
