@@ -78,7 +78,7 @@ int mqa_paged_decode_step(const float* q, const void* K_pages, const void* V_pag
   p.q = q; p.lens = lens; p.o = o; p.scores_in = scores_in; p.scores_out = scores_out;
   p.b = b; p.n = n; p.h = h; p.R = n * (h / h_kv);
   p.block_rows = pl.block_rows; p.blocks = pl.blocks; p.split = pl.split;
-  p.qscale = scale * kLog2e;
+  p.qscale = scale * kLog2e;      // (rounded, and once more with q: a logit is off by a step of its own size, as float32's scale * (q . k) and its exponential's base are)
   paged_workspace(&p, pl, workspace);
   return launch_paged_decode(p, pl, dt == MQA_BF16, static_cast<hipStream_t>(stream)) == hipSuccess ? MQA_OK : MQA_ERR_LAUNCH;
 }

@@ -345,6 +345,8 @@ hipError_t launch_paged_append(const PagedAppend& p, int is_bf16, hipStream_t st
 hipError_t launch_paged_evict(const PagedEvict& p, int is_bf16, hipStream_t st) {
   const int groups = p.b * p.c.h_kv, esz = is_bf16 ? 2 : 4, each = (p.c.positions() + kSelectThreads - 1) / kSelectThreads;
   const dim3 grid((unsigned)groups), block(kSelectThreads);
+  // As few positions a thread as hold the capacity, since a thread goes over all that it could have (one sequence of 700: 8.7 us with 3, 11.1 with 10, 15.6 with 24, gone
+  // over again 12.9; 6000: 11.9 with 10, 16.4, 16.1; 24000: 19.9 with 24, 36.7).
   if (each <= 3) hipLaunchKernelGGL(evict_select_kernel<3>, grid, block, 0, st, p);
   else if (each <= 10) hipLaunchKernelGGL(evict_select_kernel<10>, grid, block, 0, st, p);
   else if (each <= 24) hipLaunchKernelGGL(evict_select_kernel<24>, grid, block, 0, st, p);

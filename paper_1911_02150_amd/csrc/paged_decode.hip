@@ -300,9 +300,11 @@ __device__ __forceinline__ bool look_for(const PagedDecode& p, int piece, Segmen
   before_me(mine, s_waves[0], &total);
   total *= heads;
   // Whole groups where there are two for every compute unit, none long and none
-  // more than twice what a workgroup's share would be (512 sequences of up to 1000, 32 heads: 45 us, in shares 56; 64 of up to 2500, 8 heads, which are not cut
-  // by this rule 75, uncut 84).  Else as many as leave every compute unit one workgroup at most, or else two, if
-  // that is not too uneven (64 sequences of 8192, 32 heads: 53 us, in 512 pieces 58; 128 of up to 1024, 64 heads, two to a unit 33, in shares of a 768th 45); else
+  // more than twice what a workgroup's share would be (512 sequences of up to 1000, 32 heads: 45 us, in shares 56; 64 of up to 2500, 8 K/V heads, which this rule cuts,
+  // 75, uncut 84).  Else as many as leave every compute unit one workgroup at most, or else two, if
+  // that is not too uneven (64 sequences of 8192, 32 heads: 53 us, in 512 pieces 58; 128 of up to 1024, 64 heads, two to a unit 33, in shares of a 768th 45): up to a
+  // quarter over an even share each (48 of 2048, 32 heads 23.1, none over it 27.5; 100 of up to 4000 33.7 and 36.9; 90 of 3000, 8 heads 35.8 and 34.5; half over it:
+  // no better, and 128 of up to 1024, 64 heads 37.7 for 33.8); else
   // shares so small that a compute unit has several in turn (512 sequences of up to 4096, 32 heads: 126, in shares of a 512th 137, of a 1536th 133; with several
   // blocks of rows shares of a 512th: 300 of up to 6000, 64 heads 160, of a 768th 166), though
   // not below four tiles a wave (256 of 512, 64 heads: 31, else 42).
@@ -723,7 +725,7 @@ __device__ __forceinline__ void in_plain_form(const PagedDecode& p, const Segmen
 }
 
 // CACHED: several blocks of rows read the same tiles, neighbours on an XCD at about the same time: from memory once and else from L2.  (64 heads of 512
-// sequences of up to 4096: 185 us.  Two teams of four waves in a workgroup 207: a workgroup to a compute unit, whose start and end nothing covers; that with
+// sequences of up to 4096, back to back: 190 us.  When that took 185, two teams of four waves in a workgroup 207: a workgroup to a compute unit, whose start and end nothing covers; that with
 // the tiles in LDS 300; all 64 rows in a wave, two tiles on their way, 260.)
 template <typename T, int D, int HB, bool SCORED, bool CACHED, bool EXACT>
 __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2)
@@ -1025,15 +1027,16 @@ PagedPlan paged_plan(int b, int n, int h, int h_kv, int page_size, int max_pages
   pl.form = k == v && (k == 64 || k == 128) ? k : wide <= 64 ? -64 : wide <= 128 ? -128 : -256;
   const long long groups = (long long)b * h_kv;
   // 16 query rows to a workgroup where the work is so little that its latency counts, else 32, whose tiles are read half as often: 16 sequences of 2048, 32 heads
-  // 14.9 us against 18.8, 48 of them 22.6 and 22.5, 512 of up to 4096 with 64 heads 245 and 187; 8 sequences of 200, 64 heads 7.8 and 10.8; 256 wide, 32 heads, 16
-  // sequences of 2048 23.8 and 27.8, 32 of them 31.9 and 31.0.
-  // And only where a compute unit can hold them all, two each, three of 64 wide: 200 sequences of up to 100, 64 heads, 15.9 and 13.4; 64 wide 150 of 40 7.3 and 8.8.
+  // 15.0 us against 19.1, 48 of them 22.7 and 23.2, 512 of up to 4096 with 64 heads 249 and 190; 8 sequences of 200, 64 heads 7.8 and 11.0; 256 wide, 32 heads, 16
+  // sequences of 2048 24.4 and 28.5, 32 of them 32.5 and 32.0.
+  // And only where a compute unit can hold them all, two each, three of 64 wide: 200 sequences of up to 100, 64 heads, 15.5 and 13.5; 64 wide 150 of 40 7.4 and 8.7.
   // (float32 rows of more than 64: 32 query rows do not fit a wave's registers beside a tile.)
   const bool little = groups * tiles * R * (pl.form == -256 ? 4 : 2) <= 3 << 16 && groups * ((R + 15) / 16) <= (wide <= 64 ? 3 : 2) * kComputeUnits;
   pl.block_rows = R <= 16 || little || (!is_bf16 && wide > 64) ? 16 : 32;
   pl.blocks = (int)((R + pl.block_rows - 1) / pl.block_rows);
-  // One launch, a workgroup to a group, where cutting and merging would take longer (sequences of 380: 8.3 us, in pieces 10.8; of 800 17.7 and 11.8; float32 of
-  // 380 13.7 and 13.5), and to greater lengths where there is one for every compute unit (256 of up to 760: 18, in pieces 25).
+  // One launch, a workgroup to a group, where cutting and merging would take longer (8 heads, 32 sequences of 500: 10.3 us, in pieces 12.0; of 640 12.9 and 12.3, of 800 15.7
+  // and 12.6; one of 500 9.2 and 11.1, of 800 12.0 and 11.1; float32, one of 380 13.6 both, of 500 15.9 and 13.6), and to greater lengths where there is one for
+  // every compute unit (256 of up to 1000, 32 heads: 25, in pieces 32).
   const bool heavy = wide > 128 || (!is_bf16 && wide > 64);
   pl.split = tiles > (groups * pl.blocks >= kComputeUnits ? 32 : heavy ? 12 : 16);
   pl.listed = pl.split && b > kLookedFor;
