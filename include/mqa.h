@@ -338,7 +338,7 @@ int mqa_beam_reorder_kv(const void* K_src, const void* V_src, const int32_t* len
  *
  * mqa_paged_append_kv_rows: rows k_new [b,n,h_kv,k], v_new [b,n,h_kv,v] (float32) go behind the lens_in[i] rows that sequence i has, rounded as in
  * mqa_append_kv; of a padded batch only the first counts[i] (clamped to [0,n]; NULL: all n); lens_out[i] = lens_in[i] + their number.  A sequence that cannot
- * hold them keeps its rows and its length.  lens_in and lens_out must be different arrays (MQA_ERR_SHAPE if they are the same pointer).
+ * hold them keeps its rows and its length.  lens_out must be another array than lens_in and counts (MQA_ERR_SHAPE if it is the same pointer).
  * n <= max_pages * page_size, b * n * h_kv * (k + v) <= 2^33.
  */
 int mqa_paged_append_kv_rows(const float* k_new, const float* v_new, const int32_t* counts, void* K_pages, void* V_pages, const int32_t* table,

@@ -787,7 +787,7 @@ def _pages(K_pages, V_pages, table, b):
 def mqa_paged_append_kv_rows(K_pages, V_pages, table, k_new, v_new, lens, lens_out, counts=None, stream=None):
     """K_pages [num_pages,page_size,k] (multi-query) or [num_pages,h_kv,page_size,k], V_pages likewise (float32 or bfloat16), table
     [b,max_pages] int32: rows k_new [b,n,k] or [b,n,h_kv,k] / v_new, of sequence i the first counts[i] (None: all), go behind the lens[i] rows it has.
-    lens_out [b] int32, another tensor than lens, receives the new lengths and is returned."""
+    lens_out [b] int32, another tensor than lens and counts, receives the new lengths and is returned."""
     if stream is None and _native is not None:
         done = _native.paged_append(K_pages, V_pages, table, k_new, v_new, lens, lens_out, counts)
         if done is not None:

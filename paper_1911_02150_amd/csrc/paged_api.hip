@@ -43,7 +43,7 @@ int mqa_paged_append_kv_rows(const float* k_new, const float* v_new, const int32
   if (dt != MQA_F32 && dt != MQA_BF16) return MQA_ERR_DTYPE;
   if (n <= 0 || !cache_sizes_ok(b, h_kv, num_pages, page_size, max_pages, k, v) || n > max_pages * page_size) return MQA_ERR_SHAPE;
   if ((long long)b * n > (1ll << 30) / h_kv / ((k + v) >> 3)) return MQA_ERR_SHAPE;
-  if (lens_in == lens_out) return MQA_ERR_SHAPE;
+  if (lens_in == lens_out || counts == lens_out) return MQA_ERR_SHAPE;      // (read by workgroups that come after one that has written)
   if (misaligned(k_new) || misaligned(v_new) || misaligned(K_pages) || misaligned(V_pages) || misaligned(table) || misaligned(lens_in) ||
       misaligned(lens_out) || (counts && misaligned(counts)))
     return MQA_ERR_ALIGN;

@@ -130,3 +130,9 @@ def test_python_refuses_on_the_host():
         m.mqa_paged_append_kv_rows(t, t, t, t, t, t, t)
     with pytest.raises(ValueError, match="must be a device tensor"):
         m.mqa_paged_evict_kv(t, t, t, t, t, t, t, t, t, 0)
+
+
+def test_append_refuses_counts_in_place():
+    """The new lengths into the array of the counts: a sequence's other workgroups would read what the first one wrote."""
+    fn = entry("mqa_paged_append_kv_rows", 8, 9, [vp])
+    assert fn(A, B, F, C, D, E, A + 0x1000, F, *SIZES.values(), None) == SHAPE
