@@ -349,7 +349,7 @@ int mqa_paged_append_kv_rows(const float* k_new, const float* v_new, const int32
  * Attention of the newest n tokens of every sequence, n = 1 (a decoding step) or more (drafted tokens, the end of a prompt), after their rows have been
  * appended: q [b,n,h,k] -> o [b,n,h,v].  Query j of sequence i sees the positions below lens[i] - (n - 1 - j): of a sequence with fewer new tokens the last rows
  * of q are theirs, and those before them older positions'.  Head e of q reads K/V head e / (h / h_kv).  A row that
- * sees nothing is 0; what a row does not see may hold anything (infinities and NaN included).  n * h / h_kv <= 1024, b * n * h <= 2^22.
+ * sees nothing, or whose logits are all -infinity, is 0; what a row does not see may hold anything (infinities and NaN included).  n * h / h_kv <= 1024, b * n * h <= 2^22.
  * Products and sums are float32's (a bfloat16 cache's values are multiplied by three bfloat16 terms of q and of the weights, which together are the float32).
  *
  * scores_out (or NULL), [b,h_kv,max_pages * page_size] float32: the attention weight that each position has received, summed over the n * h / h_kv rows of

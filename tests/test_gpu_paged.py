@@ -796,3 +796,23 @@ def test_hundreds_of_sequences_in_a_long_table(m, b, h_kv, n, h, lengths, scored
         out, left = kw["scores_out"].cpu().numpy().reshape(total.shape), np.isnan(total)
         bound = (tolerance(q, K, 1, 0.125, lens.max()) + EPS * (2 + n * h / h_kv)) * total
         assert (out[left] == 777).all() and (np.abs(out - total)[~left] <= bound[~left]).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("k,each", [(128, 3), (64, 40), (40, 40)])
+def test_a_row_of_nothing_but_infinite_logits(m, k, each, dtype):
+    """Logits of -infinity throughout are as if nothing were seen: a row of 0 and no weight."""
+    rng = np.random.default_rng(k)
+    page = 16
+    lens = np.array([each * page - 3, 20])
+    K = np.full((2 * each, 1, page, k), 1.0)
+    K[:, :, :, 0] = -np.inf
+    V, table = pool(rng, 2 * each, 1, page, k, dtype), tables(rng, 2, each)
+    q = np.ones((2, 2, k), dtype=np.float32)
+    q[:, 1, 0] = -1                                                            # (the second row's logits: +infinity, which is NaN as a softmax)
+    scores = torch.zeros((2, each * page), device=DEV)
+    args = [on_gpu(x, d, True) if d else on_gpu(x) for x, d in ((K, dtype), (V, dtype), (table, None), (lens, None))]
+    got = m.mqa_paged_decode_step(on_gpu(q[:, :1].copy()), *args, scale=0.25, scores=scores)
+    assert not got.any() and not scores.any()
+    got = m.mqa_paged_decode_step(on_gpu(q), *args, scale=0.25)
+    assert not got[:, 0].any() and torch.isnan(got[:, 1]).all()
