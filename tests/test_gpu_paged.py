@@ -816,3 +816,36 @@ def test_a_row_of_nothing_but_infinite_logits(m, k, each, dtype):
     assert not got.any() and not scores.any()
     got = m.mqa_paged_decode_step(on_gpu(q), *args, scale=0.25)
     assert not got[:, 0].any() and torch.isnan(got[:, 1]).all()
+
+
+def test_the_list_of_a_replayed_step(m):
+    """1500 sequences in a long table, captured once: the list of their pieces is written anew at every replay, inside the workspace that the call asks for."""
+    g = torch.Generator(device=DEV).manual_seed(14)
+    b, each, page, k = 1500, 80, 16, 64
+    K, V = (torch.randn((90, page, k), generator=g, device=DEV).bfloat16() for _ in range(2))
+    table, q = torch.randint(0, 90, (b, each), generator=g, device=DEV, dtype=torch.int32), torch.randn((b, 4, k), generator=g, device=DEV)
+    lens, scores = torch.zeros(b, dtype=torch.int32, device=DEV), torch.zeros((b, each * page), device=DEV)
+    need = m.mqa_paged_decode_workspace_bytes(b, 1, 4, 1, page, each, k, k, m.MQA_BF16, True)
+    guard = torch.full((need + 4096,), 0x5a, dtype=torch.uint8, device=DEV)
+    run = lambda o, out, ws=None: m.mqa_paged_decode_step(q, K, V, table, lens, o=o, scale=0.3, scores=scores, scores_out=out, workspace=ws)  # noqa: E731
+    o, out = torch.zeros_like(q), torch.zeros_like(scores)
+    run(o, out, guard[:need])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(o, out, guard[:need])
+    whole = each * page
+    for lengths in (torch.randint(0, 30, (b,), generator=g, device=DEV), torch.full((b,), whole, device=DEV), torch.randint(600, 1000, (b,), generator=g, device=DEV),
+                    (torch.arange(b, device=DEV) % 97 == 0) * whole):
+        lens.copy_(lengths)
+        want, want_out = torch.zeros_like(q), torch.zeros_like(scores)
+        run(want, want_out)
+        guard[:need] = 0x5a
+        out.zero_()
+        torch.cuda.synchronize()
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(o, want) and torch.equal(out, want_out) and (guard[need:] == 0x5a).all()
+        some = torch.arange(0, b, 211, device=DEV)                             # (alone: other pieces, sums of another order)
+        alone = m.mqa_paged_decode_step(q[some], K, V, table[some], lens[some], scale=0.3)
+        assert (alone - want[some]).abs().max().item() <= EPS * (64 + 8 * whole ** 0.5) * 5
