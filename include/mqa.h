@@ -43,7 +43,8 @@
 extern "C" {
 #endif
 
-typedef enum { MQA_F32 = 0, MQA_BF16 = 1 } mqa_dtype; /* cache element type */
+typedef enum { MQA_F32 = 0, MQA_BF16 = 1, /* cache element type */
+               MQA_E4M3 = 2, MQA_INT8 = 3 /* 8 bits with scales: the mqa_paged_scaled_* calls only */ } mqa_dtype;
 
 typedef enum {
   MQA_OK = 0,
@@ -379,6 +380,59 @@ int mqa_paged_evict_kv(void* K_pages, void* V_pages, const int32_t* table_in, co
                        int32_t* lens_out, float* scores_out, int32_t* kept, int b, int h_kv, int num_pages, int page_size, int max_pages_in,
                        int max_pages_out, int k, int v, mqa_dtype dt, int budget, int recent, void* stream);
 
+/*
+ * Paged caches of 8 bits.  The pools hold e4m3 (MQA_E4M3: 8-bit floats with 4 exponent bits, finite up to 448, no infinities) or int8 (MQA_INT8: -127 .. 127), and beside
+ * them K_scales and V_scales, [num_pages,h_kv,page_size / block] float32: one for each `block` (which divides page_size) positions of a page and a head.  A value is
+ * that of its 8 bits times its scale.  Tables, lengths, missing pages, sharing and limits are as in the paged caches above, with k, v multiples of 16 up to 256.
+ *
+ * mqa_paged_scaled_append_kv_rows: as mqa_paged_append_kv_rows.  Of a block that gets rows, with a the largest finite |x| among its new rows and Q the type's largest number,
+ * s' is the smallest power of two, 2^-126 at least, with a <= Q s'.  A block whose first row is new gets the scale s'; one that has rows of the sequence already the larger of s' and the one
+ * it has, and if that is s', its older rows are rounded again to it.  (A scale does not become smaller while its block has rows, so that drafts that are refused may leave a block a coarser one.)  New values
+ * are rounded to the nearest number, the even one of two, infinities to +-Q; NaN is e4m3's NaN, int8's 0.  b * h_kv * ((n + block - 2) / block + 1) <= 2^23.
+ *
+ * mqa_paged_scaled_decode_step: as mqa_paged_decode_step without scores.  Scales may be any float32.
+ */
+int mqa_paged_scaled_append_kv_rows(const float* k_new, const float* v_new, const int32_t* counts, void* K_pages, float* K_scales, void* V_pages, float* V_scales,
+                                    const int32_t* table, const int32_t* lens_in, int32_t* lens_out, int b, int n, int h_kv, int num_pages, int page_size,
+                                    int block, int max_pages, int k, int v, mqa_dtype dt, void* stream);
+size_t mqa_paged_scaled_decode_workspace_bytes(int b, int n, int h, int h_kv, int page_size, int max_pages, int k, int v, mqa_dtype dt);
+int mqa_paged_scaled_decode_step(const float* q, const void* K_pages, const float* K_scales, const void* V_pages, const float* V_scales, const int32_t* table,
+                                 const int32_t* lens, float* o, int b, int n, int h, int h_kv, int num_pages, int page_size, int block, int max_pages,
+                                 int k, int v, mqa_dtype dt, float scale, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Who holds which page of a pool.  refs [num_pages] (int32) counts the entries of tables that name a page; one with a count of 0 (or less) is free.  The calls change
+ * tables and counts alone, on the device and in the stream's order (they may be captured); every pool that goes by the same tables (each layer's) then gets mqa_paged_copy_pages
+ * with the moves that they leave.  An entry outside [0,num_pages) names no page.  What a call does depends on its arguments alone: pages are given out from the lowest
+ * free one on.  Calls that change one refs must not overlap.  Limits: num_pages <= 2^24, max_pages * page_size <= 2^24, sequences * max_pages <= 2^28.
+ *
+ * fork:    sequence j of table_out [b_out,max_pages] starts as sequence parents[j] of table_in [b_in,max_pages] is: it names the pages of that one's lens_in positions (and none behind them),
+ *          their counts grow by one, lens_out[j] is its length; empty if parents[j] is outside [0,b_in).  What table_out named before is not given back (free it first).
+ *          Other arrays than table_in and lens_in.
+ * free:    every sequence gives back the pages behind its first lens[i] positions (0: all): their counts fall by one, the entries become -1.  Refused drafts, ended sequences.
+ * reserve: pages for the next counts[i] positions (clamped to [0,n]; NULL: n each) of every sequence, ready for an append: entries of the pages that they reach get a free page where they name none or
+ *          one that others name too.  The page that a sequence has begun (lens[i] not at its end) is copied if it is shared: moves[i] = {that page, the one in its place}, else
+ *          {-1,-1}; of the sequences of this call that write to a begun page, the last one keeps it if nobody else has it; a begun page that is missing stays so.
+ *          granted[i] = counts[i], what an append takes as its counts; or 0 and the sequence is as it was: where lens[i] < 0, where the positions are more than the table has, or where the pages that
+ *          this and the sequences before it need are more than are free (one that needs none is granted all the same).
+ * compact: the pages in use beyond the first used[0] (how many there are in use) move to the free ones among those, in order: moves[x] = {x-th of them, x-th free one}, {-1,-1} behind them;
+ *          moves has max(1, num_pages / 2) pairs.  table_out [b,max_pages] and refs_out name them by their new places (entries of free pages become -1).  Every table of the pool has to be in
+ *          the call, and other arrays than the inputs receive them.
+ * copy:    page moves[x,0] of each of the pools is copied to page moves[x,1], m pairs (either outside [0,num_pages): nothing); no page may be both copied from and to, or to twice.
+ *          pools and page_bytes are HOST arrays of num_pools entries (1 .. 4096): where a pool is, and the bytes of a page of it, a multiple of 4 up to 2^30; scales are pools too.
+ * The workspaces (16-byte aligned): mqa_paged_reserve_workspace_bytes / mqa_paged_compact_workspace_bytes (0: unsupported sizes).
+ */
+int mqa_paged_fork_pages(const int32_t* table_in, const int32_t* lens_in, const int32_t* parents, int32_t* table_out, int32_t* lens_out, int32_t* refs,
+                         int b_in, int b_out, int num_pages, int page_size, int max_pages, void* stream);
+int mqa_paged_free_pages(int32_t* table, const int32_t* lens, int32_t* refs, int b, int num_pages, int page_size, int max_pages, void* stream);
+size_t mqa_paged_reserve_workspace_bytes(int b, int n, int num_pages, int page_size, int max_pages);
+int mqa_paged_reserve_pages(int32_t* table, const int32_t* lens, const int32_t* counts, int32_t* refs, int32_t* granted, int32_t* moves, int b, int n,
+                            int num_pages, int page_size, int max_pages, void* workspace, size_t workspace_bytes, void* stream);
+size_t mqa_paged_compact_workspace_bytes(int b, int num_pages, int max_pages);
+int mqa_paged_compact_pages(const int32_t* table_in, const int32_t* refs_in, int32_t* table_out, int32_t* refs_out, int32_t* moves, int32_t* used, int b,
+                            int num_pages, int max_pages, void* workspace, size_t workspace_bytes, void* stream);
+int mqa_paged_copy_pages(void* const* pools, const size_t* page_bytes, int num_pools, const int32_t* moves, int m, int num_pages, void* stream);
+
 /* Same as mqa_decode_step / mha_decode_step with explicit launch tuning (NULL = defaults). */
 int mqa_decode_step_ex(const float* q, const void* K, const void* V, const int32_t* lens, float* o,
                        int b, int h, int cap, int k, int v, mqa_dtype dt, float scale,
@@ -475,6 +529,20 @@ int mqa_stack_argmax(const float* x, int32_t* out, int rows, int n, void* stream
 int mqa_stack_feed_forward_plan(int rows, int d, int ff, size_t* workspace_bytes);
 int mqa_stack_feed_forward(const float* W1, const float* W2, float* x, int rows, int d, int ff, float eps, void* workspace,
                            size_t workspace_bytes, void* stream);
+
+/*
+ * Logits as they are before a token is chosen from them (before mqa_stack_verify_drafts or mqa_stack_argmax): logits [b,n+1,vocab] -> out, which may be the same array.  Row j of sequence i stands
+ * behind the first lens[i] (clamped to [0,cap]) tokens of history [b,cap], of which the first prompts[i] (NULL: 0) are its prompt's, and the drafts [b,n] before draft j.  Of a token t, c counts
+ * the occurrences among the tokens behind the prompt and those drafts; it is seen if it is among all of them:
+ *   x = logits[i,j,t];  seen: x = x > 0 ? x / repetition[i] : x * repetition[i];  c > 0: x -= frequency[i] * c + presence[i];  x += bias;
+ *   not allowed: x = -infinity
+ * repetition, frequency, presence [b]: NULL: 1, 0, 0.  bias: the value of the last of bias_tokens [b,biases] that is t, of bias_values [b,biases] (biases = 0: none, both may be NULL).
+ * allowed [b,n+1,ceil(vocab / 32)]: token t is allowed if bit t % 32 of word t / 32 is set (NULL: all are); a grammar's mask may leave none.  Tokens outside [0,vocab) count for nothing.
+ * n <= 65536, vocab <= 2^24, cap <= 2^24, biases <= 2^24, b * ceil(vocab / 512) <= 2^23, b * max(cap, biases) <= 2^31.
+ */
+int mqa_stack_adjust_logits(const float* logits, float* out, const int32_t* history, const int32_t* lens, const int32_t* prompts, const int32_t* drafts,
+                            const float* repetition, const float* frequency, const float* presence, const int32_t* bias_tokens, const float* bias_values,
+                            const uint32_t* allowed, int b, int n, int vocab, int cap, int biases, void* stream);
 
 /*
  * Drafted tokens against the target's probabilities, and the token that follows them (speculative decoding).  logits [b,n+1,vocab]: the target's, row j those of the token at

@@ -13,7 +13,7 @@ import torch
 _PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG_DIR, "libmqa_decode.so")
 
-MQA_F32, MQA_BF16 = 0, 1
+MQA_F32, MQA_BF16, MQA_E4M3, MQA_INT8 = 0, 1, 2, 3
 MQA_PROJ_Q, MQA_PROJ_KV, MQA_PROJ_KV_MH, MQA_PROJ_O, MQA_PROJ_LINEAR = 0, 1, 2, 3, 4
 MQA_EPI_STORE, MQA_EPI_RELU, MQA_EPI_ADD = 0, 1, 2
 
@@ -28,6 +28,9 @@ EXPORTS = [
     "mqa_stack_feed_forward_plan", "mqa_stack_feed_forward",
     "mqa_paged_append_kv_rows", "mqa_paged_decode_workspace_bytes", "mqa_paged_decode_step", "mqa_paged_evict_kv",
     "mqa_stack_verify_workspace_bytes", "mqa_stack_verify_drafts",
+    "mqa_paged_scaled_append_kv_rows", "mqa_paged_scaled_decode_workspace_bytes", "mqa_paged_scaled_decode_step",
+    "mqa_paged_fork_pages", "mqa_paged_free_pages", "mqa_paged_reserve_workspace_bytes", "mqa_paged_reserve_pages", "mqa_paged_compact_workspace_bytes",
+    "mqa_paged_compact_pages", "mqa_paged_copy_pages", "mqa_stack_adjust_logits",
 ]
 
 
@@ -134,12 +137,27 @@ def load_library(path: str = LIB_PATH):
     lib.mqa_stack_verify_workspace_bytes.argtypes = [ci] * 3
     lib.mqa_stack_verify_workspace_bytes.restype = sz
     lib.mqa_stack_verify_drafts.argtypes = [vp] * 7 + [ci] * 3 + [cf, vp, sz, vp]
+    lib.mqa_paged_scaled_append_kv_rows.argtypes = [vp] * 10 + [ci] * 10 + [vp]
+    lib.mqa_paged_scaled_decode_workspace_bytes.argtypes = [ci] * 9
+    lib.mqa_paged_scaled_decode_workspace_bytes.restype = sz
+    lib.mqa_paged_scaled_decode_step.argtypes = [vp] * 8 + [ci] * 11 + [cf, vp, sz, vp]
+    lib.mqa_paged_fork_pages.argtypes = [vp] * 6 + [ci] * 5 + [vp]
+    lib.mqa_paged_free_pages.argtypes = [vp] * 3 + [ci] * 4 + [vp]
+    lib.mqa_paged_reserve_workspace_bytes.argtypes = [ci] * 5
+    lib.mqa_paged_reserve_workspace_bytes.restype = sz
+    lib.mqa_paged_reserve_pages.argtypes = [vp] * 6 + [ci] * 5 + [vp, sz, vp]
+    lib.mqa_paged_compact_workspace_bytes.argtypes = [ci] * 3
+    lib.mqa_paged_compact_workspace_bytes.restype = sz
+    lib.mqa_paged_compact_pages.argtypes = [vp] * 6 + [ci] * 3 + [vp, sz, vp]
+    lib.mqa_paged_copy_pages.argtypes = [vp, vp, ci, vp, ci, ci, vp]
+    lib.mqa_stack_adjust_logits.argtypes = [vp] * 12 + [ci] * 5 + [vp]
     lib.mqa_status_string.argtypes = [ci]
     lib.mqa_status_string.restype = ctypes.c_char_p
     for name in EXPORTS:
         if name not in ("mqa_decode_workspace_bytes", "mha_decode_workspace_bytes", "mqa_status_string",
                         "mqa_decode_beams_workspace_bytes", "mqa_decode_workspace_bytes_default", "mqa_project_kv_workspace_bytes",
-                        "mqa_project_add_layernorm_workspace_bytes", "mqa_paged_decode_workspace_bytes", "mqa_stack_verify_workspace_bytes"):
+                        "mqa_project_add_layernorm_workspace_bytes", "mqa_paged_decode_workspace_bytes", "mqa_stack_verify_workspace_bytes",
+                        "mqa_paged_scaled_decode_workspace_bytes", "mqa_paged_reserve_workspace_bytes", "mqa_paged_compact_workspace_bytes"):
             getattr(lib, name).restype = ci
     _native = _load_native(lib)
     _lib = lib
@@ -889,6 +907,208 @@ def mqa_paged_evict_kv(K_pages, V_pages, table, lens, scores, table_out, lens_ou
     if rc != 0:
         raise MqaError("mqa_paged_evict_kv", rc)
     return kept
+
+
+def _scaled_pages(K_pages, K_scales, V_pages, V_scales, table, b):
+    """(h_kv, num_pages, page_size, block, max_pages, k, v, dt) of a paged cache of 8 bits, or an error."""
+    h_kv, num_pages, page_size, max_pages, k, v = _pages(K_pages, V_pages, table, b)
+    _check(K_scales, "K_scales", torch.float32), _check(V_scales, "V_scales", torch.float32)
+    dt = {torch.float8_e4m3fn: MQA_E4M3, torch.int8: MQA_INT8}.get(K_pages.dtype)
+    if dt is None:
+        raise TypeError(f"cache dtype {K_pages.dtype} not supported (float8_e4m3fn or int8)")
+    blocks = K_scales.shape[-1] if K_scales.dim() else 0
+    if K_scales.shape != K_pages.shape[:-2] + (blocks,) or V_scales.shape != K_scales.shape or blocks <= 0 or page_size % blocks:
+        raise ValueError(f"scales {tuple(K_scales.shape)} and {tuple(V_scales.shape)} must be {tuple(K_pages.shape[:-2])} and a divisor of the page size {page_size}")
+    return h_kv, num_pages, page_size, page_size // blocks, max_pages, k, v, dt
+
+
+def mqa_paged_scaled_append_kv_rows(K_pages, K_scales, V_pages, V_scales, table, k_new, v_new, lens, lens_out, counts=None, stream=None):
+    """mqa_paged_append_kv_rows for pools of float8_e4m3fn or int8 with scales [num_pages,page_size/block] (multi-query) or [num_pages,h_kv,page_size/block] float32, one for
+    `block` positions of a page and a head: the rows are rounded to 8 bits under a power of two; a block that has rows of the sequence already keeps its scale, or its rows are
+    rounded again under a larger one.  Returns lens_out."""
+    lib = load_library()
+    _check(k_new, "k_new", torch.float32), _check(v_new, "v_new", torch.float32)
+    _check(lens, "lens", torch.int32), _check(lens_out, "lens_out", torch.int32)
+    if counts is not None:
+        _check(counts, "counts", torch.int32)
+    if k_new.dim() < 3:
+        raise ValueError(f"k_new must be [b,n,k] or [b,n,h_kv,k], not {tuple(k_new.shape)}")
+    b, n = k_new.shape[:2]
+    h_kv, num_pages, page_size, block, max_pages, k, v, dt = _scaled_pages(K_pages, K_scales, V_pages, V_scales, table, b)
+    row = (b, n) if K_pages.dim() == 3 else (b, n, h_kv)
+    if (k_new.shape != row + (k,) or v_new.shape != row + (v,) or lens.numel() != b or lens_out.numel() != b
+            or (counts is not None and counts.numel() != b)):
+        raise ValueError(f"shape mismatch in mqa_paged_scaled_append_kv_rows: k_new {tuple(k_new.shape)} v_new {tuple(v_new.shape)} K_pages {tuple(K_pages.shape)}")
+    with _on(_one_device(K_pages, K_scales, V_pages, V_scales, table, k_new, v_new, lens, lens_out, counts), stream):
+        rc = lib.mqa_paged_scaled_append_kv_rows(_ptr(k_new), _ptr(v_new), _ptr(counts), _ptr(K_pages), _ptr(K_scales), _ptr(V_pages), _ptr(V_scales), _ptr(table),
+                                                 _ptr(lens), _ptr(lens_out), b, n, h_kv, num_pages, page_size, block, max_pages, k, v, dt, _stream(stream))
+    if rc != 0:
+        raise MqaError("mqa_paged_scaled_append_kv_rows", rc)
+    return lens_out
+
+
+def mqa_paged_scaled_decode_workspace_bytes(b, n, h, h_kv, page_size, max_pages, k, v, dt) -> int:
+    """Scratch bytes that mqa_paged_scaled_decode_step uses for these sizes (0: none)."""
+    return int(load_library().mqa_paged_scaled_decode_workspace_bytes(b, n, h, h_kv, page_size, max_pages, k, v, int(dt)))
+
+
+def mqa_paged_scaled_decode_step(q, K_pages, K_scales, V_pages, V_scales, table, lens, o=None, scale=1.0, workspace=None, stream=None):
+    """mqa_paged_decode_step (without scores) over pools of 8 bits as in mqa_paged_scaled_append_kv_rows: q [b,h,k] or [b,n,h,k] -> o [b,h,v] or [b,n,h,v].
+    Workspace: a block of the call's own unless given."""
+    lib = load_library()
+    _check(q, "q", torch.float32), _check(lens, "lens", torch.int32)
+    if q.dim() not in (3, 4):
+        raise ValueError(f"q must be [b,h,k] or [b,n,h,k], not {tuple(q.shape)}")
+    b, h, n = q.shape[0], q.shape[-2], q.shape[1] if q.dim() == 4 else 1
+    h_kv, num_pages, page_size, block, max_pages, k, v, dt = _scaled_pages(K_pages, K_scales, V_pages, V_scales, table, b)
+    if q.shape[-1] != k or lens.numel() != b:
+        raise ValueError(f"shape mismatch in mqa_paged_scaled_decode_step: q {tuple(q.shape)} K_pages {tuple(K_pages.shape)} lens {tuple(lens.shape)}")
+    device = _one_device(q, K_pages, K_scales, V_pages, V_scales, table, lens, o, workspace)
+    with _on(device, stream):
+        if o is None:
+            o = torch.empty((*q.shape[:-1], v), dtype=torch.float32, device=device)
+        _check(o, "o", torch.float32)
+        if o.shape != (*q.shape[:-1], v):
+            raise ValueError(f"o must be {(*q.shape[:-1], v)}, not {tuple(o.shape)}")
+        if workspace is None:
+            workspace, nbytes = _call_workspace(mqa_paged_scaled_decode_workspace_bytes(b, n, h, h_kv, page_size, max_pages, k, v, dt), device, stream)
+        else:
+            nbytes = workspace.numel() * workspace.element_size()
+        rc = lib.mqa_paged_scaled_decode_step(_ptr(q), _ptr(K_pages), _ptr(K_scales), _ptr(V_pages), _ptr(V_scales), _ptr(table), _ptr(lens), _ptr(o), b, n, h, h_kv,
+                                              num_pages, page_size, block, max_pages, k, v, dt, float(scale), _ptr(workspace), nbytes, _stream(stream))
+    if rc != 0:
+        raise MqaError("mqa_paged_scaled_decode_step", rc)
+    return o
+
+
+def _int32(**tensors):
+    """Device tensors of int32, contiguous, with as many dimensions as their shapes here have (None: no such tensor), or an error."""
+    for name, (t, shape) in tensors.items():
+        if t is not None:
+            _check(t, name, torch.int32)
+            if t.dim() != len(shape) or any(want is not None and want != got for want, got in zip(shape, t.shape)):
+                raise ValueError(f"{name} must be [{','.join('any' if x is None else str(x) for x in shape)}], not {tuple(t.shape)}")
+
+
+def mqa_paged_fork_pages(table, lens, parents, table_out, lens_out, refs, page_size, stream=None):
+    """Sequence j of table_out [b_out,max_pages] becomes what sequence parents[j] of table [b,max_pages] is, and shares its pages: those that hold its lens positions, -1 behind them;
+    refs [num_pages], how many entries of tables name a page, counts them; lens_out [b_out] receives the length (a parent outside [0,b): empty).  All int32.  What
+    table_out named before is not given back (mqa_paged_free_pages does that).  Returns table_out."""
+    _int32(table=(table, (None, None)), parents=(parents, (None,)), refs=(refs, (None,)))
+    b, max_pages = table.shape
+    _int32(lens=(lens, (b,)), table_out=(table_out, (parents.shape[0], max_pages)), lens_out=(lens_out, (parents.shape[0],)))
+    with _on(_one_device(table, lens, parents, table_out, lens_out, refs), stream):
+        rc = load_library().mqa_paged_fork_pages(_ptr(table), _ptr(lens), _ptr(parents), _ptr(table_out), _ptr(lens_out), _ptr(refs), b, parents.shape[0],
+                                                 refs.shape[0], int(page_size), max_pages, _stream(stream))
+    _rc("mqa_paged_fork_pages", rc)
+    return table_out
+
+
+def mqa_paged_free_pages(table, lens, refs, page_size, stream=None):
+    """The pages of table [b,max_pages] behind every sequence's first lens [b] positions (0: all of them) are given back: their refs [num_pages] fall by one, their entries become -1.
+    All int32.  Returns table."""
+    _int32(table=(table, (None, None)), refs=(refs, (None,)))
+    _int32(lens=(lens, (table.shape[0],)))
+    with _on(_one_device(table, lens, refs), stream):
+        rc = load_library().mqa_paged_free_pages(_ptr(table), _ptr(lens), _ptr(refs), table.shape[0], refs.shape[0], int(page_size), table.shape[1], _stream(stream))
+    _rc("mqa_paged_free_pages", rc)
+    return table
+
+
+def mqa_paged_reserve_pages(table, lens, refs, page_size, n, counts=None, granted=None, moves=None, workspace=None, stream=None):
+    """Free pages (those with refs [num_pages] of 0) into table [b,max_pages] for the next n positions of every sequence, counts [b] of them where given, and in place of shared pages that
+    they reach.  granted [b]: how many positions (counts of the append that follows; 0 where the pages do not suffice, and the sequence is as it was); moves
+    [b,2]: the begun page that is to be copied by mqa_paged_copy_pages, and the one it is copied to, or -1.  All int32.  Returns (granted, moves)."""
+    _int32(table=(table, (None, None)), refs=(refs, (None,)))
+    b, max_pages = table.shape
+    _int32(lens=(lens, (b,)), counts=(counts, (b,)), granted=(granted, (b,)), moves=(moves, (b, 2)))
+    lib, n, page_size = load_library(), max(-1, min(int(n), 2 ** 31 - 1)), int(page_size)
+    device = _one_device(table, lens, refs, counts, granted, moves, workspace)
+    with _on(device, stream):
+        if granted is None:
+            granted = torch.empty((b,), dtype=torch.int32, device=device)
+        if moves is None:
+            moves = torch.empty((b, 2), dtype=torch.int32, device=device)
+        if workspace is None:
+            workspace, nbytes = _call_workspace(lib.mqa_paged_reserve_workspace_bytes(b, n, refs.shape[0], page_size, max_pages), device, stream)
+        else:
+            nbytes = workspace.numel() * workspace.element_size()
+        rc = lib.mqa_paged_reserve_pages(_ptr(table), _ptr(lens), _ptr(counts), _ptr(refs), _ptr(granted), _ptr(moves), b, n, refs.shape[0], page_size, max_pages,
+                                         _ptr(workspace), nbytes, _stream(stream))
+    _rc("mqa_paged_reserve_pages", rc)
+    return granted, moves
+
+
+def mqa_paged_compact_pages(table, refs, table_out, refs_out, moves, used, workspace=None, stream=None):
+    """The pages in use (refs [num_pages] above 0) that lie behind the first used[0], as many as there are, move to the free ones among those: moves [max(1,num_pages//2),2] lists (from, to) for
+    mqa_paged_copy_pages, -1 behind them; table_out [b,max_pages] and refs_out [num_pages], other tensors than table and refs, go by the new places.  All int32; every table of
+    the pool has to be in the call.  Returns moves."""
+    _int32(table=(table, (None, None)), refs=(refs, (None,)), used=(used, (1,)))
+    b, max_pages = table.shape
+    num_pages = refs.shape[0]
+    _int32(table_out=(table_out, (b, max_pages)), refs_out=(refs_out, (num_pages,)), moves=(moves, (max(1, num_pages // 2), 2)))
+    lib = load_library()
+    device = _one_device(table, refs, table_out, refs_out, moves, used, workspace)
+    with _on(device, stream):
+        if workspace is None:
+            workspace, nbytes = _call_workspace(lib.mqa_paged_compact_workspace_bytes(b, num_pages, max_pages), device, stream)
+        else:
+            nbytes = workspace.numel() * workspace.element_size()
+        rc = lib.mqa_paged_compact_pages(_ptr(table), _ptr(refs), _ptr(table_out), _ptr(refs_out), _ptr(moves), _ptr(used), b, num_pages, max_pages,
+                                         _ptr(workspace), nbytes, _stream(stream))
+    _rc("mqa_paged_compact_pages", rc)
+    return moves
+
+
+def mqa_paged_copy_pages(pools, moves, stream=None):
+    """Page moves[x,0] of each of the pools (a sequence of tensors [num_pages,...] of any type: K and V pages and their scales, of every layer) is copied to page
+    moves[x,1]; pairs with a page outside the pool are passed over.  moves [m,2] int32; no page may be both copied from and to, or to twice."""
+    pools = list(pools)
+    if not pools:
+        raise ValueError("no pools")
+    for x, t in enumerate(pools):
+        _check(t, f"pools[{x}]")
+        if t.dim() < 2 or t.shape[0] != pools[0].shape[0]:
+            raise ValueError(f"pools[{x}] must be [{pools[0].shape[0] if pools[0].dim() else 'num_pages'},...], not {tuple(t.shape)}")
+    _int32(moves=(moves, (None, 2)))
+    num_pages = pools[0].shape[0]
+    with _on(_one_device(moves, *pools), stream):
+        at = (ctypes.c_void_p * len(pools))(*[_ptr(t) for t in pools])
+        sizes = (ctypes.c_size_t * len(pools))(*[t.numel() // max(1, num_pages) * t.element_size() for t in pools])
+        rc = load_library().mqa_paged_copy_pages(at, sizes, len(pools), _ptr(moves), moves.shape[0], num_pages, _stream(stream))
+    _rc("mqa_paged_copy_pages", rc)
+
+
+def mqa_stack_adjust_logits(logits, history, lens, drafts=None, prompts=None, repetition=None, frequency=None, presence=None, bias_tokens=None, biases=None,
+                            allowed=None, out=None, stream=None):
+    """logits [b,n+1,vocab] float32 (or [b,vocab]: n = 0) -> out (may be logits).  Row j of a sequence stands behind the first lens [b] tokens of history [b,cap], the first prompts [b] of them its
+    prompt's (None: 0), and the drafts [b,n] before draft j.  A token among them: x / repetition [b] (x > 0) or x * repetition; one that is there c times, c > 0, behind the prompt: less
+    frequency [b] * c + presence [b]; then the last of the biases [b,m] whose bias_tokens [b,m] is the token is added; tokens whose bit of allowed [b,n+1,ceil(vocab/32)] (int32 words, lowest bit
+    first; None: all) is not set become -infinity.  Tokens and lengths are int32."""
+    lib = load_library()
+    _check(logits, "logits", torch.float32)
+    if logits.dim() not in (2, 3):
+        raise ValueError(f"logits must be [b,n+1,vocab] or [b,vocab], not {tuple(logits.shape)}")
+    b, vocab, n = logits.shape[0], logits.shape[-1], logits.shape[1] - 1 if logits.dim() == 3 else 0
+    m = 0 if biases is None else biases.shape[-1] if biases.dim() else -1
+    lead = (b,) if logits.dim() == 2 else (b, n + 1)
+    _int32(history=(history, (b, None)), lens=(lens, (b,)), drafts=(drafts, (b, n)), prompts=(prompts, (b,)), bias_tokens=(bias_tokens, (b, m)),
+           allowed=(allowed, lead + ((vocab + 31) // 32,)))
+    for name, t, shape in (("repetition", repetition, (b,)), ("frequency", frequency, (b,)), ("presence", presence, (b,)), ("biases", biases, (b, m)), ("out", out, logits.shape)):
+        if t is not None:
+            _check(t, name, torch.float32)
+            if t.shape != shape:
+                raise ValueError(f"{name} must be {tuple(shape)}, not {tuple(t.shape)}")
+    if (biases is None) != (bias_tokens is None):
+        raise ValueError("biases and bias_tokens go together")
+    device = _one_device(logits, history, lens, drafts, prompts, repetition, frequency, presence, bias_tokens, biases, allowed, out)
+    with _on(device, stream):
+        if out is None:
+            out = torch.empty_like(logits)
+        _rc("mqa_stack_adjust_logits", lib.mqa_stack_adjust_logits(_ptr(logits), _ptr(out), _ptr(history), _ptr(lens), _ptr(prompts), _ptr(drafts), _ptr(repetition),
+                                                                   _ptr(frequency), _ptr(presence), _ptr(bias_tokens), _ptr(biases), _ptr(allowed), b, n, vocab,
+                                                                   history.shape[1], m, _stream(stream)))
+    return out
 
 
 def mqa_stream_read(src, sink, stream=None):

@@ -10,7 +10,7 @@ PKG_DIR = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(PKG_DIR, "csrc")
 LIB_PATH = os.path.join(PKG_DIR, "libmqa_decode.so")
 SOURCES = ["api.hip", "decode_mfma.hip", "decode_direct.hip", "prompt_mfma.hip", "decode_generic.hip", "small_kernels.hip", "project.hip", "project_kv.hip", "project_kv_rows.hip", "project_terms.hip", "gemm.hip", "packed.hip", "stack_kernels.hip",
-           "paged_api.hip", "paged_cache.hip", "paged_decode.hip", "verify.hip"]
+           "paged_api.hip", "paged_cache.hip", "paged_decode.hip", "scaled_append.hip", "scaled_decode.hip", "pages.hip", "adjust_logits.hip", "verify.hip"]
 
 HIPCC_FLAGS = [
     "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",

@@ -50,6 +50,9 @@ struct PagedDecode {
   int block_rows, blocks;  // R in blocks
   int split;               // 0: piece g is group g
   float qscale;            // scale * log2(e)
+  const float* K_scales;   // caches of 8 bits: [num_pages, h_kv, page_size / block]
+  const float* V_scales;
+  int block;               // positions of a scale
 };
 
 struct PagedEvict {
@@ -78,6 +81,84 @@ PagedPlan paged_plan(int b, int n, int h, int h_kv, int page_size, int max_pages
 void paged_workspace(PagedDecode* p, const PagedPlan& plan, void* workspace);        // where its parts are
 hipError_t launch_paged_decode(const PagedDecode& p, const PagedPlan& plan, int is_bf16, hipStream_t st);
 hipError_t launch_paged_evict(const PagedEvict& p, int is_bf16, hipStream_t st);
+
+// ---- caches of 8 bits (scaled_append.hip, scaled_decode.hip): `type` is MQA_E4M3 or MQA_INT8
+struct ScaledAppend {
+  PagedAppend a;
+  float* K_scales;         // [num_pages, h_kv, page_size / block]
+  float* V_scales;
+  int block;               // positions of a scale; divides page_size
+};
+hipError_t launch_scaled_append(const ScaledAppend& p, int is_e4m3, hipStream_t st);
+PagedPlan scaled_plan(int b, int n, int h, int h_kv, int page_size, int max_pages, int k, int v, int is_e4m3);
+hipError_t launch_scaled_decode(const PagedDecode& p, const PagedPlan& plan, int is_e4m3, hipStream_t st);
+
+// ---- who holds which page (pages.hip)
+struct PageFork {
+  const int32_t* table_in;  // [b_in, max_pages]
+  const int32_t* lens_in;   // [b_in]
+  const int32_t* parents;   // [b_out]
+  int32_t* table_out;       // [b_out, max_pages]
+  int32_t* lens_out;        // [b_out]
+  int32_t* refs;            // [num_pages]
+  int b_in, b_out, num_pages, page_size, max_pages;
+};
+struct PageFree {
+  int32_t* table;           // [b, max_pages]
+  const int32_t* lens;      // [b]
+  int32_t* refs;
+  int b, num_pages, page_size, max_pages;
+};
+struct PageReserve {
+  int32_t* table;           // [b, max_pages]
+  const int32_t* lens;      // [b]
+  const int32_t* counts;    // [b], or null: n each
+  int32_t* refs;
+  int32_t* granted;         // [b]
+  int32_t* moves;           // [b, 2]
+  int b, n, num_pages, page_size, max_pages;
+};
+struct PageCompact {
+  const int32_t* table_in;  // [b, max_pages]
+  const int32_t* refs_in;   // [num_pages]
+  int32_t* table_out;
+  int32_t* refs_out;
+  int32_t* moves;           // [moves_size, 2]
+  int32_t* used;            // [1]
+  int b, num_pages, max_pages, moves_size;
+};
+constexpr int kCopyPools = 16;          // of a launch
+struct PageCopy {
+  void* pool[kCopyPools];
+  uint32_t page_bytes[kCopyPools];
+  const int32_t* moves;     // [m, 2]
+  int pools, m, num_pages;
+};
+hipError_t launch_fork(const PageFork& p, hipStream_t st);
+hipError_t launch_free(const PageFree& p, hipStream_t st);
+size_t reserve_workspace_bytes(int b, int n, int num_pages, int page_size);
+hipError_t launch_reserve(const PageReserve& p, void* workspace, hipStream_t st);
+size_t compact_workspace_bytes(int num_pages);
+hipError_t launch_compact(const PageCompact& p, void* workspace, hipStream_t st);
+hipError_t launch_copy_pages(const PageCopy& p, hipStream_t st);
+
+// adjust_logits.hip
+struct AdjustLogits {
+  const float* logits;        // [b, n + 1, vocab]
+  float* out;                 // the same, perhaps the same array
+  const int32_t* history;     // [b, cap]
+  const int32_t* lens;        // [b]
+  const int32_t* prompts;     // [b], or null: 0 each
+  const int32_t* drafts;      // [b, n]
+  const float* repetition;    // [b], or null: 1
+  const float* frequency;     // [b], or null: 0
+  const float* presence;      // [b], or null: 0
+  const int32_t* bias_tokens; // [b, biases]
+  const float* bias_values;   // [b, biases]
+  const uint32_t* allowed;    // [b, n + 1, ceil(vocab / 32)], or null: all
+  int b, n, vocab, cap, biases;
+};
+hipError_t launch_adjust(const AdjustLogits& p, hipStream_t st);
 
 // verify.hip
 struct Verify {

@@ -1,0 +1,106 @@
+// New rows into paged caches of 8 bits.
+//
+// A block of `block` positions and a head has one scale for K and one for V.  Of a block that gets rows, with a the largest finite |x| of its new rows and Q the
+// type's largest number: s' = the smallest power of two >= 2^-126 with a <= Q s'; its scale becomes s' where its first row is new, else max(s_old, s'), and the
+// rows that it had are rounded again, from q to round(q s_old / s), where that is more than s_old.  (Powers of two: the quotients are exact, so that rounding them again and again is off by less
+// than a step, and e4m3, whose steps go by the number's own size, loses nothing over other scales; int8 loses half a bit on average.)
+#include "paged.hpp"
+#include "scaled.hpp"
+
+namespace mqa {
+namespace {
+
+__device__ __forceinline__ float finite_size(float x) {
+  const float a = fabsf(x);
+  return a < INFINITY ? a : 0.f;
+}
+
+// A unit, (sequence, one of the blocks that its new rows reach, head, K or V), is THREADS threads' work: 64, or 256 where a block has many values.  Its rows are one run of
+// memory in the pool, and h_kv apart in the new rows.
+template <bool E4M3, int THREADS>
+__global__ __launch_bounds__(256)
+void scaled_append_kernel(ScaledAppend p, int reach) {
+  __shared__ float s_most[4];
+  const PagedCache& c = p.a.c;
+  const int lane = threadIdx.x % THREADS;
+  unsigned unit = blockIdx.x * (256u / THREADS) + threadIdx.x / THREADS;
+  if (unit >= (unsigned)p.a.b * reach * c.h_kv * 2) return;
+  const bool is_v = unit & 1;
+  unit >>= 1;
+  const int e = (int)(unit % (unsigned)c.h_kv);
+  unit /= (unsigned)c.h_kv;
+  const int turn = (int)(unit % (unsigned)reach), i = (int)(unit / (unsigned)reach);
+  const int L = p.a.lens_in[i];
+  const int count = p.a.counts ? min(max(p.a.counts[i], 0), p.a.n) : p.a.n;
+  const bool fits = L >= 0 && L <= c.positions() - count;
+  if (lane == 0 && turn == 0 && e == 0 && !is_v) p.a.lens_out[i] = fits ? L + count : L;
+  if (!fits) return;
+  const int first = (L / p.block + turn) * p.block;              // the block's first position, and its rows that are new
+  const int begin = max(first, L), end = min(first + p.block, L + count);
+  if (begin >= end) return;
+  const int row = paged_row(c, c.table + (size_t)i * c.max_pages, e, first);
+  if (row < 0) return;
+  const int w4 = (is_v ? c.v : c.k) >> 2;
+  float* const scale_at = (is_v ? p.V_scales : p.K_scales) + row / p.block;
+  uint32_t* const held = static_cast<uint32_t*>(is_v ? c.V : c.K) + (size_t)row * w4;
+  const float4* const fresh = reinterpret_cast<const float4*>(is_v ? p.a.v_new : p.a.k_new) + (((size_t)i * p.a.n + (begin - L)) * c.h_kv + e) * w4;
+  const int older = (begin - first) * w4, all = (end - begin) * w4;
+  const float had = *scale_at;
+  auto new4 = [&](int x) {
+    const int r = x / w4;
+    return fresh[(size_t)r * c.h_kv * w4 + (x - r * w4)];
+  };
+  float most = 0.f;
+  for (int x = lane; x < all; x += THREADS) {
+    const float4 y = new4(x);
+    most = fmaxf(most, fmaxf(fmaxf(finite_size(y.x), finite_size(y.y)), fmaxf(finite_size(y.z), finite_size(y.w))));
+  }
+#pragma unroll
+  for (int off = 32; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor(most, off));
+  if constexpr (THREADS == 256) {
+    if ((lane & 63) == 0) s_most[lane >> 6] = most;
+    __syncthreads();
+    most = fmaxf(fmaxf(s_most[0], s_most[1]), fmaxf(s_most[2], s_most[3]));
+  }
+  float s = scale_of<E4M3>(most);
+  if (older > 0 && had > s) s = had;                             // (a scale that is no number gives way)
+  const bool power = (__float_as_uint(s) & 0x007fffffu) == 0 && s >= 0x1p-126f && s <= 0x1p126f;
+  const float inv = power ? inverse_of(s) : 0.f;
+  if (older > 0 && s != had) {
+    const float ratio = had / s;
+    for (int x = lane; x < older; x += THREADS) {
+      float4 y = values4<E4M3>(held[x]);
+      y.x *= ratio; y.y *= ratio; y.z *= ratio; y.w *= ratio;
+      held[x] = round4<E4M3>(y);
+    }
+  }
+  for (int x = lane; x < all; x += THREADS) {
+    float4 y = new4(x);
+    if (power) { y.x *= inv; y.y *= inv; y.z *= inv; y.w *= inv; }
+    else { y.x /= s; y.y /= s; y.z /= s; y.w /= s; }             // (a scale that the caller has written)
+    held[older + x] = round4<E4M3>(y);
+  }
+  if constexpr (THREADS == 256) __syncthreads();                 // (every wave has read the scale)
+  if (lane == 0 && (older == 0 || s != had)) *scale_at = s;
+}
+
+}  // namespace
+
+hipError_t launch_scaled_append(const ScaledAppend& p, int is_e4m3, hipStream_t st) {
+  const int reach = (p.a.n + p.block - 2) / p.block + 1;         // blocks that n rows reach, at most
+  const unsigned units = (unsigned)p.a.b * reach * p.a.c.h_kv * 2;
+  const int wide = p.a.c.k > p.a.c.v ? p.a.c.k : p.a.c.v;
+  const int rows = p.block < p.a.n ? p.block : p.a.n;
+  const bool large = (long long)rows * wide > 8192;
+  const unsigned grid = large ? units : (units + 3) / 4;
+  if (is_e4m3) {
+    if (large) hipLaunchKernelGGL((scaled_append_kernel<true, 256>), dim3(grid), dim3(256), 0, st, p, reach);
+    else hipLaunchKernelGGL((scaled_append_kernel<true, 64>), dim3(grid), dim3(256), 0, st, p, reach);
+  } else {
+    if (large) hipLaunchKernelGGL((scaled_append_kernel<false, 256>), dim3(grid), dim3(256), 0, st, p, reach);
+    else hipLaunchKernelGGL((scaled_append_kernel<false, 64>), dim3(grid), dim3(256), 0, st, p, reach);
+  }
+  return hipGetLastError();
+}
+
+}  // namespace mqa

@@ -1,0 +1,148 @@
+"""Adjusted logits on the GPU against the float64 oracle (oracle/serving.py)."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+EPS = 2.0 ** -24          # half a step of float32
+
+
+@pytest.fixture(scope="module")
+def m():
+    import paper_1911_02150_amd as mod
+    mod.load_library()
+    return mod
+
+
+def on(x):
+    return None if x is None else torch.from_numpy(np.ascontiguousarray(x)).to(DEV)
+
+
+def words(allowed):
+    """[..., vocab] truth values as int32 words, lowest bit first."""
+    vocab = allowed.shape[-1]
+    padded = np.zeros((*allowed.shape[:-1], (vocab + 31) // 32 * 32), dtype=np.uint8)
+    padded[..., :vocab] = allowed
+    return np.packbits(padded, axis=-1, bitorder="little").view(np.int32)
+
+
+def case(rng, b, n, vocab, cap, biases, parts):
+    """Arguments for the oracle, and for the call; `parts`: which of the optional ones are there."""
+    tokens = lambda *shape: np.where(rng.random(shape) < 0.05, rng.choice([-1, vocab, 2 ** 31 - 1, -2 ** 31], shape),  # noqa: E731
+                                     (vocab * rng.random(shape) ** 3).astype(np.int64)).astype(np.int32)
+    a = dict(logits=(3 * rng.standard_normal((b, n + 1, vocab))).astype(np.float32), history=tokens(b, cap), lens=rng.integers(-2, cap + 3, b).astype(np.int32))
+    if n:
+        a["drafts"] = tokens(b, n)
+    f = lambda *shape: rng.random(shape).astype(np.float32)  # noqa: E731
+    optional = dict(prompts=rng.integers(-1, cap + 2, b).astype(np.int32), repetition=1 + f(b), frequency=f(b), presence=f(b) - np.float32(0.5),
+                    bias_tokens=tokens(b, max(1, biases)), biases=(4 * f(b, max(1, biases)) - 2), allowed=rng.random((b, n + 1, vocab)) < 0.6)
+    a.update({x: y for x, y in optional.items() if x in parts or (x == "bias_tokens" and "biases" in parts)})
+    kw = {x: on(words(y) if x == "allowed" else y) for x, y in a.items()}
+    return a, kw
+
+
+def tolerance(want, a):
+    """Half a step for the quotient or product, the two parts of the penalty, their sum, its difference and the bias, each of what is added up at most."""
+    x = np.abs(a["logits"]) * (1 if "repetition" not in a else a["repetition"].max())
+    most = sum(np.abs(a[y]).max() * z for y, z in (("frequency", a["history"].shape[1] + want.shape[1]), ("presence", 1)) if y in a) + (np.abs(a["biases"]).max() if "biases" in a else 0)
+    return EPS * 6 * (x + most)
+
+
+EVERY = ("prompts", "repetition", "frequency", "presence", "biases", "allowed")
+# b, n, vocab, cap, biases, which parts
+CASES = [
+    (1, 0, 1, 1, 1, EVERY),
+    (1, 0, 32768, 500, 0, ("prompts", "repetition", "frequency", "presence", "allowed")),
+    (3, 4, 1000, 64, 20, EVERY),
+    (2, 2, 2048, 300, 700, EVERY),
+    (2, 1, 2049, 300, 5, EVERY),
+    (2, 3, 4100, 2000, 5, EVERY),
+    (5, 0, 333, 7, 1, EVERY),
+    (2, 8, 97, 1, 3, EVERY),
+    (4, 2, 5000, 100, 0, ()),
+    (4, 2, 5001, 100, 0, ("frequency",)),
+    (2, 0, 640, 50, 0, ("repetition",)),
+    (2, 5, 640, 50, 0, ("presence", "prompts")),
+    (2, 5, 31, 50, 9, ("biases",)),
+    (2, 5, 65, 50, 0, ("allowed",)),
+    (1, 30, 512, 10, 4, EVERY),
+    (70, 1, 513, 40, 4, EVERY),
+    (300, 0, 8192, 90, 4, EVERY),
+]
+
+
+@pytest.mark.parametrize("b,n,vocab,cap,biases,parts", CASES)
+def test_adjust(m, b, n, vocab, cap, biases, parts):
+    from oracle import serving
+    rng = np.random.default_rng(b + n + vocab)
+    a, kw = case(rng, b, n, vocab, cap, biases, parts)
+    want = serving.adjust(**a)
+    logits = kw["logits"].clone()
+    got = m.mqa_stack_adjust_logits(**kw)
+    assert got is not kw["logits"] and torch.equal(kw["logits"], logits)
+    x = got.cpu().numpy().astype(np.float64)
+    hidden = np.isneginf(want)
+    assert np.array_equal(np.isneginf(x), hidden)
+    assert (np.abs(np.where(hidden, 0, x) - np.where(hidden, 0, want)) <= tolerance(want, a)).all()
+    assert m.mqa_stack_adjust_logits(**kw, out=kw["logits"]) is kw["logits"] and torch.equal(kw["logits"], got)      # in place
+    if n == 0:
+        flat = dict(kw, logits=logits[:, 0].contiguous())
+        if "allowed" in flat:
+            flat["allowed"] = flat["allowed"][:, 0].contiguous()
+        assert torch.equal(m.mqa_stack_adjust_logits(**flat), got[:, 0])
+
+
+def test_what_nothing_touches_stays(m):
+    """Tokens that are not there keep their logits, bit for bit; NaN and infinities too; what is not allowed is -infinity whatever it was; a mask may leave nothing."""
+    rng = np.random.default_rng(0)
+    logits = rng.standard_normal((2, 2, 100)).astype(np.float32)
+    logits[:, :, 3], logits[:, :, 4], logits[:, :, 5], logits[:, :, 6] = np.nan, np.inf, -np.inf, -0.0
+    allowed = np.ones((2, 2, 100), dtype=bool)
+    allowed[1, 1] = False
+    allowed[0, 0, 3:5] = False
+    one = np.ones(2, dtype=np.float32)
+    got = m.mqa_stack_adjust_logits(on(logits), on(np.array([[50, 51], [5, 4]], dtype=np.int32)), on(np.array([2, 2], dtype=np.int32)), drafts=on(np.array([[52], [6]], dtype=np.int32)),
+                                    repetition=on(2 * one), frequency=on(one), presence=on(np.array([np.inf, 1], dtype=np.float32)), allowed=on(words(allowed))).cpu().numpy()
+    rest = np.ones(100, dtype=bool)
+    rest[50:53] = False
+    rest[3:5] = False
+    assert np.array_equal(got[0, 1][rest].view(np.int32), logits[0, 1][rest].view(np.int32)) and np.isnan(got[0, 1, 3]) and got[0, 1, 4] == np.inf
+    assert np.isneginf(got[0, 0, 3:5]).all() and np.isneginf(got[0, 0, 50:52]).all() and got[0, 0, 52] == logits[0, 0, 52] and np.isneginf(got[0, 1, 52])
+    assert got[1, 0, 4] == np.inf and np.isneginf(got[1, 0, 5]) and got[1, 0, 6] == 0 and np.isneginf(got[1, 1]).all()
+
+
+def test_streams_and_graphs(m):
+    rng = np.random.default_rng(6)
+    a, kw = case(rng, 3, 2, 3000, 200, 10, EVERY)
+    out = torch.empty_like(kw["logits"])
+    m.mqa_stack_adjust_logits(**kw, out=out)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        m.mqa_stack_adjust_logits(**kw, out=out)
+    side = torch.cuda.Stream()
+    for turn in range(4):
+        _, new = case(rng, 3, 2, 3000, 200, 10, EVERY)
+        for x, y in kw.items():
+            y.copy_(new[x])
+        graph.replay()
+        torch.cuda.synchronize()
+        want = m.mqa_stack_adjust_logits(**kw)
+        assert torch.equal(out, want)
+        side.wait_stream(torch.cuda.current_stream())
+        there = m.mqa_stack_adjust_logits(**kw, stream=side)
+        torch.cuda.current_stream().wait_stream(side)
+        assert torch.equal(there, want)
+
+
+def test_what_the_binding_refuses(m):
+    x, h, lens = torch.zeros((2, 3, 50), device=DEV), torch.zeros((2, 4), dtype=torch.int32, device=DEV), torch.zeros(2, dtype=torch.int32, device=DEV)
+    f = torch.zeros(2, device=DEV)
+    drafts = torch.zeros((2, 2), dtype=torch.int32, device=DEV)
+    m.mqa_stack_adjust_logits(x, h, lens, drafts=drafts)
+    for kw, error in ((dict(), m.MqaError), (dict(drafts=drafts[:, :1].contiguous()), ValueError), (dict(drafts=drafts.long()), TypeError),
+                      (dict(drafts=drafts, repetition=f[:1]), ValueError), (dict(drafts=drafts, biases=torch.zeros((2, 3), device=DEV)), ValueError),
+                      (dict(drafts=drafts, bias_tokens=drafts), ValueError), (dict(drafts=drafts, allowed=torch.zeros((2, 3, 1), dtype=torch.int32, device=DEV)), ValueError),
+                      (dict(drafts=drafts, out=x[:, :2].contiguous()), ValueError), (dict(drafts=drafts, prompts=lens.cpu()), ValueError)):
+        with pytest.raises(error):
+            m.mqa_stack_adjust_logits(x, h, lens, **kw)
