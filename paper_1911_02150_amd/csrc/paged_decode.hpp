@@ -303,6 +303,7 @@ void paged_list_kernel(PagedDecode p) {
 
 // The sequence that a piece is of, which of the sequence's pieces (`off`), and how many a head has (`c`); false: there is no such piece.  Every workgroup looks at all
 // lengths: thread t has sequences t * each up to the next one's.
+template <int LEAST>
 __device__ __forceinline__ bool look_for(const PagedDecode& p, int piece, Segment* s, int* off, int* c) {
   __shared__ int s_waves[8][kThreads / 64], s_longest[kThreads / 64];
   __shared__ int s_at[4];
@@ -346,7 +347,7 @@ __device__ __forceinline__ bool look_for(const PagedDecode& p, int piece, Segmen
     fits = left_whole(p, longest, total);
     if (fits) cut(longest);
   }
-  for (int most = kComputeUnits; most <= 2 * kComputeUnits; most *= 2) {
+  for (int most = LEAST * kComputeUnits; most <= 2 * kComputeUnits; most *= 2) {
     const int units = most / p.blocks;
     if (!fits && p.b * heads <= units)
       for (int x = 8; x <= 10 && !fits; ++x) {
@@ -377,6 +378,7 @@ __device__ __forceinline__ bool look_for(const PagedDecode& p, int piece, Segmen
 }
 
 // This workgroup's segment; false: there is none.
+template <int LEAST>
 __device__ __forceinline__ bool find_segment(const PagedDecode& p, Segment* s) {
   const int tid = threadIdx.x, heads = p.c.h_kv;
   int piece = blockIdx.x, block = 0;
@@ -404,7 +406,7 @@ __device__ __forceinline__ bool find_segment(const PagedDecode& p, Segment* s) {
     off = piece - work.y * heads;
     c = work.z;
     s->L = paged_length(p.c, work.w);
-  } else if (!look_for(p, piece, s, &off, &c)) {
+  } else if (!look_for<LEAST>(p, piece, s, &off, &c)) {
     return false;
   }
   s->e = heads == 1 ? 0 : off / c;
@@ -882,10 +884,10 @@ void paged_matrix_kernel(PagedDecode p) {
   typedef Form<T, D> F;
   extern __shared__ __align__(16) unsigned char smem[];
   __shared__ __align__(16) int s_rows[kWaves][2][32];
-  __shared__ __align__(16) float s_scales[kScaled<T> ? kWaves : 1][2][32];
+  __shared__ __align__(16) float s_scales[kScaled<T> ? kWaves : 1][2][2][32];
   __shared__ int s_odd;
   Segment s;
-  if (!find_segment(p, &s)) return;
+  if (!find_segment<kScaled<T> ? 2 : 1>(p, &s)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i16 = lane & 15, g = lane >> 4;
   int (&places)[2][32] = s_rows[wave];
   const int32_t* table = p.c.table + (size_t)s.i * p.c.max_pages;
@@ -904,19 +906,25 @@ void paged_matrix_kernel(PagedDecode p) {
   };
   Tile<T, D> tl;
   int k_row[2], v_row[8];                                  // of the tile that is loaded next
-  // 8 bits: a lane asks for its position's scales with its place; they pass through LDS when the tile's turn has come
+  // 8 bits: a lane asks for its position's scales when it has its place, and puts them into LDS a tile later, when they are there
   const bool whole_power = kScaled<T> && (p.block & (p.block - 1)) == 0;
   const int shift = kScaled<T> ? __builtin_ctz(p.block) : 0;
-  float next_ks = 0.f, next_vs = 0.f, turn_ks = 0.f, turn_vs = 0.f;
+  float next_ks = 0.f, next_vs = 0.f;
+  auto put_scales = [&](int buf, uint32_t missing) {
+    float (&own)[2][32] = s_scales[wave][buf];
+    const bool there = !(missing >> (lane & 31) & 1);
+    own[0][lane & 31] = there ? next_ks : 0.f;
+    own[1][lane & 31] = there ? next_vs : 0.f;
+    asm volatile("" ::: "memory");
+  };
   auto publish = [&](const Place& x, int buf) -> uint32_t {      // bit e of what is returned: position e of the tile is not there
     const bool there = (unsigned)x.entry < (unsigned)p.c.num_pages;
     const int row = there ? (x.entry * p.c.h_kv + s.e) * p.c.page_size + x.inside : 0;
     places[buf][lane & 31] = row;
     if constexpr (kScaled<T>) {
       const unsigned at = whole_power ? (unsigned)row >> shift : (unsigned)row / (unsigned)p.block;
-      const float ks = p.K_scales[at], vs = p.V_scales[at];
-      next_ks = there ? ks : 0.f;
-      next_vs = there ? vs : 0.f;
+      next_ks = p.K_scales[at];
+      next_vs = p.V_scales[at];
     }
     asm volatile("" ::: "memory");
     return (uint32_t)__ballot(!there);
@@ -973,8 +981,7 @@ void paged_matrix_kernel(PagedDecode p) {
   rows.begin(p, s, s.row0, lane);
   if constexpr (kScaled<T>) {
     rows.take_exponents(qs, lane);
-    turn_ks = next_ks;
-    turn_vs = next_vs;
+    put_scales(0, bad);
   }
   uint32_t bad_next = publish(next, 1);
   next = look_up(wave + 2 * kWaves);
@@ -990,18 +997,13 @@ void paged_matrix_kernel(PagedDecode p) {
     }
     Scales scales;
     if constexpr (kScaled<T>) {
-      float (&own)[2][32] = s_scales[wave];
-      own[0][lane & 31] = turn_ks;
-      own[1][lane & 31] = turn_vs;
-      asm volatile("" ::: "memory");
+      const float (&own)[2][32] = s_scales[wave][buf ^ 1];
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         const float4 a = reinterpret_cast<const float4*>(own[0])[2 * g + x], b = reinterpret_cast<const float4*>(own[1])[2 * g + x];
         scales.k[4 * x] = a.x; scales.k[4 * x + 1] = a.y; scales.k[4 * x + 2] = a.z; scales.k[4 * x + 3] = a.w;
         scales.v[4 * x] = b.x; scales.v[4 * x + 1] = b.y; scales.v[4 * x + 2] = b.z; scales.v[4 * x + 3] = b.w;
       }
-      turn_ks = next_ks;
-      turn_vs = next_vs;
     }
     floatx4 sc[2][HB];
     Turned<T, D> turned;
@@ -1010,6 +1012,7 @@ void paged_matrix_kernel(PagedDecode p) {
       else if (x & 1) load_k(x >> 1);
       R::turn(tl, x, turned);
     });
+    if constexpr (kScaled<T>) put_scales(buf, bad_next);
     bad = bad_next;
     buf ^= 1;
     bad_next = publish(next, buf);                         // places of the tile after the next one
