@@ -377,7 +377,7 @@ __device__ __forceinline__ bool look_for(const PagedDecode& p, int piece, Segmen
   return true;
 }
 
-// This workgroup's segment; false: there is none.
+// This workgroup's segment; false: there is none.  LEAST: workgroups of a compute unit that are tried first.
 template <int LEAST>
 __device__ __forceinline__ bool find_segment(const PagedDecode& p, Segment* s) {
   const int tid = threadIdx.x, heads = p.c.h_kv;
@@ -431,17 +431,12 @@ __device__ __forceinline__ bool find_segment(const PagedDecode& p, Segment* s) {
 //     8 (i / 4) + 4u + i % 4 of the tile, so that lane (row, g) ends up with positions 8g .. 8g + 7: the weights are the second product's operand as they are.
 //   out^T[D cols x 16 rows] += V_tile^T . weights^T: lane (c, g) has 1/16 of the columns of rows 8g .. 8g + 7.
 // bf16: v_mfma_f32_16x16x32_bf16, q and the weights as three bf16 terms (24 bits: the float32 itself), V transposed 8 x 8 inside the lane.  float32:
-// v_mfma_f32_16x16x4_f32.  8 bits: a value is exact in 16; K as fp16 against q as two fp16 terms of a row brought to 2^13 .. 2^14 by a power of two (23 bits), V as
-// bf16 against the weights, each times its position's scale, as three bf16 terms; a K row's 16 bytes are two products' columns.  The rows' places are looked up a tile ahead: a lane has a position's table entry, the wave's 32 rows pass through LDS.
+// v_mfma_f32_16x16x4_f32.  The rows' places are looked up a tile ahead: a lane has a position's table entry, the wave's 32 rows pass through LDS.
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
 typedef __attribute__((ext_vector_type(4))) float floatx4;
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 typedef __attribute__((ext_vector_type(8))) uint32_t u32x8;
 typedef __attribute__((ext_vector_type(2))) uint32_t u32x2;
-typedef __attribute__((ext_vector_type(1))) uint32_t u32x1;
-typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
-typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 constexpr float kSlack = 8.f;        // log2 of the largest weight kept before the running maximum is moved (all rows of a wave together)
 
 __device__ __forceinline__ floatx4 mfma_bf16(const u32x4& a, const u32x4& b, const floatx4& c) {
@@ -456,60 +451,16 @@ __device__ __forceinline__ void split3(float a, float b, uint32_t (&t)[3]) {
   t[2] = pack_bf16_pair(a - __uint_as_float(t[1] << 16), b - __uint_as_float(t[1] & 0xffff0000u));
 }
 
-// The same with two fp16 terms, 23 bits of a float that is not too small.
-__device__ __forceinline__ floatx4 mfma_f16(const u32x4& a, const u32x4& b, const floatx4& c) {
-  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
-}
-__device__ __forceinline__ void split2(float a, float b, uint32_t (&t)[2]) {
-  const f16x2 hi = {(_Float16)a, (_Float16)b};
-  t[0] = __builtin_bit_cast(uint32_t, hi);
-  t[1] = __builtin_bit_cast(uint32_t, f16x2{(_Float16)(a - (float)hi[0]), (_Float16)(b - (float)hi[1])});
-}
-// Two of a word's values of 8 bits (the upper ones: `upper`) as fp16 and as bf16, both exact.
-template <typename T>
-__device__ __forceinline__ uint32_t two_f16(uint32_t u, bool upper) {
-  if constexpr (std::is_same<T, E4M3>::value) {
-    return __builtin_bit_cast(uint32_t, upper ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(u, 1.f, true) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(u, 1.f, false));
-  } else {                                                // 1024 + 128 + x is 0x6480 + x
-    const uint32_t biased = __builtin_amdgcn_perm(0x64646464u, u ^ 0x80808080u, upper ? 0x04030402u : 0x04010400u);
-    return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, biased) - f16x2{(_Float16)1152.f, (_Float16)1152.f});
-  }
-}
-// Values 2 x and 2 x + 1 of two rows, as bf16 pairs of one column each.
-template <typename T>
-__device__ __forceinline__ void turn2(uint32_t row0, uint32_t row1, bool upper, uint32_t* col0, uint32_t* col1) {
-  if constexpr (std::is_same<T, E4M3>::value) {
-    const uint32_t a = __builtin_bit_cast(uint32_t, upper ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(row0, 1.f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(row0, 1.f, false));
-    const uint32_t b = __builtin_bit_cast(uint32_t, upper ? __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(row1, 1.f, true) : __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(row1, 1.f, false));
-    *col0 = __builtin_amdgcn_perm(b, a, 0x05040100u);
-    *col1 = __builtin_amdgcn_perm(b, a, 0x07060302u);
-  } else {                                                // (a float of seven bits is bf16 and zeros)
-    const int at = upper ? 16 : 0;
-    auto value = [at](uint32_t u, int x) { return __float_as_uint((float)(int8_t)(u >> (at + 8 * x))); };
-    *col0 = __builtin_amdgcn_perm(value(row1, 0), value(row0, 0), 0x07060302u);
-    *col1 = __builtin_amdgcn_perm(value(row1, 1), value(row0, 1), 0x07060302u);
-  }
-}
-
 template <typename T, int D> struct Form;
-template <int D> struct Form8 {
-  static constexpr int kPieces = D / 32, kLoads = D / 64;
-  static constexpr int kTerms = 2;
-  static constexpr int kColumns = D / 16;
-  typedef typename std::conditional<D == 256, u32x4, typename std::conditional<D == 128, u32x2, u32x1>::type>::type VRow;
-  static __device__ __forceinline__ int column(int i, int j4) { return kColumns * i + 4 * j4; }
-};
-template <int D> struct Form<E4M3, D> : Form8<D> {};
-template <int D> struct Form<Int8, D> : Form8<D> {};
 template <int D> struct Form<uint16_t, D> {
-  static constexpr int kPieces = D / 32, kLoads = kPieces; // pieces of a K row in a lane that are multiplied at a time, and 16-byte loads
+  static constexpr int kPieces = D / 32;                   // 16-byte pieces of a K row in a lane
   static constexpr int kTerms = 3;
   static constexpr int kColumns = D / 16;                  // columns of a lane
   typedef typename std::conditional<D == 256, u32x8, typename std::conditional<D == 128, u32x4, u32x2>::type>::type VRow;
   static __device__ __forceinline__ int column(int i, int j4) { return kColumns * i + 4 * j4; }      // of the products 4 j4 ..: row i
 };
 template <int D> struct Form<float, D> {
-  static constexpr int kPieces = D / 16, kLoads = kPieces;
+  static constexpr int kPieces = D / 16;
   static constexpr int kTerms = 1;
   static constexpr int kColumns = D / 16;
   struct VRow { floatx4 x[D / 64]; };
@@ -525,27 +476,22 @@ template <typename T, int D, int HB> struct Lds {
 };
 
 template <typename T, int D> struct Tile {
-  u32x4 kr[2][Form<T, D>::kLoads];
+  u32x4 kr[2][Form<T, D>::kPieces];
   typename Form<T, D>::VRow vr[8];
 };
 // V as the second product wants it: bf16, transposed (its rows' registers are then free for the next tile's).
 template <typename T, int D> struct Turned {};
 template <int D> struct Turned<uint16_t, D> { u32x4 a[D / 16]; };
-template <int D> struct Turned<E4M3, D> : Turned<uint16_t, D> {};
-template <int D> struct Turned<Int8, D> : Turned<uint16_t, D> {};
-// The scales of a lane's eight positions of a tile (8 bits).
-struct Scales { float k[8], v[8]; };
 
 // A wave's rows, 16 HB of a group from row0 on, and what they have seen.
 template <typename T, int D, int HB, bool SCORED, bool EXACT>
 struct Rows {
   typedef Form<T, D> F;
   static constexpr int NH = 16 * HB, KP = F::kPieces, KT = F::kTerms, NJ = F::kColumns, QOPS = HB * KP * 64;
-  static constexpr int EACH = kScaled<T> ? 8 : 16 / sizeof(T), ALL = NH * (D / EACH), ITEMS = (ALL + kThreads - 1) / kThreads;      // values of a piece of q; pieces of a thread
+  static constexpr int EACH = 16 / sizeof(T), ALL = NH * (D / EACH), ITEMS = (ALL + kThreads - 1) / kThreads;      // values of a piece of q; pieces of a thread
   floatx4 acc[HB][NJ];
   float m_run[HB], l_run[HB];
   int lim[HB], lim_min;                // the first position that a lane's row does not see, and the first that not all rows see
-  int up[HB];                          // 8 bits: the exponent that q's row was brought down by
 
   // q: on its way, and (tid: of the 256 threads that share the rows) as operands of the first product, [term][block of 16 rows][piece][lane]
   struct Query { float4 v[ITEMS][EACH / 4]; };
@@ -562,10 +508,6 @@ struct Rows {
     }
   }
   static __device__ __forceinline__ void store_q(const PagedDecode& p, int tid, const Query& q, u32x4* qs) {
-    if constexpr (kScaled<T>) {
-      store_scaled_q(p, tid, q, qs);
-      return;
-    }
 #pragma unroll
     for (int it = 0; it < ITEMS; ++it) {
       const int idx = tid + it * kThreads, r = idx / (D / EACH), c = idx - r * (D / EACH);
@@ -593,42 +535,6 @@ struct Rows {
     }
   }
 
-  // 8 bits: columns 16 c .. of a row are piece c's, its first eight one product's, the others the next one's.  Behind the operands: the rows' exponents.
-  static __device__ __forceinline__ void store_scaled_q(const PagedDecode& p, int tid, const Query& q, u32x4* qs) {
-    int* const exponents = reinterpret_cast<int*>(qs + KT * QOPS);
-#pragma unroll
-    for (int it = 0; it < ITEMS; ++it) {
-      const int idx = tid + it * kThreads, r = idx / (D / 8), c = idx - r * (D / 8);
-      if (idx >= ALL) break;                               // (whole waves)
-      float x[8], most = 0.f;
-#pragma unroll
-      for (int y = 0; y < 2; ++y) {
-        const float4 v = q.v[it][y];
-        x[4 * y] = v.x * p.qscale; x[4 * y + 1] = v.y * p.qscale; x[4 * y + 2] = v.z * p.qscale; x[4 * y + 3] = v.w * p.qscale;
-      }
-#pragma unroll
-      for (int y = 0; y < 8; ++y) most = fmaxf(most, fabsf(x[y]));
-#pragma unroll
-      for (int off = 1; off < D / 8; off <<= 1) most = fmaxf(most, __shfl_xor(most, off));      // (the row's threads are neighbours)
-      const int up = (int)(__float_as_uint(most) >> 23) - (127 + 13);
-      const int slot = ((r >> 4) * KP + 2 * (c >> 3) + (c & 1)) * 64 + (r & 15) + 16 * (c >> 1 & 3);
-      u32x4 t[2];
-#pragma unroll
-      for (int y = 0; y < 4; ++y) {
-        uint32_t w[2];
-        split2(ldexpf(x[2 * y], -up), ldexpf(x[2 * y + 1], -up), w);
-        t[0][y] = w[0]; t[1][y] = w[1];
-      }
-      qs[slot] = t[0];
-      qs[QOPS + slot] = t[1];
-      if (c == 0) exponents[r] = up;
-    }
-  }
-  __device__ __forceinline__ void take_exponents(const u32x4* qs, int lane) {
-#pragma unroll
-    for (int hb = 0; hb < HB; ++hb) up[hb] = reinterpret_cast<const int*>(qs + KT * QOPS)[16 * hb + (lane & 15)];
-  }
-
   __device__ __forceinline__ void begin(const PagedDecode& p, const Segment& s, int row0, int lane) {
 #pragma unroll
     for (int hb = 0; hb < HB; ++hb) {
@@ -654,28 +560,18 @@ struct Rows {
     for (int n = 0; n < DEEP - 1; ++n) read(n);
 #pragma unroll
     for (int hb = 0; hb < HB; ++hb) sc[0][hb] = sc[1][hb] = floatx4{0.f, 0.f, 0.f, 0.f};
-    u32x4 k8[2];                                           // 8 bits: the piece as fp16
 #pragma unroll
     for (int n = 0; n < STEPS; ++n) {
       if (n + DEEP - 1 < STEPS) read(n + DEEP - 1);
       __builtin_amdgcn_sched_barrier(0);
       const int x = n / KT;
-      if constexpr (kScaled<T>) {
-        if (n % KT == 0)
 #pragma unroll
-          for (int u = 0; u < 2; ++u)
-#pragma unroll
-            for (int y = 0; y < 4; ++y) k8[u][y] = two_f16<T>(tl.kr[u][x >> 1][2 * (x & 1) + (y >> 1)], y & 1);
-      }
-#pragma unroll
-      for (int y = 0; y < (sizeof(T) <= 2 ? 1 : 4); ++y)
+      for (int y = 0; y < (sizeof(T) == 2 ? 1 : 4); ++y)
 #pragma unroll
         for (int hb = 0; hb < HB; ++hb)
 #pragma unroll
           for (int u = 0; u < 2; ++u) {
-            if constexpr (kScaled<T>)
-              sc[u][hb] = mfma_f16(k8[u], b[n % DEEP][hb], sc[u][hb]);
-            else if constexpr (sizeof(T) == 2)
+            if constexpr (sizeof(T) == 2)
               sc[u][hb] = mfma_bf16(tl.kr[u][x], b[n % DEEP][hb], sc[u][hb]);
             else
               sc[u][hb] = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(tl.kr[u][x][y]), __uint_as_float(b[n % DEEP][hb][y]), sc[u][hb], 0, 0, 0);
@@ -686,15 +582,7 @@ struct Rows {
   }
   // V's part of piece x: NJ / KP of its column groups
   static __device__ __forceinline__ void turn(const Tile<T, D>& tl, int x, Turned<T, D>& v) {
-    if constexpr (kScaled<T>) {
-#pragma unroll
-      for (int y = 0; y < 4; ++y) {
-        uint32_t a, b;
-        turn2<T>(tl.vr[2 * y][x >> 1], tl.vr[2 * y + 1][x >> 1], x & 1, &a, &b);
-        v.a[2 * x][y] = a;
-        v.a[2 * x + 1][y] = b;
-      }
-    } else if constexpr (sizeof(T) == 2) {
+    if constexpr (sizeof(T) == 2) {
 #pragma unroll
       for (int j = x * NJ / KP; j < (x + 1) * NJ / KP; ++j)
 #pragma unroll
@@ -703,15 +591,8 @@ struct Rows {
   }
 
   // the softmax of a tile from position p0 on; bad: bit e: position p0 + e is not there
-  __device__ __forceinline__ void weights(const PagedDecode& p, const Segment& s, int row0, int lane, int p0, uint32_t bad, floatx4 (&sc)[2][HB], float (&w)[HB][8],
-                                          const Scales& scales) {
+  __device__ __forceinline__ void weights(const PagedDecode& p, const Segment& s, int row0, int lane, int p0, uint32_t bad, floatx4 (&sc)[2][HB], float (&w)[HB][8]) {
     const int i16 = lane & 15, g = lane >> 4;
-    if constexpr (kScaled<T>) {
-#pragma unroll
-      for (int hb = 0; hb < HB; ++hb)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) sc[e >> 2][hb][e & 3] = ldexpf(sc[e >> 2][hb][e & 3] * scales.k[e], up[hb]);
-    }
     if (bad || p0 + kPagedTile > lim_min) {    // what is not there, or not seen
 #pragma unroll
       for (int e = 0; e < 8; ++e)
@@ -752,16 +633,12 @@ struct Rows {
         sum += w[hb][e];
       }
       l_run[hb] += sum;
-      if constexpr (kScaled<T>) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) w[hb][e] *= scales.v[e];
-      }
     }
   }
   // after(e): the registers of V row e are free
   template <typename After>
   __device__ __forceinline__ void second_product(const float (&w)[HB][8], const Tile<T, D>& tl, const Turned<T, D>& v, After&& after) {
-    if constexpr (sizeof(T) <= 2) {
+    if constexpr (sizeof(T) == 2) {
       u32x4 wt[HB][3];
 #pragma unroll
       for (int hb = 0; hb < HB; ++hb)
@@ -884,10 +761,9 @@ void paged_matrix_kernel(PagedDecode p) {
   typedef Form<T, D> F;
   extern __shared__ __align__(16) unsigned char smem[];
   __shared__ __align__(16) int s_rows[kWaves][2][32];
-  __shared__ __align__(16) float s_scales[kScaled<T> ? kWaves : 1][2][2][32];
   __shared__ int s_odd;
   Segment s;
-  if (!find_segment<kScaled<T> ? 2 : 1>(p, &s)) return;
+  if (!find_segment<1>(p, &s)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i16 = lane & 15, g = lane >> 4;
   int (&places)[2][32] = s_rows[wave];
   const int32_t* table = p.c.table + (size_t)s.i * p.c.max_pages;
@@ -906,26 +782,9 @@ void paged_matrix_kernel(PagedDecode p) {
   };
   Tile<T, D> tl;
   int k_row[2], v_row[8];                                  // of the tile that is loaded next
-  // 8 bits: a lane asks for its position's scales when it has its place, and puts them into LDS a tile later, when they are there
-  const bool whole_power = kScaled<T> && (p.block & (p.block - 1)) == 0;
-  const int shift = kScaled<T> ? __builtin_ctz(p.block) : 0;
-  float next_ks = 0.f, next_vs = 0.f;
-  auto put_scales = [&](int buf, uint32_t missing) {
-    float (&own)[2][32] = s_scales[wave][buf];
-    const bool there = !(missing >> (lane & 31) & 1);
-    own[0][lane & 31] = there ? next_ks : 0.f;
-    own[1][lane & 31] = there ? next_vs : 0.f;
-    asm volatile("" ::: "memory");
-  };
   auto publish = [&](const Place& x, int buf) -> uint32_t {      // bit e of what is returned: position e of the tile is not there
     const bool there = (unsigned)x.entry < (unsigned)p.c.num_pages;
-    const int row = there ? (x.entry * p.c.h_kv + s.e) * p.c.page_size + x.inside : 0;
-    places[buf][lane & 31] = row;
-    if constexpr (kScaled<T>) {
-      const unsigned at = whole_power ? (unsigned)row >> shift : (unsigned)row / (unsigned)p.block;
-      next_ks = p.K_scales[at];
-      next_vs = p.V_scales[at];
-    }
+    places[buf][lane & 31] = there ? (x.entry * p.c.h_kv + s.e) * p.c.page_size + x.inside : 0;
     asm volatile("" ::: "memory");
     return (uint32_t)__ballot(!there);
   };
@@ -941,15 +800,15 @@ void paged_matrix_kernel(PagedDecode p) {
   };
   const int k = EXACT ? D : p.c.k, v = EXACT ? D : p.c.v;
   auto load_k = [&](int x) {
-    const int piece = EXACT ? g + 4 * x : min(g + 4 * x, k / (int)(16 / sizeof(T)) - 1);
+    const int piece = EXACT ? g + 4 * x : min(g + 4 * x, k / R::EACH - 1);
 #pragma unroll
     for (int u = 0; u < 2; ++u) tl.kr[u][x] = read(reinterpret_cast<const u32x4*>(Kp + (size_t)k_row[u] * (k * sizeof(T))) + piece);
   };
   auto load_v = [&](int e) {
     const unsigned char* src = Vp + (size_t)v_row[e] * (v * sizeof(T));
-    if constexpr (sizeof(T) <= 2) {
+    if constexpr (sizeof(T) == 2) {
       constexpr int C = F::kColumns;
-      if constexpr (EXACT || C <= 8 || kScaled<T>) {
+      if constexpr (EXACT || C <= 8) {
         tl.vr[e] = read(reinterpret_cast<const typename F::VRow*>(src) + (EXACT ? i16 : min(i16, v / C - 1)));
       } else {                                             // 16 columns: two pieces
         const u32x4* at = reinterpret_cast<const u32x4*>(src);
@@ -970,7 +829,7 @@ void paged_matrix_kernel(PagedDecode p) {
   next = look_up(wave + kWaves);
   take(0);
 #pragma unroll
-  for (int x = 0; x < F::kLoads; ++x) load_k(x);
+  for (int x = 0; x < F::kPieces; ++x) load_k(x);
 #pragma unroll
   for (int e = 0; e < 8; ++e) load_v(e);
   u32x4* qs = reinterpret_cast<u32x4*>(smem);
@@ -979,10 +838,6 @@ void paged_matrix_kernel(PagedDecode p) {
 
   R rows;
   rows.begin(p, s, s.row0, lane);
-  if constexpr (kScaled<T>) {
-    rows.take_exponents(qs, lane);
-    put_scales(0, bad);
-  }
   uint32_t bad_next = publish(next, 1);
   next = look_up(wave + 2 * kWaves);
   take(1);
@@ -995,30 +850,18 @@ void paged_matrix_kernel(PagedDecode p) {
       for (int e = 0; e < 8; ++e)
         if (now >> (8 * g + e) & 1) tl.vr[e] = typename F::VRow{};
     }
-    Scales scales;
-    if constexpr (kScaled<T>) {
-      const float (&own)[2][32] = s_scales[wave][buf ^ 1];
-#pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        const float4 a = reinterpret_cast<const float4*>(own[0])[2 * g + x], b = reinterpret_cast<const float4*>(own[1])[2 * g + x];
-        scales.k[4 * x] = a.x; scales.k[4 * x + 1] = a.y; scales.k[4 * x + 2] = a.z; scales.k[4 * x + 3] = a.w;
-        scales.v[4 * x] = b.x; scales.v[4 * x + 1] = b.y; scales.v[4 * x + 2] = b.z; scales.v[4 * x + 3] = b.w;
-      }
-    }
     floatx4 sc[2][HB];
     Turned<T, D> turned;
     R::first_product(tl, qs, lane, sc, [&](int x) {
-      if constexpr (!kScaled<T>) load_k(x);
-      else if (x & 1) load_k(x >> 1);
+      load_k(x);
       R::turn(tl, x, turned);
     });
-    if constexpr (kScaled<T>) put_scales(buf, bad_next);
     bad = bad_next;
     buf ^= 1;
     bad_next = publish(next, buf);                         // places of the tile after the next one
     next = look_up(t + 3 * kWaves);
     float w[HB][8];
-    rows.weights(p, s, s.row0, lane, p0, now, sc, w, scales);
+    rows.weights(p, s, s.row0, lane, p0, now, sc, w);
     rows.second_product(w, tl, turned, load_v);
     take(buf);
   }

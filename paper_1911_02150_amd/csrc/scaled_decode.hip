@@ -1,7 +1,449 @@
-// Attention over paged caches of 8 bits with a scale for each block of positions and head (the kernels' description: paged_decode.hpp).
+// Attention over paged caches of 8 bits with a scale for each block of positions and head: o = sum_p weights[p] s_V(p) V8[p] of logits scale s_K(p) (q . K8[p]).
+//
+// The work is cut, merged, and done again in the plain form where infinities and NaN take part, as in paged_decode.hpp; the pieces are for two workgroups to a compute unit, since
+// half the bytes to a product leave the instructions, not HBM, as what bounds them (b=64, m=8192, h=32: 49 us with one, 43 with two).  A workgroup is four waves, wave w has tiles w, w + 4, ... of 32 positions for 16 or
+// 32 query rows.  Both products are v_mfma_f32_16x16x32_f16; 8 bits are exact in fp16.
+//   logits^T[32 pos x 16 rows] = K_tile . q^T: lane (i, g) has the 16-byte pieces g, g + 4, ... of two K rows, a piece's first eight columns for one product, the others for the next.  q's rows are
+//     brought by one power of two to 2^13 .. 2^14 at most and taken as two fp16 terms: 23 bits of what is not below 2^-16 of the largest, and 2^-39 of the largest of what is.
+//   out^T[D cols x 16 rows] += V_tile^T . weights^T: lane (c, g) has 1/16 of the columns of rows 8g .. 8g + 7.
+// Weights.  With s_V(p) = 2^E mant and z the logit (log2), u = z + E - ref is what the running maximum M is taken over, row by row, and w = 2^(u - M) the number that multiplies V8 (times mant, where
+// a scale is no power of two): a row's largest *contribution* is near fp16's largest number, so that two fp16 terms hold every w to 23 bits, and those that are below 2^-25 of it to 2^-35 of
+// it, whatever the scales.  The sum is over w 2^-E.  ref follows the tiles' scales (any will do: M goes with it), which keeps u small, and so its rounding.
 #include "paged_decode.hpp"
 
 namespace mqa {
+namespace {
+
+typedef __attribute__((ext_vector_type(1))) uint32_t u32x1;
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+
+__device__ __forceinline__ floatx4 mfma_f16(const u32x4& a, const u32x4& b, const floatx4& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+// a pair of floats as two fp16 pairs whose sums are the floats to 23 bits
+__device__ __forceinline__ uint32_t pack_f16_pair(float a, float b) { return __builtin_bit_cast(uint32_t, f16x2{(_Float16)a, (_Float16)b}); }
+__device__ __forceinline__ void split2(float a, float b, uint32_t (&t)[2]) {
+  t[0] = pack_f16_pair(a, b);
+  float c, d;                                              // what that leaves, an instruction each (the compiler takes two)
+  asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel_hi:[1,0,0]" : "=v"(c) : "v"(t[0]), "v"(a));
+  asm("v_fma_mix_f32 %0, %1, -1.0, %2 op_sel:[1,0,0] op_sel_hi:[1,0,0]" : "=v"(d) : "v"(t[0]), "v"(b));
+  t[1] = pack_f16_pair(c, d);
+}
+// Two bytes each of `biased`, whose bytes are int8 + 128, as fp16: 0x6400 + y is 1024 + y.
+__device__ __forceinline__ uint32_t int8_f16(uint32_t biased, uint32_t select) {
+  return __builtin_bit_cast(uint32_t, __builtin_bit_cast(f16x2, __builtin_amdgcn_perm(0x64646464u, biased, select)) - f16x2{(_Float16)1152.f, (_Float16)1152.f});
+}
+__device__ __forceinline__ uint32_t e4m3_f16(uint32_t u, bool upper) {
+  return __builtin_bit_cast(uint32_t, upper ? __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(u, 1.f, true) : __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(u, 1.f, false));
+}
+// Four values of 8 bits as two fp16 pairs.
+template <typename T>
+__device__ __forceinline__ void halves(uint32_t u, uint32_t* lo, uint32_t* hi) {
+  if constexpr (std::is_same<T, E4M3>::value) {
+    *lo = e4m3_f16(u, false);
+    *hi = e4m3_f16(u, true);
+  } else {
+    u ^= 0x80808080u;
+    *lo = int8_f16(u, 0x04010400u);
+    *hi = int8_f16(u, 0x04030402u);
+  }
+}
+// Values 2 x and 2 x + 1 (`upper`: 2 and 3) of two rows' words, as fp16 pairs of one column each.
+template <typename T>
+__device__ __forceinline__ void turn2(uint32_t row0, uint32_t row1, bool upper, uint32_t* col0, uint32_t* col1) {
+  if constexpr (std::is_same<T, E4M3>::value) {
+    const uint32_t a = e4m3_f16(row0, upper), b = e4m3_f16(row1, upper);
+    *col0 = __builtin_amdgcn_perm(b, a, 0x05040100u);
+    *col1 = __builtin_amdgcn_perm(b, a, 0x07060302u);
+  } else {
+    const uint32_t pairs = __builtin_amdgcn_perm(row1, row0, upper ? 0x07030602u : 0x05010400u) ^ 0x80808080u;
+    *col0 = int8_f16(pairs, 0x04010400u);
+    *col1 = int8_f16(pairs, 0x04030402u);
+  }
+}
+
+template <int D> struct Form8 {
+  static constexpr int kPieces = D / 32, kLoads = D / 64;  // products of 32 columns; 16-byte loads of a K row in a lane
+  static constexpr int kTerms = 2;
+  static constexpr int kColumns = D / 16;
+  typedef typename std::conditional<D == 256, u32x4, typename std::conditional<D == 128, u32x2, u32x1>::type>::type VRow;
+  static __device__ __forceinline__ int column(int i, int j4) { return kColumns * i + 4 * j4; }
+};
+template <int D> struct Form<E4M3, D> : Form8<D> {};
+template <int D> struct Form<Int8, D> : Form8<D> {};
+
+template <int D> struct Tile8 {
+  u32x4 kr[2][D / 64];
+  typename Form8<D>::VRow vr[8];
+};
+
+constexpr float kRoom = 4.f;         // log2 of the largest w over 2^kTop before the maximum is moved; with a mantissa below 2 all stay below 2^15
+constexpr float kTop = 10.f;
+constexpr int kNear = 16;            // ref is moved for scales that are so many powers of two off
+constexpr int kFar = 64;             // what is further below the tile's largest is the plain form's, unless it is below 2^kNothing: then it is nothing
+constexpr int kNothing = -100;
+
+// Of two tiles' positions, in LDS: K's scale with q's power of two, E - ref, 2^-E, the mantissa.
+struct Scales { float f[64], e[64], inv[64], mant[64]; };
+
+template <typename T, int D, int HB, bool EXACT>
+struct Rows8 : Rows<T, D, HB, false, EXACT> {
+  typedef Rows<T, D, HB, false, EXACT> R;
+  using R::acc; using R::m_run; using R::l_run; using R::lim; using R::lim_min;
+  static constexpr int NH = 16 * HB, KP = D / 32, KT = 2, NJ = D / 16, QOPS = HB * KP * 64;
+  static constexpr int ALL = NH * (D / 8), ITEMS = (ALL + kThreads - 1) / kThreads;
+
+  struct Query { float4 v[ITEMS][2]; };
+  static __device__ __forceinline__ void load_q(const PagedDecode& p, const Segment& s, int tid, Query* q) {
+#pragma unroll
+    for (int it = 0; it < ITEMS; ++it) {
+      const int idx = tid + it * kThreads, r = idx / (D / 8), c = idx - r * (D / 8);
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        q->v[it][y] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (idx < ALL && s.row0 + r < p.R && (EXACT || 8 * c < p.c.k))
+          q->v[it][y] = reinterpret_cast<const float4*>(p.q + row_offset(p, s.i, s.e, s.row0 + r) * (EXACT ? D : p.c.k) + 8 * c)[y];
+      }
+    }
+  }
+  // As operands, [term][block of 16 rows][product][lane].  Returns the exponent that they have been brought down by (an infinity or NaN among them makes NaN of its row's logits).
+  static __device__ __forceinline__ int store_q(const PagedDecode& p, int tid, Query& q, u32x4* qs, float* s_most) {
+    float most = 0.f;
+#pragma unroll
+    for (int it = 0; it < ITEMS; ++it)
+#pragma unroll
+      for (int y = 0; y < 2; ++y) {
+        float4& v = q.v[it][y];
+        v.x *= p.qscale; v.y *= p.qscale; v.z *= p.qscale; v.w *= p.qscale;
+        most = fmaxf(most, fmaxf(fmaxf(fabsf(v.x), fabsf(v.y)), fmaxf(fabsf(v.z), fabsf(v.w))));
+      }
+#pragma unroll
+    for (int off = 32; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor(most, off));
+    if ((tid & 63) == 0) s_most[tid >> 6] = most;
+    __syncthreads();
+    most = fmaxf(fmaxf(s_most[0], s_most[1]), fmaxf(s_most[2], s_most[3]));
+    const int up = (int)(__float_as_uint(most) >> 23) - (127 + 13);
+#pragma unroll
+    for (int it = 0; it < ITEMS; ++it) {
+      const int idx = tid + it * kThreads, r = idx / (D / 8), c = idx - r * (D / 8);
+      if (idx >= ALL) break;
+      const float x[8] = {q.v[it][0].x, q.v[it][0].y, q.v[it][0].z, q.v[it][0].w, q.v[it][1].x, q.v[it][1].y, q.v[it][1].z, q.v[it][1].w};
+      const int slot = ((r >> 4) * KP + 2 * (c >> 3) + (c & 1)) * 64 + (r & 15) + 16 * (c >> 1 & 3);
+      u32x4 t[2];
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        uint32_t w[2];
+        split2(ldexpf(x[2 * y], -up), ldexpf(x[2 * y + 1], -up), w);
+        t[0][y] = w[0]; t[1][y] = w[1];
+      }
+      qs[slot] = t[0];
+      qs[QOPS + slot] = t[1];
+    }
+    return __builtin_amdgcn_readfirstlane(up);
+  }
+
+  // q . K of a tile; after(x): the multiplications of product x are under way
+  template <typename After>
+  static __device__ __forceinline__ void first_product(const Tile8<D>& tl, const u32x4* qs, int lane, floatx4 (&sc)[2][HB], After&& after) {
+    constexpr int STEPS = KP * KT, DEEP = 3;               // q of a step (product, term): read while the two before are multiplied
+    u32x4 b[DEEP][HB], k[2];
+    auto read = [&](int n) {
+#pragma unroll
+      for (int hb = 0; hb < HB; ++hb) b[n % DEEP][hb] = qs[n % KT * QOPS + (hb * KP + n / KT) * 64 + lane];
+    };
+#pragma unroll
+    for (int n = 0; n < DEEP - 1; ++n) read(n);
+#pragma unroll
+    for (int hb = 0; hb < HB; ++hb) sc[0][hb] = sc[1][hb] = floatx4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int n = 0; n < STEPS; ++n) {
+      if (n + DEEP - 1 < STEPS) read(n + DEEP - 1);
+      __builtin_amdgcn_sched_barrier(0);
+      const int x = n / KT;
+      if (n % KT == 0)
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            uint32_t lo, hi;
+            halves<T>(tl.kr[u][x >> 1][2 * (x & 1) + y], &lo, &hi);
+            k[u][2 * y] = lo;
+            k[u][2 * y + 1] = hi;
+          }
+#pragma unroll
+      for (int hb = 0; hb < HB; ++hb)
+#pragma unroll
+        for (int u = 0; u < 2; ++u) sc[u][hb] = mfma_f16(k[u], b[n % DEEP][hb], sc[u][hb]);
+      if (n % KT == KT - 1) after(x);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+  // what multiplies V of a tile (the half-th of its two) from position p0 on; bad: bit e: position p0 + e is not there; mantissas: some scale is no power of two
+  __device__ __forceinline__ void weights(int lane, int p0, int half, uint32_t bad, const Scales& scales, bool mantissas, const floatx4 (&sc)[2][HB], float (&w)[HB][8]) {
+    const int g = lane >> 4;
+    auto eight = [g, half](const float (&from)[64], float (&to)[8]) {
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        const float4 y = reinterpret_cast<const float4*>(from)[8 * half + 2 * g + x];
+        to[4 * x] = y.x; to[4 * x + 1] = y.y; to[4 * x + 2] = y.z; to[4 * x + 3] = y.w;
+      }
+    };
+    float f[8], e8[8], inv[8];
+    eight(scales.f, f);
+    eight(scales.e, e8);
+    eight(scales.inv, inv);
+#pragma unroll
+    for (int hb = 0; hb < HB; ++hb)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[hb][e] = fmaf(sc[e >> 2][hb][e & 3], f[e], e8[e]);
+    if (bad || p0 + kPagedTile > lim_min) {                // what is not there, or not seen
+      int first = p0 + 8 * g;
+      asm volatile("" : "+v"(first));                      // (a branch: few tiles have such positions)
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+#pragma unroll
+        for (int hb = 0; hb < HB; ++hb)
+          if ((bad >> (8 * g + e) & 1) || first + e >= lim[hb]) w[hb][e] = -INFINITY;
+    }
+#pragma unroll
+    for (int hb = 0; hb < HB; ++hb) {
+      float mx = fmaxf(fmaxf(fmaxf(w[hb][0], w[hb][1]), fmaxf(w[hb][2], w[hb][3])), fmaxf(fmaxf(w[hb][4], w[hb][5]), fmaxf(w[hb][6], w[hb][7])));
+      if (__any(mx > m_run[hb] + (kTop + kRoom))) {        // (m_run: the maximum less kTop)
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        const float mnew = fmaxf(m_run[hb], mx - kTop);
+        const float alpha = __builtin_amdgcn_exp2f(m_run[hb] - (mnew == -INFINITY ? 0.f : mnew));
+        l_run[hb] *= alpha;
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) acc[hb][j] *= alpha;
+        m_run[hb] = mnew;
+      }
+      const float mref = m_run[hb] == -INFINITY ? 0.f : m_run[hb];
+      float sum = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        w[hb][e] = __builtin_amdgcn_exp2f(w[hb][e] - mref);
+        sum = fmaf(w[hb][e], inv[e], sum);
+      }
+      l_run[hb] += sum;
+    }
+    if (mantissas) {
+      float mant[8];
+      eight(scales.mant, mant);
+#pragma unroll
+      for (int hb = 0; hb < HB; ++hb)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[hb][e] *= mant[e];
+    }
+  }
+  static __device__ __forceinline__ void split(const float (&w)[HB][8], u32x4 (&wt)[HB][2]) {
+#pragma unroll
+    for (int hb = 0; hb < HB; ++hb)
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        uint32_t x[2];
+        split2(w[hb][2 * y], w[hb][2 * y + 1], x);
+        wt[hb][0][y] = x[0]; wt[hb][1][y] = x[1];
+      }
+  }
+  // Two of the lane's columns at a time, which are brought into the operand's order while the two before are multiplied.
+  __device__ __forceinline__ void second_product(const u32x4 (&wt)[HB][2], const Tile8<D>& tl) {
+    u32x4 v[2][2];
+    auto turn = [&](int x) {
+#pragma unroll
+      for (int y = 0; y < 4; ++y) {
+        uint32_t a, b;
+        turn2<T>(tl.vr[2 * y][x >> 1], tl.vr[2 * y + 1][x >> 1], x & 1, &a, &b);
+        v[x & 1][0][y] = a;
+        v[x & 1][1][y] = b;
+      }
+    };
+    turn(0);
+#pragma unroll
+    for (int x = 0; x < NJ / 2; ++x) {
+      __builtin_amdgcn_sched_barrier(0);
+      if (x + 1 < NJ / 2) turn(x + 1);
+#pragma unroll
+      for (int term = 0; term < 2; ++term)
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int hb = 0; hb < HB; ++hb) acc[hb][2 * x + j] = mfma_f16(v[x & 1][j], wt[hb][term], acc[hb][2 * x + j]);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+  }
+};
+
+// CACHED: several blocks of rows read the same tiles, neighbours on an XCD at about the same time: from memory once and else from L2.
+template <typename T, int D, int HB, bool CACHED, bool EXACT>
+__global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2)
+void scaled_matrix_kernel(PagedDecode p) {
+  typedef Rows8<T, D, HB, EXACT> R;
+  extern __shared__ __align__(16) unsigned char smem[];
+  __shared__ __align__(16) int s_rows[kWaves][2][64];
+  __shared__ __align__(16) Scales s_scales[kWaves][2];
+  __shared__ float s_most[kWaves];
+  __shared__ int s_odd;
+  Segment s;
+  if (!find_segment<2>(p, &s)) return;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i16 = lane & 15, g = lane >> 4;
+  int (&places)[2][64] = s_rows[wave];
+  const int32_t* table = p.c.table + (size_t)s.i * p.c.max_pages;
+  const unsigned char* Kp = static_cast<const unsigned char*>(p.c.K);
+  const unsigned char* Vp = static_cast<const unsigned char*>(p.c.V);
+  const int ntiles = (s.end - s.begin + kPagedTile - 1) / kPagedTile;
+
+  // ---- A wave's tiles in pairs (t, t + 4): their loads are on their way while the pair before is multiplied; where their rows are is found two pairs ahead, lane l has position
+  // l % 32 of tile l / 32.  (What is past the end is read as the last position, a page that holds nothing as the pool's first row.)
+  struct Place { int entry, inside; };
+  auto look_up = [&](int t) {
+    const int pos = min(s.begin + kPagedTile * (t + kWaves * (lane >> 5)) + (lane & 31), max(s.end - 1, 0));
+    const unsigned page = (unsigned)pos / (unsigned)p.c.page_size;
+    return Place{table[page], pos - (int)page * p.c.page_size};
+  };
+  Tile8<D> tl[2];
+  const bool whole_power = (p.block & (p.block - 1)) == 0;
+  const int shift = __builtin_ctz(p.block);
+  float ks, vs;                                            // the scales of the lane's position, asked for when its place is known
+  auto publish = [&](const Place& x, int buf) -> uint64_t {      // bit e of what is returned: position e of the pair is not there
+    const bool there = (unsigned)x.entry < (unsigned)p.c.num_pages;
+    const int row = there ? (x.entry * p.c.h_kv + s.e) * p.c.page_size + x.inside : 0;
+    places[buf][lane] = row;
+    asm volatile("" ::: "memory");
+    const unsigned at = whole_power ? (unsigned)row >> shift : (unsigned)row / (unsigned)p.block;
+    ks = p.K_scales[at];
+    vs = p.V_scales[at];
+    return __ballot(!there);
+  };
+  auto read = [](const auto* at) {
+    if constexpr (CACHED) return *at;
+    else return __builtin_nontemporal_load(at);
+  };
+  const int k = EXACT ? D : p.c.k, v = EXACT ? D : p.c.v;
+  int k_row[2];
+  auto take_k = [&](int buf, int half) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) k_row[u] = places[buf][32 * half + 8 * (i16 >> 2) + 4 * u + (i16 & 3)];
+  };
+  auto load_k = [&](int half, int x) {
+    const int piece = EXACT ? g + 4 * x : min(g + 4 * x, k / 16 - 1);
+#pragma unroll
+    for (int u = 0; u < 2; ++u) tl[half].kr[u][x] = read(reinterpret_cast<const u32x4*>(Kp + (size_t)k_row[u] * k) + piece);
+  };
+  auto load_v = [&](int buf, int half) {
+    constexpr int C = D / 16;
+    int v_row[8];
+    *reinterpret_cast<int4*>(v_row) = reinterpret_cast<const int4*>(places[buf])[8 * half + 2 * g];
+    *reinterpret_cast<int4*>(v_row + 4) = reinterpret_cast<const int4*>(places[buf])[8 * half + 2 * g + 1];
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      tl[half].vr[e] = read(reinterpret_cast<const typename Form8<D>::VRow*>(Vp + (size_t)v_row[e] * v) + (EXACT ? i16 : min(i16, v / C - 1)));
+  };
+
+  if (tid == 0) s_odd = 0;
+  Place next = look_up(wave);
+  typename R::Query q;                                     // requested before the first tile and converted while that is on its way
+  R::load_q(p, s, tid, &q);
+  uint64_t bad = publish(next, 0);                         // of the pair that is loaded; of the one after it
+  next = look_up(wave + 2 * kWaves);
+#pragma unroll
+  for (int half = 0; half < 2; ++half)
+    if (half == 0 || wave + kWaves < ntiles) {
+      take_k(0, half);
+#pragma unroll
+      for (int x = 0; x < D / 64; ++x) load_k(half, x);
+      load_v(0, half);
+    }
+  u32x4* qs = reinterpret_cast<u32x4*>(smem);
+  const int up = R::store_q(p, tid, q, qs, s_most);
+  __syncthreads();
+
+  R rows;
+  rows.begin(p, s, s.row0, lane);
+  // ---- the scales of the pair that `publish` was last called for, into LDS; m_run goes with ref
+  int ref = 0;
+  uint64_t nothing = 0;                                    // positions whose V is nothing beside the others'
+  bool mantissas = false, far = false;
+  auto put_scales = [&](int buf, uint64_t missing) {
+    const bool there = !(missing >> lane & 1);
+    const uint32_t bits = there ? __float_as_uint(vs) : 0x3f800000u;
+    const bool none = bits < (uint32_t)(127 + kNothing) << 23;                      // (0 and the smallest)
+    const int exponent = (int)(bits >> 23) - 127;                                   // (a negative scale's: above all others)
+    int e = there && !none ? exponent : ref;
+    if (__any(e > ref + kNear || e < ref - kNear)) {
+      int most = there && !none ? e : INT32_MIN;
+#pragma unroll
+      for (int off = 1; off < 64; off <<= 1) most = max(most, __shfl_xor(most, off));
+      most = __builtin_amdgcn_readfirstlane(most);
+#pragma unroll
+      for (int hb = 0; hb < HB; ++hb) rows.m_run[hb] -= (float)(most - ref);
+      ref = most;
+      if (!there) e = ref;
+    }
+    if (none) e = ref - kFar;
+    far = far || __any(e < ref - kFar || e > 100 || e < -125);
+    Scales& own = s_scales[wave][buf];
+    own.f[lane] = there ? ldexpf(ks, up) : 0.f;
+    own.e[lane] = (float)(e - ref);
+    own.inv[lane] = ldexpf(1.f, -e);
+    const uint32_t mant = none ? 0x3f800000u : (bits & 0x7fffffu) | 0x3f800000u;
+    own.mant[lane] = __uint_as_float(mant);
+    asm volatile("" ::: "memory");
+    nothing = __ballot(none);
+    mantissas = __any(mant != 0x3f800000u);
+  };
+  put_scales(0, bad);
+  uint64_t bad_next = publish(next, 1);
+  next = look_up(wave + 4 * kWaves);
+  int buf = 1;
+  for (int t = wave; t < ntiles; t += 2 * kWaves) {
+    const uint64_t zeros = bad | nothing;
+    const bool mantissas_now = mantissas;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      if (half == 1 && t + kWaves >= ntiles) break;        // (and there is no next pair)
+      const int p0 = s.begin + kPagedTile * (t + kWaves * half);
+      if (zeros) {
+        uint32_t mine = (uint32_t)(zeros >> (32 * half)) >> (8 * g);
+        asm volatile("" : "+v"(mine));                     // (a branch)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (mine >> e & 1) tl[half].vr[e] = typename Form8<D>::VRow{};
+      }
+      floatx4 sc[2][HB];
+      take_k(buf, half);
+      R::first_product(tl[half], qs, lane, sc, [&](int x) {
+        if (x & 1) load_k(half, x >> 1);
+      });
+      float w[HB][8];
+      rows.weights(lane, p0, half, (uint32_t)(bad >> (32 * half)), s_scales[wave][buf ^ 1], mantissas_now, sc, w);
+      u32x4 wt[HB][2];
+      R::split(w, wt);
+      if (half == 1 || t + kWaves >= ntiles) put_scales(buf, bad_next);
+      rows.second_product(wt, tl[half]);
+      load_v(buf, half);
+    }
+    bad = bad_next;
+    buf ^= 1;
+    bad_next = publish(next, buf);                         // places of the pair after the next one
+    next = look_up(t + 6 * kWaves);
+  }
+
+  if (far || rows.odd()) s_odd = 1;
+  __syncthreads();                                         // (and the q operands are read)
+  if (s_odd) {
+    in_plain_form<T>(p, s, R::NH, smem);
+    return;
+  }
+#pragma unroll
+  for (int hb = 0; hb < HB; ++hb) rows.m_run[hb] += (float)ref;      // (in which the waves differ)
+  rows.put(reinterpret_cast<float*>(smem), wave, lane);
+  __syncthreads();
+  R::finish(p, s, s.row0, reinterpret_cast<const float*>(smem), tid);
+}
+
+}  // namespace
 
 PagedPlan scaled_plan(int b, int n, int h, int h_kv, int page_size, int max_pages, int k, int v, int is_e4m3) {
   return paged_plan(b, n, h, h_kv, page_size, max_pages, k, v, 1, 0);
@@ -9,7 +451,7 @@ PagedPlan scaled_plan(int b, int n, int h, int h_kv, int page_size, int max_page
 
 template <typename T, int D, int HB, bool CACHED, bool EXACT>
 static hipError_t launch_matrix(const PagedDecode& p, const PagedPlan& pl, hipStream_t st) {
-  return launch_form<paged_matrix_kernel<T, D, HB, false, CACHED, EXACT>>(Lds<T, D, HB>::alone, p, pl, st);
+  return launch_form<scaled_matrix_kernel<T, D, HB, CACHED, EXACT>>(Lds<T, D, HB>::alone, p, pl, st);
 }
 template <typename T, int D, bool EXACT>
 static hipError_t launch_rows(const PagedDecode& p, const PagedPlan& pl, hipStream_t st) {

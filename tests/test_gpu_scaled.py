@@ -49,13 +49,15 @@ def cache_of(rng, b, each, h_kv, page, block, k, v, kind, powers=True):
     return (K, Ks, V, Vs), (bits(K, kind, one), f32(Ks, one), bits(V, kind, one), f32(Vs, one))
 
 
-def tolerance(q, K, size, scale, length):
+def tolerance(q, K, size, scale, length, kind, top):
     """Half a step for each of: k products and their sum (a logit, at most scale * |q| |K|; q's two terms have 23 bits, two half steps more in every product), its scale and the row's, the
     exponential and its argument, a weight's scale, as many sums as there are positions, each over rounding errors that do not know of one another (eight
-    standard deviations)."""
+    standard deviations).  And for every position half a step of fp16's smallest numbers, 2^-25, in units in which the row's largest weight times scale is 2^10 at least: 2^-35 of
+    `top`, which is no less than that largest one, times the type's largest number.  (A position's weight times scale w is 2^10 and more for the largest; its two fp16 terms hold
+    w (1 + e) + d, |e| <= 2^-23, |d| <= 2^-25, the second only below 2^-2, that is 2^-12 of the largest; what an earlier maximum was the unit of is scaled down.)"""
     k = q.shape[-1]
     logit = abs(scale) * np.abs(q).max() * np.abs(K[np.isfinite(K)]).max() * k ** 0.5 * 4      # (4: a sum of k products of normal numbers)
-    return EPS * ((2 * (8 + 4) + 4 + 3) * logit + 17 + 8 * length ** 0.5) * size + 1e-30
+    return EPS * ((2 * (8 + 4) + 4 + 3) * logit + 17 + 8 * length ** 0.5) * size + length * 2.0 ** -35 * {"e4m3": 448, "int8": 127}[kind] * top + 1e-30
 
 
 def attended(q, arrays, table, lens, scale):
@@ -63,8 +65,10 @@ def attended(q, arrays, table, lens, scale):
     K, Ks, V, Vs = arrays
     with np.errstate(invalid="ignore", over="ignore"):
         K, V = serving.whole(K, Ks), serving.whole(V, Vs)
+        sizes = np.abs(np.repeat(Vs, V.shape[2] // Vs.shape[2], axis=2))[..., None]
     o, _, size = paged.attend(q.astype(np.float64), K, V, table, np.array(lens), float(np.float32(scale)))
-    return o, size, K
+    top, _, _ = paged.attend(q.astype(np.float64), K, sizes, table, np.array(lens), float(np.float32(scale)))      # (the sum of weight times scale: no less than the largest)
+    return o, size, K, np.where(np.isfinite(top), top, 0)
 
 
 # b, n, h, h_kv, k, v, page size, block, lengths
@@ -107,13 +111,13 @@ def test_attention(m, b, n, h, h_kv, k, v, page, block, lens, kind):
     table = tables(rng, b, each)
     q = rng.standard_normal((b, n, h, k)).astype(np.float32)
     scale = 2 / k ** 0.5
-    want, size, K = attended(q, arrays, table, lens, scale)
+    want, size, K, top = attended(q, arrays, table, lens, scale)
     args = (f32(q[:, 0] if n == 1 else q), *cache, i32(table), i32(np.array(lens)))
     got = m.mqa_paged_scaled_decode_step(*args, scale=scale)
     given = torch.full_like(got, 777.0)
     assert got.shape == ((b, h, v) if n == 1 else (b, n, h, v)) and m.mqa_paged_scaled_decode_step(*args, scale=scale, o=given) is given and torch.equal(got, given)
     off = np.abs(got.cpu().numpy().reshape(want.shape) - want)
-    assert (off <= tolerance(q, K, size, scale, max(lens))).all(), off.max()
+    assert (off <= tolerance(q, K, size, scale, max(lens), kind, top)).all(), off.max()
 
 
 @pytest.mark.parametrize("kind", ["e4m3", "int8"])
@@ -142,13 +146,13 @@ def test_what_is_not_seen_may_hold_anything(m, n, h, h_kv, k, kind):
                 Vs[at[0], :, at[1]] = (np.inf, -np.inf, np.nan)[j % 3]
     q = rng.standard_normal((b, n, h, k)).astype(np.float32)
     one = h_kv == 1
-    want, size, _ = attended(q, (K, Ks, V, Vs), table, lens, 0.25)
+    want, size, _, top = attended(q, (K, Ks, V, Vs), table, lens, 0.25)
     got = m.mqa_paged_scaled_decode_step(f32(q), bits(K, kind, one), f32(Ks, one), bits(V, kind, one), f32(Vs, one), i32(table), i32(lens), scale=0.25)
     got = got.cpu().numpy().astype(np.float64)
     assert not got[1].any() and not got[4].any() and np.isfinite(got[:, 0]).all()
     finite = np.isfinite(want)
     assert np.array_equal(np.isnan(got), np.isnan(want)) and np.array_equal(got[~finite & ~np.isnan(want)], want[~finite & ~np.isnan(want)])
-    assert (np.abs(got - want)[finite] <= tolerance(q, clean, size, 0.25, 96)[finite]).all()
+    assert (np.abs(got - want)[finite] <= tolerance(q, clean, size, 0.25, 96, kind, top)[finite]).all()
 
 
 @pytest.mark.parametrize("kind", ["e4m3", "int8"])
@@ -165,13 +169,13 @@ def test_queries_of_any_size(m, k, kind):
     q[0, 0, 4] *= 1e-3
     q[0, 0, 4, 0] = 30
     q[0, 0, 5] *= 50
-    want, size, K = attended(q, arrays, table, lens, 0.3)
+    want, size, K, top = attended(q, arrays, table, lens, 0.3)
     got = m.mqa_paged_scaled_decode_step(f32(q[:, 0]), *cache, i32(table), i32(lens), scale=0.3).cpu().numpy()
     for r in range(8):
-        assert (np.abs(got[:, r] - want[:, 0, r]) <= tolerance(q[:, :, r], K, size[:, 0, r], 0.3, 300)).all(), r
+        assert (np.abs(got[:, r] - want[:, 0, r]) <= tolerance(q[:, :, r], K, size[:, 0, r], 0.3, 300, kind, top[:, 0, r])).all(), r
     q[0, 0, 7, 3] = np.inf
     odd = m.mqa_paged_scaled_decode_step(f32(q[:, 0]), *cache, i32(table), i32(lens), scale=0.3).cpu().numpy()
-    assert np.isnan(odd[0, 7]).all() and (np.abs(odd[:, :7] - want[:, 0, :7]) <= np.stack([tolerance(q[:, :, r], K, size[:, 0, r], 0.3, 300) for r in range(7)], 1)).all()
+    assert np.isnan(odd[0, 7]).all() and (np.abs(odd[:, :7] - want[:, 0, :7]) <= np.stack([tolerance(q[:, :, r], K, size[:, 0, r], 0.3, 300, kind, top[:, 0, r]) for r in range(7)], 1)).all()
 
 
 @pytest.mark.parametrize("kind", ["e4m3", "int8"])
@@ -188,9 +192,9 @@ def test_scales_far_apart(m, h, kind):
     Ks[table[0, 2]] = 0
     Ks[table[1, 2]] = 2.0 ** -100
     q = (0.3 * rng.standard_normal((2, 1, h, 128))).astype(np.float32)
-    want, size, K_all = attended(q, (K, Ks, V, Vs), table, lens, 0.1)
+    want, size, K_all, top = attended(q, (K, Ks, V, Vs), table, lens, 0.1)
     got = m.mqa_paged_scaled_decode_step(f32(q[:, 0]), bits(K, kind, True), f32(Ks, True), bits(V, kind, True), f32(Vs, True), i32(table), i32(lens), scale=0.1).cpu().numpy()
-    assert (np.abs(got - want[:, 0]) <= tolerance(q, K_all, size, 0.1, 470)[:, 0]).all()
+    assert (np.abs(got - want[:, 0]) <= tolerance(q, K_all, size, 0.1, 470, kind, top)[:, 0]).all()
 
 
 @pytest.mark.parametrize("kind", ["e4m3", "int8"])
@@ -200,9 +204,9 @@ def test_large_logits(m, kind):
     arrays, cache = cache_of(rng, 1, 40, 1, 16, 16, 128, 128, kind)
     table, lens = tables(rng, 1, 40), np.array([640])
     q = (20 * rng.standard_normal((1, 1, 8, 128))).astype(np.float32)
-    want, size, K = attended(q, arrays, table, lens, 1.0)
+    want, size, K, top = attended(q, arrays, table, lens, 1.0)
     got = m.mqa_paged_scaled_decode_step(f32(q[:, 0]), *cache, i32(table), i32(lens)).cpu().numpy()
-    assert (np.abs(got - want[:, 0]) <= tolerance(q, K, size, 1.0, 640)[:, 0]).all()
+    assert (np.abs(got - want[:, 0]) <= tolerance(q, K, size, 1.0, 640, kind, top)[:, 0]).all()
 
 
 # b, n, h, k, v, pages of a sequence: so many sequences that a workgroup has 32 rows, in one launch and in two, and listed
@@ -231,9 +235,9 @@ def test_many_sequences_of_many_rows(m, b, n, h, k, v, each, kind):
     q = rng.standard_normal((b, n, h, k)).astype(np.float32)
     got = m.mqa_paged_scaled_decode_step(f32(q), *cache, i32(table), i32(lens), scale=0.2).cpu().numpy()
     for i in [0, 1, 2, b // 2, b - 1, int(np.argmax(lens)), int(np.argmin(lens))]:
-        want, size, K = attended(q[i:i + 1], arrays, table[i:i + 1], lens[i:i + 1], 0.2)
+        want, size, K, top = attended(q[i:i + 1], arrays, table[i:i + 1], lens[i:i + 1], 0.2)
         off = np.abs(got[i] - want[0])
-        assert (off <= tolerance(q, K, size, 0.2, each * page)[0]).all(), (i, off.max())
+        assert (off <= tolerance(q, K, size, 0.2, each * page, kind, top)[0]).all(), (i, off.max())
 
 
 def test_a_pool_of_more_than_4_gib(m):
