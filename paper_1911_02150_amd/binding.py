@@ -52,6 +52,9 @@ _NATIVE_FUNCTIONS = [
     "mqa_beam_reorder_kv", "mqa_prefill_attention", "mha_prefill_attention",
     "mqa_paged_append_kv_rows", "mqa_paged_decode_workspace_bytes", "mqa_paged_decode_step", "mqa_paged_evict_kv",
     "mqa_stack_verify_workspace_bytes", "mqa_stack_verify_drafts",
+    "mqa_paged_scaled_append_kv_rows", "mqa_paged_scaled_decode_workspace_bytes", "mqa_paged_scaled_decode_step", "mqa_paged_fork_pages", "mqa_paged_free_pages",
+    "mqa_paged_reserve_workspace_bytes", "mqa_paged_reserve_pages", "mqa_paged_compact_workspace_bytes", "mqa_paged_compact_pages", "mqa_paged_copy_pages",
+    "mqa_stack_adjust_logits",
 ]
 
 
@@ -926,6 +929,10 @@ def mqa_paged_scaled_append_kv_rows(K_pages, K_scales, V_pages, V_scales, table,
     """mqa_paged_append_kv_rows for pools of float8_e4m3fn or int8 with scales [num_pages,page_size/block] (multi-query) or [num_pages,h_kv,page_size/block] float32, one for
     `block` positions of a page and a head: the rows are rounded to 8 bits under a power of two; a block that has rows of the sequence already keeps its scale, or its rows are
     rounded again under a larger one.  Returns lens_out."""
+    if stream is None and _native is not None:
+        done = _native.scaled_append(K_pages, K_scales, V_pages, V_scales, table, k_new, v_new, lens, lens_out, counts)
+        if done is not None:
+            return done
     lib = load_library()
     _check(k_new, "k_new", torch.float32), _check(v_new, "v_new", torch.float32)
     _check(lens, "lens", torch.int32), _check(lens_out, "lens_out", torch.int32)
@@ -955,6 +962,10 @@ def mqa_paged_scaled_decode_workspace_bytes(b, n, h, h_kv, page_size, max_pages,
 def mqa_paged_scaled_decode_step(q, K_pages, K_scales, V_pages, V_scales, table, lens, o=None, scale=1.0, workspace=None, stream=None):
     """mqa_paged_decode_step (without scores) over pools of 8 bits as in mqa_paged_scaled_append_kv_rows: q [b,h,k] or [b,n,h,k] -> o [b,h,v] or [b,n,h,v].
     Workspace: a block of the call's own unless given."""
+    if stream is None and _native is not None:
+        done = _native.scaled_decode(q, K_pages, K_scales, V_pages, V_scales, table, lens, o, scale, workspace)
+        if done is not None:
+            return done
     lib = load_library()
     _check(q, "q", torch.float32), _check(lens, "lens", torch.int32)
     if q.dim() not in (3, 4):
@@ -994,6 +1005,10 @@ def mqa_paged_fork_pages(table, lens, parents, table_out, lens_out, refs, page_s
     """Sequence j of table_out [b_out,max_pages] becomes what sequence parents[j] of table [b,max_pages] is, and shares its pages: those that hold its lens positions, -1 behind them;
     refs [num_pages], how many entries of tables name a page, counts them; lens_out [b_out] receives the length (a parent outside [0,b): empty).  All int32.  What
     table_out named before is not given back (mqa_paged_free_pages does that).  Returns table_out."""
+    if stream is None and _native is not None:
+        done = _native.fork_pages(table, lens, parents, table_out, lens_out, refs, page_size)
+        if done is not None:
+            return done
     _int32(table=(table, (None, None)), parents=(parents, (None,)), refs=(refs, (None,)))
     b, max_pages = table.shape
     _int32(lens=(lens, (b,)), table_out=(table_out, (parents.shape[0], max_pages)), lens_out=(lens_out, (parents.shape[0],)))
@@ -1007,6 +1022,10 @@ def mqa_paged_fork_pages(table, lens, parents, table_out, lens_out, refs, page_s
 def mqa_paged_free_pages(table, lens, refs, page_size, stream=None):
     """The pages of table [b,max_pages] behind every sequence's first lens [b] positions (0: all of them) are given back: their refs [num_pages] fall by one, their entries become -1.
     All int32.  Returns table."""
+    if stream is None and _native is not None:
+        done = _native.free_pages(table, lens, refs, page_size)
+        if done is not None:
+            return done
     _int32(table=(table, (None, None)), refs=(refs, (None,)))
     _int32(lens=(lens, (table.shape[0],)))
     with _on(_one_device(table, lens, refs), stream):
@@ -1019,6 +1038,10 @@ def mqa_paged_reserve_pages(table, lens, refs, page_size, n, counts=None, grante
     """Free pages (those with refs [num_pages] of 0) into table [b,max_pages] for the next n positions of every sequence, counts [b] of them where given, and in place of shared pages that
     they reach.  granted [b]: how many positions (counts of the append that follows; 0 where the pages do not suffice, and the sequence is as it was); moves
     [b,2]: the begun page that is to be copied by mqa_paged_copy_pages, and the one it is copied to, or -1.  All int32.  Returns (granted, moves)."""
+    if stream is None and _native is not None:
+        done = _native.reserve_pages(table, lens, refs, page_size, n, counts, granted, moves, workspace)
+        if done is not None:
+            return done
     _int32(table=(table, (None, None)), refs=(refs, (None,)))
     b, max_pages = table.shape
     _int32(lens=(lens, (b,)), counts=(counts, (b,)), granted=(granted, (b,)), moves=(moves, (b, 2)))
@@ -1043,6 +1066,10 @@ def mqa_paged_compact_pages(table, refs, table_out, refs_out, moves, used, works
     """The pages in use (refs [num_pages] above 0) that lie behind the first used[0], as many as there are, move to the free ones among those: moves [max(1,num_pages//2),2] lists (from, to) for
     mqa_paged_copy_pages, -1 behind them; table_out [b,max_pages] and refs_out [num_pages], other tensors than table and refs, go by the new places.  All int32; every table of
     the pool has to be in the call.  Returns moves."""
+    if stream is None and _native is not None:
+        done = _native.compact_pages(table, refs, table_out, refs_out, moves, used, workspace)
+        if done is not None:
+            return done
     _int32(table=(table, (None, None)), refs=(refs, (None,)), used=(used, (1,)))
     b, max_pages = table.shape
     num_pages = refs.shape[0]
@@ -1063,6 +1090,8 @@ def mqa_paged_compact_pages(table, refs, table_out, refs_out, moves, used, works
 def mqa_paged_copy_pages(pools, moves, stream=None):
     """Page moves[x,0] of each of the pools (a sequence of tensors [num_pages,...] of any type: K and V pages and their scales, of every layer) is copied to page
     moves[x,1]; pairs with a page outside the pool are passed over.  moves [m,2] int32; no page may be both copied from and to, or to twice."""
+    if stream is None and _native is not None and _native.copy_pages(pools, moves) is not None:
+        return
     pools = list(pools)
     if not pools:
         raise ValueError("no pools")
@@ -1085,6 +1114,10 @@ def mqa_stack_adjust_logits(logits, history, lens, drafts=None, prompts=None, re
     prompt's (None: 0), and the drafts [b,n] before draft j.  A token among them: x / repetition [b] (x > 0) or x * repetition; one that is there c times, c > 0, behind the prompt: less
     frequency [b] * c + presence [b]; then the last of the biases [b,m] whose bias_tokens [b,m] is the token is added; tokens whose bit of allowed [b,n+1,ceil(vocab/32)] (int32 words, lowest bit
     first; None: all) is not set become -infinity.  Tokens and lengths are int32."""
+    if stream is None and _native is not None:
+        done = _native.adjust_logits(logits, history, lens, drafts, prompts, repetition, frequency, presence, bias_tokens, biases, allowed, out)
+        if done is not None:
+            return done
     lib = load_library()
     _check(logits, "logits", torch.float32)
     if logits.dim() not in (2, 3):

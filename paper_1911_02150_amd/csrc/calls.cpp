@@ -40,6 +40,17 @@ struct Functions {
   decltype(&mqa_paged_evict_kv) paged_evict;
   decltype(&mqa_stack_verify_workspace_bytes) verify_workspace;
   decltype(&mqa_stack_verify_drafts) verify;
+  decltype(&mqa_paged_scaled_append_kv_rows) scaled_append;
+  decltype(&mqa_paged_scaled_decode_workspace_bytes) scaled_workspace;
+  decltype(&mqa_paged_scaled_decode_step) scaled_decode;
+  decltype(&mqa_paged_fork_pages) fork_pages;
+  decltype(&mqa_paged_free_pages) free_pages;
+  decltype(&mqa_paged_reserve_workspace_bytes) reserve_workspace;
+  decltype(&mqa_paged_reserve_pages) reserve_pages;
+  decltype(&mqa_paged_compact_workspace_bytes) compact_workspace;
+  decltype(&mqa_paged_compact_pages) compact_pages;
+  decltype(&mqa_paged_copy_pages) copy_pages;
+  decltype(&mqa_stack_adjust_logits) adjust_logits;
 } fn;
 PyObject* error_class = nullptr;
 PyObject* parameter_class = nullptr;
@@ -462,6 +473,191 @@ MQA_CALL(verify, 9) {
   return result(WITHOUT_GIL(fn.verify(lp, qp, dp, np, up, tp, ap, b, n, vocab, temperature, ws.at, ws.bytes, st)), "mqa_stack_verify_drafts", both);
 }
 
+// ---------------------------------------------------------------- caches of 8 bits
+// Their sizes and positions of a scale; false: not these
+bool scaled_of(const at::Tensor* K, const at::Tensor* Ks, const at::Tensor* V, const at::Tensor* Vs, const at::Tensor* table, int64_t b, Paged* c, int* block) {
+  if (!K || !Ks || !V || !Vs || !table || K->dim() < 3 || K->dim() > 4 || V->dim() != K->dim() || table->dim() != 2 || table->size(0) != b || V->scalar_type() != K->scalar_type() ||
+      V->sizes().slice(0, V->dim() - 1) != K->sizes().slice(0, K->dim() - 1) || Ks->dim() != K->dim() - 1 || Ks->sizes() != Vs->sizes() ||
+      Ks->sizes().slice(0, Ks->dim() - 1) != K->sizes().slice(0, K->dim() - 2) || !fits(*K) || !fits(*V) || !fits(*table))
+    return false;
+  const int dt = K->scalar_type() == at::kFloat8_e4m3fn ? MQA_E4M3 : K->scalar_type() == at::kChar ? MQA_INT8 : -1;
+  *c = Paged{K->dim() == 4 ? K->size(1) : 1, K->size(0), K->size(-2), table->size(1), K->size(-1), V->size(-1), dt};
+  const int64_t blocks = Ks->size(-1);
+  if (dt < 0 || c->size <= 0 || blocks <= 0 || c->size % blocks) return false;
+  *block = (int)(c->size / blocks);
+  return true;
+}
+
+// (K_pages, K_scales, V_pages, V_scales, table, k_new, v_new, lens, lens_out, counts)
+MQA_CALL(scaled_append, 10) {
+  const at::Tensor *K = plain(a[0]), *Ks = f32(a[1]), *V = plain(a[2]), *Vs = f32(a[3]), *table = i32(a[4]), *kn = f32(a[5]), *vn = f32(a[6]), *lens = i32(a[7]),
+                   *out = i32(a[8]), *counts;
+  Paged c;
+  int block;
+  if (!kn || !vn || !lens || !out || !maybe(a[9], at::kInt, &counts) || kn->dim() < 3 || !fits(*kn) || !scaled_of(K, Ks, V, Vs, table, kn->size(0), &c, &block)) NOT_HERE;
+  const int64_t b = kn->size(0), n = kn->size(1);
+  if (!(K->dim() == 4 ? shape_is(*kn, {b, n, c.h_kv, c.k}) && shape_is(*vn, {b, n, c.h_kv, c.v}) : shape_is(*kn, {b, n, c.k}) && shape_is(*vn, {b, n, c.v})) ||
+      lens->numel() != b || out->numel() != b || (counts && counts->numel() != b))
+    NOT_HERE;
+  const float *kp = at_of<float>(kn), *vp = at_of<float>(vn);
+  const int32_t *cp = at_of<int32_t>(counts), *tp = at_of<int32_t>(table), *lp = at_of<int32_t>(lens);
+  int32_t* op = at_of<int32_t>(out);
+  float *sk = at_of<float>(Ks), *sv = at_of<float>(Vs);
+  void *Kp = K->data_ptr(), *Vp = V->data_ptr(), *st = current_stream();
+  Py_INCREF(a[8]);
+  return result(WITHOUT_GIL(fn.scaled_append(kp, vp, cp, Kp, sk, Vp, sv, tp, lp, op, b, n, c.h_kv, c.pages, c.size, block, c.each, c.k, c.v, (mqa_dtype)c.dt, st)),
+                "mqa_paged_scaled_append_kv_rows", a[8]);
+}
+
+// (q, K_pages, K_scales, V_pages, V_scales, table, lens, o, scale, workspace)
+MQA_CALL(scaled_decode, 10) {
+  const at::Tensor *q = f32(a[0]), *K = plain(a[1]), *Ks = f32(a[2]), *V = plain(a[3]), *Vs = f32(a[4]), *table = i32(a[5]), *lens = i32(a[6]), *o;
+  float scale;
+  Paged c;
+  int block;
+  if (!q || !lens || q->dim() < 3 || q->dim() > 4 || !fits(*q) || !number(a[8], &scale) || !scaled_of(K, Ks, V, Vs, table, q->size(0), &c, &block)) NOT_HERE;
+  const int64_t b = q->size(0), n = q->dim() == 4 ? q->size(1) : 1, h = q->size(-2);
+  if (q->size(-1) != c.k || lens->numel() != b) NOT_HERE;
+  at::Tensor own;
+  Held res{q->dim() == 4 ? output(a[7], *q, {b, n, h, c.v}, &o, &own) : output(a[7], *q, {b, h, c.v}, &o, &own)};
+  if (!res.p) NOT_HERE;
+  Scratch ws;
+  if (!scratch(a[9], a[9] == Py_None ? fn.scaled_workspace(b, n, h, c.h_kv, c.size, c.each, c.k, c.v, (mqa_dtype)c.dt) : 0, *q, &ws)) NOT_HERE;
+  const float *qp = at_of<float>(q), *sk = at_of<float>(Ks), *sv = at_of<float>(Vs);
+  float* op = at_of<float>(o);
+  const int32_t *tp = at_of<int32_t>(table), *lp = at_of<int32_t>(lens);
+  const void *Kp = K->data_ptr(), *Vp = V->data_ptr();
+  void* st = current_stream();
+  return result(WITHOUT_GIL(fn.scaled_decode(qp, Kp, sk, Vp, sv, tp, lp, op, b, n, h, c.h_kv, c.pages, c.size, block, c.each, c.k, c.v, (mqa_dtype)c.dt, scale, ws.at, ws.bytes, st)),
+                "mqa_paged_scaled_decode_step", res.take());
+}
+
+// ---------------------------------------------------------------- pages
+// (table, lens, parents, table_out, lens_out, refs, page_size)
+MQA_CALL(fork_pages, 7) {
+  const at::Tensor *table = i32(a[0]), *lens = i32(a[1]), *parents = i32(a[2]), *to = i32(a[3]), *out = i32(a[4]), *refs = i32(a[5]);
+  int size;
+  if (!table || !lens || !parents || !to || !out || !refs || table->dim() != 2 || parents->dim() != 1 || refs->dim() != 1 || !fits(*table) || !fits(*parents) || !fits(*refs) ||
+      !integer(a[6], &size))
+    NOT_HERE;
+  const int64_t b = table->size(0), each = table->size(1), n = parents->size(0), pages = refs->size(0);
+  if (!shape_is(*lens, {b}) || !shape_is(*to, {n, each}) || !shape_is(*out, {n})) NOT_HERE;
+  const int32_t *tp = at_of<int32_t>(table), *lp = at_of<int32_t>(lens), *pp = at_of<int32_t>(parents);
+  int32_t *op = at_of<int32_t>(to), *np = at_of<int32_t>(out), *rp = at_of<int32_t>(refs);
+  void* st = current_stream();
+  Py_INCREF(a[3]);
+  return result(WITHOUT_GIL(fn.fork_pages(tp, lp, pp, op, np, rp, b, n, pages, size, each, st)), "mqa_paged_fork_pages", a[3]);
+}
+
+// (table, lens, refs, page_size)
+MQA_CALL(free_pages, 4) {
+  const at::Tensor *table = i32(a[0]), *lens = i32(a[1]), *refs = i32(a[2]);
+  int size;
+  if (!table || !lens || !refs || table->dim() != 2 || refs->dim() != 1 || !fits(*table) || !fits(*refs) || !integer(a[3], &size) || !shape_is(*lens, {table->size(0)})) NOT_HERE;
+  const int64_t b = table->size(0), each = table->size(1), pages = refs->size(0);
+  int32_t *tp = at_of<int32_t>(table), *rp = at_of<int32_t>(refs);
+  const int32_t* lp = at_of<int32_t>(lens);
+  void* st = current_stream();
+  Py_INCREF(a[0]);
+  return result(WITHOUT_GIL(fn.free_pages(tp, lp, rp, b, pages, size, each, st)), "mqa_paged_free_pages", a[0]);
+}
+
+// (table, lens, refs, page_size, n, counts, granted, moves, workspace)
+MQA_CALL(reserve_pages, 9) {
+  const at::Tensor *table = i32(a[0]), *lens = i32(a[1]), *refs = i32(a[2]), *counts, *granted, *moves;
+  int size, n;
+  if (!table || !lens || !refs || table->dim() != 2 || refs->dim() != 1 || !fits(*table) || !fits(*refs) || !integer(a[3], &size) || !integer(a[4], &n) ||
+      !maybe(a[5], at::kInt, &counts) || !maybe(a[6], at::kInt, &granted) || !maybe(a[7], at::kInt, &moves))
+    NOT_HERE;
+  const int64_t b = table->size(0), each = table->size(1), pages = refs->size(0);
+  if (!shape_is(*lens, {b}) || (counts && !shape_is(*counts, {b})) || (granted && !shape_is(*granted, {b})) || (moves && !shape_is(*moves, {b, 2}))) NOT_HERE;
+  Scratch ws;
+  if (!scratch(a[8], a[8] == Py_None ? fn.reserve_workspace(b, n, pages, size, each) : 0, *table, &ws)) NOT_HERE;
+  const auto ints = table->options().requires_grad(false);
+  at::Tensor new_granted, new_moves;
+  Held g{nullptr}, m{nullptr};
+  if (granted) Py_INCREF(a[6]), g.p = a[6];
+  else new_granted = at::empty({b}, ints), granted = &new_granted, g.p = THPVariable_Wrap(new_granted);
+  if (moves) Py_INCREF(a[7]), m.p = a[7];
+  else new_moves = at::empty({b, 2}, ints), moves = &new_moves, m.p = THPVariable_Wrap(new_moves);
+  if (!g.p || !m.p) NOT_HERE;
+  int32_t *tp = at_of<int32_t>(table), *rp = at_of<int32_t>(refs), *gp = at_of<int32_t>(granted), *mp = at_of<int32_t>(moves);
+  const int32_t *lp = at_of<int32_t>(lens), *cp = at_of<int32_t>(counts);
+  void* st = current_stream();
+  PyObject* both = PyTuple_Pack(2, g.p, m.p);
+  if (!both) NOT_HERE;
+  return result(WITHOUT_GIL(fn.reserve_pages(tp, lp, cp, rp, gp, mp, b, n, pages, size, each, ws.at, ws.bytes, st)), "mqa_paged_reserve_pages", both);
+}
+
+// (table, refs, table_out, refs_out, moves, used, workspace)
+MQA_CALL(compact_pages, 7) {
+  const at::Tensor *table = i32(a[0]), *refs = i32(a[1]), *to = i32(a[2]), *refs_out = i32(a[3]), *moves = i32(a[4]), *used = i32(a[5]);
+  if (!table || !refs || !to || !refs_out || !moves || !used || table->dim() != 2 || refs->dim() != 1 || !fits(*table) || !fits(*refs)) NOT_HERE;
+  const int64_t b = table->size(0), each = table->size(1), pages = refs->size(0);
+  if (!shape_is(*to, {b, each}) || !shape_is(*refs_out, {pages}) || !shape_is(*moves, {pages / 2 > 1 ? pages / 2 : 1, 2}) || !shape_is(*used, {1})) NOT_HERE;
+  Scratch ws;
+  if (!scratch(a[6], a[6] == Py_None ? fn.compact_workspace(b, pages, each) : 0, *table, &ws)) NOT_HERE;
+  const int32_t *tp = at_of<int32_t>(table), *rp = at_of<int32_t>(refs);
+  int32_t *op = at_of<int32_t>(to), *np = at_of<int32_t>(refs_out), *mp = at_of<int32_t>(moves), *up = at_of<int32_t>(used);
+  void* st = current_stream();
+  Py_INCREF(a[4]);
+  return result(WITHOUT_GIL(fn.compact_pages(tp, rp, op, np, mp, up, b, pages, each, ws.at, ws.bytes, st)), "mqa_paged_compact_pages", a[4]);
+}
+
+// (pools, moves)
+MQA_CALL(copy_pages, 2) {
+  constexpr Py_ssize_t most = 64;
+  const at::Tensor* moves = i32(a[1]);
+  if (!moves || moves->dim() != 2 || moves->size(1) != 2 || !fits(*moves) || !(PyList_CheckExact(a[0]) || PyTuple_CheckExact(a[0]))) NOT_HERE;
+  const Py_ssize_t count = PySequence_Fast_GET_SIZE(a[0]);
+  if (count < 1 || count > most) NOT_HERE;
+  void* at[most];
+  size_t sizes[most];
+  int64_t pages = 0;
+  for (Py_ssize_t i = 0; i < count; ++i) {
+    const at::Tensor* t = plain(PySequence_Fast_GET_ITEM(a[0], i));
+    if (!t || t->dim() < 2 || !fits(*t) || (i > 0 && t->size(0) != pages) || t->size(0) <= 0) NOT_HERE;
+    pages = t->size(0);
+    at[i] = t->data_ptr();
+    sizes[i] = bytes_of(*t) / (size_t)pages;
+  }
+  const int32_t* mp = at_of<int32_t>(moves);
+  const int64_t m = moves->size(0);
+  void* st = current_stream();
+  Py_INCREF(Py_True);
+  return result(WITHOUT_GIL(fn.copy_pages(at, sizes, (int)count, mp, m, pages, st)), "mqa_paged_copy_pages", Py_True);
+}
+
+// (logits, history, lens, drafts, prompts, repetition, frequency, presence, bias_tokens, biases, allowed, out)
+MQA_CALL(adjust_logits, 12) {
+  const at::Tensor *logits = f32(a[0]), *history = i32(a[1]), *lens = i32(a[2]), *drafts, *prompts, *repetition, *frequency, *presence, *tokens, *biases, *allowed, *out;
+  if (!logits || !history || !lens || logits->dim() < 2 || logits->dim() > 3 || history->dim() != 2 || !fits(*logits) || !fits(*history) || !maybe(a[3], at::kInt, &drafts) ||
+      !maybe(a[4], at::kInt, &prompts) || !maybe(a[5], at::kFloat, &repetition) || !maybe(a[6], at::kFloat, &frequency) || !maybe(a[7], at::kFloat, &presence) ||
+      !maybe(a[8], at::kInt, &tokens) || !maybe(a[9], at::kFloat, &biases) || !maybe(a[10], at::kInt, &allowed))
+    NOT_HERE;
+  const bool flat = logits->dim() == 2;
+  const int64_t b = logits->size(0), n = flat ? 0 : logits->size(1) - 1, vocab = logits->size(-1), words = (vocab + 31) / 32;
+  if (history->size(0) != b || !shape_is(*lens, {b}) || (drafts && !shape_is(*drafts, {b, n})) || (prompts && !shape_is(*prompts, {b})) ||
+      (repetition && !shape_is(*repetition, {b})) || (frequency && !shape_is(*frequency, {b})) || (presence && !shape_is(*presence, {b})) || !tokens != !biases ||
+      (allowed && !(flat ? shape_is(*allowed, {b, words}) : shape_is(*allowed, {b, n + 1, words}))))
+    NOT_HERE;
+  int64_t m = 0;
+  if (biases) {
+    if (biases->dim() != 2 || biases->size(0) != b || !fits(*biases) || tokens->sizes() != biases->sizes()) NOT_HERE;
+    m = biases->size(1);
+  }
+  at::Tensor own;
+  Held res{flat ? output(a[11], *logits, {b, vocab}, &out, &own) : output(a[11], *logits, {b, n + 1, vocab}, &out, &own)};
+  if (!res.p) NOT_HERE;
+  const float *lp = at_of<float>(logits), *rp = at_of<float>(repetition), *fp = at_of<float>(frequency), *pp = at_of<float>(presence), *vp = at_of<float>(biases);
+  const int32_t *hp = at_of<int32_t>(history), *np = at_of<int32_t>(lens), *dp = at_of<int32_t>(drafts), *mp = at_of<int32_t>(prompts), *tp = at_of<int32_t>(tokens);
+  const uint32_t* ap = at_of<uint32_t>(allowed);
+  float* op = at_of<float>(out);
+  const int64_t cap = history->size(1);
+  void* st = current_stream();
+  return result(WITHOUT_GIL(fn.adjust_logits(lp, op, hp, np, mp, dp, rp, fp, pp, tp, vp, ap, b, n, vocab, cap, m, st)), "mqa_stack_adjust_logits", res.take());
+}
+
 // (the error's class, torch.nn.Parameter, addresses in the order of Functions)
 PyObject* init(PyObject*, PyObject* const* a, Py_ssize_t n) {
   constexpr Py_ssize_t count = sizeof(Functions) / sizeof(void*);
@@ -486,7 +682,8 @@ PyObject* torch_version(PyObject*, PyObject* const*, Py_ssize_t) { return PyUnic
 
 #define ENTRY(NAME) {#NAME, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)(void)>(NAME)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {ENTRY(init), ENTRY(torch_version), ENTRY(decode), ENTRY(append_qkv), ENTRY(project), ENTRY(add_layernorm), ENTRY(memory_kv), ENTRY(attend_rows), ENTRY(beams),
-                         ENTRY(reorder), ENTRY(paged_append), ENTRY(paged_decode), ENTRY(paged_evict), ENTRY(verify), {nullptr, nullptr, 0, nullptr}};
+                         ENTRY(reorder), ENTRY(paged_append), ENTRY(paged_decode), ENTRY(paged_evict), ENTRY(verify), ENTRY(scaled_append), ENTRY(scaled_decode),
+                         ENTRY(fork_pages), ENTRY(free_pages), ENTRY(reserve_pages), ENTRY(compact_pages), ENTRY(copy_pages), ENTRY(adjust_logits), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_calls", "Native argument marshalling of binding.py", -1, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
