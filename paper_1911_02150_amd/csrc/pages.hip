@@ -60,6 +60,19 @@ __device__ __forceinline__ int before_me(int x, int* s_waves, int* all) {      /
   return before;
 }
 
+// Which of the eight pages from `first` (a multiple of 8) on have a count above 0, and which are there at all.
+__device__ __forceinline__ uint32_t in_use8(const int32_t* refs, int first, int num_pages) {
+  uint32_t bits = 0;
+  if (first + 8 <= num_pages) {
+    const int4 a = reinterpret_cast<const int4*>(refs + first)[0], b = reinterpret_cast<const int4*>(refs + first)[1];
+    bits = (a.x > 0) | (a.y > 0) << 1 | (a.z > 0) << 2 | (a.w > 0) << 3 | (b.x > 0) << 4 | (b.y > 0) << 5 | (b.z > 0) << 6 | (b.w > 0) << 7;
+  } else {
+    for (int x = 0; first + x < num_pages; ++x) bits |= (uint32_t)(refs[first + x] > 0) << x;
+  }
+  return bits;
+}
+__device__ __forceinline__ uint32_t there8(int first, int num_pages) { return first >= num_pages ? 0u : first + 8 <= num_pages ? 0xffu : (1u << (num_pages - first)) - 1; }
+
 // ---------------------------------------------------------------- reserve
 // One workgroup, in steps:
 //  1. of every page that sequences are about to write behind rows that others share: how many are, and the last of them
@@ -115,21 +128,28 @@ void reserve_kernel(PageReserve p, void* workspace) {
     const int entry = p.table[(size_t)i * p.max_pages + w.first];
     return is_page(entry, p.num_pages) && p.refs[entry] > 1 ? entry : -1;
   };
+  uint32_t used = in_use8(p.refs, 8 * tid, p.num_pages);      // (for step 3, its first pages)
+  int mine = 0;
   for (int i = tid; i < p.b; i += kReserveThreads) {
     const int page = begun_page(i);
-    if (page >= 0) s.writers[page] = make_int2(0, -1);
-  }
-  __threadfence_block();
-  __syncthreads();
-  for (int i = tid; i < p.b; i += kReserveThreads) {
-    const int page = begun_page(i);
+    s.running[i] = page;
     if (page >= 0) {
-      atomicAdd(&s.writers[page].x, 1);
-      atomicMax(&s.writers[page].y, i);
+      s.writers[page] = make_int2(0, -1);
+      mine = 1;
     }
   }
   __threadfence_block();
-  __syncthreads();
+  if (__syncthreads_or(mine)) {
+    for (int i = tid; i < p.b; i += kReserveThreads) {
+      const int page = s.running[i];
+      if (page >= 0) {
+        atomicAdd(&s.writers[page].x, 1);
+        atomicMax(&s.writers[page].y, i);
+      }
+    }
+    __threadfence_block();
+    __syncthreads();
+  }
   int total = 0;
   for (int base = 0, turn = 0; base < p.b; base += kReserveThreads, turn ^= 1) {
     const int i = base + tid;
@@ -160,13 +180,13 @@ void reserve_kernel(PageReserve p, void* workspace) {
     total += all;
   }
   int found = 0;
-  for (int base = 0, turn = 0; base < p.num_pages && found < total; base += kReserveThreads, turn ^= 1) {
+  for (int base = 0, turn = 0; base < p.num_pages && found < total; base += 8 * kReserveThreads, turn ^= 1) {
     __syncthreads();
-    const int page = base + tid;
-    const bool free = page < p.num_pages && p.refs[page] <= 0;
-    int all;
-    const int at = found + before_me<kReserveThreads>(free, s_waves[turn], &all);
-    if (free) s.pages[at] = page;
+    const int first = base + 8 * tid;
+    if (base > 0) used = in_use8(p.refs, first, p.num_pages);
+    uint32_t free = ~used & there8(first, p.num_pages);
+    int all, at = found + before_me<kReserveThreads>(__popc(free), s_waves[turn], &all);
+    for (; free; free &= free - 1) s.pages[at++] = first + __ffs(free) - 1;
     found += all;
   }
   __threadfence_block();
@@ -194,9 +214,188 @@ void reserve_kernel(PageReserve p, void* workspace) {
   }
 }
 
+// The same where every thread has a sequence and that few pages: counts of a page's writers are kept in a hash table in LDS (open addressing, at most half full), needs in registers, so that
+// three reads in a row are left: length, entries, counts.  What bounds it is those and the launch (512 sequences, five tokens each, pages of 16: 14.6 us in the form above).
+constexpr int kReserveSlots = 4, kHash = 2 * kReserveThreads;
+__global__ __launch_bounds__(kReserveThreads)
+void reserve_few_kernel(PageReserve p) {
+  __shared__ int s_waves[2][kReserveThreads / 64], s_key[kHash], s_count[kHash], s_last[kHash], s_pages[kReserveThreads * kReserveSlots];
+  const int tid = threadIdx.x;
+  uint32_t used = in_use8(p.refs, 8 * tid, p.num_pages);
+  Wanted w = {};
+  const bool wants = tid < p.b && wanted(p, tid, &w);
+  int entry[kReserveSlots], need[kReserveSlots];
+#pragma unroll
+  for (int x = 0; x < kReserveSlots; ++x) entry[x] = wants && w.first + x < w.last ? p.table[(size_t)tid * p.max_pages + w.first + x] : -1;
+  int refs[kReserveSlots];
+#pragma unroll
+  for (int x = 0; x < kReserveSlots; ++x) refs[x] = is_page(entry[x], p.num_pages) ? p.refs[entry[x]] : 0;
+  for (int x = tid; x < kHash; x += kReserveThreads) {
+    s_key[x] = -1;
+    s_count[x] = 0;
+    s_last[x] = -1;
+  }
+  __syncthreads();
+  const bool writes = wants && w.begun && refs[0] > 1;
+  int at = 0;
+  if (writes) {
+    at = (int)((uint32_t)entry[0] * 2654435761u >> 21);
+    for (;;) {
+      const int key = atomicCAS(&s_key[at], -1, entry[0]);
+      if (key == -1 || key == entry[0]) break;
+      at = (at + 1) & (kHash - 1);
+    }
+    atomicAdd(&s_count[at], 1);
+    atomicMax(&s_last[at], tid);
+  }
+  __syncthreads();
+  const bool keeps = writes && s_count[at] == refs[0] && s_last[at] == tid;
+  int needs = 0;
+#pragma unroll
+  for (int x = 0; x < kReserveSlots; ++x) {
+    const bool there = is_page(entry[x], p.num_pages), begun = w.begun && x == 0;
+    need[x] = !wants || w.first + x >= w.last || (begun && (!there || keeps)) || (there && refs[x] <= 1) ? kKept : there ? entry[x] : kMissing;
+    needs += need[x] != kKept;
+  }
+  int total;
+  const int running = before_me<kReserveThreads>(needs, s_waves[0], &total) + needs;
+  int found = 0;
+  for (int base = 0, turn = 1; base < p.num_pages && found < total; base += 8 * kReserveThreads, turn ^= 1) {
+    if (base > 0) {
+      __syncthreads();
+      used = in_use8(p.refs, base + 8 * tid, p.num_pages);
+    }
+    uint32_t free = ~used & there8(base + 8 * tid, p.num_pages);
+    int all, to = found + before_me<kReserveThreads>(__popc(free), s_waves[turn], &all);
+    for (; free && to < total; free &= free - 1) s_pages[to++] = base + 8 * tid + __ffs(free) - 1;
+    found += all;
+  }
+  __syncthreads();
+  if (tid >= p.b) return;
+  int granted = 0, from = -1, to = -1;
+  if (wants && (running <= found || (needs == 0 && !keeps))) {
+    granted = w.count;
+    int page_at = running - needs;
+#pragma unroll
+    for (int x = 0; x < kReserveSlots; ++x) {
+      if (need[x] == kKept) continue;
+      const int page = s_pages[page_at++];
+      p.table[(size_t)tid * p.max_pages + w.first + x] = page;
+      p.refs[page] = 1;
+      if (need[x] >= 0) {
+        atomicSub(p.refs + need[x], 1);
+        if (w.begun && x == 0) { from = need[x]; to = page; }
+      }
+    }
+  }
+  p.granted[tid] = granted;
+  p.moves[2 * tid] = from;
+  p.moves[2 * tid + 1] = to;
+}
+
 // ---------------------------------------------------------------- compact
-// With `used` pages in use, those from `used` on move, in order, to the free ones before it.  Three launches: pages in use of every chunk; every page's new place; tables
-// and counts by it.
+// With `used` pages in use, those from `used` on move, in order, to the free ones before it.
+//
+// Pools of up to kBitPages: a bit a page, in use or not, and the pages in use before every word of 32 are in LDS, of every workgroup: rank(page), the x-th free page and the x-th one in use (a binary
+// search over the words, and in the word) say for each page, entry and move what it becomes without another workgroup's help.  The bits come from the counts, or, in pools so large that
+// each workgroup would read many, from a launch before (65536 pages, entries 32768: 7.4 us; the three launches below 13.4; 256 pages 3.4 and 6.8).
+constexpr int kBitPages = 1 << 17, kBitWords = kBitPages / 32, kReadPages = 1 << 14;
+__device__ __forceinline__ uint32_t in_use32(const int32_t* refs, int word, int num_pages) {
+  uint32_t bits = 0;
+#pragma unroll
+  for (int x = 0; x < 4; ++x)
+    if (32 * word + 8 * x < num_pages) bits |= in_use8(refs, 32 * word + 8 * x, num_pages) << (8 * x);
+  return bits;
+}
+__global__ __launch_bounds__(256)
+void compact_bits_kernel(PageCompact p, uint32_t* bits) {      // a thread has four pages, eight neighbours a word
+  const int first = 4 * (int)(blockIdx.x * 256u + threadIdx.x);
+  uint32_t mine = 0;
+  if (first + 4 <= p.num_pages) {
+    const int4 a = *reinterpret_cast<const int4*>(p.refs_in + first);
+    mine = (a.x > 0) | (a.y > 0) << 1 | (a.z > 0) << 2 | (a.w > 0) << 3;
+  } else {
+    for (int x = 0; first + x < p.num_pages; ++x) mine |= (uint32_t)(p.refs_in[first + x] > 0) << x;
+  }
+  mine <<= first & 31;
+#pragma unroll
+  for (int off = 1; off < 8; off <<= 1) mine |= __shfl_xor(mine, off);
+  if ((threadIdx.x & 7) == 0 && first < p.num_pages) bits[first >> 5] = mine;
+}
+// The position of the x-th set bit (there are more than x).
+__device__ __forceinline__ int nth_bit(uint32_t bits, int x) {
+  int at = 0;
+#pragma unroll
+  for (int half = 16; half > 0; half >>= 1) {
+    const int low = __popc(bits & ((1u << half) - 1));
+    if (x >= low) {
+      x -= low;
+      at += half;
+      bits >>= half;
+    }
+  }
+  return at;
+}
+__global__ __launch_bounds__(256)
+void compact_few_kernel(PageCompact p, const uint32_t* bits) {
+  __shared__ uint32_t s_bits[kBitWords];
+  __shared__ int s_rank[kBitWords], s_waves[2][4];
+  const int tid = threadIdx.x, words = (p.num_pages + 31) / 32;
+  for (int x = tid; x < words; x += 256) s_bits[x] = bits ? bits[x] : in_use32(p.refs_in, x, p.num_pages);
+  __syncthreads();
+  int used = 0;
+  for (int base = 0, turn = 0; base < words; base += 1024, turn ^= 1) {
+    int count[4], sum = 0;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      const int word = base + 4 * tid + x;
+      count[x] = word < words ? __popc(s_bits[word]) : 0;
+      sum += count[x];
+    }
+    int all, before = used + before_me<256>(sum, s_waves[turn], &all);
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+      if (base + 4 * tid + x < words) s_rank[base + 4 * tid + x] = before;
+      before += count[x];
+    }
+    used += all;
+  }
+  __syncthreads();
+  auto rank = [&](int page) { return s_rank[page >> 5] + __popc(s_bits[page >> 5] & ((1u << (page & 31)) - 1)); };
+  const int stay = used < p.num_pages ? rank(used) : used, moving = used - stay;
+  // the last word before which there are no more than x pages in use (or free ones)
+  auto tail = [&](int x) {               // the x-th page in use from `used` on
+    x += stay;
+    int word = 0;
+    for (int half = kBitWords >> 1; half > 0; half >>= 1)
+      if (word + half < words && s_rank[word + half] <= x) word += half;
+    return 32 * word + nth_bit(s_bits[word], x - s_rank[word]);
+  };
+  auto hole = [&](int x) {
+    int word = 0;
+    for (int half = kBitWords >> 1; half > 0; half >>= 1)
+      if (word + half < words && 32 * (word + half) - s_rank[word + half] <= x) word += half;
+    return 32 * word + nth_bit(~s_bits[word], x - (32 * word - s_rank[word]));
+  };
+  const unsigned first = blockIdx.x * 256u + tid, step = gridDim.x * 256u;
+  for (unsigned x = first; x < (unsigned)p.num_pages; x += step) {
+    const int page = (int)x;
+    int from = -1;
+    if (page < used) from = s_bits[page >> 5] >> (page & 31) & 1 ? page : tail(page - rank(page));
+    p.refs_out[page] = from < 0 ? 0 : p.refs_in[from];
+  }
+  for (unsigned x = first; x < (unsigned)p.moves_size; x += step)
+    reinterpret_cast<int2*>(p.moves)[x] = (int)x < moving ? make_int2(tail((int)x), hole((int)x)) : make_int2(-1, -1);
+  for (unsigned x = first; x < (unsigned)p.b * (unsigned)p.max_pages; x += step) {
+    const int entry = p.table_in[x];
+    int place = -1;
+    if (is_page(entry, p.num_pages) && (s_bits[entry >> 5] >> (entry & 31) & 1)) place = entry < used ? entry : hole(rank(entry) - stay);
+    p.table_out[x] = place;
+  }
+  if (first == 0) p.used[0] = used;
+}
+
+// Larger pools: three launches, pages in use of every chunk; every page's new place; tables and counts by it.
 constexpr int kChunk = 2048;           // pages of a workgroup, eight a thread
 struct CompactSpace { int32_t* counts; int32_t* place; size_t bytes; };
 __host__ __device__ CompactSpace compact_space(int num_pages, void* at) {
@@ -205,24 +404,11 @@ __host__ __device__ CompactSpace compact_space(int num_pages, void* at) {
                       counts + (((size_t)num_pages * 4 + 15) & ~(size_t)15)};
 }
 
-__device__ __forceinline__ int in_use(const PageCompact& p, int first, uint32_t* bits) {      // of eight pages
-  int sum = 0;
-  *bits = 0;
-#pragma unroll
-  for (int x = 0; x < 8; ++x)
-    if (first + x < p.num_pages && p.refs_in[first + x] > 0) {
-      ++sum;
-      *bits |= 1u << x;
-    }
-  return sum;
-}
-
 __global__ __launch_bounds__(256)
 void compact_count_kernel(PageCompact p, void* workspace) {
   __shared__ int s_waves[4];
-  uint32_t bits;
   int all;
-  before_me<256>(in_use(p, blockIdx.x * kChunk + 8 * threadIdx.x, &bits), s_waves, &all);
+  before_me<256>(__popc(in_use8(p.refs_in, blockIdx.x * kChunk + 8 * threadIdx.x, p.num_pages)), s_waves, &all);
   if (threadIdx.x == 0) compact_space(p.num_pages, workspace).counts[blockIdx.x] = all;
 }
 
@@ -246,8 +432,8 @@ void compact_place_kernel(PageCompact p, void* workspace) {
   int stay;
   before_me<256>(mine, s_waves[2], &stay);
   const int first = blockIdx.x * kChunk + 8 * tid;
-  uint32_t bits;
-  const int here = in_use(p, first, &bits);
+  const uint32_t bits = in_use8(p.refs_in, first, p.num_pages);
+  const int here = __popc(bits);
   int all;
   int rank = all_before + before_me<256>(here, s_waves[3], &all);      // pages in use before this one
   const int moving = used - stay;
@@ -289,20 +475,32 @@ void compact_apply_kernel(PageCompact p, void* workspace) {
 }
 
 // ---------------------------------------------------------------- copies of pages
-// A workgroup a move at a time, 16 bytes (or 4, where a page's size asks for it) a thread.
+// A workgroup a move at a time, 16 bytes (or 4, where a page's size asks for it) a thread.  HBM bounds it: 12320 moves of two pages of 4 KiB, 202 MB, 36.4 us = 5.5 TB/s (with loads and
+// stores that stay in L2 40.4; four moves at a time 53).
+typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 template <typename W>
 __device__ __forceinline__ void copy_run(void* pool, uint32_t bytes, int from, int to) {
   const W* src = reinterpret_cast<const W*>(static_cast<const unsigned char*>(pool) + (size_t)from * bytes);
   W* dst = reinterpret_cast<W*>(static_cast<unsigned char*>(pool) + (size_t)to * bytes);
-  for (uint32_t x = threadIdx.x; x < bytes / sizeof(W); x += 256) dst[x] = src[x];
+  const uint32_t words = bytes / sizeof(W);
+  uint32_t x = threadIdx.x;
+  for (; x + 768 < words; x += 1024) {
+    const W a = src[x], b = src[x + 256], c = src[x + 512], d = src[x + 768];
+    __builtin_nontemporal_store(a, dst + x);
+    __builtin_nontemporal_store(b, dst + x + 256);
+    __builtin_nontemporal_store(c, dst + x + 512);
+    __builtin_nontemporal_store(d, dst + x + 768);
+  }
+  for (; x < words; x += 256) __builtin_nontemporal_store(src[x], dst + x);
 }
+constexpr int kCopyGrid = 16384;
 __global__ __launch_bounds__(256)
 void copy_pages_kernel(PageCopy p) {
   for (int m = blockIdx.x; m < p.m; m += gridDim.x) {
     const int from = p.moves[2 * m], to = p.moves[2 * m + 1];
     if (!is_page(from, p.num_pages) || !is_page(to, p.num_pages) || from == to) continue;
     for (int x = 0; x < p.pools; ++x)
-      if (p.page_bytes[x] % 16 == 0) copy_run<uint4>(p.pool[x], p.page_bytes[x], from, to);
+      if (p.page_bytes[x] % 16 == 0) copy_run<u32x4>(p.pool[x], p.page_bytes[x], from, to);
       else copy_run<uint32_t>(p.pool[x], p.page_bytes[x], from, to);
   }
 }
@@ -322,13 +520,29 @@ hipError_t launch_free(const PageFree& p, hipStream_t st) {
 size_t reserve_workspace_bytes(int b, int n, int num_pages, int page_size) { return reserve_space(b, n, num_pages, page_size, nullptr).bytes; }
 
 hipError_t launch_reserve(const PageReserve& p, void* workspace, hipStream_t st) {
-  hipLaunchKernelGGL(reserve_kernel, dim3(1), dim3(kReserveThreads), 0, st, p, workspace);
+  if (p.b <= kReserveThreads && reserve_space(p.b, p.n, p.num_pages, p.page_size, nullptr).slots <= kReserveSlots)
+    hipLaunchKernelGGL(reserve_few_kernel, dim3(1), dim3(kReserveThreads), 0, st, p);
+  else
+    hipLaunchKernelGGL(reserve_kernel, dim3(1), dim3(kReserveThreads), 0, st, p, workspace);
   return hipGetLastError();
 }
 
 size_t compact_workspace_bytes(int num_pages) { return compact_space(num_pages, nullptr).bytes; }
 
 hipError_t launch_compact(const PageCompact& p, void* workspace, hipStream_t st) {
+  const unsigned entries = (unsigned)p.b * (unsigned)p.max_pages, items = entries > (unsigned)p.num_pages ? entries : (unsigned)p.num_pages;
+  if (p.num_pages <= kBitPages) {
+    uint32_t* bits = nullptr;
+    if (p.num_pages > kReadPages) {
+      bits = static_cast<uint32_t*>(workspace);
+      hipLaunchKernelGGL(compact_bits_kernel, dim3(((unsigned)p.num_pages + 1023) / 1024), dim3(256), 0, st, p, bits);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+    const unsigned groups = (items + 255) / 256;
+    hipLaunchKernelGGL(compact_few_kernel, dim3(groups < 256 ? groups : 256), dim3(256), 0, st, p, bits);
+    return hipGetLastError();
+  }
   const unsigned chunks = ((unsigned)p.num_pages + kChunk - 1) / kChunk;
   hipLaunchKernelGGL(compact_count_kernel, dim3(chunks), dim3(256), 0, st, p, workspace);
   hipError_t e = hipGetLastError();
@@ -336,13 +550,12 @@ hipError_t launch_compact(const PageCompact& p, void* workspace, hipStream_t st)
   hipLaunchKernelGGL(compact_place_kernel, dim3(chunks), dim3(256), 0, st, p, workspace);
   e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const unsigned entries = (unsigned)p.b * (unsigned)p.max_pages, items = entries > (unsigned)p.num_pages ? entries : (unsigned)p.num_pages;
   hipLaunchKernelGGL(compact_apply_kernel, dim3((items + 255) / 256), dim3(256), 0, st, p, workspace);
   return hipGetLastError();
 }
 
 hipError_t launch_copy_pages(const PageCopy& p, hipStream_t st) {
-  hipLaunchKernelGGL(copy_pages_kernel, dim3((unsigned)(p.m < 16384 ? p.m : 16384)), dim3(256), 0, st, p);
+  hipLaunchKernelGGL(copy_pages_kernel, dim3((unsigned)(p.m < kCopyGrid ? p.m : kCopyGrid)), dim3(256), 0, st, p);
   return hipGetLastError();
 }
 

@@ -15,6 +15,8 @@ __device__ __forceinline__ float finite_size(float x) {
   return a < INFINITY ? a : 0.f;
 }
 
+constexpr int kHeld = 8;
+
 // A unit, (sequence, one of the blocks that its new rows reach, head, K or V), is THREADS threads' work: 64, or 256 where a block has many values.  Its rows are one run of
 // memory in the pool, and h_kv apart in the new rows.
 template <bool E4M3, int THREADS>
@@ -38,32 +40,38 @@ void scaled_append_kernel(ScaledAppend p, int reach) {
   const int first = (L / p.block + turn) * p.block;              // the block's first position, and its rows that are new
   const int begin = max(first, L), end = min(first + p.block, L + count);
   if (begin >= end) return;
-  const int row = paged_row(c, c.table + (size_t)i * c.max_pages, e, first);
-  if (row < 0) return;
   const int w4 = (is_v ? c.v : c.k) >> 2;
-  float* const scale_at = (is_v ? p.V_scales : p.K_scales) + row / p.block;
-  uint32_t* const held = static_cast<uint32_t*>(is_v ? c.V : c.K) + (size_t)row * w4;
   const float4* const fresh = reinterpret_cast<const float4*>(is_v ? p.a.v_new : p.a.k_new) + (((size_t)i * p.a.n + (begin - L)) * c.h_kv + e) * w4;
   const int older = (begin - first) * w4, all = (end - begin) * w4;
-  const float had = *scale_at;
-  auto new4 = [&](int x) {
-    const int r = x / w4;
-    return fresh[(size_t)r * c.h_kv * w4 + (x - r * w4)];
+  const int step = (c.h_kv - 1) * w4;                            // from one row's end to the next one's beginning
+  const bool power4 = (w4 & (w4 - 1)) == 0;
+  const int shift = __builtin_ctz(w4);
+  auto new4 = [&](int x) { return fresh[x + (step == 0 ? 0 : (power4 ? x >> shift : x / w4) * step)]; };
+  auto most_of = [](float most, const float4& y) {
+    return fmaxf(most, fmaxf(fmaxf(finite_size(y.x), finite_size(y.y)), fmaxf(finite_size(y.z), finite_size(y.w))));
   };
+  // A thread's first kHeld fours stay in registers; a block that has more of them is read twice.
+  float4 mine[kHeld];
+#pragma unroll
+  for (int u = 0; u < kHeld; ++u) mine[u] = new4(min(lane + u * THREADS, all - 1));
+  const int row = paged_row(c, c.table + (size_t)i * c.max_pages, e, first);
+  if (row < 0) return;
+  float* const scale_at = (is_v ? p.V_scales : p.K_scales) + row / p.block;
+  uint32_t* const held = static_cast<uint32_t*>(is_v ? c.V : c.K) + (size_t)row * w4;
+  const float had = older > 0 ? *scale_at : 0.f;
   float most = 0.f;
-  for (int x = lane; x < all; x += THREADS) {
-    const float4 y = new4(x);
-    most = fmaxf(most, fmaxf(fmaxf(finite_size(y.x), finite_size(y.y)), fmaxf(finite_size(y.z), finite_size(y.w))));
-  }
+#pragma unroll
+  for (int u = 0; u < kHeld; ++u) most = most_of(most, mine[u]);
+  for (int x = lane + kHeld * THREADS; x < all; x += THREADS) most = most_of(most, new4(x));
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor(most, off));
   if constexpr (THREADS == 256) {
     if ((lane & 63) == 0) s_most[lane >> 6] = most;
-    __syncthreads();
+    __syncthreads();                                             // (and every wave has read the scale)
     most = fmaxf(fmaxf(s_most[0], s_most[1]), fmaxf(s_most[2], s_most[3]));
   }
   float s = scale_of<E4M3>(most);
-  if (older > 0 && had > s) s = had;                             // (a scale that is no number gives way)
+  if (had > s) s = had;                                          // (a scale that is no number gives way)
   const bool power = (__float_as_uint(s) & 0x007fffffu) == 0 && s >= 0x1p-126f && s <= 0x1p126f;
   const float inv = power ? inverse_of(s) : 0.f;
   if (older > 0 && s != had) {
@@ -74,13 +82,15 @@ void scaled_append_kernel(ScaledAppend p, int reach) {
       held[x] = round4<E4M3>(y);
     }
   }
-  for (int x = lane; x < all; x += THREADS) {
-    float4 y = new4(x);
+  auto put = [&](int x, float4 y) {
     if (power) { y.x *= inv; y.y *= inv; y.z *= inv; y.w *= inv; }
     else { y.x /= s; y.y /= s; y.z /= s; y.w /= s; }             // (a scale that the caller has written)
     held[older + x] = round4<E4M3>(y);
-  }
-  if constexpr (THREADS == 256) __syncthreads();                 // (every wave has read the scale)
+  };
+#pragma unroll
+  for (int u = 0; u < kHeld; ++u)
+    if (lane + u * THREADS < all) put(lane + u * THREADS, mine[u]);
+  for (int x = lane + kHeld * THREADS; x < all; x += THREADS) put(x, new4(x));
   if (lane == 0 && (older == 0 || s != had)) *scale_at = s;
 }
 

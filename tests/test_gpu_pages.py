@@ -45,7 +45,8 @@ def some_tables(rng, b, each, num_pages, page, share=0.3):
 
 
 # b, pages of a sequence, pool, page size, n
-SIZES = [(1, 1, 1, 1, 1), (1, 4, 3, 16, 1), (5, 6, 40, 4, 5), (8, 10, 25, 16, 40), (64, 20, 900, 16, 1), (300, 7, 1500, 3, 9), (1500, 5, 5000, 8, 1), (3000, 3, 4000, 2, 4)]
+SIZES = [(1, 1, 1, 1, 1), (1, 4, 3, 16, 1), (5, 6, 40, 4, 5), (8, 10, 25, 16, 40), (64, 20, 900, 16, 1), (300, 7, 1500, 3, 9), (1500, 5, 5000, 8, 1), (3000, 3, 4000, 2, 4),
+         (8, 40, 200, 2, 30), (1024, 4, 20000, 16, 33), (40, 9, 30000, 5, 16)]
 
 
 @pytest.mark.parametrize("b,each,num_pages,page,n", SIZES)
@@ -109,7 +110,7 @@ def test_fork_and_free(m, b, each, num_pages, page, n):
         assert same(out, want) and same(r, refs)
 
 
-@pytest.mark.parametrize("num_pages", [1, 2, 3, 7, 64, 2047, 2048, 2049, 4096, 6000, 20000])
+@pytest.mark.parametrize("num_pages", [1, 2, 3, 7, 64, 2047, 2048, 2049, 4096, 6000, 16384, 16385, 131072, 131100])
 @pytest.mark.parametrize("full", [0.0, 0.1, 0.5, 0.95, 1.0])
 def test_compact_and_copy(m, num_pages, full):
     """Pools of several types and page sizes; what is in use is found at its new place."""
