@@ -303,7 +303,7 @@ void paged_list_kernel(PagedDecode p) {
 
 // The sequence that a piece is of, which of the sequence's pieces (`off`), and how many a head has (`c`); false: there is no such piece.  Every workgroup looks at all
 // lengths: thread t has sequences t * each up to the next one's.
-template <int LEAST>
+template <bool SCALED>
 __device__ __forceinline__ bool look_for(const PagedDecode& p, int piece, Segment* s, int* off, int* c) {
   __shared__ int s_waves[8][kThreads / 64], s_longest[kThreads / 64];
   __shared__ int s_at[4];
@@ -341,16 +341,19 @@ __device__ __forceinline__ bool look_for(const PagedDecode& p, int piece, Segmen
     for (int x = from + 1; x < to; ++x) count += pieces_of(tiles_of(p, p.lens[x]), per);
     before = before_me(count, s_waves[++turn], &all);
   };
+  // Caches of 8 bits: two workgroups to a unit from the start where a unit's share is more than 16 tiles (48 sequences of 2048, 32 heads: one 21.3 us, two 22.7; 256 of up to 2000 41.2 and
+  // 35.0; 64 of 8192 40.1 and 39.5), and up to half over an even share each (256 of up to 2000, 32 heads: 35.0, a quarter over it 44.9; 300 of up to 1500 35.6 and 45.2).
+  const int least = SCALED && total * p.blocks > 16 * kComputeUnits ? 2 : 1, over = SCALED ? 12 : 10;
   bool fits = false;
   if (many) {
     longest = max(max(s_longest[0], s_longest[1]), max(s_longest[2], s_longest[3]));
     fits = left_whole(p, longest, total);
     if (fits) cut(longest);
   }
-  for (int most = LEAST * kComputeUnits; most <= 2 * kComputeUnits; most *= 2) {
+  for (int most = least * kComputeUnits; most <= 2 * kComputeUnits; most *= 2) {
     const int units = most / p.blocks;
     if (!fits && p.b * heads <= units)
-      for (int x = 8; x <= 10 && !fits; ++x) {
+      for (int x = 8; x <= over && !fits; ++x) {
         cut((int)(((long long)total * x + 8 * units - 1) / (8 * units)));
         fits = all * heads <= units;
       }
@@ -377,8 +380,8 @@ __device__ __forceinline__ bool look_for(const PagedDecode& p, int piece, Segmen
   return true;
 }
 
-// This workgroup's segment; false: there is none.  LEAST: workgroups of a compute unit that are tried first.
-template <int LEAST>
+// This workgroup's segment; false: there is none.
+template <bool SCALED>
 __device__ __forceinline__ bool find_segment(const PagedDecode& p, Segment* s) {
   const int tid = threadIdx.x, heads = p.c.h_kv;
   int piece = blockIdx.x, block = 0;
@@ -406,7 +409,7 @@ __device__ __forceinline__ bool find_segment(const PagedDecode& p, Segment* s) {
     off = piece - work.y * heads;
     c = work.z;
     s->L = paged_length(p.c, work.w);
-  } else if (!look_for<LEAST>(p, piece, s, &off, &c)) {
+  } else if (!look_for<SCALED>(p, piece, s, &off, &c)) {
     return false;
   }
   s->e = heads == 1 ? 0 : off / c;
@@ -763,7 +766,7 @@ void paged_matrix_kernel(PagedDecode p) {
   __shared__ __align__(16) int s_rows[kWaves][2][32];
   __shared__ int s_odd;
   Segment s;
-  if (!find_segment<1>(p, &s)) return;
+  if (!find_segment<false>(p, &s)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i16 = lane & 15, g = lane >> 4;
   int (&places)[2][32] = s_rows[wave];
   const int32_t* table = p.c.table + (size_t)s.i * p.c.max_pages;

@@ -1,7 +1,6 @@
 // Attention over paged caches of 8 bits with a scale for each block of positions and head: o = sum_p weights[p] s_V(p) V8[p] of logits scale s_K(p) (q . K8[p]).
 //
-// The work is cut, merged, and done again in the plain form where infinities and NaN take part, as in paged_decode.hpp; the pieces are for two workgroups to a compute unit, since
-// half the bytes to a product leave the instructions, not HBM, as what bounds them (b=64, m=8192, h=32: 49 us with one, 43 with two).  A workgroup is four waves, wave w has tiles w, w + 4, ... of 32 positions for 16 or
+// The work is cut, merged, and done again in the plain form where infinities and NaN take part, as in paged_decode.hpp.  A workgroup is four waves, wave w has tiles w, w + 4, ... of 32 positions for 16 or
 // 32 query rows.  Both products are v_mfma_f32_16x16x32_f16; 8 bits are exact in fp16.
 //   logits^T[32 pos x 16 rows] = K_tile . q^T: lane (i, g) has the 16-byte pieces g, g + 4, ... of two K rows, a piece's first eight columns for one product, the others for the next.  q's rows are
 //     brought by one power of two to 2^13 .. 2^14 at most and taken as two fp16 terms: 23 bits of what is not below 2^-16 of the largest, and 2^-39 of the largest of what is.
@@ -287,7 +286,7 @@ void scaled_matrix_kernel(PagedDecode p) {
   __shared__ float s_most[kWaves];
   __shared__ int s_odd;
   Segment s;
-  if (!find_segment<2>(p, &s)) return;
+  if (!find_segment<true>(p, &s)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i16 = lane & 15, g = lane >> 4;
   int (&places)[2][64] = s_rows[wave];
   const int32_t* table = p.c.table + (size_t)s.i * p.c.max_pages;
@@ -410,15 +409,19 @@ void scaled_matrix_kernel(PagedDecode p) {
       }
       floatx4 sc[2][HB];
       take_k(buf, half);
+      __builtin_amdgcn_s_setprio(1);                       // (before the other wave's softmax; 1 % here)
       R::first_product(tl[half], qs, lane, sc, [&](int x) {
         if (x & 1) load_k(half, x >> 1);
       });
+      __builtin_amdgcn_s_setprio(0);
       float w[HB][8];
       rows.weights(lane, p0, half, (uint32_t)(bad >> (32 * half)), s_scales[wave][buf ^ 1], mantissas_now, sc, w);
       u32x4 wt[HB][2];
       R::split(w, wt);
       if (half == 1 || t + kWaves >= ntiles) put_scales(buf, bad_next);
+      __builtin_amdgcn_s_setprio(1);
       rows.second_product(wt, tl[half]);
+      __builtin_amdgcn_s_setprio(0);
       load_v(buf, half);
     }
     bad = bad_next;
