@@ -390,7 +390,8 @@ int mqa_paged_evict_kv(void* K_pages, void* V_pages, const int32_t* table_in, co
  * it has, and if that is s', its older rows are rounded again to it.  (A scale does not become smaller while its block has rows, so that drafts that are refused may leave a block a coarser one.)  New values
  * are rounded to the nearest number, the even one of two, infinities to +-Q; NaN is e4m3's NaN, int8's 0.  b * h_kv * ((n + block - 2) / block + 1) <= 2^23.
  *
- * mqa_paged_scaled_decode_step: as mqa_paged_decode_step without scores.  Scales may be any float32.
+ * mqa_paged_scaled_decode_step: as mqa_paged_decode_step without scores.  Scales may be any float32.  8 bits are exact in the products; q has 23 bits (of a number that is less than 2^-16 of the
+ * largest of its 16 or 32 rows: 2^-39 of that largest), and a position's weight times V's scale 23 bits, or, below 2^-12 of its row's largest, 2^-35 of that largest.
  */
 int mqa_paged_scaled_append_kv_rows(const float* k_new, const float* v_new, const int32_t* counts, void* K_pages, float* K_scales, void* V_pages, float* V_scales,
                                     const int32_t* table, const int32_t* lens_in, int32_t* lens_out, int b, int n, int h_kv, int num_pages, int page_size,

@@ -80,8 +80,9 @@ template <int D> struct Tile8 {
 constexpr float kRoom = 4.f;         // log2 of the largest w over 2^kTop before the maximum is moved; with a mantissa below 2 all stay below 2^15
 constexpr float kTop = 10.f;
 constexpr int kNear = 16;            // ref is moved for scales that are so many powers of two off
-constexpr int kFar = 64;             // what is further below the tile's largest is the plain form's, unless it is below 2^kNothing: then it is nothing
-constexpr int kNothing = -100;
+// A row's sum and its maximum go apart by the scales: from 2^-kFar to 2^kFar all numbers that count stay float32's; other scales are the plain form's, unless they are below 2^-kNothing
+// and their rows are zeros (which an append gives the smallest scale).
+constexpr int kFar = 50, kNothing = 100;
 
 // Of two tiles' positions, in LDS: K's scale with q's power of two, E - ref, 2^-E, the mantissa.
 struct Scales { float f[64], e[64], inv[64], mant[64]; };
@@ -360,11 +361,11 @@ void scaled_matrix_kernel(PagedDecode p) {
   // ---- the scales of the pair that `publish` was last called for, into LDS; m_run goes with ref
   int ref = 0;
   uint64_t nothing = 0;                                    // positions whose V is nothing beside the others'
-  bool mantissas = false, far = false;
+  bool mantissas = false, far = false, tiny = false;       // tiny: a row that is not nothing after all
   auto put_scales = [&](int buf, uint64_t missing) {
     const bool there = !(missing >> lane & 1);
     const uint32_t bits = there ? __float_as_uint(vs) : 0x3f800000u;
-    const bool none = bits < (uint32_t)(127 + kNothing) << 23;                      // (0 and the smallest)
+    const bool none = bits < (uint32_t)(127 - kNothing) << 23;                      // (0 and the smallest)
     const int exponent = (int)(bits >> 23) - 127;                                   // (a negative scale's: above all others)
     int e = there && !none ? exponent : ref;
     if (__any(e > ref + kNear || e < ref - kNear)) {
@@ -375,10 +376,9 @@ void scaled_matrix_kernel(PagedDecode p) {
 #pragma unroll
       for (int hb = 0; hb < HB; ++hb) rows.m_run[hb] -= (float)(most - ref);
       ref = most;
-      if (!there) e = ref;
+      if (!there || none) e = ref;
     }
-    if (none) e = ref - kFar;
-    far = far || __any(e < ref - kFar || e > 100 || e < -125);
+    far = far || __any(e < -kFar || e > kFar);
     Scales& own = s_scales[wave][buf];
     own.f[lane] = there ? ldexpf(ks, up) : 0.f;
     own.e[lane] = (float)(e - ref);
@@ -401,11 +401,18 @@ void scaled_matrix_kernel(PagedDecode p) {
       if (half == 1 && t + kWaves >= ntiles) break;        // (and there is no next pair)
       const int p0 = s.begin + kPagedTile * (t + kWaves * half);
       if (zeros) {
-        uint32_t mine = (uint32_t)(zeros >> (32 * half)) >> (8 * g);
-        asm volatile("" : "+v"(mine));                     // (a branch)
+        uint32_t mine = (uint32_t)(zeros >> (32 * half)) >> (8 * g), absent = (uint32_t)(bad >> (32 * half)) >> (8 * g);
+        asm volatile("" : "+v"(mine), "+v"(absent));       // (a branch)
 #pragma unroll
         for (int e = 0; e < 8; ++e)
-          if (mine >> e & 1) tl[half].vr[e] = typename Form8<D>::VRow{};
+          if (mine >> e & 1) {
+            uint32_t bits = 0;
+#pragma unroll
+            for (int x = 0; x < (D > 64 ? D / 64 : 1); ++x) bits |= tl[half].vr[e][x];
+            if (std::is_same<T, E4M3>::value) bits &= 0x7f7f7f7fu;      // (-0)
+            tiny = tiny || (bits != 0 && !(absent >> e & 1));
+            tl[half].vr[e] = typename Form8<D>::VRow{};
+          }
       }
       floatx4 sc[2][HB];
       take_k(buf, half);
@@ -430,7 +437,7 @@ void scaled_matrix_kernel(PagedDecode p) {
     next = look_up(t + 6 * kWaves);
   }
 
-  if (far || rows.odd()) s_odd = 1;
+  if (far || tiny || rows.odd()) s_odd = 1;
   __syncthreads();                                         // (and the q operands are read)
   if (s_odd) {
     in_plain_form<T>(p, s, R::NH, smem);

@@ -198,6 +198,29 @@ def test_scales_far_apart(m, h, kind):
 
 
 @pytest.mark.parametrize("kind", ["e4m3", "int8"])
+@pytest.mark.parametrize("h,each", [(8, 30), (32, 30), (8, 120)])
+def test_scales_apart_and_nothing(m, h, each, kind):
+    """V's scales from 2^-45 to 2^45, tile by tile and within tiles, K's of many sizes; blocks of zeros, which have the smallest scale, with most of a row's weight: they count in its sum; scales that are
+    no powers of two; one that is smaller than any, whose rows are no zeros and all that a sequence has."""
+    rng = np.random.default_rng(h + each)
+    (K, Ks, V, Vs), _ = cache_of(rng, 3, each, 1, 16, 16, 128, 128, kind)
+    table, lens = tables(rng, 3, each), np.array([16 * each - 5, 16 * each, 20])
+    for x in range(each):
+        Vs[table[0, x]] = 2.0 ** ((45, -45, 0, 3)[x // 2 % 4] if x < each // 2 else rng.integers(-45, 46))
+        Vs[table[1, x]] = np.float32(rng.random() + 0.5)
+    Vs[table[1, 3:9]], V[table[1, 3:9]] = 2.0 ** -126, 0
+    V[table[1, 4]] = -0.0
+    Vs[table[2]] = 2.0 ** -120
+    q = (0.3 * rng.standard_normal((3, 1, h, 128))).astype(np.float32)
+    K[table[1, 5], 0, 2] = np.sign(q[1, 0, 0]) * 96                          # (a row of zeros takes most of the weight)
+    want, size, K_all, top = attended(q, (K, Ks, V, Vs), table, lens, 0.1)
+    got = m.mqa_paged_scaled_decode_step(f32(q[:, 0]), bits(K, kind, True), f32(Ks, True), bits(V, kind, True), f32(Vs, True), i32(table), i32(lens), scale=0.1).cpu().numpy()
+    bound = tolerance(q, K_all, size, 0.1, 16 * each, kind, top)
+    bound[2] = tolerance(q, K_all, size, 0.1, 16 * each, kind, top)[2] - 1e-30 + 2.0 ** -149      # (down to float32's smallest)
+    assert (np.abs(got - want[:, 0]) <= bound[:, 0]).all()
+
+
+@pytest.mark.parametrize("kind", ["e4m3", "int8"])
 def test_large_logits(m, kind):
     """Logits of hundreds: one position takes all the weight, others none."""
     rng = np.random.default_rng(5)
