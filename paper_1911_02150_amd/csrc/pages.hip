@@ -17,9 +17,9 @@ void fork_kernel(PageFork p) {
   const int parent = p.parents[j];
   int len = 0, entry = -1;
   if ((unsigned)parent < (unsigned)p.b_in) {
+    entry = p.table_in[(size_t)parent * p.max_pages + x];      // (on its way with the length)
     len = min(max(p.lens_in[parent], 0), p.max_pages * p.page_size);
-    if (x < pages_of(len, p.page_size)) entry = p.table_in[(size_t)parent * p.max_pages + x];
-    if (!is_page(entry, p.num_pages)) entry = -1;
+    if (x >= pages_of(len, p.page_size) || !is_page(entry, p.num_pages)) entry = -1;
   }
   if (entry >= 0) atomicAdd(p.refs + entry, 1);
   p.table_out[idx] = entry;
@@ -31,9 +31,9 @@ void free_kernel(PageFree p) {
   const unsigned idx = blockIdx.x * 256u + threadIdx.x;
   if (idx >= (unsigned)p.b * (unsigned)p.max_pages) return;
   const int i = (int)(idx / (unsigned)p.max_pages), x = (int)(idx - (unsigned)i * (unsigned)p.max_pages);
+  const int entry = p.table[idx];                        // (on its way with the length)
   const int len = min(max(p.lens[i], 0), p.max_pages * p.page_size);
   if (x < pages_of(len, p.page_size)) return;
-  const int entry = p.table[idx];
   if (is_page(entry, p.num_pages)) atomicSub(p.refs + entry, 1);
   if (entry != -1) p.table[idx] = -1;
 }
