@@ -26,7 +26,7 @@ static size_t lay_out(PagedDecode* p, const PagedPlan& pl, float* at) {
   return floats * sizeof(float);
 }
 
-PagedPlan paged_plan(int b, int n, int h, int h_kv, int page_size, int max_pages, int k, int v, int is_bf16, int with_scores) {
+PagedPlan paged_plan(int b, int n, int h, int h_kv, int page_size, int max_pages, int k, int v, int is_bf16, int with_scores, int whole) {
   PagedPlan pl = {};
   const long long R = (long long)n * (h / h_kv), positions = (long long)max_pages * page_size, tiles = (positions + kPagedTile - 1) / kPagedTile;
   const int wide = k > v ? k : v;
@@ -44,7 +44,7 @@ PagedPlan paged_plan(int b, int n, int h, int h_kv, int page_size, int max_pages
   // and 12.6; one of 500 9.2 and 11.1, of 800 12.0 and 11.1; float32, one of 380 13.6 both, of 500 15.9 and 13.6), and to greater lengths where there is one for
   // every compute unit (256 of up to 1000, 32 heads: 25, in pieces 32).
   const bool heavy = wide > 128 || (!is_bf16 && wide > 64);
-  pl.split = tiles > (groups * pl.blocks >= kComputeUnits ? 32 : heavy ? 12 : 16);
+  pl.split = tiles > (groups * pl.blocks >= kComputeUnits ? whole : heavy ? 12 : 16);
   pl.listed = pl.split && b > kLookedFor;
   const long long least = groups * ((tiles + 3) / 4), most = groups + kShares;      // (pieces of four tiles; a last, shorter one in every group)
   pl.pieces = (int)(!pl.split ? groups : least < most ? least : most);
