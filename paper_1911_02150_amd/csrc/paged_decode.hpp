@@ -310,9 +310,24 @@ __device__ __forceinline__ bool look_for(const PagedDecode& p, int piece, Segmen
   const int tid = threadIdx.x, heads = p.c.h_kv;
   const int each = (p.b + kThreads - 1) / kThreads, from = tid * each, to = min(p.b, from + each);
   const int len = from < to ? p.lens[from] : 0;            // (up to 256 sequences: read once)
+  int more[kLookedFor / kThreads - 1];                     // 8 bits: so are up to kLookedFor (512 of up to 4096, 32 heads: 91 us, so 89)
+  if constexpr (SCALED) {
+#pragma unroll
+    for (int x = 0; x < kLookedFor / kThreads - 1; ++x) more[x] = from + 1 + x < to ? p.lens[from + 1 + x] : 0;
+  }
+  auto length = [&](int x) {                               // of sequence x, from < x < to
+    if constexpr (SCALED) {
+      int y = more[0];
+#pragma unroll
+      for (int z = 1; z < kLookedFor / kThreads - 1; ++z) y = x == from + 1 + z ? more[z] : y;
+      return y;
+    } else {
+      return p.lens[x];
+    }
+  };
   int mine = tiles_of(p, len), longest = mine;
   for (int x = from + 1; x < to; ++x) {
-    const int t = tiles_of(p, p.lens[x]);
+    const int t = tiles_of(p, length(x));
     mine += t;
     longest = max(longest, t);
   }
@@ -338,7 +353,7 @@ __device__ __forceinline__ bool look_for(const PagedDecode& p, int piece, Segmen
   auto cut = [&](int tiles) {
     per = whole_waves(tiles);
     count = from < to ? pieces_of(tiles_of(p, len), per) : 0;
-    for (int x = from + 1; x < to; ++x) count += pieces_of(tiles_of(p, p.lens[x]), per);
+    for (int x = from + 1; x < to; ++x) count += pieces_of(tiles_of(p, length(x)), per);
     before = before_me(count, s_waves[++turn], &all);
   };
   // Caches of 8 bits: two workgroups to a unit from the start where a unit's share is more than 16 tiles (48 sequences of 2048, 32 heads: one 21.3 us, two 22.7; 256 of up to 2000 41.2 and
@@ -364,7 +379,7 @@ __device__ __forceinline__ bool look_for(const PagedDecode& p, int piece, Segmen
     int x = from, L = len, mine = pieces_of(tiles_of(p, len), per);
     while (piece >= (before + mine) * heads) {
       before += mine;
-      L = p.lens[++x];
+      L = length(++x);
       mine = pieces_of(tiles_of(p, L), per);
     }
     s_at[0] = x;

@@ -300,7 +300,7 @@ void scaled_matrix_kernel(PagedDecode p) {
   struct Place { int entry, inside; };
   auto look_up = [&](int t) {
     const int pos = min(s.begin + kPagedTile * (t + kWaves * (lane >> 5)) + (lane & 31), max(s.end - 1, 0));
-    const unsigned page = (unsigned)pos / (unsigned)p.c.page_size;
+    const unsigned page = (p.c.page_size & (p.c.page_size - 1)) == 0 ? (unsigned)pos >> __builtin_ctz(p.c.page_size) : (unsigned)pos / (unsigned)p.c.page_size;
     return Place{table[page], pos - (int)page * p.c.page_size};
   };
   Tile8<D> tl[2];
