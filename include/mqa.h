@@ -405,7 +405,7 @@ int mqa_paged_scaled_decode_step(const float* q, const void* K_pages, const floa
  * Who holds which page of a pool.  refs [num_pages] (int32) counts the entries of tables that name a page; one with a count of 0 (or less) is free.  The calls change
  * tables and counts alone, on the device and in the stream's order (they may be captured); every pool that goes by the same tables (each layer's) then gets mqa_paged_copy_pages
  * with the moves that they leave.  An entry outside [0,num_pages) names no page.  What a call does depends on its arguments alone: pages are given out from the lowest
- * free one on.  Calls that change one refs must not overlap.  Limits: num_pages <= 2^24, max_pages * page_size <= 2^24, sequences * max_pages <= 2^28.
+ * free one on.  Calls that change one refs must not overlap.  Limits: num_pages <= 2^24, max_pages * page_size <= 2^24, sequences * max_pages <= 2^28, sequences of a reservation <= 2^20.
  *
  * fork:    sequence j of table_out [b_out,max_pages] starts as sequence parents[j] of table_in [b_in,max_pages] is: it names the pages of that one's lens_in positions (and none behind them),
  *          their counts grow by one, lens_out[j] is its length; empty if parents[j] is outside [0,b_in).  What table_out named before is not given back (free it first).
@@ -539,7 +539,7 @@ int mqa_stack_feed_forward(const float* W1, const float* W2, float* x, int rows,
  *   not allowed: x = -infinity
  * repetition, frequency, presence [b]: NULL: 1, 0, 0.  bias: the value of the last of bias_tokens [b,biases] that is t, of bias_values [b,biases] (biases = 0: none, both may be NULL).
  * allowed [b,n+1,ceil(vocab / 32)]: token t is allowed if bit t % 32 of word t / 32 is set (NULL: all are); a grammar's mask may leave none.  Tokens outside [0,vocab) count for nothing.
- * n <= 65536, vocab <= 2^24, cap <= 2^24, biases <= 2^24, b * ceil(vocab / 512) <= 2^23, b * max(cap, biases) <= 2^31.
+ * cap = 0: no history (it may be NULL).  n <= 65536, vocab <= 2^24, cap <= 2^24, biases <= 2^24, b * ceil(vocab / 512) <= 2^23, b * max(cap, biases) <= 2^31.
  */
 int mqa_stack_adjust_logits(const float* logits, float* out, const int32_t* history, const int32_t* lens, const int32_t* prompts, const int32_t* drafts,
                             const float* repetition, const float* frequency, const float* presence, const int32_t* bias_tokens, const float* bias_values,

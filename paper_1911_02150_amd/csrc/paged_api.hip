@@ -182,7 +182,7 @@ int mqa_paged_free_pages(int32_t* table, const int32_t* lens, int32_t* refs, int
 }
 
 static bool reserve_sizes_ok(int b, int n, int num_pages, int page_size, int max_pages) {
-  return table_sizes_ok(b, num_pages, page_size, max_pages) && n > 0 && n <= max_pages * page_size;
+  return table_sizes_ok(b, num_pages, page_size, max_pages) && b <= (1 << 20) && n > 0 && n <= max_pages * page_size;
 }
 
 size_t mqa_paged_reserve_workspace_bytes(int b, int n, int num_pages, int page_size, int max_pages) {
@@ -244,10 +244,10 @@ int mqa_paged_copy_pages(void* const* pools, const size_t* page_bytes, int num_p
 int mqa_stack_adjust_logits(const float* logits, float* out, const int32_t* history, const int32_t* lens, const int32_t* prompts, const int32_t* drafts,
                             const float* repetition, const float* frequency, const float* presence, const int32_t* bias_tokens, const float* bias_values,
                             const uint32_t* allowed, int b, int n, int vocab, int cap, int biases, void* stream) {
-  if (!logits || !out || !history || !lens || (n > 0 && !drafts) || (biases > 0 && (!bias_tokens || !bias_values))) return MQA_ERR_NULL;
-  if (b <= 0 || n < 0 || n > (1 << 16) || vocab <= 0 || vocab > (1 << 24) || cap <= 0 || cap > (1 << 24) || biases < 0 || biases > (1 << 24)) return MQA_ERR_SHAPE;
+  if (!logits || !out || (cap > 0 && !history) || !lens || (n > 0 && !drafts) || (biases > 0 && (!bias_tokens || !bias_values))) return MQA_ERR_NULL;
+  if (b <= 0 || n < 0 || n > (1 << 16) || vocab <= 0 || vocab > (1 << 24) || cap < 0 || cap > (1 << 24) || biases < 0 || biases > (1 << 24)) return MQA_ERR_SHAPE;
   if ((long long)b * ((vocab + 511) / 512) > (1ll << 23) || (long long)b * (cap > biases ? cap : biases) > (1ll << 31)) return MQA_ERR_SHAPE;
-  if (misaligned(logits) || misaligned(out) || misaligned(history) || misaligned(lens) || (prompts && misaligned(prompts)) || (drafts && misaligned(drafts)) ||
+  if (misaligned(logits) || misaligned(out) || (history && misaligned(history)) || misaligned(lens) || (prompts && misaligned(prompts)) || (drafts && misaligned(drafts)) ||
       (repetition && misaligned(repetition)) || (frequency && misaligned(frequency)) || (presence && misaligned(presence)) || (bias_tokens && misaligned(bias_tokens)) ||
       (bias_values && misaligned(bias_values)) || (allowed && misaligned(allowed)))
     return MQA_ERR_ALIGN;

@@ -112,6 +112,17 @@ def test_what_nothing_touches_stays(m):
     assert got[1, 0, 4] == np.inf and np.isneginf(got[1, 0, 5]) and got[1, 0, 6] == 0 and np.isneginf(got[1, 1]).all()
 
 
+def test_no_history(m):
+    """Nothing before the drafts: an array without columns, lengths of 0 or beyond."""
+    from oracle import serving
+    rng = np.random.default_rng(3)
+    logits, drafts = rng.standard_normal((2, 3, 40)).astype(np.float32), np.array([[3, 3], [39, -1]], dtype=np.int32)
+    history, lens, factor = np.zeros((2, 0), dtype=np.int32), np.array([0, 5], dtype=np.int32), np.array([1.5, 2], dtype=np.float32)
+    a = dict(logits=logits, history=history, lens=lens, drafts=drafts, repetition=factor, frequency=factor)
+    got = m.mqa_stack_adjust_logits(**{x: on(y) for x, y in a.items()}).cpu().numpy()
+    assert (np.abs(got - serving.adjust(**a)) <= EPS * 6 * (2 * np.abs(logits) + 2 * 3)).all()
+
+
 def test_streams_and_graphs(m):
     rng = np.random.default_rng(6)
     a, kw = case(rng, 3, 2, 3000, 200, 10, EVERY)

@@ -129,7 +129,7 @@ def test_reserve_refuses():
         if x != 2:
             assert call(but(ptrs, x, None)) == NULL
         assert call(but(ptrs, x, U)) == ALIGN
-    for s in bad_table_sizes() + [dict(n=0), dict(n=129)]:
+    for s in bad_table_sizes() + [dict(n=0), dict(n=129), dict(b=(1 << 20) + 1)]:
         assert call(**s) == SHAPE, s
     assert call(but(ptrs, 4, ptrs[1])) == SHAPE and call(but(ptrs, 4, ptrs[2])) == SHAPE
     assert call(ws=None) == WORKSPACE and call(nbytes=need - 1) == WORKSPACE and call(ws=U) == ALIGN
@@ -180,7 +180,7 @@ def test_adjust_refuses():
         assert call(but(ptrs, x, None)) == NULL
     for x in range(12):
         assert call(but(ptrs, x, U)) == ALIGN
-    for s in (dict(b=0), dict(n=-1), dict(n=(1 << 16) + 1), dict(vocab=0), dict(vocab=(1 << 24) + 1), dict(cap=0), dict(cap=(1 << 24) + 1), dict(biases=-1),
+    for s in (dict(b=0), dict(n=-1), dict(n=(1 << 16) + 1), dict(vocab=0), dict(vocab=(1 << 24) + 1), dict(cap=-1), dict(cap=(1 << 24) + 1), dict(biases=-1),
               dict(biases=(1 << 24) + 1), dict(b=1 << 23, vocab=513), dict(b=1 << 10, cap=(1 << 21) + 1)):
         assert call(**s) == SHAPE, s
 
