@@ -17,15 +17,17 @@ __device__ __forceinline__ float finite_size(float x) {
 
 constexpr int kHeld = 8;
 
-// A unit, (sequence, one of the blocks that its new rows reach, head, K or V), is THREADS threads' work: 64, or 256 where a block has many values.  Its rows are one run of
-// memory in the pool, and h_kv apart in the new rows.
+// A unit, (sequence, one of the blocks that its new rows reach, head, K or V), is THREADS threads' work: 64, 256 or 1024.  Its rows are one run of
+// memory in the pool, and h_kv apart in the new rows.  HBM bounds it, five bytes a value (64 prompts of 640, two widths of 128, 52 MB: 13 us = 4.0 TB/s in blocks of 16 or 64), and for a token each the launch
+// and three reads in a row: length, entry, scale (128 sequences: 3.7 us).
 template <bool E4M3, int THREADS>
-__global__ __launch_bounds__(256)
+__global__ __launch_bounds__(THREADS < 256 ? 256 : THREADS)
 void scaled_append_kernel(ScaledAppend p, int reach) {
-  __shared__ float s_most[4];
+  constexpr int WAVES = THREADS / 64, GROUP = THREADS < 256 ? 256 : THREADS;
+  __shared__ float s_most[WAVES];
   const PagedCache& c = p.a.c;
   const int lane = threadIdx.x % THREADS;
-  unsigned unit = blockIdx.x * (256u / THREADS) + threadIdx.x / THREADS;
+  unsigned unit = blockIdx.x * (unsigned)(GROUP / THREADS) + threadIdx.x / THREADS;
   if (unit >= (unsigned)p.a.b * reach * c.h_kv * 2) return;
   const bool is_v = unit & 1;
   unit >>= 1;
@@ -50,7 +52,7 @@ void scaled_append_kernel(ScaledAppend p, int reach) {
   auto most_of = [](float most, const float4& y) {
     return fmaxf(most, fmaxf(fmaxf(finite_size(y.x), finite_size(y.y)), fmaxf(finite_size(y.z), finite_size(y.w))));
   };
-  // A thread's first kHeld fours stay in registers; a block that has more of them is read twice.
+  // A thread's first kHeld fours stay in registers; a block that has more of them is read twice (64 prompts of 100 to 1000, 42 MB: all of them twice 17.5 us, once 11.6).
   float4 mine[kHeld];
 #pragma unroll
   for (int u = 0; u < kHeld; ++u) mine[u] = new4(min(lane + u * THREADS, all - 1));
@@ -65,10 +67,11 @@ void scaled_append_kernel(ScaledAppend p, int reach) {
   for (int x = lane + kHeld * THREADS; x < all; x += THREADS) most = most_of(most, new4(x));
 #pragma unroll
   for (int off = 32; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor(most, off));
-  if constexpr (THREADS == 256) {
+  if constexpr (WAVES > 1) {
     if ((lane & 63) == 0) s_most[lane >> 6] = most;
     __syncthreads();                                             // (and every wave has read the scale)
-    most = fmaxf(fmaxf(s_most[0], s_most[1]), fmaxf(s_most[2], s_most[3]));
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) most = fmaxf(most, s_most[w]);
   }
   float s = scale_of<E4M3>(most);
   if (had > s) s = had;                                          // (a scale that is no number gives way)
@@ -96,20 +99,23 @@ void scaled_append_kernel(ScaledAppend p, int reach) {
 
 }  // namespace
 
+// As few threads as hold a unit's values, 32 each, in registers.  64 prompts of 640, two widths of 128, 64 / 256 / 1024 threads: blocks of 8 14.7 / 30.8 / 85.8 us, 16 13.0 / 18.6 / 47.6,
+// 32 16.7 / 14.2 / 28.3, 64 28.1 / 13.1 / 18.4, 128 51 / 16.6 / 15.1, 256 96 / 29 / 16.7; one prompt in blocks of 16 4.3 / 3.7 / 4.8, of 256 53 / 14.9 / 6.5; 128 tokens 3.7 / 3.8 / 5.1.
+template <bool E4M3>
+static void launch_units(const ScaledAppend& p, int reach, unsigned units, long long values, hipStream_t st) {
+  // (grids of less than 2^32 threads)
+  if (values > 256 * 4 * kHeld && units < 1u << 22) hipLaunchKernelGGL((scaled_append_kernel<E4M3, 1024>), dim3(units), dim3(1024), 0, st, p, reach);
+  else if (values > 64 * 4 * kHeld && units < 1u << 24) hipLaunchKernelGGL((scaled_append_kernel<E4M3, 256>), dim3(units), dim3(256), 0, st, p, reach);
+  else hipLaunchKernelGGL((scaled_append_kernel<E4M3, 64>), dim3((units + 3) / 4), dim3(256), 0, st, p, reach);
+}
+
 hipError_t launch_scaled_append(const ScaledAppend& p, int is_e4m3, hipStream_t st) {
   const int reach = (p.a.n + p.block - 2) / p.block + 1;         // blocks that n rows reach, at most
   const unsigned units = (unsigned)p.a.b * reach * p.a.c.h_kv * 2;
   const int wide = p.a.c.k > p.a.c.v ? p.a.c.k : p.a.c.v;
-  const int rows = p.block < p.a.n ? p.block : p.a.n;
-  const bool large = (long long)rows * wide > 8192;
-  const unsigned grid = large ? units : (units + 3) / 4;
-  if (is_e4m3) {
-    if (large) hipLaunchKernelGGL((scaled_append_kernel<true, 256>), dim3(grid), dim3(256), 0, st, p, reach);
-    else hipLaunchKernelGGL((scaled_append_kernel<true, 64>), dim3(grid), dim3(256), 0, st, p, reach);
-  } else {
-    if (large) hipLaunchKernelGGL((scaled_append_kernel<false, 256>), dim3(grid), dim3(256), 0, st, p, reach);
-    else hipLaunchKernelGGL((scaled_append_kernel<false, 64>), dim3(grid), dim3(256), 0, st, p, reach);
-  }
+  const long long values = (long long)(p.block < p.a.n ? p.block : p.a.n) * wide;
+  if (is_e4m3) launch_units<true>(p, reach, units, values, st);
+  else launch_units<false>(p, reach, units, values, st);
   return hipGetLastError();
 }
 

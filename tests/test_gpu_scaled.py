@@ -297,6 +297,9 @@ APPEND = [
     (5, 7, 3, 16, 112, 21, 7, [0, 6, 13, 20, 2], None),
     (3, 2, 1, 128, 128, 16, 16, [-1, 1 << 30, 95], None),
     (1, 300, 1, 208, 96, 300, 100, [55], None),
+    (2, 400, 1, 256, 112, 300, 300, [299, 10], [400, 1]),
+    (3, 40, 2, 128, 80, 32, 32, [31, 0, 32], [40, 33, 1]),
+    (2, 100, 1, 144, 64, 64, 64, [1, 64], None),
 ]
 
 
