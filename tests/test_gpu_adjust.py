@@ -69,6 +69,11 @@ CASES = [
     (1, 30, 512, 10, 4, EVERY),
     (70, 1, 513, 40, 4, EVERY),
     (300, 0, 8192, 90, 4, EVERY),
+    (3, 1, 4096, 8195, 3, EVERY),
+    (5, 0, 4101, 20001, 2, EVERY),
+    (3, 16, 6001, 2047, 30, EVERY),
+    (1, 700, 36, 5, 2, EVERY),
+    (7, 3, 2052, 3, 2, EVERY),
 ]
 
 
