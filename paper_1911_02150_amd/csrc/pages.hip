@@ -77,7 +77,7 @@ __device__ __forceinline__ uint32_t there8(int first, int num_pages) { return fi
 // One workgroup, in steps:
 //  1. of every page that sequences are about to write behind rows that others share: how many are, and the last of them
 //  2. what every sequence needs: per page of its new positions nothing (kKept), a page (kMissing), or a page in place of a shared one (that one's number);
-//     and how many pages that makes, running over the sequences
+//     and how many pages that makes, running over the sequences (a thread has four neighbouring entries at a time)
 //  3. as many free pages as are needed, or as there are
 //  4. to the sequences whose running number is there: their pages
 // (Step 4 reads what step 2 has written down and no counts, since it changes them.)
@@ -86,8 +86,8 @@ constexpr int kKept = -2, kMissing = -1;
 
 struct ReserveSpace {
   int2* writers;       // [num_pages]: how many, the last (written before they are read, where they are read)
-  int32_t* needs;      // [b, slots]
-  int32_t* running;    // [b]
+  int2* needs;         // [b, slots]: what, and which of the pages it would be
+  int2* running;       // [b]: pages before the sequence (-1: it keeps one that others are about to leave), and with it
   int32_t* pages;      // free ones
   int slots;
   size_t bytes;
@@ -95,14 +95,41 @@ struct ReserveSpace {
 __host__ __device__ ReserveSpace reserve_space(int b, int n, int num_pages, int page_size, void* at) {
   ReserveSpace s;
   s.slots = (int)((n + (long long)page_size - 2) / page_size) + 1;      // pages that n rows reach, at most
-  const size_t writers = ((size_t)num_pages * 8 + 15) & ~(size_t)15, needs = ((size_t)b * s.slots * 4 + 15) & ~(size_t)15, running = ((size_t)b * 4 + 15) & ~(size_t)15;
+  const size_t writers = ((size_t)num_pages * 8 + 15) & ~(size_t)15, needs = ((size_t)b * s.slots * 8 + 15) & ~(size_t)15, running = ((size_t)b * 8 + 15) & ~(size_t)15;
   unsigned char* const p = static_cast<unsigned char*>(at);
   s.writers = reinterpret_cast<int2*>(p);
-  s.needs = reinterpret_cast<int32_t*>(p + writers);
-  s.running = reinterpret_cast<int32_t*>(p + writers + needs);
+  s.needs = reinterpret_cast<int2*>(p + writers);
+  s.running = reinterpret_cast<int2*>(p + writers + needs);
   s.pages = reinterpret_cast<int32_t*>(p + writers + needs + running);
   s.bytes = writers + needs + running + (((size_t)num_pages * 4 + 15) & ~(size_t)15);
   return s;
+}
+
+// put(x, page) for the x-th free page, x < total at least if there are so many; how many it has come to.  `used`: of a thread's first eight pages.
+template <int T, typename Put>
+__device__ __forceinline__ int find_free(const int32_t* refs, int num_pages, uint32_t used, int total, int (&s_waves)[2][T / 64], Put put) {
+  const int tid = threadIdx.x;
+  auto give = [&](uint32_t free, int first, int at) {
+    for (; free; free &= free - 1) put(at++, first + __ffs(free) - 1);
+  };
+  if (total == 0) return 0;
+  __syncthreads();
+  uint32_t free = ~used & there8(8 * tid, num_pages);
+  int found, at = before_me<T>(__popc(free), s_waves[0], &found);
+  give(free, 8 * tid, at);
+  for (int base = 8 * T; base < num_pages && found < total; base += 16 * T) {      // then twice eight
+    uint32_t more[2];
+#pragma unroll
+    for (int g = 0; g < 2; ++g) more[g] = ~in_use8(refs, base + 8 * (T * g + tid), num_pages) & there8(base + 8 * (T * g + tid), num_pages);
+    __syncthreads();
+    int all;
+    const int before = before_me<T>(__popc(more[0]) | __popc(more[1]) << 16, s_waves[1], &all);      // (up to 8 T each)
+    give(more[0], base + 8 * tid, found + (before & 0xffff));
+    found += all & 0xffff;
+    give(more[1], base + 8 * (T + tid), found + (before >> 16));
+    found += all >> 16;
+  }
+  return found;
 }
 
 // The new positions of sequence i: false: there are none, or no room.
@@ -132,7 +159,7 @@ void reserve_kernel(PageReserve p, void* workspace) {
   int mine = 0;
   for (int i = tid; i < p.b; i += kReserveThreads) {
     const int page = begun_page(i);
-    s.running[i] = page;
+    s.running[i].x = page;
     if (page >= 0) {
       s.writers[page] = make_int2(0, -1);
       mine = 1;
@@ -141,7 +168,7 @@ void reserve_kernel(PageReserve p, void* workspace) {
   __threadfence_block();
   if (__syncthreads_or(mine)) {
     for (int i = tid; i < p.b; i += kReserveThreads) {
-      const int page = s.running[i];
+      const int page = s.running[i].x;
       if (page >= 0) {
         atomicAdd(&s.writers[page].x, 1);
         atomicMax(&s.writers[page].y, i);
@@ -150,67 +177,81 @@ void reserve_kernel(PageReserve p, void* workspace) {
     __threadfence_block();
     __syncthreads();
   }
+  const int items = p.b * s.slots;
   int total = 0;
-  for (int base = 0, turn = 0; base < p.b; base += kReserveThreads, turn ^= 1) {
-    const int i = base + tid;
-    int needs = 0;
-    bool keeps = false;
-    if (i < p.b && wanted(p, i, &w)) {
-      for (int x = w.first; x < w.last; ++x) {
-        const int entry = p.table[(size_t)i * p.max_pages + x];
-        const bool there = is_page(entry, p.num_pages);
-        const int refs = there ? p.refs[entry] : 0;
-        int need = there && refs <= 1 ? kKept : there ? entry : kMissing;
-        if (w.begun && x == w.first) {
-          if (!there) need = kKept;                    // (rows on no page: they stay nowhere)
-          if (need >= 0) {
-            // (past L1, which the atomics do not go through)
-            const int others = __hip_atomic_load(&s.writers[entry].x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            if (others == refs && __hip_atomic_load(&s.writers[entry].y, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == i) { need = kKept; keeps = true; }
-          }
-        }
-        s.needs[(size_t)i * s.slots + (x - w.first)] = need;
-        needs += need != kKept;
-      }
+  for (int base = 0, turn = 0; base < items; base += 4 * kReserveThreads, turn ^= 1) {
+    int seq[4], slot[4], entry[4], refs[4], need[4], needs = 0;
+    bool ours[4], begun[4], keeps[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int item = min(base + 4 * tid + u, items - 1);
+      seq[u] = item / s.slots;
+      slot[u] = item - seq[u] * s.slots;
+      ours[u] = wanted(p, seq[u], &w) && w.first + slot[u] < w.last && base + 4 * tid + u < items;
+      begun[u] = w.begun && slot[u] == 0;
+      entry[u] = ours[u] ? p.table[(size_t)seq[u] * p.max_pages + w.first + slot[u]] : -1;
     }
-    int all;
-    const int before = before_me<kReserveThreads>(needs, s_waves[turn], &all);
-    // (who keeps a page that others are about to leave may do so only if they do)
-    if (i < p.b) s.running[i] = needs == 0 && !keeps ? 0 : total + before + needs;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) refs[u] = is_page(entry[u], p.num_pages) ? p.refs[entry[u]] : 0;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const bool there = is_page(entry[u], p.num_pages);
+      need[u] = !ours[u] || (there && refs[u] <= 1) ? kKept : there ? entry[u] : kMissing;
+      keeps[u] = false;
+      if (ours[u] && begun[u]) {
+        if (!there) need[u] = kKept;                   // (rows on no page: they stay nowhere)
+        if (need[u] >= 0) {
+          // (past L1, which the atomics do not go through)
+          const int others = __hip_atomic_load(&s.writers[entry[u]].x, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+          if (others == refs[u] && __hip_atomic_load(&s.writers[entry[u]].y, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) == seq[u]) { need[u] = kKept; keeps[u] = true; }
+        }
+      }
+      needs += need[u] != kKept;
+    }
+    int all, before = total + before_me<kReserveThreads>(needs, s_waves[turn], &all);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      if (base + 4 * tid + u >= items) break;
+      s.needs[base + 4 * tid + u] = make_int2(need[u], before);
+      // (who keeps a page that others are about to leave may do so only if they do)
+      if (slot[u] == 0) s.running[seq[u]].x = keeps[u] ? -1 : before;
+      before += need[u] != kKept;
+      if (slot[u] == s.slots - 1) s.running[seq[u]].y = before;
+    }
     total += all;
   }
-  int found = 0;
-  for (int base = 0, turn = 0; base < p.num_pages && found < total; base += 8 * kReserveThreads, turn ^= 1) {
-    __syncthreads();
-    const int first = base + 8 * tid;
-    if (base > 0) used = in_use8(p.refs, first, p.num_pages);
-    uint32_t free = ~used & there8(first, p.num_pages);
-    int all, at = found + before_me<kReserveThreads>(__popc(free), s_waves[turn], &all);
-    for (; free; free &= free - 1) s.pages[at++] = first + __ffs(free) - 1;
-    found += all;
-  }
+  const int found = find_free<kReserveThreads>(p.refs, p.num_pages, used, total, s_waves, [&](int x, int page) { s.pages[x] = page; });
   __threadfence_block();
   __syncthreads();
-  for (int i = tid; i < p.b; i += kReserveThreads) {
-    int granted = 0, from = -1, to = -1;
-    if (wanted(p, i, &w) && s.running[i] <= found) {
-      granted = w.count;
-      int at = s.running[i];
-      for (int x = w.last - 1; x >= w.first; --x) {      // (from its last page backwards)
-        const int need = s.needs[(size_t)i * s.slots + (x - w.first)];
-        if (need == kKept) continue;
-        const int page = s.pages[--at];
-        p.table[(size_t)i * p.max_pages + x] = page;
-        p.refs[page] = 1;
-        if (need >= 0) {
-          atomicSub(p.refs + need, 1);
-          if (w.begun && x == w.first) { from = need; to = page; }
-        }
+  for (int base = 0; base < items; base += 4 * kReserveThreads) {
+    int2 need[4], running[4];
+    int page[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int item = min(base + u * kReserveThreads + tid, items - 1);
+      need[u] = s.needs[item];
+      running[u] = s.running[item / s.slots];
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) page[u] = need[u].x != kKept && need[u].y < found ? s.pages[need[u].y] : 0;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int item = base + u * kReserveThreads + tid;
+      if (item >= items) break;
+      const int i = item / s.slots, x = item - i * s.slots;
+      const bool there = wanted(p, i, &w) && (running[u].y <= found || running[u].x == running[u].y);
+      if (there && need[u].x != kKept) {
+        p.table[(size_t)i * p.max_pages + w.first + x] = page[u];
+        p.refs[page[u]] = 1;
+        if (need[u].x >= 0) atomicSub(p.refs + need[u].x, 1);
+      }
+      if (x == 0) {
+        const bool moves = there && need[u].x >= 0 && w.begun;
+        p.granted[i] = there ? w.count : 0;
+        p.moves[2 * i] = moves ? need[u].x : -1;
+        p.moves[2 * i + 1] = moves ? page[u] : -1;
       }
     }
-    p.granted[i] = granted;
-    p.moves[2 * i] = from;
-    p.moves[2 * i + 1] = to;
   }
 }
 
@@ -259,17 +300,9 @@ void reserve_few_kernel(PageReserve p) {
   }
   int total;
   const int running = before_me<kReserveThreads>(needs, s_waves[0], &total) + needs;
-  int found = 0;
-  for (int base = 0, turn = 1; base < p.num_pages && found < total; base += 8 * kReserveThreads, turn ^= 1) {
-    if (base > 0) {
-      __syncthreads();
-      used = in_use8(p.refs, base + 8 * tid, p.num_pages);
-    }
-    uint32_t free = ~used & there8(base + 8 * tid, p.num_pages);
-    int all, to = found + before_me<kReserveThreads>(__popc(free), s_waves[turn], &all);
-    for (; free && to < total; free &= free - 1) s_pages[to++] = base + 8 * tid + __ffs(free) - 1;
-    found += all;
-  }
+  const int found = find_free<kReserveThreads>(p.refs, p.num_pages, used, total, s_waves, [&](int x, int page) {
+    if (x < total) s_pages[x] = page;
+  });
   __syncthreads();
   if (tid >= p.b) return;
   int granted = 0, from = -1, to = -1;

@@ -46,7 +46,7 @@ def some_tables(rng, b, each, num_pages, page, share=0.3):
 
 # b, pages of a sequence, pool, page size, n
 SIZES = [(1, 1, 1, 1, 1), (1, 4, 3, 16, 1), (5, 6, 40, 4, 5), (8, 10, 25, 16, 40), (64, 20, 900, 16, 1), (300, 7, 1500, 3, 9), (1500, 5, 5000, 8, 1), (3000, 3, 4000, 2, 4),
-         (8, 40, 200, 2, 30), (1024, 4, 20000, 16, 33), (40, 9, 30000, 5, 16)]
+         (8, 40, 200, 2, 30), (1024, 4, 20000, 16, 33), (40, 9, 30000, 5, 16), (40, 200, 30000, 4, 700), (3, 1500, 9000, 1, 1500)]
 
 
 @pytest.mark.parametrize("b,each,num_pages,page,n", SIZES)
@@ -73,6 +73,22 @@ def test_reserve(m, b, each, num_pages, page, n):
         granted, moves = m.mqa_paged_reserve_pages(t, i32(lens), r, page, min(n, each * page), counts=None if counts is None else i32(counts))
         want, want_moves = serving.reserve(table, lens, refs, page, min(n, each * page), counts)
         assert same(granted, want) and same(moves, want_moves) and same(t, table) and same(r, refs), turn
+
+
+@pytest.mark.parametrize("b,n,num_pages", [(64, 5, 65536), (1000, 1, 70001), (4, 600, 65536), (1, 4096, 100000), (2000, 3, 40000)])
+def test_reserve_from_pools_nearly_full(m, b, n, num_pages):
+    """Free pages far apart, and fewer than are needed in some."""
+    from oracle import serving
+    rng = np.random.default_rng(num_pages + n)
+    page, each = 4, -(-n // 4) + 2
+    for free in (b * each, b * each // 3, 5, 0):
+        table, lens = np.full((b, each), -1), rng.integers(0, 8, b)
+        refs = np.ones(num_pages, dtype=np.int64)
+        refs[num_pages - 1 - np.sort(rng.choice(num_pages // 2, free, replace=False))] = 0
+        t, r = i32(table), i32(refs)
+        granted, moves = m.mqa_paged_reserve_pages(t, i32(lens), r, page, n)
+        want, want_moves = serving.reserve(table, lens, refs, page, n, None)
+        assert same(granted, want) and same(moves, want_moves) and same(t, table) and same(r, refs), free
 
 
 def test_reserve_where_the_pages_run_out(m):
