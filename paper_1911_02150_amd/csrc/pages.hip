@@ -8,34 +8,75 @@ namespace {
 __device__ __forceinline__ bool is_page(int entry, int num_pages) { return (unsigned)entry < (unsigned)num_pages; }
 __device__ __forceinline__ int pages_of(int len, int page_size) { return (int)(((unsigned)len + (unsigned)page_size - 1) / (unsigned)page_size); }
 
-// ---------------------------------------------------------------- fork, free: a thread an entry
+// ---------------------------------------------------------------- fork, free
+// A thread has a column of kRun neighbouring sequences' entries, and one atomic for those that follow each other and name the same page, as siblings' do: the counts' atomics bound it, and for
+// few entries the launch and three reads in a row (one of 256 pages to 512: 5.6 us, an entry a thread 11.9, runs of eight 5.3; 64 to 512 of them 3.6, 3.1 and 4.5).
+constexpr int kRun = 4;
+
+template <int SIGN>
+struct Run {                             // of one page's entries
+  int page = -1, count = 0;
+  __device__ __forceinline__ void end(int32_t* refs) {
+    if (count) atomicAdd(refs + page, SIGN * count);
+  }
+  __device__ __forceinline__ void add(int32_t* refs, int entry) {
+    if (entry != page) {
+      end(refs);
+      page = entry;
+      count = 0;
+    }
+    ++count;
+  }
+};
+
 __global__ __launch_bounds__(256)
 void fork_kernel(PageFork p) {
   const unsigned idx = blockIdx.x * 256u + threadIdx.x;
-  if (idx >= (unsigned)p.b_out * (unsigned)p.max_pages) return;
-  const int j = (int)(idx / (unsigned)p.max_pages), x = (int)(idx - (unsigned)j * (unsigned)p.max_pages);
-  const int parent = p.parents[j];
-  int len = 0, entry = -1;
-  if ((unsigned)parent < (unsigned)p.b_in) {
-    entry = p.table_in[(size_t)parent * p.max_pages + x];      // (on its way with the length)
-    len = min(max(p.lens_in[parent], 0), p.max_pages * p.page_size);
-    if (x >= pages_of(len, p.page_size) || !is_page(entry, p.num_pages)) entry = -1;
+  const int j0 = kRun * (int)(idx / (unsigned)p.max_pages), x = (int)(idx % (unsigned)p.max_pages);
+  if (j0 >= p.b_out) return;
+  int parent[kRun], entry[kRun], len[kRun];
+#pragma unroll
+  for (int u = 0; u < kRun; ++u) parent[u] = p.parents[min(j0 + u, p.b_out - 1)];
+#pragma unroll
+  for (int u = 0; u < kRun; ++u) {
+    const bool there = (unsigned)parent[u] < (unsigned)p.b_in;
+    entry[u] = there ? p.table_in[(size_t)parent[u] * p.max_pages + x] : -1;
+    len[u] = there ? p.lens_in[parent[u]] : 0;
   }
-  if (entry >= 0) atomicAdd(p.refs + entry, 1);
-  p.table_out[idx] = entry;
-  if (x == 0) p.lens_out[j] = len;
+  Run<1> run;
+#pragma unroll
+  for (int u = 0; u < kRun; ++u) {
+    if (j0 + u >= p.b_out) break;
+    len[u] = min(max(len[u], 0), p.max_pages * p.page_size);
+    if (x >= pages_of(len[u], p.page_size) || !is_page(entry[u], p.num_pages)) entry[u] = -1;
+    if (entry[u] >= 0) run.add(p.refs, entry[u]);
+    p.table_out[(size_t)(j0 + u) * p.max_pages + x] = entry[u];
+    if (x == 0) p.lens_out[j0 + u] = len[u];
+  }
+  run.end(p.refs);
 }
 
 __global__ __launch_bounds__(256)
 void free_kernel(PageFree p) {
   const unsigned idx = blockIdx.x * 256u + threadIdx.x;
-  if (idx >= (unsigned)p.b * (unsigned)p.max_pages) return;
-  const int i = (int)(idx / (unsigned)p.max_pages), x = (int)(idx - (unsigned)i * (unsigned)p.max_pages);
-  const int entry = p.table[idx];                        // (on its way with the length)
-  const int len = min(max(p.lens[i], 0), p.max_pages * p.page_size);
-  if (x < pages_of(len, p.page_size)) return;
-  if (is_page(entry, p.num_pages)) atomicSub(p.refs + entry, 1);
-  if (entry != -1) p.table[idx] = -1;
+  const int i0 = kRun * (int)(idx / (unsigned)p.max_pages), x = (int)(idx % (unsigned)p.max_pages);
+  if (i0 >= p.b) return;
+  int entry[kRun], len[kRun];
+#pragma unroll
+  for (int u = 0; u < kRun; ++u) {
+    const int i = min(i0 + u, p.b - 1);
+    entry[u] = p.table[(size_t)i * p.max_pages + x];
+    len[u] = p.lens[i];
+  }
+  Run<-1> run;
+#pragma unroll
+  for (int u = 0; u < kRun; ++u) {
+    if (i0 + u >= p.b) break;
+    if (x < pages_of(min(max(len[u], 0), p.max_pages * p.page_size), p.page_size)) continue;
+    if (is_page(entry[u], p.num_pages)) run.add(p.refs, entry[u]);
+    if (entry[u] != -1) p.table[(size_t)(i0 + u) * p.max_pages + x] = -1;
+  }
+  run.end(p.refs);
 }
 
 // ---------------------------------------------------------------- sums over a workgroup
@@ -81,6 +122,7 @@ __device__ __forceinline__ uint32_t there8(int first, int num_pages) { return fi
 //  3. as many free pages as are needed, or as there are
 //  4. to the sequences whose running number is there: their pages
 // (Step 4 reads what step 2 has written down and no counts, since it changes them.)
+// What bounds it is the latency of what a step reads, a round of 4096 entries after the other (a prompt of 4096 in pages of 16 8 us; 64 of 512 10.1; with a sequence's entries one thread's 106 and 25.6).
 constexpr int kReserveThreads = 1024;
 constexpr int kKept = -2, kMissing = -1;
 
@@ -256,7 +298,8 @@ void reserve_kernel(PageReserve p, void* workspace) {
 }
 
 // The same where every thread has a sequence and that few pages: counts of a page's writers are kept in a hash table in LDS (open addressing, at most half full), needs in registers, so that
-// three reads in a row are left: length, entries, counts.  What bounds it is those and the launch (512 sequences, five tokens each, pages of 16: 14.6 us in the form above).
+// three reads in a row are left: length, entries, counts.  What bounds it is those and the launch (512 sequences, five tokens each, pages of 16, 7.6 us; four 4.6; with each sequence a thread of
+// the form above 14.6 and 6.9), and in pools that are nearly full the search (1.5 us for 16384 pages).
 constexpr int kReserveSlots = 4, kHash = 2 * kReserveThreads;
 __global__ __launch_bounds__(kReserveThreads)
 void reserve_few_kernel(PageReserve p) {
@@ -331,8 +374,9 @@ void reserve_few_kernel(PageReserve p) {
 //
 // Pools of up to kBitPages: a bit a page, in use or not, and the pages in use before every word of 32 are in LDS, of every workgroup: rank(page), the x-th free page and the x-th one in use (a binary
 // search over the words, and in the word) say for each page, entry and move what it becomes without another workgroup's help.  The bits come from the counts, or, in pools so large that
-// each workgroup would read many, from a launch before (65536 pages, entries 32768: 7.4 us; the three launches below 13.4; 256 pages 3.4 and 6.8).
-constexpr int kBitPages = 1 << 17, kBitWords = kBitPages / 32, kReadPages = 1 << 14;
+// each workgroup would read many, from a launch before.  The launches and the reads in a row bound it (256 pages 5.9 us, 16384 8.3, 65536 11.3; by the three launches below 131072 12.6, so 16.7;
+// 256 7.5).
+constexpr int kBitPages = 1 << 16, kBitWords = kBitPages / 32, kReadPages = 1 << 14;
 __device__ __forceinline__ uint32_t in_use32(const int32_t* refs, int word, int num_pages) {
   uint32_t bits = 0;
 #pragma unroll
@@ -508,8 +552,8 @@ void compact_apply_kernel(PageCompact p, void* workspace) {
 }
 
 // ---------------------------------------------------------------- copies of pages
-// A workgroup a move at a time, 16 bytes (or 4, where a page's size asks for it) a thread.  HBM bounds it: 12320 moves of two pages of 4 KiB, 202 MB, 36.4 us = 5.5 TB/s (with loads and
-// stores that stay in L2 40.4; four moves at a time 53).
+// A workgroup a move at a time, 16 bytes (or 4, where a page's size asks for it) a thread.  HBM bounds it: 12320 moves of two pages of 4 KiB, 202 MB, 33.4 us = 6.05 TB/s (with stores that stay in L2
+// 40.4; with loads that do not 36.4, and where eight moves copy the same page 11.1, so 7.2).
 typedef __attribute__((ext_vector_type(4))) uint32_t u32x4;
 template <typename W>
 __device__ __forceinline__ void copy_run(void* pool, uint32_t bytes, int from, int to) {
@@ -541,12 +585,12 @@ void copy_pages_kernel(PageCopy p) {
 }  // namespace
 
 hipError_t launch_fork(const PageFork& p, hipStream_t st) {
-  hipLaunchKernelGGL(fork_kernel, dim3(((unsigned)p.b_out * (unsigned)p.max_pages + 255) / 256), dim3(256), 0, st, p);
+  hipLaunchKernelGGL(fork_kernel, dim3(((unsigned)((p.b_out + kRun - 1) / kRun) * (unsigned)p.max_pages + 255) / 256), dim3(256), 0, st, p);
   return hipGetLastError();
 }
 
 hipError_t launch_free(const PageFree& p, hipStream_t st) {
-  hipLaunchKernelGGL(free_kernel, dim3(((unsigned)p.b * (unsigned)p.max_pages + 255) / 256), dim3(256), 0, st, p);
+  hipLaunchKernelGGL(free_kernel, dim3(((unsigned)((p.b + kRun - 1) / kRun) * (unsigned)p.max_pages + 255) / 256), dim3(256), 0, st, p);
   return hipGetLastError();
 }
 
