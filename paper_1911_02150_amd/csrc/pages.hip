@@ -149,15 +149,14 @@ __host__ __device__ ReserveSpace reserve_space(int b, int n, int num_pages, int 
 
 // put(x, page) for the x-th free page, x < total at least if there are so many; how many it has come to.  `used`: of a thread's first eight pages.
 template <int T, typename Put>
-__device__ __forceinline__ int find_free(const int32_t* refs, int num_pages, uint32_t used, int total, int (&s_waves)[2][T / 64], Put put) {
+__device__ __forceinline__ int find_free(const int32_t* refs, int num_pages, uint32_t used, int total, int* s_waves, Put put) {
   const int tid = threadIdx.x;
   auto give = [&](uint32_t free, int first, int at) {
     for (; free; free &= free - 1) put(at++, first + __ffs(free) - 1);
   };
   if (total == 0) return 0;
-  __syncthreads();
   uint32_t free = ~used & there8(8 * tid, num_pages);
-  int found, at = before_me<T>(__popc(free), s_waves[0], &found);
+  int found, at = before_me<T>(__popc(free), s_waves, &found);
   give(free, 8 * tid, at);
   for (int base = 8 * T; base < num_pages && found < total; base += 16 * T) {      // then twice eight
     uint32_t more[2];
@@ -165,7 +164,7 @@ __device__ __forceinline__ int find_free(const int32_t* refs, int num_pages, uin
     for (int g = 0; g < 2; ++g) more[g] = ~in_use8(refs, base + 8 * (T * g + tid), num_pages) & there8(base + 8 * (T * g + tid), num_pages);
     __syncthreads();
     int all;
-    const int before = before_me<T>(__popc(more[0]) | __popc(more[1]) << 16, s_waves[1], &all);      // (up to 8 T each)
+    const int before = before_me<T>(__popc(more[0]) | __popc(more[1]) << 16, s_waves, &all);      // (up to 8 T each)
     give(more[0], base + 8 * tid, found + (before & 0xffff));
     found += all & 0xffff;
     give(more[1], base + 8 * (T + tid), found + (before >> 16));
@@ -262,7 +261,8 @@ void reserve_kernel(PageReserve p, void* workspace) {
     }
     total += all;
   }
-  const int found = find_free<kReserveThreads>(p.refs, p.num_pages, used, total, s_waves, [&](int x, int page) { s.pages[x] = page; });
+  __syncthreads();
+  const int found = find_free<kReserveThreads>(p.refs, p.num_pages, used, total, s_waves[0], [&](int x, int page) { s.pages[x] = page; });
   __threadfence_block();
   __syncthreads();
   for (int base = 0; base < items; base += 4 * kReserveThreads) {
@@ -343,7 +343,7 @@ void reserve_few_kernel(PageReserve p) {
   }
   int total;
   const int running = before_me<kReserveThreads>(needs, s_waves[0], &total) + needs;
-  const int found = find_free<kReserveThreads>(p.refs, p.num_pages, used, total, s_waves, [&](int x, int page) {
+  const int found = find_free<kReserveThreads>(p.refs, p.num_pages, used, total, s_waves[1], [&](int x, int page) {
     if (x < total) s_pages[x] = page;
   });
   __syncthreads();

@@ -8,6 +8,10 @@
 // Weights.  With s_V(p) = 2^E mant and z the logit (log2), u = z + E - ref is what the running maximum M is taken over, row by row, and w = 2^(u - M) the number that multiplies V8 (times mant, where
 // a scale is no power of two): a row's largest *contribution* is near fp16's largest number, so that two fp16 terms hold every w to 23 bits, and those that are below 2^-25 of it to 2^-35 of
 // it, whatever the scales.  The sum is over w 2^-E.  ref follows the tiles' scales (any will do: M goes with it), which keeps u small, and so its rounding.
+//
+// What bounds it: 64 sequences of 8192 and 32 rows, 136 MB, take 36 us = 3.8 TB/s, vector instructions (the conversions of 8 bits, the softmax) a third of the SIMDs' cycles and the products a sixth;
+// 512 sequences of up to 4096 and 64 rows 121 us, vector instructions half and products a quarter: a SIMD's registers hold two waves, which leave each other's waits open.  Measured and slower: a
+// tile at a time for each wave (48.7 and 150), a wave's two tiles as one of 64 positions (50 and 172, by registers that spill; with fewer of them as long as now).
 #include "paged_decode.hpp"
 
 namespace mqa {
@@ -275,7 +279,7 @@ struct Rows8 : Rows<T, D, HB, false, EXACT> {
   }
 };
 
-// Loads that stay in L2: several blocks of rows read the same tiles, neighbours on an XCD at about the same time, and half a row is a load (b=64, m=8192, h=32: non-temporal
+// Loads that stay in L2: several blocks of rows read the same tiles, neighbours on an XCD at about the same time, and half a row is a load (64 sequences of 8192, 32 rows: non-temporal
 // 38.6 us, so 35.2).
 template <typename T, int D, int HB, bool EXACT>
 __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2)
