@@ -303,31 +303,15 @@ void paged_list_kernel(PagedDecode p) {
 
 // The sequence that a piece is of, which of the sequence's pieces (`off`), and how many a head has (`c`); false: there is no such piece.  Every workgroup looks at all
 // lengths: thread t has sequences t * each up to the next one's.
-template <bool SCALED>
 __device__ __forceinline__ bool look_for(const PagedDecode& p, int piece, Segment* s, int* off, int* c) {
   __shared__ int s_waves[8][kThreads / 64], s_longest[kThreads / 64];
   __shared__ int s_at[4];
   const int tid = threadIdx.x, heads = p.c.h_kv;
   const int each = (p.b + kThreads - 1) / kThreads, from = tid * each, to = min(p.b, from + each);
   const int len = from < to ? p.lens[from] : 0;            // (up to 256 sequences: read once)
-  int more[kLookedFor / kThreads - 1];                     // 8 bits: so are up to kLookedFor (512 of up to 4096, 32 heads: 91 us, so 89)
-  if constexpr (SCALED) {
-#pragma unroll
-    for (int x = 0; x < kLookedFor / kThreads - 1; ++x) more[x] = from + 1 + x < to ? p.lens[from + 1 + x] : 0;
-  }
-  auto length = [&](int x) {                               // of sequence x, from < x < to
-    if constexpr (SCALED) {
-      int y = more[0];
-#pragma unroll
-      for (int z = 1; z < kLookedFor / kThreads - 1; ++z) y = x == from + 1 + z ? more[z] : y;
-      return y;
-    } else {
-      return p.lens[x];
-    }
-  };
   int mine = tiles_of(p, len), longest = mine;
   for (int x = from + 1; x < to; ++x) {
-    const int t = tiles_of(p, length(x));
+    const int t = tiles_of(p, p.lens[x]);
     mine += t;
     longest = max(longest, t);
   }
@@ -353,78 +337,30 @@ __device__ __forceinline__ bool look_for(const PagedDecode& p, int piece, Segmen
   auto cut = [&](int tiles) {
     per = whole_waves(tiles);
     count = from < to ? pieces_of(tiles_of(p, len), per) : 0;
-    for (int x = from + 1; x < to; ++x) count += pieces_of(tiles_of(p, length(x)), per);
+    for (int x = from + 1; x < to; ++x) count += pieces_of(tiles_of(p, p.lens[x]), per);
     before = before_me(count, s_waves[++turn], &all);
   };
-  // Caches of 8 bits: two workgroups to a unit from the start where a unit's share is more than 16 tiles (48 sequences of 2048, 32 heads: one 21.3 us, two 22.7; 256 of up to 2000 41.2 and
-  // 35.0; 64 of 8192 40.1 and 39.5), and up to half over an even share each (256 of up to 2000, 32 heads: 35.0, a quarter over it 44.9; 300 of up to 1500 35.6 and 45.2).
-  const int least = SCALED && total * p.blocks > 16 * kComputeUnits ? 2 : 1, over = SCALED ? 12 : 10;
   bool fits = false;
   if (many) {
     longest = max(max(s_longest[0], s_longest[1]), max(s_longest[2], s_longest[3]));
     fits = left_whole(p, longest, total);
     if (fits) cut(longest);
   }
-  for (int most = least * kComputeUnits; most <= 2 * kComputeUnits; most *= 2) {
+  for (int most = kComputeUnits; most <= 2 * kComputeUnits; most *= 2) {
     const int units = most / p.blocks;
     if (!fits && p.b * heads <= units)
-      for (int x = 8; x <= over && !fits; ++x) {
+      for (int x = 8; x <= 10 && !fits; ++x) {
         cut((int)(((long long)total * x + 8 * units - 1) / (8 * units)));
         fits = all * heads <= units;
       }
   }
   if (!fits) cut(share_of(p, total));
   if (piece >= all * heads) return false;
-  if constexpr (SCALED) {
-    // 8 bits: the long pieces come first, by quarters of the longest that there may be, so that short ones fill the end (512 sequences of up to 4096, 64 heads: 133.6 us in the
-    // sequences' order, so 128.8).  A quarter's counts are 16 bits of a sum.
-    __shared__ unsigned long long s_quarters[kThreads / 64];
-    const int lane = tid & 63;
-    auto pieces = [&](int x, int* quarter) {               // of the thread's x-th sequence
-      const int t = tiles_of(p, x == 0 ? len : length(from + x)), c = pieces_of(t, per);
-      *quarter = 3 - min(3, 4 * ((t + c - 1) / c) / (per + 1));
-      return from + x < to ? c : 0;
-    };
-    unsigned long long sum = 0;
-    int quarter;
-#pragma unroll
-    for (int x = 0; x < kLookedFor / kThreads; ++x)
-      if (x < each) {
-        const int c = pieces(x, &quarter);
-        sum += (unsigned long long)c << (16 * quarter);
-      }
-    unsigned long long incl = sum;
-#pragma unroll
-    for (int off = 1; off < 64; off <<= 1) {
-      const unsigned long long y = __shfl_up(incl, off);
-      if (lane >= off) incl += y;
-    }
-    if (lane == 63) s_quarters[tid >> 6] = incl;
-    __syncthreads();
-    unsigned long long ahead = incl - sum, whole = 0;
-#pragma unroll
-    for (int w = 0; w < kThreads / 64; ++w) {
-      if (w < tid >> 6) ahead += s_quarters[w];
-      whole += s_quarters[w];
-    }
-    ahead += (whole << 16) + (whole << 32) + (whole << 48);      // (and the quarters before)
-#pragma unroll
-    for (int x = 0; x < kLookedFor / kThreads; ++x)
-      if (x < each) {
-        const int c = pieces(x, &quarter), first = (int)(ahead >> (16 * quarter) & 0xffff);
-        if (first * heads <= piece && piece < (first + c) * heads) {
-          s_at[0] = from + x;
-          s_at[1] = piece - first * heads;
-          s_at[2] = x == 0 ? len : length(from + x);
-          s_at[3] = c;
-        }
-        ahead += (unsigned long long)c << (16 * quarter);
-      }
-  } else if (before * heads <= piece && piece < (before + count) * heads) {      // one thread
+  if (before * heads <= piece && piece < (before + count) * heads) {      // one thread
     int x = from, L = len, mine = pieces_of(tiles_of(p, len), per);
     while (piece >= (before + mine) * heads) {
       before += mine;
-      L = length(++x);
+      L = p.lens[++x];
       mine = pieces_of(tiles_of(p, L), per);
     }
     s_at[0] = x;
@@ -432,6 +368,141 @@ __device__ __forceinline__ bool look_for(const PagedDecode& p, int piece, Segmen
     s_at[2] = L;
     s_at[3] = mine;
   }
+  __syncthreads();
+  s->i = __builtin_amdgcn_readfirstlane(s_at[0]);
+  *off = __builtin_amdgcn_readfirstlane(s_at[1]);
+  *c = __builtin_amdgcn_readfirstlane(s_at[3]);
+  s->L = paged_length(p.c, __builtin_amdgcn_readfirstlane(s_at[2]));
+  return true;
+}
+
+// The same for caches of 8 bits, where a thread keeps the lengths of its sequences, up to four, and the long pieces come first.  Up to 64 sequences: each wave looks for
+// itself, without the others (8 sequences of 32768, 64 heads 110.8 us, so 107.8; 64 of 4096, 32 heads of 8 118.8 and 115.7).
+__device__ __forceinline__ bool look_for_scaled(const PagedDecode& p, int piece, Segment* s, int* off, int* c) {
+  constexpr int kEach = kLookedFor / kThreads, kWaves = kThreads / 64;
+  __shared__ int s_waves[2][kWaves], s_longest[kWaves], s_at[4];
+  __shared__ unsigned long long s_quarters[kWaves];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, heads = p.c.h_kv;
+  const bool alone = p.b <= 64;
+  const int each = alone ? 1 : (p.b + kThreads - 1) / kThreads, from = (alone ? lane : tid) * each, have = min(p.b - from, each);      // sequences of this thread (below 0: none)
+  int len[kEach], mine = 0, longest = 0;
+#pragma unroll
+  for (int x = 0; x < kEach; ++x) len[x] = x < have ? p.lens[from + x] : 0;
+#pragma unroll
+  for (int x = 0; x < kEach; ++x) {
+    const int t = tiles_of(p, len[x]);
+    mine += t;
+    longest = max(longest, t);
+  }
+  int turn = 0;
+  auto sum_before = [&](int x, int* all) {
+    if (!alone) return before_me(x, s_waves[turn ^= 1], all);      // (its places are written again two barriers later)
+    int incl = x;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int y = __shfl_up(incl, o);
+      if (lane >= o) incl += y;
+    }
+    *all = __builtin_amdgcn_readlane(incl, 63);
+    return incl - x;
+  };
+  const bool many = p.b * heads * p.blocks >= 2 * kComputeUnits;
+  if (many) {
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) longest = max(longest, __shfl_xor(longest, o));
+    if (lane == 0 && !alone) s_longest[wave] = longest;
+  }
+  int total;
+  sum_before(mine, &total);
+  total *= heads;
+  int per = 0, all = 0;
+  float inverse = 0.f;
+  auto pieces = [&](int tiles) {                           // (less than 2^20 tiles: the quotient is off by one at most)
+    const int a = tiles + per - 1;
+    int n = (int)((float)a * inverse);
+    const int rest = a - n * per;
+    n += (rest >= per) - (rest < 0);
+    return max(1, n);
+  };
+  auto cut = [&](int tiles) {
+    per = whole_waves(tiles);
+    inverse = 1.f / (float)per;
+    int count = 0;
+#pragma unroll
+    for (int x = 0; x < kEach; ++x)
+      if (x < each) count += x < have ? pieces(tiles_of(p, len[x])) : 0;
+    sum_before(count, &all);
+  };
+  // As above, but two workgroups to a unit from the start where a unit's share is more than 16 tiles (48 sequences of 2048, 32 heads: one 21.3 us, two 22.7; 256 of up to 2000 41.2 and
+  // 35.0; 64 of 8192 40.1 and 39.5), and up to half over an even share each (256 of up to 2000, 32 heads: 35.0, a quarter over it 44.9; 300 of up to 1500 35.6 and 45.2).
+  bool fits = false;
+  if (many) {
+    if (!alone) longest = max(max(s_longest[0], s_longest[1]), max(s_longest[2], s_longest[3]));
+    fits = left_whole(p, longest, total);
+    if (fits) cut(longest);
+  }
+  for (int most = total * p.blocks > 16 * kComputeUnits ? 2 * kComputeUnits : kComputeUnits; most <= 2 * kComputeUnits; most *= 2) {
+    const int units = most / p.blocks;
+    if (!fits && p.b * heads <= units)
+      for (int x = 8; x <= 12 && !fits; ++x) {
+        cut((int)(((long long)total * x + 8 * units - 1) / (8 * units)));
+        fits = all * heads <= units;
+      }
+  }
+  if (!fits) cut(share_of(p, total));
+  if (piece >= all * heads) return false;
+  // The long pieces come first, by quarters of the longest that there may be, so that short ones fill the end (512 sequences of up to 4096, 64 heads: 133.6 us in the
+  // sequences' order, so 128.8).  A quarter's counts are 16 bits of a sum.
+  int n[kEach], quarter[kEach];
+  unsigned long long sum = 0;
+#pragma unroll
+  for (int x = 0; x < kEach; ++x)
+    if (x < each) {
+      const int t = tiles_of(p, len[x]), of = pieces(t);
+      quarter[x] = 3 - ((4 * t >= of * per) + (4 * t >= 2 * of * per) + (4 * t >= 3 * of * per));
+      n[x] = x < have ? of : 0;
+      sum += (unsigned long long)n[x] << (16 * quarter[x]);
+    }
+  unsigned long long incl = sum, whole = 0;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const unsigned long long y = __shfl_up(incl, o);
+    if (lane >= o) incl += y;
+  }
+  unsigned long long ahead = incl - sum;
+  if (alone) {
+    whole = (unsigned long long)(uint32_t)__builtin_amdgcn_readlane((int)(incl >> 32), 63) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)incl, 63);
+  } else {
+    if (lane == 63) s_quarters[wave] = incl;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      if (w < wave) ahead += s_quarters[w];
+      whole += s_quarters[w];
+    }
+  }
+  ahead += (whole << 16) + (whole << 32) + (whole << 48);      // (and the quarters before)
+  if (alone) {
+    const int first = (int)(ahead >> (16 * quarter[0]) & 0xffff);
+    const int who = __builtin_ctzll(__ballot(first * heads <= piece && piece < (first + n[0]) * heads));      // (one of them)
+    s->i = who;
+    *off = piece - __builtin_amdgcn_readlane(first, who) * heads;
+    *c = __builtin_amdgcn_readlane(n[0], who);
+    s->L = paged_length(p.c, __builtin_amdgcn_readlane(len[0], who));
+    return true;
+  }
+#pragma unroll
+  for (int x = 0; x < kEach; ++x)
+    if (x < each) {
+      const int first = (int)(ahead >> (16 * quarter[x]) & 0xffff);
+      if (first * heads <= piece && piece < (first + n[x]) * heads) {
+        s_at[0] = from + x;
+        s_at[1] = piece - first * heads;
+        s_at[2] = len[x];
+        s_at[3] = n[x];
+      }
+      ahead += (unsigned long long)n[x] << (16 * quarter[x]);
+    }
   __syncthreads();
   s->i = __builtin_amdgcn_readfirstlane(s_at[0]);
   *off = __builtin_amdgcn_readfirstlane(s_at[1]);
@@ -469,7 +540,7 @@ __device__ __forceinline__ bool find_segment(const PagedDecode& p, Segment* s) {
     off = piece - work.y * heads;
     c = work.z;
     s->L = paged_length(p.c, work.w);
-  } else if (!look_for<SCALED>(p, piece, s, &off, &c)) {
+  } else if (SCALED ? !look_for_scaled(p, piece, s, &off, &c) : !look_for(p, piece, s, &off, &c)) {
     return false;
   }
   s->e = heads == 1 ? 0 : off / c;

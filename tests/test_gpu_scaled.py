@@ -120,6 +120,26 @@ def test_attention(m, b, n, h, h_kv, k, v, page, block, lens, kind):
     assert (off <= tolerance(q, K, size, scale, max(lens), kind, top)).all(), off.max()
 
 
+# lengths whose pieces fit none of the even shares; as few as a wave looks through and one more; long ones among short ones; more than a thread has one of
+UNEVEN = [([830] * 150 + [20] * 100, 1, 1), ([700, 0, 1, 33] * 16, 2, 2), ([40, 1300, 7, 260, 0] * 13, 1, 2), ([9, 2600] + [64] * 61, 4, 4), ([300, 31, 650] * 90, 1, 2), ([64, 0, 1100, 3, 90] * 110, 1, 1),
+          ([33] * 1023 + [2100], 1, 1)]
+
+
+@pytest.mark.parametrize("lens,h_kv,h", UNEVEN)
+def test_pieces_of_uneven_lengths(m, lens, h_kv, h):
+    """Every piece is somebody's, in a table of a capacity that is cut."""
+    b, k, page, block, kind, scale = len(lens), 32, 16, 16, "int8", 0.25
+    rng = np.random.default_rng(b + h)
+    each = -(-max(lens) // page)
+    arrays, cache = cache_of(rng, b, each, h_kv, page, block, k, k, kind)
+    table = tables(rng, b, each)
+    q = rng.standard_normal((b, 1, h, k)).astype(np.float32)
+    want, size, K, top = attended(q, arrays, table, lens, scale)
+    wide = np.concatenate([table, np.full((b, 1000 - each), -1)], 1)
+    got = m.mqa_paged_scaled_decode_step(f32(q[:, 0]), *cache, i32(wide), i32(np.array(lens)), scale=scale)
+    assert (np.abs(got.cpu().numpy().reshape(want.shape) - want) <= tolerance(q, K, size, scale, max(lens), kind, top)).all()
+
+
 @pytest.mark.parametrize("kind", ["e4m3", "int8"])
 @pytest.mark.parametrize("n,h,h_kv,k", [(1, 8, 1, 128), (4, 8, 1, 128), (3, 4, 4, 64), (2, 40, 1, 128), (2, 4, 2, 32)])
 def test_what_is_not_seen_may_hold_anything(m, n, h, h_kv, k, kind):
