@@ -56,9 +56,9 @@ __device__ __forceinline__ void halves(uint32_t u, uint32_t* lo, uint32_t* hi) {
 template <typename T>
 __device__ __forceinline__ void turn2(uint32_t row0, uint32_t row1, bool upper, uint32_t* col0, uint32_t* col1) {
   if constexpr (std::is_same<T, E4M3>::value) {
-    const uint32_t a = e4m3_f16(row0, upper), b = e4m3_f16(row1, upper);
-    *col0 = __builtin_amdgcn_perm(b, a, 0x05040100u);
-    *col1 = __builtin_amdgcn_perm(b, a, 0x07060302u);
+    const uint32_t pairs = __builtin_amdgcn_perm(row1, row0, upper ? 0x07030602u : 0x05010400u);
+    *col0 = e4m3_f16(pairs, false);
+    *col1 = e4m3_f16(pairs, true);
   } else {
     const uint32_t pairs = __builtin_amdgcn_perm(row1, row0, upper ? 0x07030602u : 0x05010400u) ^ 0x80808080u;
     *col0 = int8_f16(pairs, 0x04010400u);
@@ -151,34 +151,44 @@ struct Rows8 : Rows<T, D, HB, false, EXACT> {
   template <typename After>
   static __device__ __forceinline__ void first_product(const Tile8<D>& tl, const u32x4* qs, int lane, floatx4 (&sc)[2][HB], After&& after) {
     constexpr int STEPS = KP * KT, DEEP = 3;               // q of a step (product, term): read while the two before are multiplied
-    u32x4 b[DEEP][HB], k[2];
+    u32x4 b[DEEP][HB], k[2][2];
     auto read = [&](int n) {
 #pragma unroll
       for (int hb = 0; hb < HB; ++hb) b[n % DEEP][hb] = qs[n % KT * QOPS + (hb * KP + n / KT) * 64 + lane];
+    };
+    auto convert = [&](int x) {
+#pragma unroll
+      for (int u = 0; u < 2; ++u)
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          uint32_t lo, hi;
+          halves<T>(tl.kr[u][x >> 1][2 * (x & 1) + y], &lo, &hi);
+          k[x & 1][u][2 * y] = lo;
+          k[x & 1][u][2 * y + 1] = hi;
+        }
     };
 #pragma unroll
     for (int n = 0; n < DEEP - 1; ++n) read(n);
 #pragma unroll
     for (int hb = 0; hb < HB; ++hb) sc[0][hb] = sc[1][hb] = floatx4{0.f, 0.f, 0.f, 0.f};
+    convert(0);
 #pragma unroll
     for (int n = 0; n < STEPS; ++n) {
       if (n + DEEP - 1 < STEPS) read(n + DEEP - 1);
-      __builtin_amdgcn_sched_barrier(0);
       const int x = n / KT;
-      if (n % KT == 0)
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int y = 0; y < 2; ++y) {
-            uint32_t lo, hi;
-            halves<T>(tl.kr[u][x >> 1][2 * (x & 1) + y], &lo, &hi);
-            k[u][2 * y] = lo;
-            k[u][2 * y + 1] = hi;
-          }
+      if (n % KT == KT - 1 && x + 1 < KP) convert(x + 1);
 #pragma unroll
       for (int hb = 0; hb < HB; ++hb)
 #pragma unroll
-        for (int u = 0; u < 2; ++u) sc[u][hb] = mfma_f16(k[u], b[n % DEEP][hb], sc[u][hb]);
+        for (int u = 0; u < 2; ++u) sc[u][hb] = mfma_f16(k[x & 1][u], b[n % DEEP][hb], sc[u][hb]);
+      if (n % KT == KT - 1 && x + 1 < KP) {
+#pragma unroll
+        for (int z = 0; z < 2 * HB; ++z) {
+          __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x2, 4 / HB, 0);
+        }
+      }
+      __builtin_amdgcn_sched_barrier(0);
       if (n % KT == KT - 1) after(x);
     }
     __builtin_amdgcn_sched_barrier(0);
@@ -281,7 +291,8 @@ struct Rows8 : Rows<T, D, HB, false, EXACT> {
 
 // Loads that stay in L2: several blocks of rows read the same tiles, neighbours on an XCD at about the same time, and half a row is a load (64 sequences of 8192, 32 rows: non-temporal
 // 38.6 us, so 35.2).
-template <typename T, int D, int HB, bool EXACT>
+// NEAR: pools of less than 4 GiB, whose loads take 32-bit offsets (512 sequences of up to 4096, 64 heads: 122 us, so 118.7; 32 of up to 2048, 8 K/V heads of 64 21.8 and 20.9).
+template <typename T, int D, int HB, bool EXACT, bool NEAR>
 __global__ __launch_bounds__(kThreads, D > 128 ? 1 : 2)
 void scaled_matrix_kernel(PagedDecode p) {
   typedef Rows8<T, D, HB, EXACT> R;
@@ -323,6 +334,10 @@ void scaled_matrix_kernel(PagedDecode p) {
   };
   const int k = EXACT ? D : p.c.k, v = EXACT ? D : p.c.v;
   int k_row[2];
+  auto offset = [](int row, int width, int column) {       // of a row's bytes
+    if constexpr (NEAR) return (uint32_t)row * (uint32_t)width + (uint32_t)column;
+    else return (size_t)row * width + column;
+  };
   auto take_k = [&](int buf, int half) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) k_row[u] = places[buf][32 * half + 8 * (i16 >> 2) + 4 * u + (i16 & 3)];
@@ -330,7 +345,7 @@ void scaled_matrix_kernel(PagedDecode p) {
   auto load_k = [&](int half, int x) {
     const int piece = EXACT ? g + 4 * x : min(g + 4 * x, k / 16 - 1);
 #pragma unroll
-    for (int u = 0; u < 2; ++u) tl[half].kr[u][x] = reinterpret_cast<const u32x4*>(Kp + (size_t)k_row[u] * k)[piece];
+    for (int u = 0; u < 2; ++u) tl[half].kr[u][x] = reinterpret_cast<const u32x4*>(Kp + offset(k_row[u], k, 16 * piece))[0];
   };
   auto load_v = [&](int buf, int half) {
     constexpr int C = D / 16;
@@ -339,7 +354,7 @@ void scaled_matrix_kernel(PagedDecode p) {
     *reinterpret_cast<int4*>(v_row + 4) = reinterpret_cast<const int4*>(places[buf])[8 * half + 2 * g + 1];
 #pragma unroll
     for (int e = 0; e < 8; ++e)
-      tl[half].vr[e] = reinterpret_cast<const typename Form8<D>::VRow*>(Vp + (size_t)v_row[e] * v)[EXACT ? i16 : min(i16, v / C - 1)];
+      tl[half].vr[e] = reinterpret_cast<const typename Form8<D>::VRow*>(Vp + offset(v_row[e], v, C * (EXACT ? i16 : min(i16, v / C - 1))))[0];
   };
 
   if (tid == 0) s_odd = 0;
@@ -462,10 +477,15 @@ PagedPlan scaled_plan(int b, int n, int h, int h_kv, int page_size, int max_page
   return paged_plan(b, n, h, h_kv, page_size, max_pages, k, v, 1, 0, 64);
 }
 
+template <typename T, int D, int HB, bool EXACT>
+static hipError_t launch_pools(const PagedDecode& p, const PagedPlan& pl, hipStream_t st) {
+  const size_t rows = (size_t)p.c.num_pages * p.c.h_kv * p.c.page_size, widest = p.c.k > p.c.v ? p.c.k : p.c.v;
+  return rows * widest < (size_t)1 << 32 ? launch_form<scaled_matrix_kernel<T, D, HB, EXACT, true>>(Lds<T, D, HB>::alone, p, pl, st)
+                                         : launch_form<scaled_matrix_kernel<T, D, HB, EXACT, false>>(Lds<T, D, HB>::alone, p, pl, st);
+}
 template <typename T, int D, bool EXACT>
 static hipError_t launch_rows(const PagedDecode& p, const PagedPlan& pl, hipStream_t st) {
-  return pl.block_rows == 32 ? launch_form<scaled_matrix_kernel<T, D, 2, EXACT>>(Lds<T, D, 2>::alone, p, pl, st)
-                             : launch_form<scaled_matrix_kernel<T, D, 1, EXACT>>(Lds<T, D, 1>::alone, p, pl, st);
+  return pl.block_rows == 32 ? launch_pools<T, D, 2, EXACT>(p, pl, st) : launch_pools<T, D, 1, EXACT>(p, pl, st);
 }
 template <typename T>
 static hipError_t launch_widths(const PagedDecode& p, const PagedPlan& pl, hipStream_t st) {

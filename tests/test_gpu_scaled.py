@@ -283,6 +283,27 @@ def test_many_sequences_of_many_rows(m, b, n, h, k, v, each, kind):
         assert (off <= tolerance(q, K, size, 0.2, each * page, kind, top)[0]).all(), (i, off.max())
 
 
+@pytest.mark.parametrize("k,v,h,kind", [(64, 64, 8, "e4m3"), (64, 64, 33, "int8"), (128, 128, 9, "int8"), (128, 128, 40, "e4m3"), (48, 32, 20, "int8"), (96, 112, 8, "e4m3"), (80, 128, 17, "int8"),
+                                        (256, 192, 9, "e4m3"), (16, 256, 20, "int8")])
+def test_every_form_over_more_than_4_gib(m, k, v, h, kind):
+    """What it is over a small pool of the same pages."""
+    page, few, b = 64, 24, 2
+    pages = (1 << 32) // (page * max(k, v)) + 40
+    rng = np.random.default_rng(k + v + h)
+    arrays, small = cache_of(rng, b, few // b, 1, page, 16, k, v, kind)
+    table, lens = tables(rng, b, few // b), i32(np.array([few // b * page - 5, 300]))
+    q = f32(rng.standard_normal((b, h, k)))
+    want = m.mqa_paged_scaled_decode_step(q, *small, i32(table), lens, scale=0.3)
+    places = torch.from_numpy(np.concatenate([rng.permutation(few // 2), pages - 1 - rng.permutation(few // 2)])).to(DEV)
+    large = []
+    for t in small:
+        pool = torch.zeros((pages, *t.shape[1:]), dtype=torch.float32 if t.dtype == torch.float32 else torch.uint8, device=DEV)
+        pool[places] = t if t.dtype == torch.float32 else t.view(torch.uint8)
+        large.append(pool if t.dtype == torch.float32 else pool.view(t.dtype))
+    got = m.mqa_paged_scaled_decode_step(q, *large, i32(places.cpu().numpy()[table]), lens, scale=0.3)
+    assert torch.equal(got, want)
+
+
 def test_a_pool_of_more_than_4_gib(m):
     """Rows whose offsets do not fit 32 bits."""
     page, pages, k = 64, (4 << 30) // (64 * 128) + 70, 128
