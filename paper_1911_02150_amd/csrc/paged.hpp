@@ -77,8 +77,8 @@ constexpr int kPagedTile = 32;
 constexpr int kPagedMaxRows = 1024;     // query rows of a K/V head
 
 hipError_t launch_paged_append(const PagedAppend& p, int is_bf16, hipStream_t st);
-// whole: tiles of a group, at most, that stay whole where there is a group for every compute unit
-PagedPlan paged_plan(int b, int n, int h, int h_kv, int page_size, int max_pages, int k, int v, int is_bf16, int with_scores, int whole = 32);
+// scaled: a cache of 8 bits
+PagedPlan paged_plan(int b, int n, int h, int h_kv, int page_size, int max_pages, int k, int v, int is_bf16, int with_scores, bool scaled = false);
 void paged_workspace(PagedDecode* p, const PagedPlan& plan, void* workspace);        // where its parts are
 hipError_t launch_paged_decode(const PagedDecode& p, const PagedPlan& plan, int is_bf16, hipStream_t st);
 hipError_t launch_paged_evict(const PagedEvict& p, int is_bf16, hipStream_t st);

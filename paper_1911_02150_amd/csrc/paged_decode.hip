@@ -26,7 +26,7 @@ static size_t lay_out(PagedDecode* p, const PagedPlan& pl, float* at) {
   return floats * sizeof(float);
 }
 
-PagedPlan paged_plan(int b, int n, int h, int h_kv, int page_size, int max_pages, int k, int v, int is_bf16, int with_scores, int whole) {
+PagedPlan paged_plan(int b, int n, int h, int h_kv, int page_size, int max_pages, int k, int v, int is_bf16, int with_scores, bool scaled) {
   PagedPlan pl = {};
   const long long R = (long long)n * (h / h_kv), positions = (long long)max_pages * page_size, tiles = (positions + kPagedTile - 1) / kPagedTile;
   const int wide = k > v ? k : v;
@@ -42,9 +42,13 @@ PagedPlan paged_plan(int b, int n, int h, int h_kv, int page_size, int max_pages
   pl.blocks = (int)((R + pl.block_rows - 1) / pl.block_rows);
   // One launch, a workgroup to a group, where cutting and merging would take longer (8 heads, 32 sequences of 500: 10.3 us, in pieces 12.0; of 640 12.9 and 12.3, of 800 15.7
   // and 12.6; one of 500 9.2 and 11.1, of 800 12.0 and 11.1; float32, one of 380 13.6 both, of 500 15.9 and 13.6), and to greater lengths where there is one for
-  // every compute unit (256 of up to 1000, 32 heads: 25, in pieces 32).
+  // every compute unit (256 of up to 1000, 32 heads: 25, in pieces 32).  8 bits: longer ones (8 heads, 32 of 640 11.7, in pieces 13.1, of 800 13.2 and 13.4; one of 640 11.5 and 12.3, of 1100 15.8 and
+  // 12.5), and where there are 64 workgroups too (16 of up to 1000, 8 K/V heads of 64, 12.1 and 14.2; 64 of up to 800, 32 heads, 14.3 and 16.7); 300 of 1500, 32 heads, 37.5 and 56, of up to 1500 36.4
+  // and 35.0, 512 of up to 2000 44.8 and 49.6.
   const bool heavy = wide > 128 || (!is_bf16 && wide > 64);
-  pl.split = tiles > (groups * pl.blocks >= kComputeUnits ? whole : heavy ? 12 : 16);
+  const long long one = groups * pl.blocks;
+  const int whole = scaled ? (one >= kComputeUnits ? 64 : heavy ? 12 : one >= 64 ? 32 : 24) : one >= kComputeUnits ? 32 : heavy ? 12 : 16;
+  pl.split = tiles > whole;
   pl.listed = pl.split && b > kLookedFor;
   const long long least = groups * ((tiles + 3) / 4), most = groups + kShares;      // (pieces of four tiles; a last, shorter one in every group)
   pl.pieces = (int)(!pl.split ? groups : least < most ? least : most);

@@ -241,7 +241,7 @@ __device__ __forceinline__ int before_me(int x, int* s_waves, int* all) {
   return before;
 }
 
-constexpr int kComputeUnits = 256, kShares = 768, kSharesOfMany = 512, kLeast = 16, kLongest = 64;
+constexpr int kComputeUnits = 256, kShares = 768, kSharesOfMany = 512, kLeast = 16, kLongest = 64, kLongestScaled = 256;
 
 // Tiles of a piece, at most: a whole number for each of the workgroup's four waves.
 __device__ __forceinline__ int whole_waves(int tiles) { return max(1, (tiles + 3) >> 2) * 4; }
@@ -406,7 +406,7 @@ __device__ __forceinline__ bool look_for_scaled(const PagedDecode& p, int piece,
     *all = __builtin_amdgcn_readlane(incl, 63);
     return incl - x;
   };
-  const bool many = p.b * heads * p.blocks >= 2 * kComputeUnits;
+  const bool many = p.b * heads * p.blocks >= kComputeUnits;
   if (many) {
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) longest = max(longest, __shfl_xor(longest, o));
@@ -433,12 +433,13 @@ __device__ __forceinline__ bool look_for_scaled(const PagedDecode& p, int piece,
       if (x < each) count += x < have ? pieces(tiles_of(p, len[x])) : 0;
     sum_before(count, &all);
   };
-  // As above, but two workgroups to a unit from the start where a unit's share is more than 16 tiles (48 sequences of 2048, 32 heads: one 21.3 us, two 22.7; 256 of up to 2000 41.2 and
+  // As above, but whole groups where there is one for every compute unit and none is longer than the units' mean, up to 256 tiles (512 sequences of up to 4000, 32 heads: 73.5 us, as above 83.5; 64
+  // heads 121 and 129.5; 300 of up to 6000, 64 heads 100.7 and 113.9; 300 of 2500, 32 heads, 62.5 and 73; 200 of up to 3000, 64 heads 69.7 and 67.8), two workgroups to a unit from the start where a unit's share is more than 16 tiles (48 sequences of 2048, 32 heads: one 21.3 us, two 22.7; 256 of up to 2000 41.2 and
   // 35.0; 64 of 8192 40.1 and 39.5), and up to half over an even share each (256 of up to 2000, 32 heads: 35.0, a quarter over it 44.9; 300 of up to 1500 35.6 and 45.2).
   bool fits = false;
   if (many) {
     if (!alone) longest = max(max(s_longest[0], s_longest[1]), max(s_longest[2], s_longest[3]));
-    fits = left_whole(p, longest, total);
+    fits = longest <= kLongestScaled && longest * (kComputeUnits / p.blocks) <= total;
     if (fits) cut(longest);
   }
   for (int most = total * p.blocks > 16 * kComputeUnits ? 2 * kComputeUnits : kComputeUnits; most <= 2 * kComputeUnits; most *= 2) {

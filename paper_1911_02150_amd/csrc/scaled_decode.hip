@@ -473,9 +473,7 @@ void scaled_matrix_kernel(PagedDecode p) {
 }  // namespace
 
 PagedPlan scaled_plan(int b, int n, int h, int h_kv, int page_size, int max_pages, int k, int v, int is_e4m3) {
-  // Groups of up to 64 tiles whole where there is one for every compute unit (300 sequences of 1500, 32 heads: 37.5 us, cut 56; 512 of up to 2000 44.8 and 49.6; 300 of up to 1500 36.4 and 35.0;
-  // of up to 128: 40 of up to 4000, 8 K/V heads of 64, 37.8, cut 31.0).
-  return paged_plan(b, n, h, h_kv, page_size, max_pages, k, v, 1, 0, 64);
+  return paged_plan(b, n, h, h_kv, page_size, max_pages, k, v, 1, 0, true);
 }
 
 template <typename T, int D, int HB, bool EXACT>
