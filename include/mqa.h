@@ -350,7 +350,7 @@ int mqa_paged_append_kv_rows(const float* k_new, const float* v_new, const int32
  * Attention of the newest n tokens of every sequence, n = 1 (a decoding step) or more (drafted tokens, the end of a prompt), after their rows have been
  * appended: q [b,n,h,k] -> o [b,n,h,v].  Query j of sequence i sees the positions below lens[i] - (n - 1 - j): of a sequence with fewer new tokens the last rows
  * of q are theirs, and those before them older positions'.  Head e of q reads K/V head e / (h / h_kv).  A row that
- * sees nothing, or whose logits are all -infinity, is 0; what a row does not see may hold anything (infinities and NaN included).  n * h / h_kv <= 1024, b * n * h <= 2^22.
+ * sees nothing, or whose logits are all -infinity, is 0; what a row does not see may hold anything (infinities and NaN included), and so may q where a row sees nothing.  n * h / h_kv <= 1024, b * n * h <= 2^22.
  * Products and sums are float32's (a bfloat16 cache's values are multiplied by three bfloat16 terms of q and of the weights, which together are the float32).
  *
  * scores_out (or NULL), [b,h_kv,max_pages * page_size] float32: the attention weight that each position has received, summed over the n * h / h_kv rows of
@@ -390,8 +390,8 @@ int mqa_paged_evict_kv(void* K_pages, void* V_pages, const int32_t* table_in, co
  * it has, and if that is s', its older rows are rounded again to it.  (A scale does not become smaller while its block has rows, so that drafts that are refused may leave a block a coarser one.)  New values
  * are rounded to the nearest number, the even one of two, infinities to +-Q; NaN is e4m3's NaN, int8's 0.  b * h_kv * ((n + block - 2) / block + 1) <= 2^23.
  *
- * mqa_paged_scaled_decode_step: as mqa_paged_decode_step without scores.  Scales may be any float32.  8 bits are exact in the products; q has 23 bits (of a number that is less than 2^-16 of the
- * largest of its 16 or 32 rows: 2^-39 of that largest), and a position's weight times V's scale 23 bits, or, below 2^-12 of its row's largest, 2^-35 of that largest.
+ * mqa_paged_scaled_decode_step: as mqa_paged_decode_step without scores.  Scales may be any float32.  8 bits are exact in the products; q has 23 bits, or 2^-30 of its row's largest
+ * number where that is more, and a position's weight times V's scale 23 bits, or, below 2^-12 of its row's largest, 2^-35 of that largest.
  */
 int mqa_paged_scaled_append_kv_rows(const float* k_new, const float* v_new, const int32_t* counts, void* K_pages, float* K_scales, void* V_pages, float* V_scales,
                                     const int32_t* table, const int32_t* lens_in, int32_t* lens_out, int b, int n, int h_kv, int num_pages, int page_size,

@@ -3,7 +3,7 @@
 // The work is cut, merged, and done again in the plain form where infinities and NaN take part, as in paged_decode.hpp.  A workgroup is four waves, wave w has tiles w, w + 4, ... of 32 positions for 16 or
 // 32 query rows.  Both products are v_mfma_f32_16x16x32_f16; 8 bits are exact in fp16.
 //   logits^T[32 pos x 16 rows] = K_tile . q^T: lane (i, g) has the 16-byte pieces g, g + 4, ... of two K rows, a piece's first eight columns for one product, the others for the next.  q's rows are
-//     brought by one power of two to 2^13 .. 2^14 at most and taken as two fp16 terms: 23 bits of what is not below 2^-16 of the largest, and 2^-39 of the largest of what is.
+//     brought by a power of two to 2^14 at most and taken as two fp16 terms: by the same one where their sizes are much the same, else each by its own, and its logits back.
 //   out^T[D cols x 16 rows] += V_tile^T . weights^T: lane (c, g) has 1/16 of the columns of rows 8g .. 8g + 7.
 // Weights.  With s_V(p) = 2^E mant and z the logit (log2), u = z + E - ref is what the running maximum M is taken over, row by row, and w = 2^(u - M) the number that multiplies V8 (times mant, where
 // a scale is no power of two): a row's largest *contribution* is near fp16's largest number, so that two fp16 terms hold every w to 23 bits, and those that are below 2^-25 of it to 2^-35 of
@@ -89,6 +89,10 @@ constexpr int kNear = 16;            // ref is moved for scales that are so many
 // and their rows are zeros (which an append gives the smallest scale).
 constexpr int kFar = 50, kNothing = 100;
 
+// Rows of q whose largest numbers are no further than 2^kSameSize apart share a power of two: two fp16 terms then hold a row's numbers to 23 bits, or to 2^-30 of its largest (a row of its own: 2^-38).  Beyond
+// 2^kNoSize they are the plain form's.
+constexpr int kSameSize = 8, kNoSize = 64;
+
 // Of two tiles' positions, in LDS: K's scale with q's power of two, E - ref, 2^-E, the mantissa.
 struct Scales { float f[64], e[64], inv[64], mant[64]; };
 
@@ -104,42 +108,64 @@ struct Rows8 : Rows<T, D, HB, false, EXACT> {
 #pragma unroll
     for (int it = 0; it < ITEMS; ++it) {
       const int idx = tid + it * kThreads, r = idx / (D / 8), c = idx - r * (D / 8);
+      const bool sees = idx < ALL && s.row0 + r < p.R && row_limit(p, s.L, s.row0 + r) > s.begin;      // (what a row that sees nothing here holds is nobody's)
 #pragma unroll
       for (int y = 0; y < 2; ++y) {
         q->v[it][y] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (idx < ALL && s.row0 + r < p.R && (EXACT || 8 * c < p.c.k))
+        if (sees && (EXACT || 8 * c < p.c.k))
           q->v[it][y] = reinterpret_cast<const float4*>(p.q + row_offset(p, s.i, s.e, s.row0 + r) * (EXACT ? D : p.c.k) + 8 * c)[y];
       }
     }
   }
-  // As operands, [term][block of 16 rows][product][lane].  Returns the exponent that they have been brought down by (an infinity or NaN among them makes NaN of its row's logits).
-  static __device__ __forceinline__ int store_q(const PagedDecode& p, int tid, Query& q, u32x4* qs, float* s_most) {
-    float most = 0.f;
+  // As operands, [term][block of 16 rows][product][lane], all brought down by 2^up, which is returned, so that the largest is 2^13 or more and less than 2^14; a row that is far below that by
+  // 2^up back[row] (then *apart is set).  NaN makes NaN of its row's logits; an infinity, and rows too far apart, are the plain form's (*odd).
+  static __device__ __forceinline__ int store_q(const PagedDecode& p, int tid, Query& q, u32x4* qs, float* s_most, float* back, int* apart, int* odd) {
+    float mine[ITEMS], most = 0.f;
 #pragma unroll
-    for (int it = 0; it < ITEMS; ++it)
+    for (int it = 0; it < ITEMS; ++it) {
+      mine[it] = 0.f;
 #pragma unroll
       for (int y = 0; y < 2; ++y) {
         float4& v = q.v[it][y];
         v.x *= p.qscale; v.y *= p.qscale; v.z *= p.qscale; v.w *= p.qscale;
-        most = fmaxf(most, fmaxf(fmaxf(fabsf(v.x), fabsf(v.y)), fmaxf(fabsf(v.z), fabsf(v.w))));
+        mine[it] = fmaxf(mine[it], fmaxf(fmaxf(fabsf(v.x), fabsf(v.y)), fmaxf(fabsf(v.z), fabsf(v.w))));
       }
+      most = fmaxf(most, mine[it]);
+    }
 #pragma unroll
     for (int off = 32; off > 0; off >>= 1) most = fmaxf(most, __shfl_xor(most, off));
     if ((tid & 63) == 0) s_most[tid >> 6] = most;
     __syncthreads();
     most = fmaxf(fmaxf(s_most[0], s_most[1]), fmaxf(s_most[2], s_most[3]));
-    const int up = (int)(__float_as_uint(most) >> 23) - (127 + 13);
+    auto exponent = [](float x) { return (int)(__float_as_uint(x) >> 23); };
+    const int highest = exponent(most), up = highest - (127 + 13);
+    if (highest == 255) *odd = 1;
 #pragma unroll
     for (int it = 0; it < ITEMS; ++it) {
-      const int idx = tid + it * kThreads, r = idx / (D / 8), c = idx - r * (D / 8);
+      constexpr int W = D / 8;                             // lanes of a row
+      const int idx = tid + it * kThreads, r = idx / W, c = idx - r * W;
+      const uint64_t some = __ballot(mine[it] > 0.f), large = __ballot(exponent(mine[it]) + kSameSize >= highest);
+      auto of_row = [tid](uint64_t lanes) { return (uint32_t)(lanes >> (tid & 63 & ~(W - 1))) & (uint32_t)((1ull << W) - 1); };
+      int by = up;
+      if (const bool small = of_row(some) && !of_row(large); __any(small)) {
+        float here = mine[it];
+#pragma unroll
+        for (int off = 1; off < W; off <<= 1) here = fmaxf(here, __shfl_xor(here, off));
+        if (small) {
+          by = exponent(here) - (127 + 13);
+          *apart = 1;
+          if (up - by > kNoSize) *odd = 1;
+        }
+      }
       if (idx >= ALL) break;
+      if (c == 0) back[r] = ldexpf(1.f, by - up);
       const float x[8] = {q.v[it][0].x, q.v[it][0].y, q.v[it][0].z, q.v[it][0].w, q.v[it][1].x, q.v[it][1].y, q.v[it][1].z, q.v[it][1].w};
       const int slot = ((r >> 4) * KP + 2 * (c >> 3) + (c & 1)) * 64 + (r & 15) + 16 * (c >> 1 & 3);
       u32x4 t[2];
 #pragma unroll
       for (int y = 0; y < 4; ++y) {
         uint32_t w[2];
-        split2(ldexpf(x[2 * y], -up), ldexpf(x[2 * y + 1], -up), w);
+        split2(ldexpf(x[2 * y], -by), ldexpf(x[2 * y + 1], -by), w);
         t[0][y] = w[0]; t[1][y] = w[1];
       }
       qs[slot] = t[0];
@@ -194,8 +220,9 @@ struct Rows8 : Rows<T, D, HB, false, EXACT> {
     }
     __builtin_amdgcn_sched_barrier(0);
   }
-  // what multiplies V of a tile (the half-th of its two) from position p0 on; bad: bit e: position p0 + e is not there; mantissas: some scale is no power of two
-  __device__ __forceinline__ void weights(int lane, int p0, int half, uint32_t bad, const Scales& scales, bool mantissas, const floatx4 (&sc)[2][HB], float (&w)[HB][8]) {
+  // what multiplies V of a tile (the half-th of its two) from position p0 on; apart, back: as store_q has them; bad: bit e: position p0 + e is not there; mantissas: some scale is no power
+  // of two
+  __device__ __forceinline__ void weights(int lane, int p0, int half, int apart, const float* back, uint32_t bad, const Scales& scales, bool mantissas, const floatx4 (&sc)[2][HB], float (&w)[HB][8]) {
     const int g = lane >> 4;
     auto eight = [g, half](const float (&from)[64], float (&to)[8]) {
 #pragma unroll
@@ -212,6 +239,16 @@ struct Rows8 : Rows<T, D, HB, false, EXACT> {
     for (int hb = 0; hb < HB; ++hb)
 #pragma unroll
       for (int e = 0; e < 8; ++e) w[hb][e] = fmaf(sc[e >> 2][hb][e & 3], f[e], e8[e]);
+    if (apart) {                                           // (what e8 rounds away goes by the product that is not yet brought back, and comes down with it)
+      int row = lane & 15;
+      asm volatile("" : "+v"(row));                        // (nothing of it before the branch)
+#pragma unroll
+      for (int hb = 0; hb < HB; ++hb) {
+        const float y = back[16 * hb + row];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) w[hb][e] = fmaf(w[hb][e] - e8[e], y, e8[e]);
+      }
+    }
     if (bad || p0 + kPagedTile > lim_min) {                // what is not there, or not seen
       int first = p0 + 8 * g;
       asm volatile("" : "+v"(first));                      // (a branch: few tiles have such positions)
@@ -300,8 +337,8 @@ void scaled_matrix_kernel(PagedDecode p) {
   extern __shared__ __align__(16) unsigned char smem[];
   __shared__ __align__(16) int s_rows[kWaves][2][64];
   __shared__ __align__(16) Scales s_scales[kWaves][2];
-  __shared__ float s_most[kWaves];
-  __shared__ int s_odd;
+  __shared__ float s_most[kWaves], s_back[R::NH];
+  __shared__ int s_odd, s_apart;
   Segment s;
   if (!find_segment<true>(p, &s)) return;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), i16 = lane & 15, g = lane >> 4;
@@ -358,7 +395,7 @@ void scaled_matrix_kernel(PagedDecode p) {
       tl[half].vr[e] = reinterpret_cast<const typename Form8<D>::VRow*>(Vp + offset(v_row[e], v, C * (EXACT ? i16 : min(i16, v / C - 1))))[0];
   };
 
-  if (tid == 0) s_odd = 0;
+  if (tid == 0) s_odd = s_apart = 0;
   Place next = look_up(wave);
   typename R::Query q;                                     // requested before the first tile and converted while that is on its way
   R::load_q(p, s, tid, &q);
@@ -373,8 +410,9 @@ void scaled_matrix_kernel(PagedDecode p) {
       load_v(0, half);
     }
   u32x4* qs = reinterpret_cast<u32x4*>(smem);
-  const int up = R::store_q(p, tid, q, qs, s_most);
+  const int up = R::store_q(p, tid, q, qs, s_most, s_back, &s_apart, &s_odd);
   __syncthreads();
+  const int apart = __builtin_amdgcn_readfirstlane(s_apart);
 
   R rows;
   rows.begin(p, s, s.row0, lane);
@@ -442,7 +480,7 @@ void scaled_matrix_kernel(PagedDecode p) {
       });
       __builtin_amdgcn_s_setprio(0);
       float w[HB][8];
-      rows.weights(lane, p0, half, (uint32_t)(bad >> (32 * half)), s_scales[wave][buf ^ 1], mantissas_now, sc, w);
+      rows.weights(lane, p0, half, apart, s_back, (uint32_t)(bad >> (32 * half)), s_scales[wave][buf ^ 1], mantissas_now, sc, w);
       u32x4 wt[HB][2];
       R::split(w, wt);
       if (half == 1 || t + kWaves >= ntiles) put_scales(buf, bad_next);
