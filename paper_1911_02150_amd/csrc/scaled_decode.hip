@@ -239,19 +239,16 @@ struct Rows8 : Rows<T, D, HB, false, EXACT> {
     for (int hb = 0; hb < HB; ++hb)
 #pragma unroll
       for (int e = 0; e < 8; ++e) w[hb][e] = fmaf(sc[e >> 2][hb][e & 3], f[e], e8[e]);
-    if (apart) {                                           // (what e8 rounds away goes by the product that is not yet brought back, and comes down with it)
-      int row = lane & 15;
-      asm volatile("" : "+v"(row));                        // (nothing of it before the branch)
+    if (bad || p0 + kPagedTile > lim_min) {                // what is not there, or not seen (rows apart: in every tile, so that others have one branch here)
+      int first = p0 + 8 * g, row = lane & 15;
+      asm volatile("" : "+v"(first), "+v"(row));           // (a branch: few tiles have such positions)
+      if (apart)                                           // (what e8 rounds away goes by the product that is not yet brought back, and comes down with it)
 #pragma unroll
-      for (int hb = 0; hb < HB; ++hb) {
-        const float y = back[16 * hb + row];
+        for (int hb = 0; hb < HB; ++hb) {
+          const float y = back[16 * hb + row];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[hb][e] = fmaf(w[hb][e] - e8[e], y, e8[e]);
-      }
-    }
-    if (bad || p0 + kPagedTile > lim_min) {                // what is not there, or not seen
-      int first = p0 + 8 * g;
-      asm volatile("" : "+v"(first));                      // (a branch: few tiles have such positions)
+          for (int e = 0; e < 8; ++e) w[hb][e] = fmaf(w[hb][e] - e8[e], y, e8[e]);
+        }
 #pragma unroll
       for (int e = 0; e < 8; ++e)
 #pragma unroll
@@ -416,6 +413,7 @@ void scaled_matrix_kernel(PagedDecode p) {
 
   R rows;
   rows.begin(p, s, s.row0, lane);
+  if (apart) rows.lim_min = 0;
   // ---- the scales of the pair that `publish` was last called for, into LDS; m_run goes with ref
   int ref = 0;
   uint64_t nothing = 0;                                    // positions whose V is nothing beside the others'
