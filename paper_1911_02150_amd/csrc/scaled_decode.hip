@@ -436,7 +436,8 @@ void scaled_matrix_kernel(PagedDecode p) {
     }
     far = far || __any(e < -kFar || e > kFar);
     Scales& own = s_scales[wave][buf];
-    own.f[lane] = there ? ldexpf(ks, up) : 0.f;
+    const float f = there ? ldexpf(ks, up) : 0.f;
+    own.f[lane] = fmaf(f, 0.f, f);                         // (NaN for an infinite one, which would make -infinity, unnoticed, of logits that are finite or NaN)
     own.e[lane] = (float)(e - ref);
     own.inv[lane] = ldexpf(1.f, -e);
     const uint32_t mant = none ? 0x3f800000u : (bits & 0x7fffffu) | 0x3f800000u;
