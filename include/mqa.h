@@ -391,7 +391,7 @@ int mqa_paged_evict_kv(void* K_pages, void* V_pages, const int32_t* table_in, co
  * are rounded to the nearest number, the even one of two, infinities to +-Q; NaN is e4m3's NaN, int8's 0.  b * h_kv * ((n + block - 2) / block + 1) <= 2^23.
  *
  * mqa_paged_scaled_decode_step: as mqa_paged_decode_step without scores.  Scales may be any float32.  8 bits are exact in the products; q has 23 bits, or 2^-30 of its row's largest
- * number where that is more, and a position's weight times V's scale 23 bits, or, below 2^-12 of its row's largest, 2^-35 of that largest.
+ * number where that is more, and a position's weight times V's scale 23 bits, or, below 2^-12 of its row's largest, 2^-35 of that largest (zeros with a scale below 2^-100 count as with 2^-50).
  */
 int mqa_paged_scaled_append_kv_rows(const float* k_new, const float* v_new, const int32_t* counts, void* K_pages, float* K_scales, void* V_pages, float* V_scales,
                                     const int32_t* table, const int32_t* lens_in, int32_t* lens_out, int b, int n, int h_kv, int num_pages, int page_size,

@@ -6,7 +6,7 @@
 //     brought by a power of two to 2^14 at most and taken as two fp16 terms: by the same one where their sizes are much the same, else each by its own, and its logits back.
 //   out^T[D cols x 16 rows] += V_tile^T . weights^T: lane (c, g) has 1/16 of the columns of rows 8g .. 8g + 7.
 // Weights.  With s_V(p) = 2^E mant and z the logit (log2), u = z + E - ref is what the running maximum M is taken over, row by row, and w = 2^(u - M) the number that multiplies V8 (times mant, where
-// a scale is no power of two): a row's largest *contribution* is near fp16's largest number, so that two fp16 terms hold every w to 23 bits, and those that are below 2^-25 of it to 2^-35 of
+// a scale is no power of two): a row's largest *contribution* is 2^10 at least, so that two fp16 terms hold every w to 23 bits, and those that are below 2^-12 of it to 2^-35 of
 // it, whatever the scales.  The sum is over w 2^-E.  ref follows the tiles' scales (any will do: M goes with it), which keeps u small, and so its rounding.
 //
 // What bounds it: 64 sequences of 8192 and 32 rows, 136 MB, take 33 us = 4.1 TB/s, vector instructions (the conversions of 8 bits, the softmax) a third of the SIMDs' cycles and the products a sixth;
@@ -86,7 +86,7 @@ constexpr float kRoom = 4.f;         // log2 of the largest w over 2^kTop before
 constexpr float kTop = 10.f;
 constexpr int kNear = 16;            // ref is moved for scales that are so many powers of two off
 // A row's sum and its maximum go apart by the scales: from 2^-kFar to 2^kFar all numbers that count stay float32's; other scales are the plain form's, unless they are below 2^-kNothing
-// and their rows are zeros (which an append gives the smallest scale).
+// and their rows are zeros (which an append gives the smallest scale), and then as good as 2^-kFar.
 constexpr int kFar = 50, kNothing = 100;
 
 // Rows of q whose largest numbers are no further than 2^kSameSize apart share a power of two: two fp16 terms then hold a row's numbers to 23 bits, or to 2^-30 of its largest (a row of its own: 2^-38).  Beyond
@@ -435,6 +435,7 @@ void scaled_matrix_kernel(PagedDecode p) {
       if (!there || none) e = ref;
     }
     far = far || __any(e < -kFar || e > kFar);
+    if (none) e = -kFar;                                   // (zeros: all that is in the sum and hardly anything in the maximum, however much of the weight they have)
     Scales& own = s_scales[wave][buf];
     const float f = there ? ldexpf(ks, up) : 0.f;
     own.f[lane] = fmaf(f, 0.f, f);                         // (NaN for an infinite one, which would make -infinity, unnoticed, of logits that are finite or NaN)

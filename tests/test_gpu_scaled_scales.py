@@ -51,3 +51,27 @@ def test_logits_of_any_size_are_told_apart(m, kind):
     got = m.mqa_paged_scaled_decode_step(f32(q), bits(K, kind, True), f32(Ks, True), bits(V, kind, True), f32(Vs, True), i32([[0]]), i32([3])).cpu().numpy()
     want = V[0, 0, 1] * Vs[0, 0, 1]
     assert (np.abs(got - want) <= 2 * EPS * np.abs(want)).all()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+@pytest.mark.parametrize("lead", [5, 20, 40, 58, 90])
+@pytest.mark.parametrize("h,k,each", [(8, 128, 7), (32, 128, 7), (16, 64, 40), (20, 48, 7), (9, 256, 30)])
+def test_zeros_with_the_weight_leave_the_others_their_accuracy(m, h, k, each, lead, kind):
+    """Two blocks of zeros, as an append leaves them, whose logits are 2^lead times the others' in weight: they count in the sum, and otherwise as if they had a scale of 2^-50."""
+    rng = np.random.default_rng(h + k + lead)
+    (K, Ks, V, Vs), _ = cache_of(rng, 1, each, 1, 16, 16, k, k, kind)
+    table, lens = tables(rng, 1, each), np.array([16 * each - 3])
+    direction = np.sign(rng.standard_normal(k))
+    q = (direction * 0.5 + 0.05 * rng.standard_normal((1, 1, h, k))).astype(np.float32)
+    zeros = table[0, [1, each - 2]]
+    V[zeros], Vs[zeros] = 0, 2.0 ** -126
+    K[zeros], Ks[zeros] = direction * 64, 2.0 ** -6                         # logits of about k / 2, times the scale
+    scale = float(np.float32(lead / np.log2(np.e) / (k / 2)))
+    counted = Vs.copy()
+    counted[zeros] = 2.0 ** -50
+    want, size, K_all, top = attended(q, (K, Ks, V, Vs), table, lens, scale)
+    _, _, _, top = attended(q, (K, Ks, V, counted), table, lens, scale)
+    got = m.mqa_paged_scaled_decode_step(f32(q[:, 0]), bits(K, kind, True), f32(Ks, True), bits(V, kind, True), f32(Vs, True), i32(table), i32(lens), scale=scale).cpu().numpy()
+    bound = tolerance(q, K_all, size, scale, 16 * each, kind, top)
+    off = np.abs(got - want[:, 0])
+    assert (off <= bound[:, 0]).all(), (off / bound[:, 0]).max()
