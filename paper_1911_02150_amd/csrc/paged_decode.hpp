@@ -6,6 +6,7 @@
 // Positions on pages that hold nothing have weight 0, and a row that sees nothing is 0.
 #pragma once
 #include "paged.hpp"
+#include "pieces.hpp"
 
 #include <type_traits>
 
@@ -241,20 +242,6 @@ __device__ __forceinline__ int before_me(int x, int* s_waves, int* all) {
   return before;
 }
 
-constexpr int kComputeUnits = 256, kShares = 768, kSharesOfMany = 512, kLeast = 16, kLongest = 64, kLongestScaled = 256;
-
-// Tiles of a piece, at most: a whole number for each of the workgroup's four waves.
-__device__ __forceinline__ int whole_waves(int tiles) { return max(1, (tiles + 3) >> 2) * 4; }
-__device__ __forceinline__ int pieces_of(int tiles, int per) { return max(1, (int)((unsigned)(tiles + per - 1) / (unsigned)per)); }
-// Many groups: are they left whole?  total: of all groups
-__device__ __forceinline__ bool left_whole(const PagedDecode& p, int longest, int total) {
-  return longest <= kLongest && longest * (kComputeUnits / p.blocks) <= total;
-}
-__device__ __forceinline__ int share_of(const PagedDecode& p, int total) {
-  const int shares = p.blocks > 1 ? kSharesOfMany : kShares;
-  return max(kLeast, (total + shares - 1) / shares);
-}
-
 // Thousands of sequences: what look_for finds from all lengths, found once, by one workgroup: p.work[0].x: pieces of one head of all sequences, and behind it for
 // each of them {sequence, pieces before the sequence's, the sequence's, its length}.  Looked for by every workgroup it grows with the square of the sequences: 32768 of up
 // to 20 positions, 8 heads, 5912 us, from the list 397; 2048 54 and 33; of 300 to 1200, 32 heads, 4096 389 and 315, 1024 91 and 92, 300 38 and 47 (a launch more).
@@ -278,7 +265,7 @@ void paged_list_kernel(PagedDecode p) {
   total *= p.c.h_kv;
 #pragma unroll
   for (int w = 0; w < kListThreads / 64; ++w) longest = max(longest, s_longest[w]);
-  const int per = whole_waves(left_whole(p, longest, total) ? longest : share_of(p, total));
+  const int per = listed_share(p.blocks, longest, total);
   int before = 0;
   for (int base = 0, turn = 0; base < p.b; base += kListThreads * kListEach, turn ^= 1) {
     const int first = base + kListEach * tid;
@@ -343,7 +330,7 @@ __device__ __forceinline__ bool look_for(const PagedDecode& p, int piece, Segmen
   bool fits = false;
   if (many) {
     longest = max(max(s_longest[0], s_longest[1]), max(s_longest[2], s_longest[3]));
-    fits = left_whole(p, longest, total);
+    fits = left_whole(p.blocks, longest, total);
     if (fits) cut(longest);
   }
   for (int most = kComputeUnits; most <= 2 * kComputeUnits; most *= 2) {
@@ -354,7 +341,7 @@ __device__ __forceinline__ bool look_for(const PagedDecode& p, int piece, Segmen
         fits = all * heads <= units;
       }
   }
-  if (!fits) cut(share_of(p, total));
+  if (!fits) cut(share_of(p.blocks, total));
   if (piece >= all * heads) return false;
   if (before * heads <= piece && piece < (before + count) * heads) {      // one thread
     int x = from, L = len, mine = pieces_of(tiles_of(p, len), per);
@@ -406,7 +393,7 @@ __device__ __forceinline__ bool look_for_scaled(const PagedDecode& p, int piece,
     *all = __builtin_amdgcn_readlane(incl, 63);
     return incl - x;
   };
-  const bool many = p.b * heads * p.blocks >= kComputeUnits;
+  const bool many = scaled_many(p.b, heads, p.blocks);
   if (many) {
 #pragma unroll
     for (int o = 1; o < 64; o <<= 1) longest = max(longest, __shfl_xor(longest, o));
@@ -415,52 +402,26 @@ __device__ __forceinline__ bool look_for_scaled(const PagedDecode& p, int piece,
   int total;
   sum_before(mine, &total);
   total *= heads;
-  int per = 0, all = 0;
-  float inverse = 0.f;
-  auto pieces = [&](int tiles) {                           // (less than 2^20 tiles: the quotient is off by one at most)
-    const int a = tiles + per - 1;
-    int n = (int)((float)a * inverse);
-    const int rest = a - n * per;
-    n += (rest >= per) - (rest < 0);
-    return max(1, n);
-  };
-  auto cut = [&](int tiles) {
-    per = whole_waves(tiles);
-    inverse = 1.f / (float)per;
+  if (many && !alone) longest = max(max(s_longest[0], s_longest[1]), max(s_longest[2], s_longest[3]));
+  PiecesOf pieces = {};
+  int all = 0;                                             // pieces of one head
+  scaled_cut(p.b, heads, p.blocks, longest, total, [&](int tiles) {
+    pieces = PiecesOf::cut(tiles);
     int count = 0;
 #pragma unroll
     for (int x = 0; x < kEach; ++x)
       if (x < each) count += x < have ? pieces(tiles_of(p, len[x])) : 0;
     sum_before(count, &all);
-  };
-  // As above, but whole groups where there is one for every compute unit and none is longer than the units' mean, up to 256 tiles (512 sequences of up to 4000, 32 heads: 73.5 us, as above 83.5; 64
-  // heads 121 and 129.5; 300 of up to 6000, 64 heads 100.7 and 113.9; 300 of 2500, 32 heads, 62.5 and 73; 200 of up to 3000, 64 heads 69.7 and 67.8), two workgroups to a unit from the start where a unit's share is more than 16 tiles (48 sequences of 2048, 32 heads: one 21.3 us, two 22.7; 256 of up to 2000 41.2 and
-  // 35.0; 64 of 8192 40.1 and 39.5), and up to half over an even share each (256 of up to 2000, 32 heads: 35.0, a quarter over it 44.9; 300 of up to 1500 35.6 and 45.2).
-  bool fits = false;
-  if (many) {
-    if (!alone) longest = max(max(s_longest[0], s_longest[1]), max(s_longest[2], s_longest[3]));
-    fits = longest <= kLongestScaled && longest * (kComputeUnits / p.blocks) <= total;
-    if (fits) cut(longest);
-  }
-  for (int most = total * p.blocks > 16 * kComputeUnits ? 2 * kComputeUnits : kComputeUnits; most <= 2 * kComputeUnits; most *= 2) {
-    const int units = most / p.blocks;
-    if (!fits && p.b * heads <= units)
-      for (int x = 8; x <= 12 && !fits; ++x) {
-        cut((int)(((long long)total * x + 8 * units - 1) / (8 * units)));
-        fits = all * heads <= units;
-      }
-  }
-  if (!fits) cut(share_of(p, total));
+    return all;
+  });
   if (piece >= all * heads) return false;
-  // The long pieces come first, by quarters of the longest that there may be, so that short ones fill the end (512 sequences of up to 4096, 64 heads: 133.6 us in the
-  // sequences' order, so 128.8).  A quarter's counts are 16 bits of a sum.
   int n[kEach], quarter[kEach];
   unsigned long long sum = 0;
 #pragma unroll
   for (int x = 0; x < kEach; ++x)
     if (x < each) {
       const int t = tiles_of(p, len[x]), of = pieces(t);
-      quarter[x] = 3 - ((4 * t >= of * per) + (4 * t >= 2 * of * per) + (4 * t >= 3 * of * per));
+      quarter[x] = quarter_of(t, of, pieces.per);
       n[x] = x < have ? of : 0;
       sum += (unsigned long long)n[x] << (16 * quarter[x]);
     }
@@ -482,7 +443,7 @@ __device__ __forceinline__ bool look_for_scaled(const PagedDecode& p, int piece,
       whole += s_quarters[w];
     }
   }
-  ahead += (whole << 16) + (whole << 32) + (whole << 48);      // (and the quarters before)
+  ahead += quarters_before(whole);
   if (alone) {
     const int first = (int)(ahead >> (16 * quarter[0]) & 0xffff);
     const int who = __builtin_ctzll(__ballot(first * heads <= piece && piece < (first + n[0]) * heads));      // (one of them)
