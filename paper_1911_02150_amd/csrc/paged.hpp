@@ -91,7 +91,7 @@ struct ScaledAppend {
   int block;               // positions of a scale; divides page_size
 };
 hipError_t launch_scaled_append(const ScaledAppend& p, int is_e4m3, hipStream_t st);
-PagedPlan scaled_plan(int b, int n, int h, int h_kv, int page_size, int max_pages, int k, int v, int is_e4m3);
+PagedPlan scaled_plan(int b, int n, int h, int h_kv, int page_size, int max_pages, int k, int v);
 hipError_t launch_scaled_decode(const PagedDecode& p, const PagedPlan& plan, int is_e4m3, hipStream_t st);
 
 // ---- who holds which page (pages.hip)

@@ -128,7 +128,7 @@ int mqa_paged_scaled_append_kv_rows(const float* k_new, const float* v_new, cons
 
 size_t mqa_paged_scaled_decode_workspace_bytes(int b, int n, int h, int h_kv, int page_size, int max_pages, int k, int v, mqa_dtype dt) {
   if ((dt != MQA_E4M3 && dt != MQA_INT8) || !decode_sizes_ok(b, n, h, h_kv, page_size, max_pages, k, v) || !scaled_sizes_ok(page_size, 1, k, v)) return 0;
-  return scaled_plan(b, n, h, h_kv, page_size, max_pages, k, v, dt == MQA_E4M3).bytes;
+  return scaled_plan(b, n, h, h_kv, page_size, max_pages, k, v).bytes;
 }
 
 int mqa_paged_scaled_decode_step(const float* q, const void* K_pages, const float* K_scales, const void* V_pages, const float* V_scales, const int32_t* table,
@@ -141,7 +141,7 @@ int mqa_paged_scaled_decode_step(const float* q, const void* K_pages, const floa
     return MQA_ERR_SHAPE;
   if (misaligned(q) || misaligned(K_pages) || misaligned(K_scales) || misaligned(V_pages) || misaligned(V_scales) || misaligned(table) || misaligned(lens) || misaligned(o))
     return MQA_ERR_ALIGN;
-  const PagedPlan pl = scaled_plan(b, n, h, h_kv, page_size, max_pages, k, v, dt == MQA_E4M3);
+  const PagedPlan pl = scaled_plan(b, n, h, h_kv, page_size, max_pages, k, v);
   if (pl.bytes) {
     if (!workspace || workspace_bytes < pl.bytes) return MQA_ERR_WORKSPACE;
     if (misaligned(workspace)) return MQA_ERR_ALIGN;

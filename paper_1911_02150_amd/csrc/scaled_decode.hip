@@ -68,7 +68,7 @@ __device__ __forceinline__ void turn2(uint32_t row0, uint32_t row1, bool upper, 
 }
 
 template <int D> struct Form8 {
-  static constexpr int kPieces = D / 32, kLoads = D / 64;  // products of 32 columns; 16-byte loads of a K row in a lane
+  static constexpr int kPieces = D / 32;                   // products of 32 columns
   static constexpr int kTerms = 2;
   static constexpr int kColumns = D / 16;
   typedef typename std::conditional<D == 256, u32x4, typename std::conditional<D == 128, u32x2, u32x1>::type>::type VRow;
@@ -510,7 +510,7 @@ void scaled_matrix_kernel(PagedDecode p) {
 
 }  // namespace
 
-PagedPlan scaled_plan(int b, int n, int h, int h_kv, int page_size, int max_pages, int k, int v, int is_e4m3) {
+PagedPlan scaled_plan(int b, int n, int h, int h_kv, int page_size, int max_pages, int k, int v) {
   return paged_plan(b, n, h, h_kv, page_size, max_pages, k, v, 1, 0, true);
 }
 
