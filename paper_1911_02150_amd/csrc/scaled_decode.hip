@@ -10,7 +10,7 @@
 // it, whatever the scales.  The sum is over w 2^-E.  ref follows the tiles' scales (any will do: M goes with it), which keeps u small, and so its rounding.
 //
 // What bounds it: 64 sequences of 8192 and 32 rows, 136 MB, take 33 us = 4.1 TB/s, vector instructions (the conversions of 8 bits, the softmax) a third of the SIMDs' cycles and the products a sixth;
-// 512 sequences of up to 4096 and 64 rows 107 us, vector instructions 43 % and products 27: a SIMD's registers hold two waves, which leave each other's waits open.  Measured and slower: a
+// 512 sequences of up to 4096 and 64 rows 107 us, vector instructions 42 % and products 26: a SIMD's registers hold two waves, which leave each other's waits open.  Measured and slower: a
 // tile at a time for each wave (48.7 and 150), a wave's two tiles as one of 64 positions (50 and 172, by registers that spill; with fewer of them 36 and 121, as the pairs took then), K converted
 // where it is multiplied and V's numbers paired after their conversion (35 and 121).
 #include "paged_decode.hpp"
