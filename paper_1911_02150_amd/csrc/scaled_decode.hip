@@ -438,7 +438,7 @@ void scaled_matrix_kernel(PagedDecode p) {
     if (none) e = -kFar;                                   // (zeros: all that is in the sum and hardly anything in the maximum, however much of the weight they have)
     Scales& own = s_scales[wave][buf];
     const float f = there ? ldexpf(ks, up) : 0.f;
-    own.f[lane] = fmaf(f, 0.f, f);                         // (NaN for an infinite one, which would make -infinity, unnoticed, of logits that are finite or NaN)
+    own.f[lane] = fmaf(f * 0x1p32f, 0.f, f);               // (NaN from 2^96 on: a product, of up to 2^31 and this, that came out as -infinity would go unnoticed)
     own.e[lane] = (float)(e - ref);
     own.inv[lane] = ldexpf(1.f, -e);
     const uint32_t mant = none ? 0x3f800000u : (bits & 0x7fffffu) | 0x3f800000u;

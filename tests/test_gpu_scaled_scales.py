@@ -75,3 +75,19 @@ def test_zeros_with_the_weight_leave_the_others_their_accuracy(m, h, k, each, le
     bound = tolerance(q, K_all, size, scale, 16 * each, kind, top)
     off = np.abs(got - want[:, 0])
     assert (off <= bound[:, 0]).all(), (off / bound[:, 0]).max()
+
+
+@pytest.mark.parametrize("kind", KINDS)
+def test_logits_of_any_size_beside_larger_queries(m, kind):
+    """The same with K's scales of 2^105 and every second row's queries 2^-20, 2^50 below the others', whose products are all with zeros: the others' mean is V's."""
+    (K, Ks, V, Vs), _ = cache_of(np.random.default_rng(4), 1, 1, 1, 3, 1, 64, 64, kind)
+    K[:] = 0
+    K[0, 0, :, 0] = 3, 1, 2
+    Ks[:] = 2.0 ** 105
+    q = np.zeros((1, 16, 64), dtype=np.float32)
+    q[:, 0::2, 1:] = 2.0 ** 30
+    q[:, 1::2, 0] = -2.0 ** -20
+    got = m.mqa_paged_scaled_decode_step(f32(q), bits(K, kind, True), f32(Ks, True), bits(V, kind, True), f32(Vs, True), i32([[0]]), i32([3])).cpu().numpy()
+    held = V[0, 0] * Vs[0, 0][:, None]
+    assert (np.abs(got[0, 1::2] - held[1]) <= 2 * EPS * np.abs(held[1])).all()
+    assert (np.abs(got[0, 0::2] - held.mean(0)) <= 12 * EPS * np.abs(held).mean(0)).all()
