@@ -90,7 +90,8 @@ constexpr int kNear = 16;            // ref is moved for scales that are so many
 constexpr int kFar = 50, kNothing = 100;
 
 // Rows of q whose largest numbers are no further than 2^kSameSize apart share a power of two: two fp16 terms then hold a row's numbers to 23 bits, or to 2^-30 of its largest (a row of its own: 2^-38).  Beyond
-// 2^kNoSize they are the plain form's.
+// 2^kNoSize they are the plain form's.  (64 sequences of 8192, 32 heads: every second row 2^10 smaller 40.9 us, all alike 38.8; 512 of up to 4096, 64 heads 121 and 112; 2^70 smaller, in the plain form,
+// 1275 and 6001.)
 constexpr int kSameSize = 8, kNoSize = 64;
 
 // Of two tiles' positions, in LDS: K's scale with q's power of two, E - ref, 2^-E, the mantissa.
